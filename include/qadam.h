@@ -90,16 +90,18 @@ enum qadam_error {
   QADAM_ERR_HYPER = -8,       /* beta/theta outside [0,1), eps <= 0 or a bad step size */
   QADAM_ERR_CUDA = -9,        /* a CUDA call failed; see qadam_last_cuda_error      */
   QADAM_ERR_PLACEMENT = -10,  /* placement is not one of the two values             */
-  QADAM_ERR_CAPACITY = -11    /* beyond the fixed capacity of qadam_worker_scales_static */
+  QADAM_ERR_CAPACITY = -11,   /* beyond the fixed capacity of qadam_worker_scales_static */
+  QADAM_ERR_TYPE = -12        /* an element type, code width or state width that is not offered */
 };
 
 /* Bits of the device status word. */
 enum {
   QADAM_ST_NONFINITE = 1u,    /* a max-abs scale was Inf or NaN: outputs of that step are unspecified */
-  QADAM_ST_TIMEOUT = 2u       /* a bounded wait inside a kernel ran out and the kernel returned early:
+  QADAM_ST_TIMEOUT = 2u,      /* a bounded wait inside a kernel ran out and the kernel returned early:
                                  x, m, v, e and the outputs of that step are partly written and the
                                  context cannot continue; restore the state from a copy and create a
                                  new context */
+  QADAM_ST_INDEX = 4u         /* a token was not below the number of rows: read as a zero row, left out of a gradient */
 };
 
 typedef struct {
@@ -349,6 +351,181 @@ int64_t qadam_launch_count(const qadam_ctx* ctx);
 
 /* Releases the host-side context.  Device buffers stay the caller's. */
 int qadam_destroy(qadam_ctx* ctx);
+
+/* ===========================================================================================
+ * The training step around the quantized step: AdamW over many tensors, the norm of their
+ * gradients, and the two operators at an embedding table.  They are contexts and calls of their
+ * own and share nothing with a qadam_ctx but the conventions above, with these differences:
+ *  - every call takes the stream that it enqueues on, which belongs to the context's device (to
+ *    the current device where there is no context).  The device that is current stays current;
+ *  - calls of one context, and calls that share a workspace, must be ordered by the caller (one
+ *    stream, or events between streams): they use the same scratch.  That goes for graphs that
+ *    captured such calls too.  Everything but the create, query and poll calls may be captured;
+ *  - a tensor may start at any multiple of its element's size (16-byte alignment is faster).
+ * =========================================================================================== */
+
+enum { QADAM_F32 = 0, QADAM_BF16 = 1, QADAM_F16 = 2 };       /* element types */
+
+/* ---- norm of many gradients -------------------------------------------------------------- */
+
+/* A list of tensors, told by their lengths and types. */
+typedef struct {
+  int32_t num_tensors;        /* 1 .. 2^20 */
+  int32_t reserved;           /* must be 0 */
+  const int64_t* len;         /* host, [num_tensors], each >= 0 (0: an empty tensor)           */
+  const int32_t* type;        /* host, [num_tensors], QADAM_F32 ...; NULL: all QADAM_F32       */
+} qadam_tensor_list;
+
+typedef struct qadam_norm qadam_norm;
+
+/* Scratch of a norm context: `workspace_bytes` bytes of device memory, 256-byte aligned. */
+int qadam_norm_query_sizes(const qadam_tensor_list* list, size_t* workspace_bytes);
+
+/* Creates a norm context on the current device.  Writes its tables into the workspace
+ * (synchronously); the lists need not outlive the call. */
+int qadam_norm_create(const qadam_tensor_list* list, void* workspace, size_t workspace_bytes, qadam_norm** out);
+
+/* The tensors that later runs read: host array [num_tensors] of device pointers (copied).  NULL
+ * for a tensor without a gradient, which counts as zero.  Host call, nothing is enqueued.
+ * QADAM_ERR_ALIGN for a pointer that is no multiple of its element's size. */
+int qadam_norm_bind(qadam_norm* ctx, const void* const* tensors);
+
+/* out[0] = sqrt(sum of the squares of all elements), out[1] = min(1, max_norm / out[0]): the
+ * factor that clips the gradients to max_norm (> 0, may be infinite).  out: device, 2 binary32,
+ * 8-byte aligned.  Squares are formed and summed in binary64, in an order fixed by the list and
+ * the device, and rounded once: the same bits every time.  If the norm is not finite (an element
+ * is not, or the result is beyond binary32), out[1] is NaN: a step given that factor changes
+ * nothing (see below). */
+int qadam_norm_run(qadam_norm* ctx, float max_norm, float* out, void* stream);
+int64_t qadam_norm_launch_count(const qadam_norm* ctx);
+int qadam_norm_destroy(qadam_norm* ctx);
+
+/* ---- AdamW over many tensors --------------------------------------------------------------
+ * One step t for weights x, gradient g and clipping factor c of every tensor, each operation one
+ * rounded binary32 operation (beta1, beta2, eps, lr as given; c1 = 1 - beta1, c2 = 1 - beta2, the
+ * other constants rounded once from binary64):
+ *     g' = g c                                                (no c: g' = g)
+ *     m  = beta1 m + c1 g'          v = beta2 v + c2 (g' g')
+ *     x  = x k - a (m / (sqrt(v) b + eps))
+ *     k  = 1 - lr decay,  a = lr / (1 - beta1^t),  b = 1 / sqrt(1 - beta2^t)
+ * This is Adam with bias correction and epsilon outside the root, unlike the step of the paper
+ * above, and with decay that does not pass through the moments.
+ *
+ * Layout: moments and master weights are in the padded layout: tensor s starts at off[s], the
+ * running sum of lengths rounded up to 128; pads are 0 and stay 0.  Weights and gradients are
+ * the caller's own tensors, each contiguous and anywhere.
+ *
+ * Weights of 16 bits are rounded to nearest after each step, which loses a step smaller than half
+ * of a weight's last place; with master = 1 the step reads and writes binary32 master weights
+ * instead, and the 16-bit tensors are rounded copies that are only written.
+ *
+ * 8-bit moments (state_bits = 8): m and r = sqrt(v) as codes of one byte and one binary32 scale
+ * per 128 elements (a row of the padded layout): the largest |m| (r) of the row, at least 2^-126.
+ * y = |m| / scale is a floating-point number of 3 mantissa bits, code = 8 (exponent of y) +
+ * mantissa + 127, 0 below code 1, the sign in bit 7: 1.0 is code 127.  r has 4 mantissa bits,
+ * code = 16 exponent + mantissa + 255, at least 1 unless r = 0: a second moment that is not zero
+ * does not become zero.  A row's largest value is held exactly, so a row that decays as a whole
+ * decays in its scale.  The others are rounded at random (up or down to the next code, so that the
+ * mean is right): to nearest, a moment whose change in one step is below half a code's step would
+ * never move, and with beta2 = 0.999 that is nearly all of them.  The 16 bits h of element i of a
+ * tensor at off: half-word 4 ((i / 128) mod 2) + i mod 4 of the Philox4x32-10 block with counter
+ * ((off + 256 (i / 256) + 4 ((i mod 128) / 4)) / 4 [low, high], t [low, high]) and key seed [low,
+ * high]; (2 (h mod 64) + 1) / 128 of a step is added to the mantissa of m, (2 (h / 64) + 1) / 2048
+ * to that of r, before the rest is cut off.  A row with a non-finite moment has a non-finite
+ * scale, sets QADAM_ST_NONFINITE and stays non-finite, as a 32-bit moment would. */
+
+typedef struct qadam_adamw qadam_adamw;
+
+typedef struct {
+  int32_t num_tensors;        /* S, 1 .. 2^20                                                     */
+  int32_t state_bits;         /* 32 or 8                                                          */
+  const int64_t* len;         /* host, [S], each >= 0                                             */
+  const int32_t* weight_type; /* host, [S], QADAM_F32 ...; NULL: all QADAM_F32                    */
+  const int32_t* grad_type;   /* host, [S], independent of weight_type; NULL: all QADAM_F32       */
+  const float* decay;         /* host, [S], each >= 0 and finite; NULL: none                      */
+  float beta1, beta2;         /* in [0, 1)                                                        */
+  float eps;                  /* > 0, finite                                                      */
+  float lr;                   /* default step size, >= 0 and finite                               */
+  int32_t master;             /* 1: binary32 master weights; 0: none                              */
+  int32_t reserved;           /* must be 0                                                        */
+  uint64_t seed;              /* key of the random stream; read only with state_bits = 8          */
+} qadam_adamw_config;
+
+typedef struct {
+  void* const* weights;       /* host, [S] device pointers (copied); may be NULL for empty tensors */
+  float* master;              /* [D] with master = 1: set to the weights by the caller; else NULL  */
+  void* m;                    /* [D] binary32, or [D] codes; zeros at the start                    */
+  void* v;                    /* [D] binary32, or [D] codes of r; zeros at the start               */
+  float* m_scale;             /* [D/128] with state_bits = 8 (zeros at the start), else NULL       */
+  float* r_scale;             /* the same for r                                                    */
+  int64_t* count;             /* one: steps taken by qadam_adamw_step_counted                      */
+  void* workspace;            /* 256-byte aligned; the library keeps tables here                   */
+  size_t workspace_bytes;
+  uint32_t* status;           /* one word; qadam_adamw_create clears it                            */
+} qadam_adamw_buffers;        /* device pointers 16-byte aligned, but for weights, count and status */
+
+/* Any output pointer may be NULL.  off: host [S]. */
+int qadam_adamw_query_sizes(const qadam_adamw_config* cfg, int64_t* D, int64_t* off, size_t* workspace_bytes);
+
+/* Creates a context on the current device (tables are written synchronously). */
+int qadam_adamw_create(const qadam_adamw_config* cfg, const qadam_adamw_buffers* bufs, qadam_adamw** out);
+
+/* The gradients that later steps read, as qadam_norm_bind.  A tensor whose gradient is NULL is left as it is. */
+int qadam_adamw_bind(qadam_adamw* ctx, const void* const* grads);
+
+/* Step t = `step` >= 1 with step size lr (< 0: the configuration's).  grad_scale: device, one
+ * binary32, or NULL.  If it is not finite, the step changes nothing and sets QADAM_ST_NONFINITE.
+ * Steps need not be in order: t only enters the bias corrections and the random stream.  A captured
+ * call repeats its t and lr. */
+int qadam_adamw_step(qadam_adamw* ctx, int64_t step, float lr, const float* grad_scale, void* stream);
+
+/* The same with t and lr on the device, for a step that is captured once and replayed: t is one more
+ * than *count, which is advanced (not by a step that a grad_scale stops), lr is read from device
+ * memory (one binary32, >= 0; NULL: the configuration's). */
+int qadam_adamw_step_counted(qadam_adamw* ctx, const float* lr, const float* grad_scale, void* stream);
+
+/* 8-bit moments as binary32 values: m32, v32 ([D], device, 16-byte aligned; either may be NULL).
+ * QADAM_ERR_TYPE with state_bits = 32, whose moments are the buffers themselves. */
+int qadam_adamw_moments(qadam_adamw* ctx, float* m32, float* v32, void* stream);
+
+/* Waits for `stream`, then copies the status word to *host_status. */
+int qadam_adamw_poll_status(qadam_adamw* ctx, void* stream, uint32_t* host_status);
+int64_t qadam_adamw_launch_count(const qadam_adamw* ctx);
+int qadam_adamw_destroy(qadam_adamw* ctx);
+
+/* ---- embedding rows and their gradient ---------------------------------------------------- */
+
+/* out[t][:] = round(scale * table[ids[t]][:]), t = 0 .. count - 1: one binary32 product, one rounding
+ * to out_type.  table: device, [rows][stride >= width] of `type`; ids: device, id_bits = 32 or 64;
+ * out: device, [count][out_stride >= width], not overlapping the table.  A negative id is a padded
+ * position: a row of zeros.  An id >= rows: a row of zeros, and QADAM_ST_INDEX in *status (device,
+ * may be NULL).  count = 0 is allowed. */
+int qadam_embedding_lookup(const void* table, int32_t type, int64_t rows, int64_t width, int64_t stride,
+                           const void* ids, int32_t id_bits, int64_t count, float scale,
+                           void* out, int32_t out_type, int64_t out_stride, uint32_t* status, void* stream);
+
+/* The same from the weights that a worker holds: table[i][j] is element first + i * width + j of the
+ * broadcast Q_x(x), decoded from its packed codes (wcodes of a context with this kx, 16-byte aligned,
+ * wcode_bytes of them; kx = 0 .. 14).  For a tensor of a parameter vector `first` is its seg_off.
+ * QADAM_ERR_SIZE if the rows end beyond the codes. */
+int qadam_held_lookup(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t rows, int64_t width,
+                      const void* ids, int32_t id_bits, int64_t count, float scale,
+                      void* out, int32_t out_type, int64_t out_stride, uint32_t* status, void* stream);
+
+/* Scratch of qadam_embedding_grad for batches of up to `count` tokens. */
+int qadam_embedding_grad_query_sizes(int64_t count, int64_t rows, int64_t width, size_t* workspace_bytes);
+
+/* grad[i][:] = round(scale * sum of dy[t][:] over the t with ids[t] = i), for all i < rows; rows without
+ * a token become 0.  accumulate = 1: round(grad[i][:] + scale * sum) for rows with a token, the others
+ * are left as they are.  dy: device, [count][dy_stride >= width]; grad: device, [rows][grad_stride >=
+ * width], only its first `width` columns are written.  Sums are binary32, over tokens sorted by id, in an
+ * order that depends on the sizes alone: the same bits every time.  Tokens that are negative or equal to `padding`
+ * (-1: none) are left out; ids >= rows are left out and set QADAM_ST_INDEX in *status (device, may be
+ * NULL).  count <= 2^30, rows < 2^31 - 1, width <= 2^22, count * width <= 2^44. */
+int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const void* dy, int32_t dy_type,
+                         int64_t dy_stride, float scale, int64_t padding, void* grad, int32_t grad_type,
+                         int64_t rows, int64_t width, int64_t grad_stride, int32_t accumulate,
+                         void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
 
 const char* qadam_strerror(int err);
 

@@ -14,7 +14,8 @@ import torch
 
 PLACE_SERVER, PLACE_WORKER = 0, 1
 GRID_POW2, GRID_UNIFORM, GRID_STOCHASTIC = 0, 1, 2
-ST_NONFINITE, ST_TIMEOUT = 1, 2
+ST_NONFINITE, ST_TIMEOUT, ST_INDEX = 1, 2, 4
+F32, BF16, F16 = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libqadam.so")
@@ -26,6 +27,13 @@ exported_symbols = (
     "qadam_profile_enable", "qadam_profile_read", "qadam_worker_scales_static",
     "qadam_worker_pass_model", "qadam_set_moment_rates", "qadam_set_regularization",
     "qadam_create_ex", "qadam_server_step_range", "qadam_finish_step", "qadam_shard_cuts",
+    "qadam_norm_query_sizes", "qadam_norm_create", "qadam_norm_bind", "qadam_norm_run",
+    "qadam_norm_launch_count", "qadam_norm_destroy",
+    "qadam_adamw_query_sizes", "qadam_adamw_create", "qadam_adamw_bind", "qadam_adamw_step",
+    "qadam_adamw_step_counted", "qadam_adamw_moments", "qadam_adamw_poll_status",
+    "qadam_adamw_launch_count", "qadam_adamw_destroy",
+    "qadam_embedding_lookup", "qadam_held_lookup", "qadam_embedding_grad_query_sizes",
+    "qadam_embedding_grad",
 )
 
 SERVER_AUTO, SERVER_PLAIN = 0, 1
@@ -70,6 +78,28 @@ class QAdamBuffers(C.Structure):
         ("scales", C.c_void_p), ("gcodes", C.c_void_p), ("wcodes", C.c_void_p),
         ("wresid", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("status", C.c_void_p), ("wfeedback", C.c_void_p),
+    ]
+
+
+class TensorList(C.Structure):
+    _fields_ = [("num_tensors", C.c_int32), ("reserved", C.c_int32), ("len", C.POINTER(C.c_int64)),
+                ("type", C.POINTER(C.c_int32))]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [
+        ("num_tensors", C.c_int32), ("state_bits", C.c_int32), ("len", C.POINTER(C.c_int64)),
+        ("weight_type", C.POINTER(C.c_int32)), ("grad_type", C.POINTER(C.c_int32)), ("decay", C.POINTER(C.c_float)),
+        ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("lr", C.c_float),
+        ("master", C.c_int32), ("reserved", C.c_int32), ("seed", C.c_uint64),
+    ]
+
+
+class AdamWBuffers(C.Structure):
+    _fields_ = [
+        ("weights", C.POINTER(C.c_void_p)), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+        ("m_scale", C.c_void_p), ("r_scale", C.c_void_p), ("count", C.c_void_p), ("workspace", C.c_void_p),
+        ("workspace_bytes", C.c_size_t), ("status", C.c_void_p),
     ]
 
 
@@ -128,6 +158,31 @@ def load_library():
     L.qadam_set_moment_rates.argtypes = [C.c_void_p, C.c_float, C.c_float]
     L.qadam_set_regularization.restype = C.c_int
     L.qadam_set_regularization.argtypes = [C.c_void_p, C.c_float]
+    vp, i32, i64, f32, size, out = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t, C.POINTER(C.c_void_p)
+    for name, args in {
+        "norm_query_sizes": [C.POINTER(TensorList), C.POINTER(size)],
+        "norm_create": [C.POINTER(TensorList), vp, size, out],
+        "norm_bind": [vp, C.POINTER(vp)],
+        "norm_run": [vp, f32, vp, vp],
+        "norm_destroy": [vp],
+        "adamw_query_sizes": [C.POINTER(AdamWConfig), C.POINTER(i64), C.POINTER(i64), C.POINTER(size)],
+        "adamw_create": [C.POINTER(AdamWConfig), C.POINTER(AdamWBuffers), out],
+        "adamw_bind": [vp, C.POINTER(vp)],
+        "adamw_step": [vp, i64, f32, vp, vp],
+        "adamw_step_counted": [vp, vp, vp, vp],
+        "adamw_moments": [vp, vp, vp, vp],
+        "adamw_poll_status": [vp, vp, C.POINTER(C.c_uint32)],
+        "adamw_destroy": [vp],
+        "embedding_lookup": [vp, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp, vp],
+        "held_lookup": [vp, size, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp, vp],
+        "embedding_grad_query_sizes": [i64, i64, i64, C.POINTER(size)],
+        "embedding_grad": [vp, i32, i64, vp, i32, i64, f32, i64, vp, i32, i64, i64, i64, i32, vp, size, vp, vp],
+    }.items():
+        fn = getattr(L, "qadam_" + name)
+        fn.restype, fn.argtypes = C.c_int, args
+    for name in ("norm_launch_count", "adamw_launch_count"):
+        fn = getattr(L, "qadam_" + name)
+        fn.restype, fn.argtypes = i64, [vp]
     L.qadam_launch_count.restype = C.c_int64
     L.qadam_launch_count.argtypes = [C.c_void_p]
     L.qadam_destroy.restype = C.c_int
@@ -393,6 +448,16 @@ class QAdam:
 
     def poll_status(self) -> int:
         return qadam_poll_status(self.ctx)
+
+    def lookup(self, segment: int, width: int, ids: torch.Tensor, scale: float = 1.0, out_dtype=torch.bfloat16, **kw):
+        """Rows of a tensor as the workers hold it (the broadcast of the last step), see `held_lookup`."""
+        from .embedding import held_lookup
+        if self.kx < 0:
+            raise ValueError("nothing is broadcast in packed form with kx = -1: look the rows up in x")
+        if width < 1 or self.seg_len[segment] % width:
+            raise ValueError(f"segment {segment} of {self.seg_len[segment]} elements has no rows of {width}")
+        return held_lookup(self.wcodes[:self.wcode_bytes], self.kx, ids, self.seg_len[segment] // width, width, scale=scale,
+                           out_dtype=out_dtype, first=self.seg_off[segment], **kw)
 
     def set_moment_rates(self, beta_t: float, theta_t: float) -> None:
         """beta_t, theta_t of Algorithm 1 for the steps that follow."""

@@ -1144,6 +1144,7 @@ const char* qadam_strerror(int err) {
     case QADAM_ERR_CUDA: return "a CUDA call failed";
     case QADAM_ERR_PLACEMENT: return "invalid placement";
     case QADAM_ERR_CAPACITY: return "size beyond the fixed capacity of the allocation-free entry point";
+    case QADAM_ERR_TYPE: return "element type, code width or state width not offered";
     default: return "unknown error";
   }
 }
