@@ -96,17 +96,28 @@ int enqueue_lookup(LookupParams p, bool held, cudaStream_t st) {
 
 // ---------------------------------------------------------------- gradient: tokens sorted by id
 //
-// Stable sort of (id, place) by the bits of the id, at most 9 bits a pass: counts of each digit in each
-// CTA's run of tokens, their running sum (all smaller digits, then the same digit in earlier runs), and
-// every token to its place.  Stable, so a row's tokens stay in the order of the batch.
+// (row, place) of every token, stable by row, so a row's tokens stay in the order of the batch.  The
+// launches that sort leave most of the GPU idle: further CTAs of theirs clear the gradient meanwhile.
 
-constexpr int kSortThreads = 512;
+constexpr int kSortThreads = 256;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 8;                              // tokens per thread
-constexpr int kSortRun = kSortThreads * kSortItems;        // 4096 tokens per CTA
+constexpr int kSortRun = kSortThreads * kSortItems;        // 2048 tokens per CTA
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kScanThreads = 1024;
+constexpr int kDirectRuns = 512;                           // up to so many runs every CTA adds up the counts for itself
+constexpr int kRankTokens = 8192;                          // up to so many tokens are ranked by comparing all pairs
+constexpr int kRankPer = 32;                               // tokens that a CTA ranks
+constexpr int kClearCtas = 148 * 6;
+
+struct ClearParams {
+  void* grad;
+  int type, width;
+  long long rows, stride;
+  long long begin, end;        // this launch's share: 16-byte words where rows touch, else rows
+  int dense;                   // rows touch and begin on 16 bytes
+  int ctas;                    // CTAs of the launch that clear
+};
 
 struct SortParams {
   const void* ids;             // of the first pass; later passes read keys
@@ -115,18 +126,37 @@ struct SortParams {
   const unsigned* places;
   unsigned* out_keys;
   unsigned* out_places;
-  unsigned* counts;            // [digits][runs]
+  unsigned* counts;            // [runs][digits]
   int count, runs;
   int shift, digits;
+  int scanned;                 // counts are places already (scan_counts_kernel)
   unsigned rows;
   long long padding;
   unsigned* status;
+  unsigned* num_long;          // of the sums, cleared by the first launch
+  ClearParams clear;
 };
 
+__device__ void clear_share(const ClearParams& c, int cta) {
+  if (c.dense) {
+    uint4* w = static_cast<uint4*>(c.grad);
+    for (long long i = c.begin + (long long)cta * kSortThreads + threadIdx.x; i < c.end; i += (long long)c.ctas * kSortThreads)
+      w[i] = make_uint4(0u, 0u, 0u, 0u);
+  } else {
+    const bool fits = aligned4(c.grad, c.type) && c.stride % 4 == 0;
+    const Raw4 zero = {{0u, 0u, 0u, 0u}};
+    for (long long r = c.begin + cta; r < c.end; r += c.ctas) {
+      char* row = static_cast<char*>(c.grad) + r * c.stride * type_bytes(c.type);
+      for (int col = 4 * threadIdx.x; col < c.width; col += 4 * kSortThreads)
+        store_raw4(row, c.type, col, c.width, fits && col + 4 <= c.width, zero);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kSortThreads) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
+
 // The sort's key of a token: its row, or `rows` for one that is left out.
-__device__ __forceinline__ unsigned sort_key(const SortParams& p, int t) {
-  if (p.keys != nullptr) return p.keys[t];
-  const long long id = load_id(p.ids, p.id_bits, t);
+__device__ __forceinline__ unsigned key_of(const SortParams& p, long long id) {
   if (id < 0 || id == p.padding) return p.rows;
   if (id >= (long long)p.rows) {
     if (p.status != nullptr) atomicOr(p.status, QADAM_ST_INDEX);
@@ -135,67 +165,190 @@ __device__ __forceinline__ unsigned sort_key(const SortParams& p, int t) {
   return (unsigned)id;
 }
 
-__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid_constant__ SortParams p) {
-  __shared__ unsigned n[kDigits];
-  for (int d = threadIdx.x; d < p.digits; d += kSortThreads) n[d] = 0u;
-  __syncthreads();
+// Keys of the N tokens first, first + step, ...; 0 behind the last.  All loads are under way before the first is
+// looked at.
+template <int N>
+__device__ __forceinline__ void load_keys(const SortParams& p, long long first, int step, unsigned (&key)[N]) {
+  if (p.keys != nullptr) {
 #pragma unroll
-  for (int j = 0; j < kSortItems; ++j) {
-    const long long t = (long long)blockIdx.x * kSortRun + j * kSortThreads + threadIdx.x;
-    if (t < p.count) atomicAdd(&n[(sort_key(p, (int)t) >> p.shift) & (p.digits - 1)], 1u);
+    for (int j = 0; j < N; ++j) key[j] = first + j * step < p.count ? p.keys[first + j * step] : 0u;
+    return;
   }
-  __syncthreads();
-  for (int d = threadIdx.x; d < p.digits; d += kSortThreads) p.counts[(size_t)d * p.runs + blockIdx.x] = n[d];
+  long long id[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) id[j] = first + j * step < p.count ? load_id(p.ids, p.id_bits, first + j * step) : 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) key[j] = key_of(p, id[j]);
 }
 
-// Running sum of n counts in place, by one CTA: every thread a contiguous part.
-__global__ void __launch_bounds__(kScanThreads) scan_counts_kernel(unsigned* counts, long long n) {
-  __shared__ unsigned warp_total[kScanThreads / 32];
-  const long long part = (n + kScanThreads - 1) / kScanThreads;
-  const long long lo = min(n, threadIdx.x * part), hi = min(n, lo + part);
-  unsigned sum = 0u;
-  for (long long i = lo; i < hi; ++i) sum += counts[i];
-  const int lane = threadIdx.x % 32;
+// Few tokens: a token's place is the number of tokens before it, by row and place in one number (`shift` bits
+// of place).  T^2 comparisons of a cycle or two on all lanes.
+__global__ void __launch_bounds__(kSortThreads) rank_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ uint4 ranked[];                        // p.count numbers, filled up with the largest
+  __shared__ unsigned before[kSortWarps][kRankPer];
+  const int ctas = (p.count + kRankPer - 1) / kRankPer;
+  if ((int)blockIdx.x >= ctas) {
+    clear_share(p.clear, blockIdx.x - ctas);
+    return;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.num_long = 0u;
+  unsigned* all = reinterpret_cast<unsigned*>(ranked);
+  const int four = (p.count + 4 * kSortWarps - 1) / (4 * kSortWarps);       // quads per warp
+  for (int t0 = threadIdx.x; t0 < 4 * kSortWarps * four; t0 += 8 * kSortThreads) {
+    unsigned key[8];
+    load_keys<8>(p, t0, kSortThreads, key);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = t0 + j * kSortThreads;
+      if (t < 4 * kSortWarps * four) all[t] = t < p.count ? key[j] << p.shift | (unsigned)t : 0xFFFFFFFFu;
+    }
+  }
+  __syncthreads();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int mine = blockIdx.x * kRankPer + lane;
+  const unsigned x = all[min(mine, p.count - 1)];
+  unsigned n = 0u;
+#pragma unroll 4
+  for (int q = warp * four; q < (warp + 1) * four; ++q) {
+    const uint4 y = ranked[q];
+    n += y.x < x ? 1u : 0u;
+    n += y.y < x ? 1u : 0u;
+    n += y.z < x ? 1u : 0u;
+    n += y.w < x ? 1u : 0u;
+  }
+  before[warp][lane] = n;
+  __syncthreads();
+  if (warp != 0 || mine >= p.count) return;
+#pragma unroll
+  for (int w = 1; w < kSortWarps; ++w) n += before[w][lane];
+  p.out_keys[n] = x >> p.shift;
+  p.out_places[n] = (unsigned)mine;
+}
+
+// Many tokens: at most 9 bits a pass, lowest first.  Counts of each digit in each CTA's run of tokens; then
+// every token to its place, behind all smaller digits and the same digit in earlier runs.
+__global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid_constant__ SortParams p) {
+  __shared__ unsigned n[kDigits];
+  if ((int)blockIdx.x >= p.runs) {
+    clear_share(p.clear, blockIdx.x - p.runs);
+    return;
+  }
+  if (p.keys == nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.num_long = 0u;
+  for (int d = threadIdx.x; d < p.digits; d += kSortThreads) n[d] = 0u;
+  unsigned key[kSortItems];
+  const long long first = (long long)blockIdx.x * kSortRun + threadIdx.x;
+  load_keys<kSortItems>(p, first, kSortThreads, key);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kSortItems; ++j)
+    if (first + j * kSortThreads < p.count) atomicAdd(&n[(key[j] >> p.shift) & (p.digits - 1)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += kSortThreads) p.counts[(size_t)blockIdx.x * p.digits + d] = n[d];
+}
+
+// Exclusive running sum over the digits, in place (shared memory), by the whole CTA.
+__device__ __forceinline__ void scan_digits(unsigned* total, int digits, unsigned* warp_total) {
+  constexpr int kPer = kDigits / kSortThreads;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  unsigned x[kPer], sum = 0u;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int d = threadIdx.x * kPer + k;
+    x[k] = d < digits ? total[d] : 0u;
+    sum += x[k];
+  }
   unsigned upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const unsigned other = __shfl_up_sync(0xFFFFFFFFu, upto, o);
     if (lane >= o) upto += other;
   }
-  if (lane == 31) warp_total[threadIdx.x / 32] = upto;
+  if (lane == 31) warp_total[warp] = upto;
   __syncthreads();
-  if (threadIdx.x < 32) {
-    unsigned w = warp_total[lane], s = w;
+  unsigned at = upto - sum;
+  for (int w = 0; w < warp; ++w) at += warp_total[w];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned other = __shfl_up_sync(0xFFFFFFFFu, s, o);
-      if (lane >= o) s += other;
-    }
-    warp_total[lane] = s - w;
+  for (int k = 0; k < kPer; ++k) {
+    const int d = threadIdx.x * kPer + k;
+    if (d < digits) total[d] = at;
+    at += x[k];
   }
   __syncthreads();
-  unsigned at = warp_total[threadIdx.x / 32] + upto - sum;
-  for (long long i = lo; i < hi; ++i) {
-    const unsigned c = counts[i];
-    counts[i] = at;
-    at += c;
+}
+
+// Counts to places for very many runs, by one CTA.
+__global__ void __launch_bounds__(kSortThreads) scan_counts_kernel(unsigned* counts, int runs, int digits) {
+  __shared__ unsigned total[kDigits], warp_total[kSortWarps];
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+    unsigned n = 0u;
+#pragma unroll 8
+    for (int r = 0; r < runs; ++r) n += counts[(size_t)r * digits + d];
+    total[d] = n;
+  }
+  __syncthreads();
+  scan_digits(total, digits, warp_total);
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+    unsigned at = total[d];
+#pragma unroll 8
+    for (int r = 0; r < runs; ++r) {
+      const unsigned n = counts[(size_t)r * digits + d];
+      counts[(size_t)r * digits + d] = at;
+      at += n;
+    }
   }
 }
 
 __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_constant__ SortParams p) {
-  // tokens of each digit that a warp has seen, then where the warp's tokens of that digit begin
+  // tokens of each digit that a warp has seen, then where the warp's tokens of that digit begin in the run
   __shared__ unsigned short seen[kSortWarps][kDigits];
+  __shared__ unsigned start[kDigits], warp_total[kSortWarps];
+  if ((int)blockIdx.x >= p.runs) {
+    clear_share(p.clear, blockIdx.x - p.runs);
+    return;
+  }
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&seen[0][0])[i] = 0;
-  __syncthreads();
+  for (int i = threadIdx.x; i < kSortWarps * kDigits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(&seen[0][0])[i] = 0u;
   unsigned key[kSortItems];
   unsigned short rank[kSortItems];
   const long long base = (long long)blockIdx.x * kSortRun + warp * (32 * kSortItems) + lane;
+  load_keys<kSortItems>(p, base, 32, key);
+  // counts of two neighbouring digits of all runs, and of the runs before this one
+  const int d2 = 2 * threadIdx.x;
+  static_assert(kDigits == 2 * kSortThreads, "two digits to a thread");
+  uint2 earlier = make_uint2(0u, 0u);
+  if (d2 < p.digits) {
+    const uint2* counts = reinterpret_cast<const uint2*>(p.counts + d2);
+    const size_t step = (size_t)p.digits / 2;
+    if (p.scanned) {
+      earlier = counts[blockIdx.x * step];
+      start[d2] = 0u;
+      start[d2 + 1] = 0u;
+    } else {
+      uint2 n = make_uint2(0u, 0u);
+      for (int r0 = 0; r0 < p.runs; r0 += 16) {
+        uint2 x[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = r0 + j < p.runs ? counts[(r0 + j) * step] : make_uint2(0u, 0u);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (r0 + j == (int)blockIdx.x) earlier = n;
+          n.x += x[j].x;
+          n.y += x[j].y;
+        }
+      }
+      start[d2] = n.x;
+      start[d2 + 1] = n.y;
+    }
+  }
+  __syncthreads();
+  scan_digits(start, p.digits, warp_total);
+  if (d2 < p.digits) {
+    start[d2] += earlier.x;
+    start[d2 + 1] += earlier.y;
+  }
 #pragma unroll
   for (int j = 0; j < kSortItems; ++j) {
-    const long long t = base + 32 * j;
-    const bool live = t < p.count;
-    key[j] = live ? sort_key(p, (int)t) : 0u;
+    const bool live = base + 32 * j < p.count;
     const unsigned d = live ? (key[j] >> p.shift) & (p.digits - 1) : (unsigned)p.digits + lane;   // nobody's peer
     const unsigned peers = __match_any_sync(0xFFFFFFFFu, d);
     const int before = __popc(peers & ((1u << lane) - 1u));
@@ -207,11 +360,14 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   }
   __syncthreads();
   for (int d = threadIdx.x; d < p.digits; d += kSortThreads) {
-    unsigned at = 0u;
+    unsigned short n[kSortWarps];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) n[w] = seen[w][d];
+    unsigned short at = 0;
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const unsigned n = seen[w][d];
-      seen[w][d] = (unsigned short)at;
-      at += n;
+      seen[w][d] = at;
+      at = (unsigned short)(at + n[w]);
     }
   }
   __syncthreads();
@@ -220,7 +376,7 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
     const long long t = base + 32 * j;
     if (t < p.count) {
       const unsigned d = (key[j] >> p.shift) & (p.digits - 1);
-      const unsigned to = p.counts[(size_t)d * p.runs + blockIdx.x] + seen[warp][d] + rank[j];
+      const unsigned to = start[d] + seen[warp][d] + rank[j];
       p.out_keys[to] = key[j];
       p.out_places[to] = p.places != nullptr ? p.places[t] : (unsigned)t;
     }
@@ -229,20 +385,23 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
 
 // ---------------------------------------------------------------- gradient: sums
 //
-// The sorted tokens are cut into chunks of kChunk.  A warp adds up one chunk's rows in 128 columns, four to
-// a lane, and writes a row that begins and ends in its chunk.  A row's tokens that cross a chunk's end leave
-// a partial sum there; the rows that cross are put together from those in order.
+// The sorted tokens are cut into chunks of at most 32.  A warp takes one chunk in a tile of columns, 16 bytes to a
+// lane, and adds up the rows that begin in its chunk, following the last one into the next chunk.  Only a row that
+// covers whole chunks beyond the one that it begins in is split: it leaves a partial sum in each of its chunks
+// and its first chunk in a list, and a second launch adds those up in order.
 
 constexpr int kChunk = 32;
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
-constexpr int kSumColumns = 128;
-constexpr int kAhead = 8;                                  // rows asked for at a time
+constexpr int kAhead = 8;                                  // rows a warp has asked for
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinCtas = 148 * 3;
 
 struct GradParams {
   const unsigned* keys;        // sorted; `rows` behind the last
   const unsigned* places;
-  int count, chunks;
+  int count, chunk, chunks;    // chunk: tokens
   const void* dy;
   int dy_type;
   long long dy_stride;
@@ -250,154 +409,282 @@ struct GradParams {
   void* grad;
   int grad_type;
   long long rows, grad_stride;
-  int width, tiles;            // tiles: of 128 columns
+  int width, tiles;            // tiles: of 512 bytes of dy
+  int vector;                  // rows of dy are aligned to 16 bytes
   int accumulate;
-  float* partial;              // [chunks][2][tiles * 128]: the run that began in an earlier chunk, the one that goes on
+  float* partial;              // [chunks][2][tiles * columns]: of the row that began in an earlier chunk, of the one that goes on
+  unsigned* long_rows;         // chunks in which a split row begins
+  unsigned* num_long;
 };
 
-__global__ void __launch_bounds__(kSumThreads) zero_rows_kernel(const __grid_constant__ GradParams p) {
-  const int quads = (p.width + 3) / 4;
-  const bool fits = aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0;
-  const Raw4 zero = {{0u, 0u, 0u, 0u}};
-  const long long n = p.rows * quads;
-  for (long long q = (long long)blockIdx.x * kSumThreads + threadIdx.x; q < n; q += (long long)gridDim.x * kSumThreads) {
-    const long long row = q / quads;
-    const int col = 4 * (int)(q - row * quads);
-    store_raw4(static_cast<char*>(p.grad) + row * p.grad_stride * type_bytes(p.grad_type), p.grad_type, col, p.width,
-               fits && col + 4 <= p.width, zero);
+// A lane's columns: neighbours where rows are aligned to 16 bytes, else 32 apart, so that a warp's accesses stay
+// next to each other.
+template <int COLS>
+struct Columns {
+  int first;                   // column of k = 0
+  int step;
+  __device__ Columns(const GradParams& p, int tile) {
+    const int lane = threadIdx.x % 32;
+    step = p.vector ? 1 : 32;
+    first = tile * 32 * COLS + (p.vector ? lane * COLS : lane);
+  }
+  __device__ int at(int k) const { return first + k * step; }
+};
+
+// Asks for a lane's part of a row; it arrives in `to` (shared memory that no other lane uses).
+template <int COLS>
+__device__ __forceinline__ void ask_row(uint4* to, const void* row, const Columns<COLS>& c, int width) {
+  if (c.step == 1 && c.first + COLS <= width) {
+    const unsigned dst = (unsigned)__cvta_generic_to_shared(to);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(static_cast<const char*>(row) + (size_t)c.first * (16 / COLS))
+                 : "memory");
+  } else {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) {
+      if (c.at(k) >= width) break;
+      if constexpr (COLS == 4) w[k] = static_cast<const uint32_t*>(row)[c.at(k)];
+      else w[k / 2] |= (uint32_t) static_cast<const unsigned short*>(row)[c.at(k)] << (16 * (k % 2));
+    }
+    *to = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
-__device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, int col, bool fits, const float (&sum)[4]) {
-  if (col >= p.width) return;
+template <int COLS>
+__device__ __forceinline__ void row_floats(const uint4& r, int type, float (&x)[COLS]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  if constexpr (COLS == 4) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(w[k]);
+  } else if (type == QADAM_BF16) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = __uint_as_float(w[k] << 16);
+      x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = half_bits_to_float(w[k] & 0xFFFFu);
+      x[2 * k + 1] = half_bits_to_float(w[k] >> 16);
+    }
+  }
+}
+
+template <int COLS>
+__device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, const Columns<COLS>& c, bool fits, const float (&sum)[COLS]) {
   char* dst = static_cast<char*>(p.grad) + (long long)row * p.grad_stride * type_bytes(p.grad_type);
-  const bool whole = fits && col + 4 <= p.width;
-  float x[4];
+  if (c.step == 1) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, sum[k]);
-  if (p.accumulate) {
-    float old[4];
-    to_floats(load_raw4(dst, p.grad_type, col, p.width, whole), p.grad_type, old);
+    for (int q = 0; q < COLS; q += 4) {
+      const int col = c.first + q;
+      if (col >= p.width) break;
+      const bool whole = fits && col + 4 <= p.width;
+      float x[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(old[k], x[k]);
+      for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, sum[q + k]);
+      if (p.accumulate) {
+        float old[4];
+        to_floats(load_raw4(dst, p.grad_type, col, p.width, whole), p.grad_type, old);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(old[k], x[k]);
+      }
+      store_raw4(dst, p.grad_type, col, p.width, whole, from_floats(x, p.grad_type));
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) {
+      const int col = c.at(k);
+      if (col >= p.width) break;
+      float x[4] = {__fmul_rn(p.scale, sum[k]), 0.0f, 0.0f, 0.0f};
+      if (p.accumulate) {
+        float old[4];
+        to_floats(load_raw4(dst, p.grad_type, col, col + 1, false), p.grad_type, old);
+        x[0] = __fadd_rn(old[0], x[0]);
+      }
+      store_raw4(dst, p.grad_type, col, col + 1, false, from_floats(x, p.grad_type));
+    }
   }
-  store_raw4(dst, p.grad_type, col, p.width, whole, from_floats(x, p.grad_type));
 }
 
-__device__ __forceinline__ float* partial_row(const GradParams& p, int chunk, int which, int col) {
-  return p.partial + ((long long)chunk * 2 + which) * ((long long)p.tiles * kSumColumns) + col;
+// Partial sums lie lane by lane.
+template <int COLS>
+__device__ __forceinline__ float4* partial_of(const GradParams& p, int chunk, int which, int tile) {
+  return reinterpret_cast<float4*>(p.partial + ((((long long)chunk * 2 + which) * p.tiles + tile) * 32 + threadIdx.x % 32) * COLS);
 }
 
-__global__ void __launch_bounds__(kSumThreads) sum_chunks_kernel(const __grid_constant__ GradParams p) {
+template <int COLS>
+__global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid_constant__ GradParams p) {
+  __shared__ uint4 ring[kSumWarps][kAhead][32];
   const long long unit = (long long)blockIdx.x * kSumWarps + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
   if (unit >= (long long)p.chunks * p.tiles) return;
-  const int chunk = (int)(unit / p.tiles), col = (int)(unit % p.tiles) * kSumColumns + 4 * lane;
-  const int begin = chunk * kChunk, n = min(kChunk, p.count - begin);
+  const int chunk = (int)(unit / p.tiles), tile = (int)(unit % p.tiles);
+  const int begin = chunk * p.chunk, n = min(p.chunk, p.count - begin);
   const unsigned none = (unsigned)p.rows;
-  unsigned key = none, place = 0u;
-  if (lane < n) {
-    key = p.keys[begin + lane];
-    place = p.places[begin + lane];
-  }
-  const unsigned first = __shfl_sync(0xFFFFFFFFu, key, 0), last = __shfl_sync(0xFFFFFFFFu, key, n - 1);
+  // this chunk's tokens and the next one's, and whether its first row began before it, or before the chunk before it
+  const unsigned key0 = begin + lane < p.count ? p.keys[begin + lane] : none;
+  const unsigned key1 = begin + 32 + lane < p.count ? p.keys[begin + 32 + lane] : none;
+  const unsigned place0 = begin + lane < p.count ? p.places[begin + lane] : 0u;
+  const unsigned place1 = begin + 32 + lane < p.count ? p.places[begin + 32 + lane] : 0u;
+  const unsigned before = begin > 0 ? p.keys[begin - 1] : none;
+  const unsigned long_before = begin > p.chunk ? p.keys[begin - p.chunk - 1] : none;
+  auto key_at = [&](int i) { return i < 32 ? __shfl_sync(0xFFFFFFFFu, key0, i) : __shfl_sync(0xFFFFFFFFu, key1, i - 32); };
+  const unsigned first = key_at(0), last = key_at(n - 1);
   if (first == none) return;
-  const bool from_before = begin > 0 && p.keys[begin - 1] == first;
-  const bool goes_on = last != none && begin + n < p.count && p.keys[begin + n] == last;
-  const bool dy_fits = aligned4(p.dy, p.dy_type) && p.dy_stride % 4 == 0;
-  const bool grad_fits = aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0;
-  const int row_bytes_of = type_bytes(p.dy_type);
-  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  unsigned current = first;
-  bool at_first = true;
-  for (int j0 = 0; j0 < n; j0 += kAhead) {
-    Raw4 raw[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const unsigned row = __shfl_sync(0xFFFFFFFFu, place, j0 + a);
-      const unsigned k = __shfl_sync(0xFFFFFFFFu, key, j0 + a);
-      raw[a] = {{0u, 0u, 0u, 0u}};
-      if (k != none && col < p.width)
-        raw[a] = load_raw4(static_cast<const char*>(p.dy) + (long long)row * p.dy_stride * row_bytes_of, p.dy_type, col, p.width,
-                           dy_fits && col + 4 <= p.width);
+  const bool whole = n == p.chunk && first == last;                 // the chunk is part of one row
+  const bool from_before = before == first;
+  const bool split_before = from_before && (whole || long_before == first);     // and leaves a partial sum here
+  // the last row: goes on into a chunk that is part of it, or ends in the next chunk
+  const bool split_after = last != none && key_at(n) == last && begin + 2 * p.chunk <= p.count && key_at(2 * p.chunk - 1) == last &&
+                           n == p.chunk;
+  // which of the window's 64 tokens are this warp's: none of a row that the chunk before follows up to here
+  int from = 0, to = n;
+  if (from_before && !split_before) {
+    while (from < n && key_at(from) == first) ++from;               // (fewer than a chunk)
+    if (from == n) return;
+  }
+  if (!split_after && !(split_before && whole) && last != none) {
+    while (to < 64 && key_at(to) == last) ++to;
+  }
+  const Columns<COLS> c(p, tile);
+  const bool fits = aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0;
+  uint4(*mine)[32] = ring[threadIdx.x / 32];
+  auto ask = [&](int i) {
+    if (i < to) {
+      const unsigned row = i < 32 ? __shfl_sync(0xFFFFFFFFu, place0, i) : __shfl_sync(0xFFFFFFFFu, place1, i - 32);
+      if (key_at(i) != none)
+        ask_row<COLS>(&mine[i % kAhead][lane], static_cast<const char*>(p.dy) + (long long)row * p.dy_stride * (16 / COLS), c, p.width);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = from; i < from + kAhead; ++i) ask(i);
+  float sum[COLS];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const unsigned k = __shfl_sync(0xFFFFFFFFu, key, j0 + a);
-      if (k != current) {
-        if (current != none) {
-          if (at_first && from_before) *reinterpret_cast<float4*>(partial_row(p, chunk, 0, col)) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-          else finish_row(p, current, col, grad_fits, sum);
-        }
-        at_first = false;
-        current = k;
-        sum[0] = sum[1] = sum[2] = sum[3] = 0.0f;
+  for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
+  unsigned current = key_at(from);
+  bool leaves = split_before;                                       // the current row's sum is a partial one of slot 0
+#pragma unroll 1
+  for (int i = from; i < to; ++i) {
+    if (current == none) break;
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    float x[COLS];
+    row_floats<COLS>(mine[i % kAhead][lane], p.dy_type, x);
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) sum[k] = __fadd_rn(sum[k], x[k]);
+    ask(i + kAhead);
+    const unsigned next = i + 1 < to ? key_at(i + 1) : none;
+    if (next != current || i + 1 == to) {
+      const bool goes_on = i + 1 == to && split_after;
+      if (leaves || goes_on) {
+        float4* out = partial_of<COLS>(p, chunk, leaves ? 0 : 1, tile);
+#pragma unroll
+        for (int q = 0; q < COLS / 4; ++q) out[q] = make_float4(sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]);
+        if (!leaves && tile == 0 && lane == 0) p.long_rows[atomicAdd(p.num_long, 1u)] = (unsigned)chunk;
+      } else {
+        finish_row<COLS>(p, current, c, fits, sum);
       }
-      float x[4];
-      to_floats(raw[a], p.dy_type, x);
+      leaves = false;
+      current = next;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] = __fadd_rn(sum[i], x[i]);
+      for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
     }
   }
-  if (current == none) return;
-  if (at_first && from_before) *reinterpret_cast<float4*>(partial_row(p, chunk, 0, col)) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-  else if (goes_on) *reinterpret_cast<float4*>(partial_row(p, chunk, 1, col)) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-  else finish_row(p, current, col, grad_fits, sum);
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// One CTA per chunk and 128 columns: the run that begins in the chunk and goes on beyond it, if there is one.
-__global__ void __launch_bounds__(kSumThreads) join_chunks_kernel(const __grid_constant__ GradParams p) {
-  __shared__ float4 part[kSumWarps][32];
-  const int chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int col = blockIdx.y * kSumColumns + 4 * lane;
-  const int begin = chunk * kChunk, end = begin + kChunk;
-  if (end >= p.count) return;
-  const unsigned key = p.keys[end - 1];
-  if (key == (unsigned)p.rows || p.keys[end] != key) return;                    // nothing goes on
-  if (p.keys[begin] == key && begin > 0 && p.keys[begin - 1] == key) return;    // it began earlier
-  int lo = end, hi = p.count;                                                   // first place behind the run
+// First place in [lo, hi) whose key is above `key`, by the whole warp.
+__device__ __forceinline__ int behind(const unsigned* keys, unsigned key, int lo, int hi) {
+  const int lane = threadIdx.x % 32;
   while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (p.keys[mid] == key) lo = mid + 1;
-    else hi = mid;
+    const int step = (hi - lo + 31) / 32;
+    const long long at = (long long)lo + (long long)lane * step;
+    const int n = __popc(__ballot_sync(0xFFFFFFFFu, at < hi && keys[min(at, (long long)hi - 1)] <= key));
+    if (n == 0) return lo;
+    hi = (int)min((long long)hi, (long long)lo + (long long)n * step);
+    lo += (n - 1) * step + 1;
   }
-  const int last = (lo - 1) / kChunk;                                           // chunk the run ends in
-  const int n = last - chunk + 1, each = (n + kSumWarps - 1) / kSumWarps;
-  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = warp * each; i < min(n, (warp + 1) * each); ++i) {
-    const float4 x = *reinterpret_cast<const float4*>(partial_row(p, chunk + i, i == 0 ? 1 : 0, col));
-    sum[0] = __fadd_rn(sum[0], x.x);
-    sum[1] = __fadd_rn(sum[1], x.y);
-    sum[2] = __fadd_rn(sum[2], x.z);
-    sum[3] = __fadd_rn(sum[3], x.w);
+  return lo;
+}
+
+// The split rows, one to a CTA and tile at a time: every warp adds up a part of the row's chunks, in order, and the
+// first one the parts.
+template <int COLS>
+__global__ void __launch_bounds__(kJoinThreads) join_rows_kernel(const __grid_constant__ GradParams p) {
+  __shared__ float4 part[kJoinWarps][COLS / 4][32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const long long work = (long long)*p.num_long * p.tiles;
+  for (long long w = blockIdx.x; w < work; w += gridDim.x) {
+    const int chunk = (int)p.long_rows[w / p.tiles], tile = (int)(w % p.tiles);
+    const int next = (chunk + 1) * p.chunk;
+    const unsigned key = p.keys[next];
+    const int pieces = (behind(p.keys, key, next, p.count) - 1) / p.chunk - chunk + 1;
+    const int each = (pieces + kJoinWarps - 1) / kJoinWarps;
+    const int lo = warp * each, hi = min(pieces, lo + each);
+    float sum[COLS];
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
+    for (int i0 = lo; i0 < hi; i0 += 4) {
+      float4 x[4][COLS / 4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < COLS / 4; ++q)
+          x[j][q] = i0 + j < hi ? partial_of<COLS>(p, chunk + i0 + j, i0 + j == 0, tile)[q] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < COLS / 4; ++q) {
+          sum[4 * q] = __fadd_rn(sum[4 * q], x[j][q].x);
+          sum[4 * q + 1] = __fadd_rn(sum[4 * q + 1], x[j][q].y);
+          sum[4 * q + 2] = __fadd_rn(sum[4 * q + 2], x[j][q].z);
+          sum[4 * q + 3] = __fadd_rn(sum[4 * q + 3], x[j][q].w);
+        }
+    }
+    __syncthreads();                                                 // the last row's parts have been read
+#pragma unroll
+    for (int q = 0; q < COLS / 4; ++q) part[warp][q][lane] = make_float4(sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]);
+    __syncthreads();
+    if (warp == 0) {
+      for (int o = 1; o < kJoinWarps && o * each < pieces; ++o)
+#pragma unroll
+        for (int q = 0; q < COLS / 4; ++q) {
+          const float4 x = part[o][q][lane];
+          sum[4 * q] = __fadd_rn(sum[4 * q], x.x);
+          sum[4 * q + 1] = __fadd_rn(sum[4 * q + 1], x.y);
+          sum[4 * q + 2] = __fadd_rn(sum[4 * q + 2], x.z);
+          sum[4 * q + 3] = __fadd_rn(sum[4 * q + 3], x.w);
+        }
+      finish_row<COLS>(p, key, Columns<COLS>(p, tile), aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0, sum);
+    }
   }
-  part[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-  __syncthreads();
-  if (warp != 0) return;
-  for (int w = 1; w < min(kSumWarps, n); ++w) {
-    const float4 x = part[w][lane];
-    sum[0] = __fadd_rn(sum[0], x.x);
-    sum[1] = __fadd_rn(sum[1], x.y);
-    sum[2] = __fadd_rn(sum[2], x.z);
-    sum[3] = __fadd_rn(sum[3], x.w);
-  }
-  finish_row(p, key, col, aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0, sum);
 }
 
 // ---------------------------------------------------------------- host side
 
+// A chunk is 32 tokens, or fewer where that would leave SMs without enough warps to keep their loads in
+// flight: below `kWarps` warps over 512 bytes of columns.
+constexpr int64_t kWarps = 148 * 16;
+
 struct GradLayout {
-  size_t keys[2], places[2], counts, partial, bytes;
-  int runs, chunks, tiles;
+  size_t keys[2], places[2], counts, partial, long_rows, bytes;
+  int runs, chunk, chunks;
 };
 
 int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
   if (count < 0 || count > (int64_t)1 << 30 || rows < 1 || rows >= 0x7FFFFFFF || width < 1 || width > (int64_t)1 << 22)
     return QADAM_ERR_SIZE;
+  const int64_t tiles = (width + 127) / 128;                 // 512 bytes of binary32; half as many of 16-bit types
   l->runs = (int)((count + kSortRun - 1) / kSortRun);
-  l->chunks = (int)((count + kChunk - 1) / kChunk);
-  l->tiles = (int)((width + kSumColumns - 1) / kSumColumns);
-  if ((int64_t)l->chunks * l->tiles > (int64_t)1 << 32) return QADAM_ERR_SIZE;      // (warps of one launch)
+  // tokens from which chunks of 16 and 32 are taken
+  const int64_t at16 = kWarps * 16 / ((width + 255) / 256), at32 = 2 * at16;
+  l->chunk = count >= at32 ? 32 : count >= at16 ? 16 : 8;
+  l->chunks = (int)((count + l->chunk - 1) / l->chunk);
+  // room for any shorter batch too
+  const int64_t room = std::max(std::max((std::min(count, at16) + 7) / 8, count >= at16 ? (std::min(count, at32) + 15) / 16 : 0),
+                                count >= at32 ? (count + 31) / 32 : 0);
+  if (room * tiles > (int64_t)1 << 33) return QADAM_ERR_SIZE;
   size_t at = 0;
   const size_t list = round_up256((size_t)count * sizeof(unsigned));
   for (int i = 0; i < 2; ++i) {
@@ -408,8 +695,10 @@ int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
   }
   l->counts = at;
   at += round_up256((size_t)l->runs * kDigits * sizeof(unsigned));
+  l->long_rows = at;                                         // their number before them
+  at += 256 + round_up256((size_t)room * sizeof(unsigned));
   l->partial = at;
-  at += (size_t)l->chunks * 2 * l->tiles * kSumColumns * sizeof(float);
+  at += (size_t)room * 2 * ((width + 255) / 256 * 256) * sizeof(float);
   l->bytes = at + 256;
   return QADAM_OK;
 }
@@ -504,42 +793,85 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   auto list = [&](size_t off) { return reinterpret_cast<unsigned*>(ws + off); };
 
   GradParams g = {};
-  g.count = (int)count; g.chunks = l.chunks;
+  g.count = (int)count; g.chunk = l.chunk; g.chunks = l.chunks;
   g.dy = dy; g.dy_type = dy_type; g.dy_stride = dy_stride; g.scale = scale;
   g.grad = grad; g.grad_type = grad_type; g.rows = rows; g.grad_stride = grad_stride;
-  g.width = (int)width; g.tiles = l.tiles; g.accumulate = accumulate;
-  if (!accumulate) {
-    const long long quads = rows * ((width + 3) / 4);
-    zero_rows_kernel<<<(int)std::min<long long>((quads + kSumThreads - 1) / kSumThreads, 148 * 8), kSumThreads, 0, st>>>(g);
-    if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
-  }
-  if (count == 0) return QADAM_OK;
+  g.width = (int)width; g.accumulate = accumulate;
+  const int cols = 16 / type_bytes(dy_type);
+  g.tiles = (int)((width + 32 * cols - 1) / (32 * cols));
 
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                        // keys 0 .. rows
+  int place_bits = 0;
+  while (((count - 1) >> place_bits) > 0) ++place_bits;
+  const bool ranked = count <= kRankTokens && bits + place_bits <= 32;
   const int passes = (bits + kDigitBits - 1) / kDigitBits, digit = (bits + passes - 1) / passes;
+  const bool scanned = l.runs > kDirectRuns;
+
   SortParams s = {};
+  ClearParams& c = s.clear;
+  c.grad = grad; c.type = grad_type; c.width = (int)width; c.rows = rows; c.stride = grad_stride;
+  const int64_t row_bytes = width * type_bytes(grad_type);
+  c.dense = grad_stride == width && is_aligned(grad, 16) && rows * row_bytes % 16 == 0;
+  // what there is to clear is dealt out evenly to the launches that sort
+  const long long to_clear = accumulate ? 0 : c.dense ? rows * row_bytes / 16 : rows;
+  const int launches = count == 0 || ranked ? 1 : 2 * passes;
+  int launch = 0;
+  auto share = [&]() {
+    c.begin = to_clear * launch / launches;
+    c.end = to_clear * (launch + 1) / launches;
+    ++launch;
+    const long long each = c.dense ? kSortThreads : 1;
+    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearCtas);
+  };
+  if (count == 0) {
+    share();
+    if (c.ctas > 0) clear_kernel<<<c.ctas, kSortThreads, 0, st>>>(c);
+    return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
+  }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
-  s.padding = padding; s.status = status; s.digits = 1 << digit;
+  s.padding = padding; s.status = status; s.digits = 1 << digit; s.scanned = scanned;
   s.counts = list(l.counts);
-  for (int i = 0; i < passes; ++i) {
-    s.shift = i * digit;
-    s.keys = i == 0 ? nullptr : list(l.keys[(i + 1) % 2]);
-    s.places = i == 0 ? nullptr : list(l.places[(i + 1) % 2]);
-    s.out_keys = list(l.keys[i % 2]);
-    s.out_places = list(l.places[i % 2]);
-    count_digits_kernel<<<l.runs, kSortThreads, 0, st>>>(s);
-    scan_counts_kernel<<<1, kScanThreads, 0, st>>>(s.counts, (long long)l.runs << digit);
-    place_kernel<<<l.runs, kSortThreads, 0, st>>>(s);
+  s.num_long = list(l.long_rows);
+  s.out_keys = list(l.keys[0]);
+  s.out_places = list(l.places[0]);
+  if (ranked) {
+    s.shift = place_bits;
+    share();
+    const int four = ((int)count + 4 * kSortWarps - 1) / (4 * kSortWarps);
+    rank_kernel<<<((int)count + kRankPer - 1) / kRankPer + c.ctas, kSortThreads, (size_t)four * kSortWarps * 16, st>>>(s);
     if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  } else {
+    for (int i = 0; i < passes; ++i) {
+      s.shift = i * digit;
+      s.keys = i == 0 ? nullptr : list(l.keys[(i + 1) % 2]);
+      s.places = i == 0 ? nullptr : list(l.places[(i + 1) % 2]);
+      s.out_keys = list(l.keys[i % 2]);
+      s.out_places = list(l.places[i % 2]);
+      share();
+      count_digits_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
+      if (scanned) scan_counts_kernel<<<1, kSortThreads, 0, st>>>(s.counts, l.runs, s.digits);
+      share();
+      place_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
+      if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+    }
   }
   g.keys = s.out_keys;
   g.places = s.out_places;
   g.partial = reinterpret_cast<float*>(ws + l.partial);
-  const long long units = (long long)l.chunks * l.tiles;
-  const long long grid = (units + kSumWarps - 1) / kSumWarps;
-  sum_chunks_kernel<<<(unsigned)grid, kSumThreads, 0, st>>>(g);
-  if (l.chunks > 1) join_chunks_kernel<<<dim3((unsigned)l.chunks, (unsigned)l.tiles), kSumThreads, 0, st>>>(g);
+  g.num_long = s.num_long;
+  g.long_rows = s.num_long + 64;
+  g.vector = is_aligned(dy, 16) && dy_stride % cols == 0;
+  const long long units = (long long)l.chunks * g.tiles;
+  const unsigned grid = (unsigned)((units + kSumWarps - 1) / kSumWarps);
+  if (cols == 4) sum_chunks_kernel<4><<<grid, kSumThreads, 0, st>>>(g);
+  else sum_chunks_kernel<8><<<grid, kSumThreads, 0, st>>>(g);
+  // a row is split from two whole chunks on
+  if (l.chunks > 1) {
+    const int ctas = (int)std::min<long long>(units, kJoinCtas);
+    if (cols == 4) join_rows_kernel<4><<<ctas, kJoinThreads, 0, st>>>(g);
+    else join_rows_kernel<8><<<ctas, kJoinThreads, 0, st>>>(g);
+  }
   return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
