@@ -99,16 +99,18 @@ int enqueue_lookup(LookupParams p, bool held, cudaStream_t st) {
 // (row, place) of every token, stable by row, so a row's tokens stay in the order of the batch.  The
 // launches that sort leave most of the GPU idle: further CTAs of theirs clear the gradient meanwhile.
 
-constexpr int kSortThreads = 256;
+constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 8;                              // tokens per thread
-constexpr int kSortRun = kSortThreads * kSortItems;        // 2048 tokens per CTA
+constexpr int kSortRun = kSortThreads * kSortItems;        // 8192 tokens per CTA
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kDirectRuns = 512;                           // up to so many runs every CTA adds up the counts for itself
+constexpr int kDirectRuns = 256;                           // up to so many runs every CTA adds up the counts for itself
 constexpr int kRankTokens = 8192;                          // up to so many tokens are ranked by comparing all pairs
-constexpr int kRankPer = 32;                               // tokens that a CTA ranks
-constexpr int kClearCtas = 148 * 6;
+constexpr int kRankThreads = 512;
+constexpr int kRankWarps = kRankThreads / 32;
+constexpr int kRankPer = 64;                               // tokens that a CTA ranks: 128 CTAs at the most
+constexpr int kClearThreads = 148 * 1024;                  // beside the CTAs that sort
 
 struct ClearParams {
   void* grad;
@@ -133,27 +135,28 @@ struct SortParams {
   unsigned rows;
   long long padding;
   unsigned* status;
-  unsigned* num_long;          // of the sums, cleared by the first launch
+  unsigned* joined;            // counters of the sums, cleared by the first launch
+  long long counters;
   ClearParams clear;
 };
 
 __device__ void clear_share(const ClearParams& c, int cta) {
   if (c.dense) {
     uint4* w = static_cast<uint4*>(c.grad);
-    for (long long i = c.begin + (long long)cta * kSortThreads + threadIdx.x; i < c.end; i += (long long)c.ctas * kSortThreads)
+    for (long long i = c.begin + (long long)cta * blockDim.x + threadIdx.x; i < c.end; i += (long long)c.ctas * blockDim.x)
       w[i] = make_uint4(0u, 0u, 0u, 0u);
   } else {
     const bool fits = aligned4(c.grad, c.type) && c.stride % 4 == 0;
     const Raw4 zero = {{0u, 0u, 0u, 0u}};
     for (long long r = c.begin + cta; r < c.end; r += c.ctas) {
       char* row = static_cast<char*>(c.grad) + r * c.stride * type_bytes(c.type);
-      for (int col = 4 * threadIdx.x; col < c.width; col += 4 * kSortThreads)
+      for (int col = 4 * threadIdx.x; col < c.width; col += 4 * blockDim.x)
         store_raw4(row, c.type, col, c.width, fits && col + 4 <= c.width, zero);
     }
   }
 }
 
-__global__ void __launch_bounds__(kSortThreads) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
+__global__ void __launch_bounds__(kRankThreads) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
 
 // The sort's key of a token: its row, or `rows` for one that is left out.
 __device__ __forceinline__ unsigned key_of(const SortParams& p, long long id) {
@@ -181,48 +184,62 @@ __device__ __forceinline__ void load_keys(const SortParams& p, long long first, 
   for (int j = 0; j < N; ++j) key[j] = key_of(p, id[j]);
 }
 
+__device__ __forceinline__ void clear_counters(const SortParams& p, int cta, int ctas) {
+  for (long long i = (long long)cta * blockDim.x + threadIdx.x; i < p.counters; i += (long long)ctas * blockDim.x) p.joined[i] = 0u;
+}
+
+// Quads of tokens that each warp of rank_kernel goes over.
+__host__ __device__ inline int rank_quads(int count) { return (count + 4 * kRankWarps - 1) / (4 * kRankWarps); }
+
 // Few tokens: a token's place is the number of tokens before it, by row and place in one number (`shift` bits
 // of place).  T^2 comparisons of a cycle or two on all lanes.
-__global__ void __launch_bounds__(kSortThreads) rank_kernel(const __grid_constant__ SortParams p) {
+__global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constant__ SortParams p) {
   extern __shared__ uint4 ranked[];                        // p.count numbers, filled up with the largest
-  __shared__ unsigned before[kSortWarps][kRankPer];
+  __shared__ unsigned before[kRankWarps][kRankPer];
   const int ctas = (p.count + kRankPer - 1) / kRankPer;
   if ((int)blockIdx.x >= ctas) {
     clear_share(p.clear, blockIdx.x - ctas);
     return;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.num_long = 0u;
+  clear_counters(p, blockIdx.x, ctas);
   unsigned* all = reinterpret_cast<unsigned*>(ranked);
-  const int four = (p.count + 4 * kSortWarps - 1) / (4 * kSortWarps);       // quads per warp
-  for (int t0 = threadIdx.x; t0 < 4 * kSortWarps * four; t0 += 8 * kSortThreads) {
+  const int four = rank_quads(p.count);
+  for (int t0 = threadIdx.x; t0 < 4 * kRankWarps * four; t0 += 8 * kRankThreads) {
     unsigned key[8];
-    load_keys<8>(p, t0, kSortThreads, key);
+    load_keys<8>(p, t0, kRankThreads, key);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int t = t0 + j * kSortThreads;
-      if (t < 4 * kSortWarps * four) all[t] = t < p.count ? key[j] << p.shift | (unsigned)t : 0xFFFFFFFFu;
+      const int t = t0 + j * kRankThreads;
+      if (t < 4 * kRankWarps * four) all[t] = t < p.count ? key[j] << p.shift | (unsigned)t : 0xFFFFFFFFu;
     }
   }
   __syncthreads();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int mine = blockIdx.x * kRankPer + lane;
-  const unsigned x = all[min(mine, p.count - 1)];
-  unsigned n = 0u;
+  const unsigned x0 = all[min(mine, p.count - 1)], x1 = all[min(mine + 32, p.count - 1)];
+  unsigned n0 = 0u, n1 = 0u;
 #pragma unroll 4
   for (int q = warp * four; q < (warp + 1) * four; ++q) {
     const uint4 y = ranked[q];
-    n += y.x < x ? 1u : 0u;
-    n += y.y < x ? 1u : 0u;
-    n += y.z < x ? 1u : 0u;
-    n += y.w < x ? 1u : 0u;
+    n0 += y.x < x0 ? 1u : 0u;
+    n1 += y.x < x1 ? 1u : 0u;
+    n0 += y.y < x0 ? 1u : 0u;
+    n1 += y.y < x1 ? 1u : 0u;
+    n0 += y.z < x0 ? 1u : 0u;
+    n1 += y.z < x1 ? 1u : 0u;
+    n0 += y.w < x0 ? 1u : 0u;
+    n1 += y.w < x1 ? 1u : 0u;
   }
-  before[warp][lane] = n;
+  before[warp][lane] = n0;
+  before[warp][lane + 32] = n1;
   __syncthreads();
-  if (warp != 0 || mine >= p.count) return;
+  const int t = blockIdx.x * kRankPer + threadIdx.x;
+  if (threadIdx.x >= kRankPer || t >= p.count) return;
+  unsigned n = 0u;
 #pragma unroll
-  for (int w = 1; w < kSortWarps; ++w) n += before[w][lane];
-  p.out_keys[n] = x >> p.shift;
-  p.out_places[n] = (unsigned)mine;
+  for (int w = 0; w < kRankWarps; ++w) n += before[w][threadIdx.x];
+  p.out_keys[n] = all[t] >> p.shift;
+  p.out_places[n] = (unsigned)t;
 }
 
 // Many tokens: at most 9 bits a pass, lowest first.  Counts of each digit in each CTA's run of tokens; then
@@ -233,7 +250,7 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid
     clear_share(p.clear, blockIdx.x - p.runs);
     return;
   }
-  if (p.keys == nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.num_long = 0u;
+  if (p.keys == nullptr) clear_counters(p, blockIdx.x, p.runs);
   for (int d = threadIdx.x; d < p.digits; d += kSortThreads) n[d] = 0u;
   unsigned key[kSortItems];
   const long long first = (long long)blockIdx.x * kSortRun + threadIdx.x;
@@ -246,18 +263,12 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid
   for (int d = threadIdx.x; d < p.digits; d += kSortThreads) p.counts[(size_t)blockIdx.x * p.digits + d] = n[d];
 }
 
-// Exclusive running sum over the digits, in place (shared memory), by the whole CTA.
+// Exclusive running sum over the digits, in place (shared memory), by the whole CTA: a digit to a thread.
 __device__ __forceinline__ void scan_digits(unsigned* total, int digits, unsigned* warp_total) {
-  constexpr int kPer = kDigits / kSortThreads;
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  unsigned x[kPer], sum = 0u;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int d = threadIdx.x * kPer + k;
-    x[k] = d < digits ? total[d] : 0u;
-    sum += x[k];
-  }
-  unsigned upto = sum;
+  static_assert(kDigits <= kSortThreads, "a digit to a thread");
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, d = threadIdx.x;
+  const unsigned x = d < digits ? total[d] : 0u;
+  unsigned upto = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const unsigned other = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -265,14 +276,9 @@ __device__ __forceinline__ void scan_digits(unsigned* total, int digits, unsigne
   }
   if (lane == 31) warp_total[warp] = upto;
   __syncthreads();
-  unsigned at = upto - sum;
-  for (int w = 0; w < warp; ++w) at += warp_total[w];
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int d = threadIdx.x * kPer + k;
-    if (d < digits) total[d] = at;
-    at += x[k];
-  }
+  unsigned at = upto - x;
+  for (int w = 0; w < warp && d < digits; ++w) at += warp_total[w];
+  if (d < digits) total[d] = at;
   __syncthreads();
 }
 
@@ -312,40 +318,35 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   unsigned short rank[kSortItems];
   const long long base = (long long)blockIdx.x * kSortRun + warp * (32 * kSortItems) + lane;
   load_keys<kSortItems>(p, base, 32, key);
-  // counts of two neighbouring digits of all runs, and of the runs before this one
-  const int d2 = 2 * threadIdx.x;
-  static_assert(kDigits == 2 * kSortThreads, "two digits to a thread");
-  uint2 earlier = make_uint2(0u, 0u);
-  if (d2 < p.digits) {
-    const uint2* counts = reinterpret_cast<const uint2*>(p.counts + d2);
-    const size_t step = (size_t)p.digits / 2;
+  unsigned place[kSortItems];
+#pragma unroll
+  for (int j = 0; j < kSortItems; ++j)
+    place[j] = p.places == nullptr ? (unsigned)(base + 32 * j) : base + 32 * j < p.count ? p.places[base + 32 * j] : 0u;
+  // this thread's digit in all runs, and in the runs before this one
+  const int digit = threadIdx.x;
+  unsigned earlier = 0u;
+  if (digit < p.digits) {
+    const unsigned* counts = p.counts + digit;
+    unsigned n = 0u;
     if (p.scanned) {
-      earlier = counts[blockIdx.x * step];
-      start[d2] = 0u;
-      start[d2 + 1] = 0u;
+      earlier = counts[(size_t)blockIdx.x * p.digits];
     } else {
-      uint2 n = make_uint2(0u, 0u);
-      for (int r0 = 0; r0 < p.runs; r0 += 16) {
-        uint2 x[16];
+      for (int r0 = 0; r0 < p.runs; r0 += 32) {
+        unsigned x[32];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = r0 + j < p.runs ? counts[(r0 + j) * step] : make_uint2(0u, 0u);
+        for (int j = 0; j < 32; ++j) x[j] = r0 + j < p.runs ? counts[(size_t)(r0 + j) * p.digits] : 0u;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < 32; ++j) {
           if (r0 + j == (int)blockIdx.x) earlier = n;
-          n.x += x[j].x;
-          n.y += x[j].y;
+          n += x[j];
         }
       }
-      start[d2] = n.x;
-      start[d2 + 1] = n.y;
     }
+    start[digit] = n;
   }
   __syncthreads();
   scan_digits(start, p.digits, warp_total);
-  if (d2 < p.digits) {
-    start[d2] += earlier.x;
-    start[d2 + 1] += earlier.y;
-  }
+  if (digit < p.digits) start[digit] += earlier;
 #pragma unroll
   for (int j = 0; j < kSortItems; ++j) {
     const bool live = base + 32 * j < p.count;
@@ -360,14 +361,17 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   }
   __syncthreads();
   for (int d = threadIdx.x; d < p.digits; d += kSortThreads) {
-    unsigned short n[kSortWarps];
+    unsigned at = 0u;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) n[w] = seen[w][d];
-    unsigned short at = 0;
+    for (int w0 = 0; w0 < kSortWarps; w0 += 16) {
+      unsigned n[16];
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      seen[w][d] = at;
-      at = (unsigned short)(at + n[w]);
+      for (int w = 0; w < 16; ++w) n[w] = seen[w0 + w][d];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        seen[w0 + w][d] = (unsigned short)at;
+        at += n[w];
+      }
     }
   }
   __syncthreads();
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
       const unsigned d = (key[j] >> p.shift) & (p.digits - 1);
       const unsigned to = start[d] + seen[warp][d] + rank[j];
       p.out_keys[to] = key[j];
-      p.out_places[to] = p.places != nullptr ? p.places[t] : (unsigned)t;
+      p.out_places[to] = place[j];
     }
   }
 }
@@ -387,16 +391,15 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
 //
 // The sorted tokens are cut into chunks of at most 32.  A warp takes one chunk in a tile of columns, 16 bytes to a
 // lane, and adds up the rows that begin in its chunk, following the last one into the next chunk.  Only a row that
-// covers whole chunks beyond the one that it begins in is split: it leaves a partial sum in each of its chunks
-// and its first chunk in a list, and a second launch adds those up in order.
+// covers whole chunks beyond the one that it begins in is split: it leaves a partial sum in each of its chunks.
+// Whoever leaves the last one in a group of 32 chunks adds up the group's, and whoever does that last adds up the
+// groups': in the order of the tokens, whoever it is.
 
 constexpr int kChunk = 32;
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr int kAhead = 8;                                  // rows a warp has asked for
-constexpr int kJoinThreads = 512;
-constexpr int kJoinWarps = kJoinThreads / 32;
-constexpr int kJoinCtas = 148 * 3;
+constexpr int kGroup = 32;                                 // chunks
 
 struct GradParams {
   const unsigned* keys;        // sorted; `rows` behind the last
@@ -410,11 +413,10 @@ struct GradParams {
   int grad_type;
   long long rows, grad_stride;
   int width, tiles;            // tiles: of 512 bytes of dy
-  int vector;                  // rows of dy are aligned to 16 bytes
+  int vector, grad_vector;     // rows of dy are aligned to 16 bytes, of the gradient to four elements
   int accumulate;
   float* partial;              // [chunks][2][tiles * columns]: of the row that began in an earlier chunk, of the one that goes on
-  unsigned* long_rows;         // chunks in which a split row begins
-  unsigned* num_long;
+  unsigned* joined;            // [3 chunks][tiles]: partial sums left in the group that begins there (2), groups
 };
 
 // A lane's columns: neighbours where rows are aligned to 16 bytes, else 32 apart, so that a warp's accesses stay
@@ -429,34 +431,19 @@ struct Columns {
     first = tile * 32 * COLS + (p.vector ? lane * COLS : lane);
   }
   __device__ int at(int k) const { return first + k * step; }
+  __device__ bool together(int width) const { return step == 1 && first + COLS <= width; }
 };
 
-// Asks for a lane's part of a row; it arrives in `to` (shared memory that no other lane uses).
-template <int COLS>
-__device__ __forceinline__ void ask_row(uint4* to, const void* row, const Columns<COLS>& c, int width) {
-  if (c.step == 1 && c.first + COLS <= width) {
-    const unsigned dst = (unsigned)__cvta_generic_to_shared(to);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(static_cast<const char*>(row) + (size_t)c.first * (16 / COLS))
-                 : "memory");
-  } else {
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int k = 0; k < COLS; ++k) {
-      if (c.at(k) >= width) break;
-      if constexpr (COLS == 4) w[k] = static_cast<const uint32_t*>(row)[c.at(k)];
-      else w[k / 2] |= (uint32_t) static_cast<const unsigned short*>(row)[c.at(k)] << (16 * (k % 2));
-    }
-    *to = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
+template <int TYPE>
+constexpr int kCols = TYPE == QADAM_F32 ? 4 : 8;           // in 16 bytes
 
-template <int COLS>
-__device__ __forceinline__ void row_floats(const uint4& r, int type, float (&x)[COLS]) {
+template <int TYPE>
+__device__ __forceinline__ void row_floats(const uint4& r, float (&x)[kCols<TYPE>]) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-  if constexpr (COLS == 4) {
+  if constexpr (TYPE == QADAM_F32) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(w[k]);
-  } else if (type == QADAM_BF16) {
+  } else if constexpr (TYPE == QADAM_BF16) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       x[2 * k] = __uint_as_float(w[k] << 16);
@@ -471,39 +458,64 @@ __device__ __forceinline__ void row_floats(const uint4& r, int type, float (&x)[
   }
 }
 
+// A lane's part of a row that is not 16 aligned bytes.
 template <int COLS>
-__device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, const Columns<COLS>& c, bool fits, const float (&sum)[COLS]) {
-  char* dst = static_cast<char*>(p.grad) + (long long)row * p.grad_stride * type_bytes(p.grad_type);
-  if (c.step == 1) {
+__device__ __noinline__ uint4 gather_row(const void* row, Columns<COLS> c, int width) {
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int q = 0; q < COLS; q += 4) {
-      const int col = c.first + q;
-      if (col >= p.width) break;
-      const bool whole = fits && col + 4 <= p.width;
-      float x[4];
+  for (int k = 0; k < COLS; ++k) {
+    if (c.at(k) >= width) break;
+    if constexpr (COLS == 4) w[k] = static_cast<const uint32_t*>(row)[c.at(k)];
+    else w[k / 2] |= (uint32_t) static_cast<const unsigned short*>(row)[c.at(k)] << (16 * (k % 2));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ char* grad_row(const GradParams& p, unsigned row) {
+  return static_cast<char*>(p.grad) + (long long)row * p.grad_stride * type_bytes(p.grad_type);
+}
+
+template <int COLS>
+struct Sum {
+  float x[COLS];
+};
+
+// A row's last step where its columns are not all there, or not aligned.
+template <int COLS>
+__device__ __noinline__ void finish_row_apart(const GradParams& p, char* dst, Columns<COLS> c, Sum<COLS> sum) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, sum[q + k]);
-      if (p.accumulate) {
-        float old[4];
-        to_floats(load_raw4(dst, p.grad_type, col, p.width, whole), p.grad_type, old);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(old[k], x[k]);
-      }
-      store_raw4(dst, p.grad_type, col, p.width, whole, from_floats(x, p.grad_type));
+  for (int k = 0; k < COLS; ++k) {
+    const int col = c.at(k);
+    if (col >= p.width) break;
+    float x[4] = {__fmul_rn(p.scale, sum.x[k]), 0.0f, 0.0f, 0.0f};
+    if (p.accumulate) {
+      float old[4];
+      to_floats(load_raw4(dst, p.grad_type, col, col + 1, false), p.grad_type, old);
+      x[0] = __fadd_rn(old[0], x[0]);
     }
-  } else {
+    store_raw4(dst, p.grad_type, col, col + 1, false, from_floats(x, p.grad_type));
+  }
+}
+
+template <int COLS>
+__device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, const Columns<COLS>& c, const Sum<COLS>& sum) {
+  char* dst = grad_row(p, row);
+  if (!p.grad_vector || !c.together(p.width)) {
+    if (c.first < p.width) finish_row_apart<COLS>(p, dst, c, sum);
+    return;
+  }
 #pragma unroll
-    for (int k = 0; k < COLS; ++k) {
-      const int col = c.at(k);
-      if (col >= p.width) break;
-      float x[4] = {__fmul_rn(p.scale, sum[k]), 0.0f, 0.0f, 0.0f};
-      if (p.accumulate) {
-        float old[4];
-        to_floats(load_raw4(dst, p.grad_type, col, col + 1, false), p.grad_type, old);
-        x[0] = __fadd_rn(old[0], x[0]);
-      }
-      store_raw4(dst, p.grad_type, col, col + 1, false, from_floats(x, p.grad_type));
+  for (int q = 0; q < COLS; q += 4) {
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, sum.x[q + k]);
+    if (p.accumulate) {
+      float old[4];
+      to_floats(load_raw4(dst, p.grad_type, c.first + q, 0, true), p.grad_type, old);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(old[k], x[k]);
     }
+    store_raw4(dst, p.grad_type, c.first + q, 0, true, from_floats(x, p.grad_type));
   }
 }
 
@@ -513,94 +525,15 @@ __device__ __forceinline__ float4* partial_of(const GradParams& p, int chunk, in
   return reinterpret_cast<float4*>(p.partial + ((((long long)chunk * 2 + which) * p.tiles + tile) * 32 + threadIdx.x % 32) * COLS);
 }
 
-template <int COLS>
-__global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid_constant__ GradParams p) {
-  __shared__ uint4 ring[kSumWarps][kAhead][32];
-  const long long unit = (long long)blockIdx.x * kSumWarps + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
-  if (unit >= (long long)p.chunks * p.tiles) return;
-  const int chunk = (int)(unit / p.tiles), tile = (int)(unit % p.tiles);
-  const int begin = chunk * p.chunk, n = min(p.chunk, p.count - begin);
-  const unsigned none = (unsigned)p.rows;
-  // this chunk's tokens and the next one's, and whether its first row began before it, or before the chunk before it
-  const unsigned key0 = begin + lane < p.count ? p.keys[begin + lane] : none;
-  const unsigned key1 = begin + 32 + lane < p.count ? p.keys[begin + 32 + lane] : none;
-  const unsigned place0 = begin + lane < p.count ? p.places[begin + lane] : 0u;
-  const unsigned place1 = begin + 32 + lane < p.count ? p.places[begin + 32 + lane] : 0u;
-  const unsigned before = begin > 0 ? p.keys[begin - 1] : none;
-  const unsigned long_before = begin > p.chunk ? p.keys[begin - p.chunk - 1] : none;
-  auto key_at = [&](int i) { return i < 32 ? __shfl_sync(0xFFFFFFFFu, key0, i) : __shfl_sync(0xFFFFFFFFu, key1, i - 32); };
-  const unsigned first = key_at(0), last = key_at(n - 1);
-  if (first == none) return;
-  const bool whole = n == p.chunk && first == last;                 // the chunk is part of one row
-  const bool from_before = before == first;
-  const bool split_before = from_before && (whole || long_before == first);     // and leaves a partial sum here
-  // the last row: goes on into a chunk that is part of it, or ends in the next chunk
-  const bool split_after = last != none && key_at(n) == last && begin + 2 * p.chunk <= p.count && key_at(2 * p.chunk - 1) == last &&
-                           n == p.chunk;
-  // which of the window's 64 tokens are this warp's: none of a row that the chunk before follows up to here
-  int from = 0, to = n;
-  if (from_before && !split_before) {
-    while (from < n && key_at(from) == first) ++from;               // (fewer than a chunk)
-    if (from == n) return;
-  }
-  if (!split_after && !(split_before && whole) && last != none) {
-    while (to < 64 && key_at(to) == last) ++to;
-  }
-  const Columns<COLS> c(p, tile);
-  const bool fits = aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0;
-  uint4(*mine)[32] = ring[threadIdx.x / 32];
-  auto ask = [&](int i) {
-    if (i < to) {
-      const unsigned row = i < 32 ? __shfl_sync(0xFFFFFFFFu, place0, i) : __shfl_sync(0xFFFFFFFFu, place1, i - 32);
-      if (key_at(i) != none)
-        ask_row<COLS>(&mine[i % kAhead][lane], static_cast<const char*>(p.dy) + (long long)row * p.dy_stride * (16 / COLS), c, p.width);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-#pragma unroll 1
-  for (int i = from; i < from + kAhead; ++i) ask(i);
-  float sum[COLS];
-#pragma unroll
-  for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
-  unsigned current = key_at(from);
-  bool leaves = split_before;                                       // the current row's sum is a partial one of slot 0
-#pragma unroll 1
-  for (int i = from; i < to; ++i) {
-    if (current == none) break;
-    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-    float x[COLS];
-    row_floats<COLS>(mine[i % kAhead][lane], p.dy_type, x);
-#pragma unroll
-    for (int k = 0; k < COLS; ++k) sum[k] = __fadd_rn(sum[k], x[k]);
-    ask(i + kAhead);
-    const unsigned next = i + 1 < to ? key_at(i + 1) : none;
-    if (next != current || i + 1 == to) {
-      const bool goes_on = i + 1 == to && split_after;
-      if (leaves || goes_on) {
-        float4* out = partial_of<COLS>(p, chunk, leaves ? 0 : 1, tile);
-#pragma unroll
-        for (int q = 0; q < COLS / 4; ++q) out[q] = make_float4(sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]);
-        if (!leaves && tile == 0 && lane == 0) p.long_rows[atomicAdd(p.num_long, 1u)] = (unsigned)chunk;
-      } else {
-        finish_row<COLS>(p, current, c, fits, sum);
-      }
-      leaves = false;
-      current = next;
-#pragma unroll
-      for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
-    }
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-}
-
-// First place in [lo, hi) whose key is above `key`, by the whole warp.
-__device__ __forceinline__ int behind(const unsigned* keys, unsigned key, int lo, int hi) {
+// First place in [lo, hi) whose key is not below `key` (AFTER: is above it), by the whole warp.
+template <bool AFTER>
+__device__ __forceinline__ int search(const unsigned* keys, unsigned key, int lo, int hi) {
   const int lane = threadIdx.x % 32;
   while (lo < hi) {
     const int step = (hi - lo + 31) / 32;
     const long long at = (long long)lo + (long long)lane * step;
-    const int n = __popc(__ballot_sync(0xFFFFFFFFu, at < hi && keys[min(at, (long long)hi - 1)] <= key));
+    const unsigned k = keys[min(at, (long long)hi - 1)];
+    const int n = __popc(__ballot_sync(0xFFFFFFFFu, at < hi && (AFTER ? k <= key : k < key)));
     if (n == 0) return lo;
     hi = (int)min((long long)hi, (long long)lo + (long long)n * step);
     lo += (n - 1) * step + 1;
@@ -608,67 +541,183 @@ __device__ __forceinline__ int behind(const unsigned* keys, unsigned key, int lo
   return lo;
 }
 
-// The split rows, one to a CTA and tile at a time: every warp adds up a part of the row's chunks, in order, and the
-// first one the parts.
+// Counts a partial sum that this warp has left; true if it is the last of `of`, whose sums can then be read.
+__device__ __forceinline__ bool left_last(unsigned* counter, int of) {
+  __threadfence();
+  __syncwarp();
+  unsigned n = 0u;
+  if (threadIdx.x % 32 == 0) n = atomicAdd(counter, 1u);
+  n = __shfl_sync(0xFFFFFFFFu, n, 0);
+  __threadfence();
+  return n == (unsigned)of - 1u;
+}
+
 template <int COLS>
-__global__ void __launch_bounds__(kJoinThreads) join_rows_kernel(const __grid_constant__ GradParams p) {
-  __shared__ float4 part[kJoinWarps][COLS / 4][32];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const long long work = (long long)*p.num_long * p.tiles;
-  for (long long w = blockIdx.x; w < work; w += gridDim.x) {
-    const int chunk = (int)p.long_rows[w / p.tiles], tile = (int)(w % p.tiles);
-    const int next = (chunk + 1) * p.chunk;
-    const unsigned key = p.keys[next];
-    const int pieces = (behind(p.keys, key, next, p.count) - 1) / p.chunk - chunk + 1;
-    const int each = (pieces + kJoinWarps - 1) / kJoinWarps;
-    const int lo = warp * each, hi = min(pieces, lo + each);
-    float sum[COLS];
+__device__ __forceinline__ void add_left(const GradParams& p, int chunk, bool begins, int tile, Sum<COLS>& sum) {
+  const float4* from = partial_of<COLS>(p, chunk, begins ? 1 : 0, tile);
 #pragma unroll
-    for (int k = 0; k < COLS; ++k) sum[k] = 0.0f;
-    for (int i0 = lo; i0 < hi; i0 += 4) {
-      float4 x[4][COLS / 4];
+  for (int q = 0; q < COLS / 4; ++q) {
+    const float4 x = __ldcg(from + q);
+    sum.x[4 * q] = __fadd_rn(sum.x[4 * q], x.x);
+    sum.x[4 * q + 1] = __fadd_rn(sum.x[4 * q + 1], x.y);
+    sum.x[4 * q + 2] = __fadd_rn(sum.x[4 * q + 2], x.z);
+    sum.x[4 * q + 3] = __fadd_rn(sum.x[4 * q + 3], x.w);
+  }
+}
+
+// This chunk's part of a split row.  Its group's chunks of the row: those that begin with the row, and the one before
+// them if it ends with it.
+template <int COLS>
+__device__ __noinline__ void leave_part(const GradParams& p, unsigned row, int chunk, int tile, Columns<COLS> c, Sum<COLS> sum) {
+  const int lane = threadIdx.x % 32, group = chunk / kGroup * kGroup;
+  const long long head = (long long)(group + lane) * p.chunk;
+  const bool with = group + lane < p.chunks && p.keys[head] == row;              // chunk `group + lane` begins with the row
+  const bool more = group + lane < p.chunks && head > 0 && p.keys[head - 1] == row;      // and the one before ends with it
+  const unsigned begins = __ballot_sync(0xFFFFFFFFu, with), follows = __ballot_sync(0xFFFFFFFFu, with && more);
+  // `begins` is a run of ones, or empty where the row begins in the group's last chunk
+  int first = begins == 0u ? kGroup - 1 : __ffs(begins) - 1;
+  const int last = begins == 0u ? kGroup - 1 : 31 - __clz(begins);
+  const bool before = begins != 0u && ((follows >> first) & 1u) != 0u;           // the row began before chunk `first`
+  const bool in_group = begins == 0u || first > 0 || !before;                     // the row begins in this group
+  if (before && first > 0) --first;
+  const int g0 = group + first, g1 = group + last;
+  const bool starts = in_group && chunk == g0;
+  float4* out = partial_of<COLS>(p, chunk, starts ? 1 : 0, tile);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+  for (int q = 0; q < COLS / 4; ++q) out[q] = make_float4(sum.x[4 * q], sum.x[4 * q + 1], sum.x[4 * q + 2], sum.x[4 * q + 3]);
+  if (!left_last(p.joined + ((long long)g0 * 2 + (in_group ? 1 : 0)) * p.tiles + tile, g1 - g0 + 1)) return;
 #pragma unroll
-        for (int q = 0; q < COLS / 4; ++q)
-          x[j][q] = i0 + j < hi ? partial_of<COLS>(p, chunk + i0 + j, i0 + j == 0, tile)[q] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int k = 0; k < COLS; ++k) sum.x[k] = 0.0f;
+#pragma unroll 4
+  for (int i = g0; i <= g1; ++i) add_left<COLS>(p, i, in_group && i == g0, tile, sum);
+  const bool onward = last == kGroup - 1 && (long long)(g1 + 1) * p.chunk < p.count && p.keys[(long long)(g1 + 1) * p.chunk] == row;
+  if (!in_group || onward) {
+    // more groups: this one's sum takes the place of its first part
+    float4* all = partial_of<COLS>(p, g0, in_group ? 1 : 0, tile);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+    for (int q = 0; q < COLS / 4; ++q) all[q] = make_float4(sum.x[4 * q], sum.x[4 * q + 1], sum.x[4 * q + 2], sum.x[4 * q + 3]);
+    const int row_first = in_group ? g0 : search<false>(p.keys, row, 0, group * p.chunk) / p.chunk;
+    const int row_last = onward ? (search<true>(p.keys, row, (g1 + 1) * p.chunk, p.count) - 1) / p.chunk : g1;
+    const int groups = row_last / kGroup - row_first / kGroup + 1;
+    if (!left_last(p.joined + ((long long)p.chunks * 2 + row_first) * p.tiles + tile, groups)) return;
 #pragma unroll
-        for (int q = 0; q < COLS / 4; ++q) {
-          sum[4 * q] = __fadd_rn(sum[4 * q], x[j][q].x);
-          sum[4 * q + 1] = __fadd_rn(sum[4 * q + 1], x[j][q].y);
-          sum[4 * q + 2] = __fadd_rn(sum[4 * q + 2], x[j][q].z);
-          sum[4 * q + 3] = __fadd_rn(sum[4 * q + 3], x[j][q].w);
-        }
+    for (int k = 0; k < COLS; ++k) sum.x[k] = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < groups; ++i) {
+      const int at = max(row_first, (row_first / kGroup + i) * kGroup);
+      add_left<COLS>(p, at, at == row_first, tile, sum);
     }
-    __syncthreads();                                                 // the last row's parts have been read
-#pragma unroll
-    for (int q = 0; q < COLS / 4; ++q) part[warp][q][lane] = make_float4(sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]);
-    __syncthreads();
-    if (warp == 0) {
-      for (int o = 1; o < kJoinWarps && o * each < pieces; ++o)
-#pragma unroll
-        for (int q = 0; q < COLS / 4; ++q) {
-          const float4 x = part[o][q][lane];
-          sum[4 * q] = __fadd_rn(sum[4 * q], x.x);
-          sum[4 * q + 1] = __fadd_rn(sum[4 * q + 1], x.y);
-          sum[4 * q + 2] = __fadd_rn(sum[4 * q + 2], x.z);
-          sum[4 * q + 3] = __fadd_rn(sum[4 * q + 3], x.w);
-        }
-      finish_row<COLS>(p, key, Columns<COLS>(p, tile), aligned4(p.grad, p.grad_type) && p.grad_stride % 4 == 0, sum);
+  }
+  finish_row<COLS>(p, row, c, sum);
+}
+
+// Bound by HBM where few tokens share a row (rows of dy in, rows of the gradient out), if the loop stays short: a
+// row of 512 bytes is one iteration, and everything that is the same for all lanes (addresses, where rows end) is
+// worked out once per chunk.  Rows arrive through shared memory (cp.async), so that the ring of rows under way takes
+// no registers.
+template <int TYPE>
+__global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid_constant__ GradParams p) {
+  constexpr int COLS = kCols<TYPE>;
+  __shared__ uint4 ring[kSumWarps][kAhead][32];
+  __shared__ unsigned long long address[kSumWarps][2 * kChunk];
+  const long long unit = (long long)blockIdx.x * kSumWarps + threadIdx.x / 32;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  if (unit >= (long long)p.chunks * p.tiles) return;
+  const int chunk = (int)(unit / p.tiles), tile = (int)(unit % p.tiles);
+  const int begin = chunk * p.chunk, n = min(p.chunk, p.count - begin);
+  const unsigned none = (unsigned)p.rows;
+  // a window of 64 tokens from the chunk's first on, the rows before it and before the chunk before it
+  const unsigned key0 = begin + lane < p.count ? p.keys[begin + lane] : none;
+  const unsigned key1 = begin + 32 + lane < p.count ? p.keys[begin + 32 + lane] : none;
+  const unsigned place0 = begin + lane < p.count ? p.places[begin + lane] : 0u;
+  const unsigned place1 = begin + 32 + lane < p.count ? p.places[begin + 32 + lane] : 0u;
+  const unsigned before = begin > 0 ? p.keys[begin - 1] : none;
+  const unsigned long_before = begin > p.chunk ? p.keys[begin - p.chunk - 1] : none;
+  const long long row_bytes = p.dy_stride * (16 / COLS);
+  address[warp][lane] = reinterpret_cast<unsigned long long>(p.dy) + (unsigned long long)(place0 * row_bytes);
+  address[warp][32 + lane] = reinterpret_cast<unsigned long long>(p.dy) + (unsigned long long)(place1 * row_bytes);
+  const unsigned first = __shfl_sync(0xFFFFFFFFu, key0, 0);
+  if (first == none) return;
+  // bit i: token i is the last of its row in the window
+  const unsigned up0 = __shfl_down_sync(0xFFFFFFFFu, key0, 1), up1 = __shfl_down_sync(0xFFFFFFFFu, key1, 1);
+  const unsigned second = __shfl_sync(0xFFFFFFFFu, key1, 0);
+  unsigned long long ends = __ballot_sync(0xFFFFFFFFu, key0 != (lane == 31 ? second : up0));
+  ends |= (unsigned long long)__ballot_sync(0xFFFFFFFFu, lane == 31 || key1 != up1) << 32;
+  const int live = __popc(__ballot_sync(0xFFFFFFFFu, key0 != none)) + __popc(__ballot_sync(0xFFFFFFFFu, key1 != none));
+  const bool from_before = before == first;
+  const int end0 = __ffsll((long long)ends);                         // behind the first row
+  const bool full = n == p.chunk;
+  const bool whole = full && end0 >= n;                              // the chunk is part of one row
+  const bool split_before = from_before && (whole || long_before == first);      // and leaves a partial sum here
+  // tokens from .. to are this warp's: none of a row that the chunk before follows up to here, and all of its own last
+  // one unless that goes on into a chunk that is part of it
+  const int from = from_before && !split_before ? end0 : 0;
+  const int last_end = __ffsll((long long)(ends >> (n - 1))) + n - 1;            // behind the row of the chunk's last token
+  const bool split_after = full && live >= n && last_end >= 2 * p.chunk;
+  const int to = min(live, split_after || (split_before && whole) ? n : last_end);
+  if (from >= n || from >= live) return;
+  __syncwarp();
+
+  const Columns<COLS> c(p, tile);
+  const bool together = c.together(p.width), some = c.first < p.width;
+  const unsigned long long lane_bytes = (unsigned long long)c.first * (16 / COLS);
+  const unsigned slot0 = (unsigned)__cvta_generic_to_shared(&ring[warp][0][lane]);
+  auto ask = [&](unsigned i) {
+    if (i < (unsigned)to && some) {
+      const unsigned long long row = address[warp][i];
+      if (together)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + i % kAhead * 512u), "l"(row + lane_bytes) : "memory");
+      else
+        ring[warp][i % kAhead][lane] = gather_row<COLS>(reinterpret_cast<const void*>(row), c, p.width);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (p.accumulate && some) {
+    // rows that will be added to are brought near while those of dy arrive
+    for (int i = from; i < to; ++i)
+      if (((ends >> i) & 1ull) != 0)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(grad_row(p, p.keys[begin + i]) + (size_t)c.first * type_bytes(p.grad_type)));
+  }
+#pragma unroll 1
+  for (unsigned i = from; i < (unsigned)from + kAhead; ++i) ask(i);
+  Sum<COLS> sum;
+#pragma unroll
+  for (int k = 0; k < COLS; ++k) sum.x[k] = 0.0f;
+  bool leaves = split_before;                                        // the row's sum is a partial one
+  // bit 0: this token ends its row, or what this warp has of it
+  ends = (ends | 1ull << (to - 1)) >> from;
+#pragma unroll 1
+  for (unsigned i = from; i < (unsigned)to; ++i) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    float x[COLS];
+    row_floats<TYPE>(ring[warp][i % kAhead][lane], x);
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) sum.x[k] = __fadd_rn(sum.x[k], x[k]);
+    ask(i + kAhead);
+    if (((unsigned)ends & 1u) != 0u) {
+      const bool goes_on = i + 1 == (unsigned)to && split_after;
+      if (leaves || goes_on) {
+        leave_part<COLS>(p, p.keys[begin + i], chunk, tile, c, sum);
+      } else {
+        finish_row<COLS>(p, p.keys[begin + i], c, sum);
+      }
+      leaves = false;
+#pragma unroll
+      for (int k = 0; k < COLS; ++k) sum.x[k] = 0.0f;
+    }
+    ends >>= 1;
   }
 }
 
 // ---------------------------------------------------------------- host side
 
-// A chunk is 32 tokens, or fewer where that would leave SMs without enough warps to keep their loads in
+// A chunk is 32 tokens, or fewer (down to 2) where that would leave SMs without enough warps to keep their loads in
 // flight: below `kWarps` warps over 512 bytes of columns.
 constexpr int64_t kWarps = 148 * 16;
+constexpr int kLeastChunk = 2;
 
 struct GradLayout {
-  size_t keys[2], places[2], counts, partial, long_rows, bytes;
+  size_t keys[2], places[2], counts, partial, joined, bytes;
   int runs, chunk, chunks;
 };
 
@@ -677,13 +726,15 @@ int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
     return QADAM_ERR_SIZE;
   const int64_t tiles = (width + 127) / 128;                 // 512 bytes of binary32; half as many of 16-bit types
   l->runs = (int)((count + kSortRun - 1) / kSortRun);
-  // tokens from which chunks of 16 and 32 are taken
-  const int64_t at16 = kWarps * 16 / ((width + 255) / 256), at32 = 2 * at16;
-  l->chunk = count >= at32 ? 32 : count >= at16 ? 16 : 8;
+  int64_t room = 1;                                          // chunks of any batch up to this one
+  for (int chunk = kLeastChunk;; chunk *= 2) {
+    const int64_t enough = kWarps * 2 * chunk / ((width + 255) / 256);        // tokens for chunks of twice as many
+    room = std::max<int64_t>(room, (std::min(count, enough) + chunk - 1) / chunk);
+    l->chunk = chunk;
+    if (chunk == kChunk || count < enough) break;
+  }
+  if (l->chunk == kChunk) room = std::max<int64_t>(room, (count + kChunk - 1) / kChunk);
   l->chunks = (int)((count + l->chunk - 1) / l->chunk);
-  // room for any shorter batch too
-  const int64_t room = std::max(std::max((std::min(count, at16) + 7) / 8, count >= at16 ? (std::min(count, at32) + 15) / 16 : 0),
-                                count >= at32 ? (count + 31) / 32 : 0);
   if (room * tiles > (int64_t)1 << 33) return QADAM_ERR_SIZE;
   size_t at = 0;
   const size_t list = round_up256((size_t)count * sizeof(unsigned));
@@ -695,8 +746,8 @@ int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
   }
   l->counts = at;
   at += round_up256((size_t)l->runs * kDigits * sizeof(unsigned));
-  l->long_rows = at;                                         // their number before them
-  at += 256 + round_up256((size_t)room * sizeof(unsigned));
+  l->joined = at;
+  at += round_up256((size_t)(room * 3 * tiles) * sizeof(unsigned));
   l->partial = at;
   at += (size_t)room * 2 * ((width + 255) / 256 * 256) * sizeof(float);
   l->bytes = at + 256;
@@ -817,29 +868,29 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   const long long to_clear = accumulate ? 0 : c.dense ? rows * row_bytes / 16 : rows;
   const int launches = count == 0 || ranked ? 1 : 2 * passes;
   int launch = 0;
-  auto share = [&]() {
+  auto share = [&](int threads) {
     c.begin = to_clear * launch / launches;
     c.end = to_clear * (launch + 1) / launches;
     ++launch;
-    const long long each = c.dense ? kSortThreads : 1;
-    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearCtas);
+    const long long each = c.dense ? threads : 1;
+    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearThreads / threads);
   };
   if (count == 0) {
-    share();
-    if (c.ctas > 0) clear_kernel<<<c.ctas, kSortThreads, 0, st>>>(c);
+    share(kRankThreads);
+    if (c.ctas > 0) clear_kernel<<<c.ctas, kRankThreads, 0, st>>>(c);
     return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
   }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
   s.padding = padding; s.status = status; s.digits = 1 << digit; s.scanned = scanned;
   s.counts = list(l.counts);
-  s.num_long = list(l.long_rows);
+  s.joined = list(l.joined);
+  s.counters = (long long)l.chunks * 3 * g.tiles;
   s.out_keys = list(l.keys[0]);
   s.out_places = list(l.places[0]);
   if (ranked) {
     s.shift = place_bits;
-    share();
-    const int four = ((int)count + 4 * kSortWarps - 1) / (4 * kSortWarps);
-    rank_kernel<<<((int)count + kRankPer - 1) / kRankPer + c.ctas, kSortThreads, (size_t)four * kSortWarps * 16, st>>>(s);
+    share(kRankThreads);
+    rank_kernel<<<((int)count + kRankPer - 1) / kRankPer + c.ctas, kRankThreads, (size_t)rank_quads((int)count) * kRankWarps * 16, st>>>(s);
     if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
   } else {
     for (int i = 0; i < passes; ++i) {
@@ -848,10 +899,10 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
       s.places = i == 0 ? nullptr : list(l.places[(i + 1) % 2]);
       s.out_keys = list(l.keys[i % 2]);
       s.out_places = list(l.places[i % 2]);
-      share();
+      share(kSortThreads);
       count_digits_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
       if (scanned) scan_counts_kernel<<<1, kSortThreads, 0, st>>>(s.counts, l.runs, s.digits);
-      share();
+      share(kSortThreads);
       place_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
       if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
     }
@@ -859,19 +910,14 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   g.keys = s.out_keys;
   g.places = s.out_places;
   g.partial = reinterpret_cast<float*>(ws + l.partial);
-  g.num_long = s.num_long;
-  g.long_rows = s.num_long + 64;
+  g.joined = s.joined;
   g.vector = is_aligned(dy, 16) && dy_stride % cols == 0;
+  g.grad_vector = is_aligned(grad, 4 * type_bytes(grad_type)) && grad_stride % 4 == 0;
   const long long units = (long long)l.chunks * g.tiles;
   const unsigned grid = (unsigned)((units + kSumWarps - 1) / kSumWarps);
-  if (cols == 4) sum_chunks_kernel<4><<<grid, kSumThreads, 0, st>>>(g);
-  else sum_chunks_kernel<8><<<grid, kSumThreads, 0, st>>>(g);
-  // a row is split from two whole chunks on
-  if (l.chunks > 1) {
-    const int ctas = (int)std::min<long long>(units, kJoinCtas);
-    if (cols == 4) join_rows_kernel<4><<<ctas, kJoinThreads, 0, st>>>(g);
-    else join_rows_kernel<8><<<ctas, kJoinThreads, 0, st>>>(g);
-  }
+  if (dy_type == QADAM_F32) sum_chunks_kernel<QADAM_F32><<<grid, kSumThreads, 0, st>>>(g);
+  else if (dy_type == QADAM_BF16) sum_chunks_kernel<QADAM_BF16><<<grid, kSumThreads, 0, st>>>(g);
+  else sum_chunks_kernel<QADAM_F16><<<grid, kSumThreads, 0, st>>>(g);
   return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
