@@ -877,7 +877,8 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   };
   if (count == 0) {
     share(kRankThreads);
-    if (c.ctas > 0) clear_kernel<<<c.ctas, kRankThreads, 0, st>>>(c);
+    if (c.ctas == 0) return QADAM_OK;
+    clear_kernel<<<c.ctas, kRankThreads, 0, st>>>(c);
     return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
   }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
