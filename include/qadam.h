@@ -422,7 +422,7 @@ int qadam_norm_destroy(qadam_norm* ctx);
  * 8-bit moments (state_bits = 8): m and r = sqrt(v) as codes of one byte and one binary32 scale
  * per 128 elements (a row of the padded layout): the largest |m| (r) of the row, at least 2^-126.
  * y = |m| / scale is a floating-point number of 3 mantissa bits, code = 8 (exponent of y) +
- * mantissa + 127, 0 below code 1, the sign in bit 7: 1.0 is code 127.  r has 4 mantissa bits,
+ * mantissa + 127, 0 below code 1, the sign bit of m in bit 7: 1.0 is code 127.  r has 4 mantissa bits,
  * code = 16 exponent + mantissa + 255, at least 1 unless r = 0: a second moment that is not zero
  * does not become zero.  A row's largest value is held exactly, so a row that decays as a whole
  * decays in its scale.  The others are rounded at random (up or down to the next code, so that the

@@ -18,6 +18,7 @@ using namespace qadam;
 namespace {
 
 constexpr int kAdamThreads = 256;
+constexpr int kAdamCtas = 4;                                   // at least so many per SM
 constexpr int kPair = 256;                                     // elements of two rows: what a warp takes at a time
 constexpr int kAdamTile = kAdamThreads / 32 * kPair;           // 2048 elements per CTA
 constexpr unsigned kLeastScale = 0x00800000u;                  // 2^-126
@@ -46,6 +47,11 @@ __host__ __device__ inline StepScalars step_scalars(double lr, float beta1, floa
   return s;
 }
 
+// Keys of the ten rounds of Philox4x32-10.
+struct RoundKeys {
+  unsigned k[20];
+};
+
 struct AdamParams {
   const Tile* tiles;           // runs of at most kAdamTile elements: offset inside the tensor, count, tensor
   const AdamTensor* tensors;
@@ -60,41 +66,56 @@ struct AdamParams {
   void* v;
   float* m_scale;
   float* r_scale;
-  unsigned seed_lo, seed_hi;
+  RoundKeys keys;
   unsigned* status;
 };
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
-// Code 1 .. top stands for the floating-point number whose leading bits (MANTISSA of the fraction) are code +
-// kBase; the top code is 1.0.  0 is zero.
+// A code c >= 1 stands for the floating-point number whose leading bits (MANTISSA of the fraction) are c + kBase; the
+// top code is 1.0, code 0 is zero.  Four codes lie in a word: the bits of number k go straight from their byte to
+// their place in the float, and back.
 template <int MANTISSA>
 struct Code {
   static constexpr int kDrop = 23 - MANTISSA;
-  static constexpr int kTop = MANTISSA == 3 ? 127 : 255;
-  static constexpr int kBase = (127 << MANTISSA) - kTop;
-  __device__ static float value(unsigned code) { return code == 0u ? 0.0f : __uint_as_float((code + kBase) << kDrop); }
-  // y in [0, 1] (a NaN gives the top code): `add` < 2^kDrop, then what does not fit is cut off
-  __device__ static int of(float y, unsigned add) {
-    return min((int)((__float_as_uint(y) + add) >> kDrop) - kBase, kTop);
+  static constexpr unsigned kTop = MANTISSA == 3 ? 127u : 255u;
+  static constexpr unsigned kBase = ((127u << MANTISSA) - kTop) << kDrop;
+  __device__ __forceinline__ static unsigned shifted(unsigned word, int left) { return left >= 0 ? word << left : word >> -left; }
+  // magnitude of the code in byte k
+  __device__ __forceinline__ static float value(unsigned word, int k) {
+    const unsigned c = shifted(word, kDrop - 8 * k) & (kTop << kDrop);
+    return c == 0u ? 0.0f : __uint_as_float(c + kBase);
+  }
+  // the code of y in [0, 1], in byte k: `add` < 2^kDrop, then what does not fit is cut off; at least `least` (a code
+  // in its float's place)
+  __device__ __forceinline__ static unsigned of(float y, unsigned add, int least, int k) {
+    const int c = max((int)(__float_as_uint(y) + add - kBase), least);
+    return shifted((unsigned)c, 8 * k - kDrop) & (kTop << (8 * k));
   }
 };
 using CodeM = Code<3>;
 using CodeR = Code<4>;
 
-// One row of 128 elements, four to a lane: its scale, and 1 / scale.
-__device__ __forceinline__ float row_scale(const float (&x)[4], float& inv) {
+// The largest bit pattern of four numbers without their signs: a NaN's is above all others'.
+__device__ __forceinline__ unsigned largest4(const float (&x)[4]) {
   unsigned top = 0u;
 #pragma unroll
   for (int k = 0; k < 4; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-  top = max(__reduce_max_sync(0xFFFFFFFFu, top), kLeastScale);
-  const float scale = __uint_as_float(top);
-  inv = __fdiv_rn(1.0f, scale);
-  return scale;
+  return top;
+}
+
+__device__ __forceinline__ uint4 philox(uint4 c, const RoundKeys& keys) {
+#pragma unroll
+  for (int round = 0; round < 10; ++round) {
+    const unsigned long long a = (unsigned long long)0xD2511F53u * c.x, b = (unsigned long long)0xCD9E8D57u * c.z;
+    c = make_uint4((unsigned)(b >> 32) ^ c.y ^ keys.k[2 * round], (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ keys.k[2 * round + 1],
+                   (unsigned)a);
+  }
+  return c;
 }
 
 template <bool EIGHT, int CAP>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamParams p,
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __grid_constant__ AdamParams p,
                                                              const __grid_constant__ Pointers<CAP> grads) {
   const Tile tile = p.tiles[p.first + blockIdx.x];
   const void* g = grads.at[tile.seg - p.tensor_base];
@@ -143,10 +164,8 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   uint4 coins = make_uint4(0u, 0u, 0u, 0u);
   if constexpr (EIGHT) {
     const unsigned long long quad = (unsigned long long)((T.off + begin) / 4 + lane);
-    coins = philox4x32_10(make_uint4((unsigned)quad, (unsigned)(quad >> 32), (unsigned)now.t, (unsigned)(now.t >> 32)),
-                          make_uint2(p.seed_lo, p.seed_hi));
+    coins = philox(make_uint4((unsigned)quad, (unsigned)(quad >> 32), (unsigned)now.t, (unsigned)(now.t >> 32)), p.keys);
   }
-  bool nonfinite = false;
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (r >= rows) break;
@@ -157,10 +176,9 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (EIGHT) {
-        const unsigned a = cm[r] >> (8 * k);
-        const float y = __fmul_rn(CodeM::value(a & 127u), sm[r]);
-        m[r][k] = (a & 128u) != 0u ? -y : y;
-        const float z = __fmul_rn(CodeR::value((cr[r] >> (8 * k)) & 255u), sr[r]);
+        const float y = __fmul_rn(CodeM::value(cm[r], k), sm[r]);
+        m[r][k] = __uint_as_float(__float_as_uint(y) | ((cm[r] << (24 - 8 * k)) & 0x80000000u));
+        const float z = __fmul_rn(CodeR::value(cr[r], k), sr[r]);
         v[r][k] = __fmul_rn(z, z);
       }
       const float gc = __fmul_rn(gx[k], c);
@@ -172,35 +190,37 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     }
     if (p.master != nullptr)
       *reinterpret_cast<float4*>(p.master + at) = make_float4(x[0], x[1], x[2], x[3]);
-    if (p.master == nullptr || T.w != nullptr)
-      store_raw4(T.w, T.wtype, i, T.len, wfits && i + 4 <= T.len, from_floats(x, T.wtype));
+    store_raw4(T.w, T.wtype, i, T.len, wfits && i + 4 <= T.len, from_floats(x, T.wtype));
     if constexpr (EIGHT) {
-      float im, ir;
-      const float nm = row_scale(m[r], im), nr = row_scale(root, ir);
-      nonfinite |= !finite(nm) || !finite(nr);
+      // the row's two scales, and one division for both: even lanes take m's, odd lanes r's
+      const unsigned tm = __reduce_max_sync(0xFFFFFFFFu, largest4(m[r])), tr = __reduce_max_sync(0xFFFFFFFFu, largest4(root));
+      const float mine = __uint_as_float(max((lane & 1) == 0 ? tm : tr, kLeastScale));
+      const float inverse = __fdiv_rn(1.0f, mine);
+      const float im = __shfl_sync(0xFFFFFFFFu, inverse, 0), ir = __shfl_sync(0xFFFFFFFFu, inverse, 1);
       uint32_t om = 0u, orr = 0u;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
+        // h: low half of a word for k = 0, 2, high half for 1, 3
         const unsigned word = r == 0 ? (k < 2 ? coins.x : coins.y) : (k < 2 ? coins.z : coins.w);
-        const unsigned h = k % 2 == 0 ? word & 0xFFFFu : word >> 16;
-        const int a = max(CodeM::of(__fmul_rn(fabsf(m[r][k]), im), ((h & 63u) << 14) + (1u << 13)), 0);
-        om |= (unsigned)(a | (m[r][k] < 0.0f && a > 0 ? 128 : 0)) << (8 * k);
-        const int b = max(CodeR::of(__fmul_rn(root[k], ir), ((h >> 6) << 9) + (1u << 8)), root[k] > 0.0f ? 1 : 0);
-        orr |= (unsigned)b << (8 * k);
+        const unsigned add_m = ((k % 2 == 0 ? word << 14 : word >> 2) & (63u << 14)) | (1u << 13);
+        const unsigned add_r = ((k % 2 == 0 ? word << 3 : word >> 13) & (1023u << 9)) | (1u << 8);
+        const unsigned sign = CodeM::shifted(__float_as_uint(m[r][k]), 8 * k - 24) & (128u << (8 * k));
+        om |= CodeM::of(__fmul_rn(fabsf(m[r][k]), im), add_m, 0, k) | sign;
+        orr |= CodeR::of(__fmul_rn(root[k], ir), add_r, root[k] > 0.0f ? 1 << CodeR::kDrop : 0, k);
       }
+      // a row that is not finite: code 0 times its scale is a NaN
+      if (!finite(__uint_as_float(tm))) om = 0u;
+      if (!finite(__uint_as_float(tr))) orr = 0u;
       *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.m) + at) = om;
       *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.v) + at) = orr;
-      if (lane == 0) {
-        p.m_scale[at / 128] = nm;
-        p.r_scale[at / 128] = nr;
+      if (lane < 2) {
+        (lane == 0 ? p.m_scale : p.r_scale)[at / 128] = mine;
+        if (!finite(mine)) atomicOr(p.status, QADAM_ST_NONFINITE);
       }
     } else {
       *reinterpret_cast<float4*>(static_cast<float*>(p.m) + at) = make_float4(m[r][0], m[r][1], m[r][2], m[r][3]);
       *reinterpret_cast<float4*>(static_cast<float*>(p.v) + at) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
     }
-  }
-  if constexpr (EIGHT) {
-    if (nonfinite && lane == 0) atomicOr(p.status, QADAM_ST_NONFINITE);
   }
 }
 
@@ -223,7 +243,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_moments_kernel(const uint3
       const float s = m_scale[q / 32];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float y = __fmul_rn(CodeM::value((a >> (8 * k)) & 127u), s);
+        const float y = __fmul_rn(CodeM::value(a, k), s);
         x[k] = ((a >> (8 * k)) & 128u) != 0u ? -y : y;
       }
       m32[q] = make_float4(x[0], x[1], x[2], x[3]);
@@ -233,7 +253,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_moments_kernel(const uint3
       const float s = r_scale[q / 32];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float z = __fmul_rn(CodeR::value((a >> (8 * k)) & 255u), s);
+        const float z = __fmul_rn(CodeR::value(a, k), s);
         x[k] = __fmul_rn(z, z);
       }
       v32[q] = make_float4(x[0], x[1], x[2], x[3]);
@@ -329,7 +349,10 @@ int enqueue_step(qadam_adamw* c, const StepScalars& now, const StepScalars* coun
   p.master = c->buf.master;
   p.m = c->buf.m; p.v = c->buf.v;
   p.m_scale = c->buf.m_scale; p.r_scale = c->buf.r_scale;
-  p.seed_lo = (unsigned)c->cfg.seed; p.seed_hi = (unsigned)(c->cfg.seed >> 32);
+  for (unsigned i = 0; i < 10; ++i) {
+    p.keys.k[2 * i] = (unsigned)c->cfg.seed + i * 0x9E3779B9u;
+    p.keys.k[2 * i + 1] = (unsigned)(c->cfg.seed >> 32) + i * 0xBB67AE85u;
+  }
   p.status = c->buf.status;
   const int tensors = (int)c->geo.tensors.size(), tiles = (int)c->geo.tiles.size();
   for (int s = 0; s < tensors; s += kManyPointers) {

@@ -107,7 +107,7 @@ def adamw8(x, cm, sm, cr, sr, g, k, eps, off, t, seed, scale=None):
     x, m, v = adamw32(x.reshape(shape), m, v * v, g.reshape(shape), k, eps, scale)
     h = coins(off, x.size, t, seed).reshape(shape)
     nm, zm = encode_rows(np.abs(m), 3, (2 * (h % 64) + 1) / 128, False)
-    nm = np.where((m < 0) & (nm > 0), nm + 128, nm).astype(np.uint8)
+    nm = (nm + 128 * np.signbit(m)).astype(np.uint8)
     nr, zr = encode_rows(np.sqrt(v), 4, (2 * (h // 64) + 1) / 2048, True)
     return x.reshape(-1), nm.reshape(-1), zm, nr.reshape(-1), zr
 
