@@ -408,6 +408,7 @@ int qadam_norm_destroy(qadam_norm* ctx);
  *     m  = beta1 m + c1 g'          v = beta2 v + c2 (g' g')
  *     x  = x k - a (m / (sqrt(v) b + eps))
  *     k  = 1 - lr decay,  a = lr / (1 - beta1^t),  b = 1 / sqrt(1 - beta2^t)
+ * (with 8-bit moments the quotient in x is a product with a reciprocal, off by at most 3 in its last place).
  * This is Adam with bias correction and epsilon outside the root, unlike the step of the paper
  * above, and with decay that does not pass through the moments.
  *
@@ -444,7 +445,7 @@ typedef struct {
   const int32_t* grad_type;   /* host, [S], independent of weight_type; NULL: all QADAM_F32       */
   const float* decay;         /* host, [S], each >= 0 and finite; NULL: none                      */
   float beta1, beta2;         /* in [0, 1)                                                        */
-  float eps;                  /* > 0, finite                                                      */
+  float eps;                  /* >= 2^-100, finite                                                */
   float lr;                   /* default step size, >= 0 and finite                               */
   int32_t master;             /* 1: binary32 master weights; 0: none                              */
   int32_t reserved;           /* must be 0                                                        */

@@ -21,15 +21,20 @@ constexpr int kAdamThreads = 256;
 constexpr int kAdamCtas = 4;                                   // at least so many per SM
 constexpr int kPair = 256;                                     // elements of two rows: what a warp takes at a time
 constexpr int kAdamTile = kAdamThreads / 32 * kPair;           // 2048 elements per CTA
+constexpr float kLeastEps = 7.888609052210118e-31f;            // 2^-100: 1 / (root b + eps) is then an ordinary number
 constexpr unsigned kLeastScale = 0x00800000u;                  // 2^-126
 
-struct AdamTensor {
-  void* w;
-  long long off, len;          // padded layout
+// A run of at most kAdamTile elements of one tensor.
+struct __align__(16) AdamTile {
+  void* w;                     // the tensor
+  long long begin, at;         // the run's first element: inside the tensor, in the padded layout
+  int left;                    // elements of the tensor from there on (no more than 2^30 are counted)
+  int seg;
   float decay;
-  int wtype, gtype;
-  int first_tile;
+  short wtype, gtype;
+  int reserved[2];
 };
+static_assert(sizeof(AdamTile) == 48, "three 16-byte words");
 
 // What depends on the step, rounded once from binary64.
 struct StepScalars {
@@ -53,9 +58,8 @@ struct RoundKeys {
 };
 
 struct AdamParams {
-  const Tile* tiles;           // runs of at most kAdamTile elements: offset inside the tensor, count, tensor
-  const AdamTensor* tensors;
-  int first;                   // tile of the first CTA
+  const AdamTile* tiles;
+  int first, num_tiles;        // of this launch
   int tensor_base;             // tensor of the first gradient pointer
   float beta1, beta2, c1, c2, eps;
   StepScalars now;
@@ -88,8 +92,8 @@ struct Code {
   }
   // the code of y in [0, 1], in byte k: `add` < 2^kDrop, then what does not fit is cut off; at least `least` (a code
   // in its float's place)
-  __device__ __forceinline__ static unsigned of(float y, unsigned add, int least, int k) {
-    const int c = max((int)(__float_as_uint(y) + add - kBase), least);
+  __device__ __forceinline__ static unsigned of(float y, unsigned add, unsigned least, int k) {
+    const int c = max((int)(__float_as_uint(y) + add - kBase), (int)least);
     return shifted((unsigned)c, 8 * k - kDrop) & (kTop << (8 * k));
   }
 };
@@ -114,113 +118,272 @@ __device__ __forceinline__ uint4 philox(uint4 c, const RoundKeys& keys) {
   return c;
 }
 
-template <bool EIGHT, int CAP>
-__global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __grid_constant__ AdamParams p,
-                                                             const __grid_constant__ Pointers<CAP> grads) {
-  const Tile tile = p.tiles[p.first + blockIdx.x];
-  const void* g = grads.at[tile.seg - p.tensor_base];
-  if (g == nullptr) return;
-  float c = 1.0f;
+// One element's moments and its root.
+__device__ __forceinline__ void moments(const AdamParams& p, float g, float& m, float& v, float& root) {
+  m = __fadd_rn(__fmul_rn(p.beta1, m), __fmul_rn(p.c1, g));
+  v = __fadd_rn(__fmul_rn(p.beta2, v), __fmul_rn(p.c2, __fmul_rn(g, g)));
+  root = __fsqrt_rn(v);
+}
+
+__device__ __forceinline__ StepScalars scalars_of(const AdamParams& p) { return p.counted != nullptr ? *p.counted : p.now; }
+
+// Whether the step is taken at all, and the factor of its gradients.
+__device__ __forceinline__ bool gradient_factor(const AdamParams& p, float& c) {
+  c = 1.0f;
   if (p.grad_scale != nullptr) {
     c = *p.grad_scale;
     if (!finite(c)) {
       if (threadIdx.x == 0) atomicOr(p.status, QADAM_ST_NONFINITE);
-      return;
+      return false;
     }
   }
-  const AdamTensor T = p.tensors[tile.seg];
+  return true;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamParams p,
+                                                             const __grid_constant__ Pointers<CAP> grads) {
+  const AdamTile T = p.tiles[p.first + blockIdx.x];
+  const void* g = grads.at[T.seg - p.tensor_base];
+  float c;
+  if (g == nullptr || !gradient_factor(p, c)) return;
   const int lane = threadIdx.x % 32;
-  const long long begin = tile.off + threadIdx.x / 32 * kPair;          // of the warp's two rows, inside the tensor
-  const long long i0 = begin + 4 * lane;
-  const int rows = begin >= T.len ? 0 : begin + 128 >= T.len ? 1 : 2;
+  const int i0 = threadIdx.x / 32 * kPair;                   // of the warp's two rows, inside the tile
+  const int rows = i0 >= T.left ? 0 : i0 + 128 >= T.left ? 1 : 2;
   if (rows == 0) return;
   const bool gfits = aligned4(g, T.gtype), wfits = aligned4(T.w, T.wtype);
 
   Raw4 rg[2], rx[2];
-  float m[2][4], v[2][4];
-  uint32_t cm[2], cr[2];
-  float sm[2], sr[2];
+  float4 rm[2], rv[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (r >= rows) break;
-    const long long i = i0 + 128 * r, at = T.off + i;
-    rg[r] = load_raw4(g, T.gtype, i, T.len, gfits && i + 4 <= T.len);
-    if (p.master != nullptr) rx[r] = load_raw4(p.master + T.off, QADAM_F32, i, T.len, true);
-    else rx[r] = load_raw4(T.w, T.wtype, i, T.len, wfits && i + 4 <= T.len);
-    if constexpr (EIGHT) {
-      cm[r] = *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.m) + at);
-      cr[r] = *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.v) + at);
-      sm[r] = p.m_scale[at / 128];
-      sr[r] = p.r_scale[at / 128];
-    } else {
-      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p.m) + at);
-      const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(p.v) + at);
-      m[r][0] = a.x; m[r][1] = a.y; m[r][2] = a.z; m[r][3] = a.w;
-      v[r][0] = b.x; v[r][1] = b.y; v[r][2] = b.z; v[r][3] = b.w;
-    }
+    const int i = i0 + 128 * r + 4 * lane;
+    rg[r] = load_raw4(g, T.gtype, T.begin + i, T.begin + T.left, gfits && i + 4 <= T.left);
+    if (p.master != nullptr) rx[r] = load_raw4(p.master + T.at, QADAM_F32, i, T.left, true);
+    else rx[r] = load_raw4(T.w, T.wtype, T.begin + i, T.begin + T.left, wfits && i + 4 <= T.left);
+    rm[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(p.m) + T.at + i);
+    rv[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(p.v) + T.at + i);
   }
-  const StepScalars now = p.counted != nullptr ? *p.counted : p.now;
+  const StepScalars now = scalars_of(p);
   const float keep = (float)(1.0 - now.lr * (double)T.decay);
-  uint4 coins = make_uint4(0u, 0u, 0u, 0u);
-  if constexpr (EIGHT) {
-    const unsigned long long quad = (unsigned long long)((T.off + begin) / 4 + lane);
-    coins = philox(make_uint4((unsigned)quad, (unsigned)(quad >> 32), (unsigned)now.t, (unsigned)(now.t >> 32)), p.keys);
-  }
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (r >= rows) break;
-    const long long i = i0 + 128 * r, at = T.off + i;
-    float gx[4], x[4], root[4];
+    const int i = i0 + 128 * r + 4 * lane;
+    float gx[4], x[4], m[4] = {rm[r].x, rm[r].y, rm[r].z, rm[r].w}, v[4] = {rv[r].x, rv[r].y, rv[r].z, rv[r].w};
     to_floats(rg[r], T.gtype, gx);
     to_floats(rx[r], p.master != nullptr ? (int)QADAM_F32 : T.wtype, x);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if constexpr (EIGHT) {
-        const float y = __fmul_rn(CodeM::value(cm[r], k), sm[r]);
-        m[r][k] = __uint_as_float(__float_as_uint(y) | ((cm[r] << (24 - 8 * k)) & 0x80000000u));
-        const float z = __fmul_rn(CodeR::value(cr[r], k), sr[r]);
-        v[r][k] = __fmul_rn(z, z);
-      }
-      const float gc = __fmul_rn(gx[k], c);
-      m[r][k] = __fadd_rn(__fmul_rn(p.beta1, m[r][k]), __fmul_rn(p.c1, gc));
-      v[r][k] = __fadd_rn(__fmul_rn(p.beta2, v[r][k]), __fmul_rn(p.c2, __fmul_rn(gc, gc)));
-      root[k] = __fsqrt_rn(v[r][k]);
-      const float d = __fadd_rn(__fmul_rn(root[k], now.b), p.eps);
-      x[k] = __fsub_rn(__fmul_rn(x[k], keep), __fmul_rn(now.a, __fdiv_rn(m[r][k], d)));
+      float root;
+      moments(p, __fmul_rn(gx[k], c), m[k], v[k], root);
+      const float d = __fadd_rn(__fmul_rn(root, now.b), p.eps);
+      x[k] = __fsub_rn(__fmul_rn(x[k], keep), __fmul_rn(now.a, __fdiv_rn(m[k], d)));
     }
-    if (p.master != nullptr)
-      *reinterpret_cast<float4*>(p.master + at) = make_float4(x[0], x[1], x[2], x[3]);
-    store_raw4(T.w, T.wtype, i, T.len, wfits && i + 4 <= T.len, from_floats(x, T.wtype));
-    if constexpr (EIGHT) {
-      // the row's two scales, and one division for both: even lanes take m's, odd lanes r's
-      const unsigned tm = __reduce_max_sync(0xFFFFFFFFu, largest4(m[r])), tr = __reduce_max_sync(0xFFFFFFFFu, largest4(root));
-      const float mine = __uint_as_float(max((lane & 1) == 0 ? tm : tr, kLeastScale));
-      const float inverse = __fdiv_rn(1.0f, mine);
-      const float im = __shfl_sync(0xFFFFFFFFu, inverse, 0), ir = __shfl_sync(0xFFFFFFFFu, inverse, 1);
-      uint32_t om = 0u, orr = 0u;
+    if (p.master != nullptr) *reinterpret_cast<float4*>(p.master + T.at + i) = make_float4(x[0], x[1], x[2], x[3]);
+    store_raw4(T.w, T.wtype, T.begin + i, T.begin + T.left, wfits && i + 4 <= T.left, from_floats(x, T.wtype));
+    *reinterpret_cast<float4*>(static_cast<float*>(p.m) + T.at + i) = make_float4(m[0], m[1], m[2], m[3]);
+    *reinterpret_cast<float4*>(static_cast<float*>(p.v) + T.at + i) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// ---------------------------------------------------------------- 8-bit moments
+//
+// 16 bytes an element with binary32 master weights or weights, 10 with 16-bit weights, and some 90 instructions: codes
+// in and out, a root, a reciprocal, ten Philox rounds per 8 elements.  That is more than the time of the bytes leaves
+// for: bound by instruction issue, so types are the kernel's and not the row's, products go two at a time, and
+// what a row or a pair of rows needs once is worked out by different lanes of one instruction.
+
+constexpr int kEightPairs = 2;                                 // that a warp takes one after the other
+constexpr int kEightTile = kAdamThreads / 32 * kPair * kEightPairs;      // 4096 elements per CTA
+
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Two products at a time; what they feed is added one by one, so that every operation is rounded.
+__device__ __forceinline__ void mul4(float (&out)[4], const float (&a)[4], const float (&b)[4]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // h: low half of a word for k = 0, 2, high half for 1, 3
-        const unsigned word = r == 0 ? (k < 2 ? coins.x : coins.y) : (k < 2 ? coins.z : coins.w);
-        const unsigned add_m = ((k % 2 == 0 ? word << 14 : word >> 2) & (63u << 14)) | (1u << 13);
-        const unsigned add_r = ((k % 2 == 0 ? word << 3 : word >> 13) & (1023u << 9)) | (1u << 8);
-        const unsigned sign = CodeM::shifted(__float_as_uint(m[r][k]), 8 * k - 24) & (128u << (8 * k));
-        om |= CodeM::of(__fmul_rn(fabsf(m[r][k]), im), add_m, 0, k) | sign;
-        orr |= CodeR::of(__fmul_rn(root[k], ir), add_r, root[k] > 0.0f ? 1 << CodeR::kDrop : 0, k);
-      }
-      // a row that is not finite: code 0 times its scale is a NaN
-      if (!finite(__uint_as_float(tm))) om = 0u;
-      if (!finite(__uint_as_float(tr))) orr = 0u;
-      *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.m) + at) = om;
-      *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.v) + at) = orr;
-      if (lane < 2) {
-        (lane == 0 ? p.m_scale : p.r_scale)[at / 128] = mine;
-        if (!finite(mine)) atomicOr(p.status, QADAM_ST_NONFINITE);
-      }
-    } else {
-      *reinterpret_cast<float4*>(static_cast<float*>(p.m) + at) = make_float4(m[r][0], m[r][1], m[r][2], m[r][3]);
-      *reinterpret_cast<float4*>(static_cast<float*>(p.v) + at) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
+  for (int k = 0; k < 4; k += 2) {
+    const float2 r = mul2_rn(make_float2(a[k], a[k + 1]), make_float2(b[k], b[k + 1]));
+    out[k] = r.x;
+    out[k + 1] = r.y;
+  }
+}
+__device__ __forceinline__ void mul4(float (&out)[4], const float (&a)[4], float b) {
+  const float bb[4] = {b, b, b, b};
+  mul4(out, a, bb);
+}
+
+// A lane's four elements of a row: the step, but for the moments' codes.  g: scaled.
+__device__ __forceinline__ void step_row(const AdamParams& p, float step_a, float step_b, float keep, const float (&g)[4], float (&x)[4],
+                                         uint32_t cm, uint32_t cr, float sm, float sr, float (&m)[4], float (&root)[4]) {
+  float v[4], a[4], b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    m[k] = CodeM::value(cm, k);
+    v[k] = CodeR::value(cr, k);
+  }
+  mul4(m, m, sm);
+  mul4(v, v, sr);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m[k] = __uint_as_float(__float_as_uint(m[k]) | ((cm << (24 - 8 * k)) & 0x80000000u));
+  mul4(v, v, v);
+  mul4(a, m, p.beta1);
+  mul4(b, g, p.c1);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m[k] = __fadd_rn(a[k], b[k]);
+  mul4(a, v, p.beta2);
+  mul4(b, g, g);
+  mul4(b, b, p.c2);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    root[k] = __fsqrt_rn(__fadd_rn(a[k], b[k]));
+    const float q = __fmul_rn(m[k], reciprocal(fmaf(root[k], step_b, p.eps)));
+    x[k] = fmaf(-step_a, q, __fmul_rn(x[k], keep));
+  }
+}
+
+// A lane's codes of a row.  w0, w1: the elements' random bits, the low half of a word for k = 0, 2, the high half for 1, 3.
+__device__ __forceinline__ uint2 codes_of(const float (&m)[4], const float (&root)[4], float im, float ir, unsigned w0, unsigned w1) {
+  float a[4], b[4];
+  mul4(a, m, im);
+  mul4(b, root, ir);
+  uint2 out = make_uint2(0u, 0u);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const unsigned word = k < 2 ? w0 : w1;
+    const unsigned add_m = ((k % 2 == 0 ? word << 14 : word >> 2) & (63u << 14)) | (1u << 13);
+    const unsigned add_r = ((k % 2 == 0 ? word << 3 : word >> 13) & (1023u << 9)) | (1u << 8);
+    out.x |= CodeM::of(fabsf(a[k]), add_m, 0u, k) | (CodeM::shifted(__float_as_uint(m[k]), 8 * k - 24) & (128u << (8 * k)));
+    // at least code 1 unless the root is 0: the root of the smallest binary32 number is far above 2^-126
+    out.y |= CodeR::of(b[k], add_r, min(__float_as_uint(root[k]), 1u << CodeR::kDrop), k);
+  }
+  return out;
+}
+
+// Both rows' codes, and scales.  Lane l works out the reciprocal of scale l mod 4: m's and r's of the first row, of
+// the second.  at: the lane's first element.
+__device__ __forceinline__ void put_moments(const AdamParams& p, long long t, long long at, int rows, const float (&m)[2][4],
+                                            const float (&root)[2][4]) {
+  const int lane = threadIdx.x % 32;
+  const unsigned long long quad = (unsigned long long)at / 4;
+  const uint4 coins = philox(make_uint4((unsigned)quad, (unsigned)(quad >> 32), (unsigned)t, (unsigned)(t >> 32)), p.keys);
+  const unsigned m0 = __reduce_max_sync(0xFFFFFFFFu, largest4(m[0])), r0 = __reduce_max_sync(0xFFFFFFFFu, largest4(root[0]));
+  const unsigned m1 = __reduce_max_sync(0xFFFFFFFFu, largest4(m[1])), r1 = __reduce_max_sync(0xFFFFFFFFu, largest4(root[1]));
+  const float mine = __uint_as_float(max((lane & 2) == 0 ? ((lane & 1) == 0 ? m0 : r0) : ((lane & 1) == 0 ? m1 : r1), kLeastScale));
+  const float inverse = __fdiv_rn(1.0f, mine);
+  const unsigned odd = __ballot_sync(0xFFFFFFFFu, !finite(mine));
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (r >= rows) break;
+    uint2 c = codes_of(m[r], root[r], __shfl_sync(0xFFFFFFFFu, inverse, 2 * r), __shfl_sync(0xFFFFFFFFu, inverse, 2 * r + 1),
+                       r == 0 ? coins.x : coins.z, r == 0 ? coins.y : coins.w);
+    if (odd != 0u) {                                           // a row that is not finite: code 0 times its scale is a NaN
+      if (((odd >> (2 * r)) & 1u) != 0u) c.x = 0u;
+      if (((odd >> (2 * r + 1)) & 1u) != 0u) c.y = 0u;
     }
+    *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.m) + at + 128 * r) = c.x;
+    *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(p.v) + at + 128 * r) = c.y;
+  }
+  if (lane < 2 * rows) ((lane & 1) == 0 ? p.m_scale : p.r_scale)[at / 128 + lane / 2] = mine;
+  if (odd != 0u && lane == 0) atomicOr(p.status, QADAM_ST_NONFINITE);
+}
+
+// Two rows at the end of their tensor, or of a tensor that is not aligned.
+__device__ __noinline__ void step_pair_apart(const AdamParams& p, const void* g, int t, int i0, float c) {
+  const int lane = threadIdx.x % 32;
+  const StepScalars now = scalars_of(p);
+  const AdamTile T = p.tiles[t];
+  const float keep = (float)(1.0 - now.lr * (double)T.decay);
+  const bool gfits = aligned4(g, T.gtype), wfits = aligned4(T.w, T.wtype);
+  const int rows = i0 + 128 >= T.left ? 1 : 2;
+  float m[2][4] = {}, root[2][4] = {};
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    const int i = i0 + 128 * r + 4 * lane;
+    const long long at = T.at + i;
+    float gx[4], x[4];
+    to_floats(load_raw4(g, T.gtype, T.begin + i, T.begin + T.left, gfits && i + 4 <= T.left), T.gtype, gx);
+    if (p.master != nullptr) to_floats(load_raw4(p.master + T.at, QADAM_F32, i, T.left, true), QADAM_F32, x);
+    else to_floats(load_raw4(T.w, T.wtype, T.begin + i, T.begin + T.left, wfits && i + 4 <= T.left), T.wtype, x);
+    mul4(gx, gx, c);
+    step_row(p, now.a, now.b, keep, gx, x, *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.m) + at),
+             *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.v) + at), p.m_scale[at / 128], p.r_scale[at / 128], m[r], root[r]);
+    if (p.master != nullptr) *reinterpret_cast<float4*>(p.master + at) = make_float4(x[0], x[1], x[2], x[3]);
+    store_raw4(T.w, T.wtype, T.begin + i, T.begin + T.left, wfits && i + 4 <= T.left, from_floats(x, T.wtype));
+  }
+  put_moments(p, now.t, T.at + i0 + 4 * lane, rows, m, root);
+}
+
+template <bool HALF>
+__device__ __forceinline__ Raw4 load_whole4(const char* p) {
+  if constexpr (HALF) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    return {{q.x, q.y, 0u, 0u}};
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    return {{q.x, q.y, q.z, q.w}};
+  }
+}
+
+template <bool W16, bool G16, bool MASTER, int CAP>
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw8_kernel(const __grid_constant__ AdamParams p,
+                                                                         const __grid_constant__ Pointers<CAP> grads) {
+  constexpr bool X16 = W16 && !MASTER;                         // what the step reads
+  constexpr int kGBytes = G16 ? 2 : 4, kWBytes = W16 ? 2 : 4;
+  const int t = p.first + blockIdx.x;
+  const AdamTile& T = p.tiles[t];
+  const char* const g = static_cast<const char*>(grads.at[T.seg - p.tensor_base]);
+  float c;
+  if (g == nullptr || !gradient_factor(p, c)) return;
+  const int lane = threadIdx.x % 32;
+  const int left = T.left, gtype = T.gtype, wtype = T.wtype;
+  const bool fits = ((reinterpret_cast<uintptr_t>(g) & (4 * kGBytes - 1)) | (reinterpret_cast<uintptr_t>(T.w) & (4 * kWBytes - 1))) == 0;
+  const int first = threadIdx.x / 32 * (kPair * kEightPairs);  // of the warp's elements in the tile
+  const char* from = g + (T.begin + first + 4 * lane) * kGBytes;
+  char* w = static_cast<char*>(T.w) + (T.begin + first + 4 * lane) * kWBytes;
+  long long at = T.at + first + 4 * lane;
+  const float a = scalars_of(p).a, b = scalars_of(p).b;
+  const float keep = (float)(1.0 - scalars_of(p).lr * (double)T.decay);
+#pragma unroll 1
+  for (int i0 = first; i0 < first + kPair * kEightPairs && i0 < left; i0 += kPair) {
+    if (!fits || i0 + kPair > left) {
+      step_pair_apart(p, g, t, i0, c);
+    } else {
+      Raw4 rg[2], rx[2];
+      uint32_t cm[2], cr[2];
+      float sm[2], sr[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        rg[r] = load_whole4<G16>(from + 128 * kGBytes * r);
+        rx[r] = load_whole4<X16>(MASTER ? reinterpret_cast<const char*>(p.master + at + 128 * r) : w + 128 * kWBytes * r);
+        cm[r] = *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.m) + at + 128 * r);
+        cr[r] = *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.v) + at + 128 * r);
+        sm[r] = p.m_scale[at / 128 + r];
+        sr[r] = p.r_scale[at / 128 + r];
+      }
+      float m[2][4], root[2][4];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float gx[4], x[4];
+        to_floats(rg[r], G16 ? gtype : (int)QADAM_F32, gx);
+        to_floats(rx[r], X16 ? wtype : (int)QADAM_F32, x);
+        mul4(gx, gx, c);
+        step_row(p, a, b, keep, gx, x, cm[r], cr[r], sm[r], sr[r], m[r], root[r]);
+        if constexpr (MASTER) *reinterpret_cast<float4*>(p.master + at + 128 * r) = make_float4(x[0], x[1], x[2], x[3]);
+        const Raw4 rw = from_floats(x, W16 ? wtype : (int)QADAM_F32);
+        if constexpr (W16) *reinterpret_cast<uint2*>(w + 256 * r) = make_uint2(rw.w[0], rw.w[1]);
+        else *reinterpret_cast<uint4*>(w + 512 * r) = make_uint4(rw.w[0], rw.w[1], rw.w[2], rw.w[3]);
+      }
+      put_moments(p, scalars_of(p).t, at, 2, m, root);
+    }
+    from += kPair * kGBytes;
+    w += kPair * kWBytes;
+    at += kPair;
   }
 }
 
@@ -262,10 +425,15 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_moments_kernel(const uint3
 }
 
 struct AdamGeometry {
-  std::vector<AdamTensor> tensors;
-  std::vector<Tile> tiles;
+  struct Run {                 // tiles of one launch
+    int first, num, tensor_base, tensors, kind;
+  };
+  std::vector<AdamTile> tiles;
+  std::vector<Run> runs;
+  std::vector<int> wtype, gtype;                             // [S]
+  std::vector<int64_t> off, len;
   int64_t D = 0;
-  size_t off_tensors = 0, off_now = 0, workspace_bytes = 0;
+  size_t off_now = 0, workspace_bytes = 0;
 };
 
 int adam_geometry(const qadam_adamw_config* c, AdamGeometry* g) {
@@ -274,7 +442,7 @@ int adam_geometry(const qadam_adamw_config* c, AdamGeometry* g) {
   if (!c->len) return QADAM_ERR_NULL;
   if (c->state_bits != 32 && c->state_bits != 8) return QADAM_ERR_TYPE;
   if (c->master != 0 && c->master != 1) return QADAM_ERR_SIZE;
-  if (!(c->beta1 >= 0.0f && c->beta1 < 1.0f) || !(c->beta2 >= 0.0f && c->beta2 < 1.0f) || !(c->eps > 0.0f) ||
+  if (!(c->beta1 >= 0.0f && c->beta1 < 1.0f) || !(c->beta2 >= 0.0f && c->beta2 < 1.0f) || !(c->eps >= kLeastEps) ||
       !std::isfinite(c->eps) || !(c->lr >= 0.0f) || !std::isfinite(c->lr))
     return QADAM_ERR_HYPER;
   int64_t tiles = 0, off = 0;
@@ -285,25 +453,34 @@ int adam_geometry(const qadam_adamw_config* c, AdamGeometry* g) {
     tiles += (c->len[s] + kAdamTile - 1) / kAdamTile;
     if (tiles > (int64_t)1 << 30) return QADAM_ERR_SIZE;
   }
-  g->tensors.resize(c->num_tensors);
+  const size_t S = (size_t)c->num_tensors;
   g->tiles.reserve((size_t)tiles);
-  for (int s = 0; s < c->num_tensors; ++s) {
-    AdamTensor& t = g->tensors[s];
-    t.w = nullptr;
-    t.off = off;
-    t.len = c->len[s];
-    t.decay = c->decay ? c->decay[s] : 0.0f;
-    t.wtype = c->weight_type ? c->weight_type[s] : QADAM_F32;
-    t.gtype = c->grad_type ? c->grad_type[s] : QADAM_F32;
-    t.first_tile = (int)g->tiles.size();
-    for (int64_t o = 0; o < c->len[s]; o += kAdamTile)
-      g->tiles.push_back(Tile{(long long)o, (int)std::min<int64_t>(kAdamTile, c->len[s] - o), s});
+  g->wtype.resize(S); g->gtype.resize(S); g->off.resize(S);
+  g->len.assign(c->len, c->len + S);
+  for (size_t s = 0; s < S; ++s) {
+    g->wtype[s] = c->weight_type ? c->weight_type[s] : QADAM_F32;
+    g->gtype[s] = c->grad_type ? c->grad_type[s] : QADAM_F32;
+    g->off[s] = off;
     off += (c->len[s] + kAlign - 1) / kAlign * kAlign;
   }
+  // a launch takes the tensors that it has pointers for; with 8-bit moments, those of one kind
+  const int64_t tile = c->state_bits == 8 ? kEightTile : kAdamTile;
+  for (size_t base = 0; base < S; base += kManyPointers) {
+    const size_t end = std::min(S, base + kManyPointers);
+    for (int kind = 0; kind < (c->state_bits == 8 ? 4 : 1); ++kind) {
+      const int first = (int)g->tiles.size();
+      for (size_t s = base; s < end; ++s) {
+        if (c->state_bits == 8 && kind != (g->wtype[s] == QADAM_F32 ? 0 : 2) + (g->gtype[s] == QADAM_F32 ? 0 : 1)) continue;
+        for (int64_t o = 0; o < c->len[s]; o += tile)
+          g->tiles.push_back(AdamTile{nullptr, (long long)o, (long long)(g->off[s] + o), (int)std::min<int64_t>(c->len[s] - o, 1 << 30),
+                                      (int)s, c->decay ? c->decay[s] : 0.0f, (short)g->wtype[s], (short)g->gtype[s], {0, 0}});
+      }
+      const int num = (int)g->tiles.size() - first;
+      if (num > 0) g->runs.push_back({first, num, (int)base, (int)(end - base), kind});
+    }
+  }
   g->D = off;
-  size_t wo = round_up256(g->tiles.size() * sizeof(Tile));
-  g->off_tensors = wo;
-  wo += round_up256(g->tensors.size() * sizeof(AdamTensor));
+  size_t wo = round_up256(g->tiles.size() * sizeof(AdamTile));
   g->off_now = wo;
   wo += 256;
   g->workspace_bytes = wo;
@@ -324,22 +501,38 @@ struct qadam_adamw {
 
 namespace {
 
-template <bool EIGHT, int CAP>
-int launch_adam(qadam_adamw* c, const AdamParams& p, int grid, int tensors, cudaStream_t st) {
+template <bool W16, bool G16, bool MASTER, int CAP>
+bool launch_eight(const AdamParams& p, const Pointers<CAP>& grads, cudaStream_t st) {
+  adamw8_kernel<W16, G16, MASTER, CAP><<<p.num_tiles, kAdamThreads, 0, st>>>(p, grads);
+  return cuda_call(cudaGetLastError());
+}
+
+template <int CAP>
+bool launch_adam(qadam_adamw* c, const AdamParams& p, const AdamGeometry::Run& run, cudaStream_t st) {
   static_assert(sizeof(Pointers<CAP>) + sizeof(AdamParams) <= 32764, "kernel parameters");
   Pointers<CAP> grads;
-  std::copy(c->grads.begin() + p.tensor_base, c->grads.begin() + p.tensor_base + tensors, grads.at);
-  adamw_kernel<EIGHT, CAP><<<grid, kAdamThreads, 0, st>>>(p, grads);
-  if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  std::copy(c->grads.begin() + run.tensor_base, c->grads.begin() + run.tensor_base + run.tensors, grads.at);
   c->launches += 1;
-  return QADAM_OK;
+  if (c->cfg.state_bits == 32) {
+    adamw_kernel<CAP><<<p.num_tiles, kAdamThreads, 0, st>>>(p, grads);
+    return cuda_call(cudaGetLastError());
+  }
+  switch (run.kind + (p.master != nullptr ? 4 : 0)) {
+    case 0: return launch_eight<false, false, false>(p, grads, st);
+    case 1: return launch_eight<false, true, false>(p, grads, st);
+    case 2: return launch_eight<true, false, false>(p, grads, st);
+    case 3: return launch_eight<true, true, false>(p, grads, st);
+    case 4: return launch_eight<false, false, true>(p, grads, st);
+    case 5: return launch_eight<false, true, true>(p, grads, st);
+    case 6: return launch_eight<true, false, true>(p, grads, st);
+    default: return launch_eight<true, true, true>(p, grads, st);
+  }
 }
 
 int enqueue_step(qadam_adamw* c, const StepScalars& now, const StepScalars* counted, const float* grad_scale, cudaStream_t st) {
   AdamParams p;
   unsigned char* ws = static_cast<unsigned char*>(c->buf.workspace);
-  p.tiles = reinterpret_cast<const Tile*>(ws);
-  p.tensors = reinterpret_cast<const AdamTensor*>(ws + c->geo.off_tensors);
+  p.tiles = reinterpret_cast<const AdamTile*>(ws);
   p.beta1 = c->cfg.beta1; p.beta2 = c->cfg.beta2;
   p.c1 = 1.0f - c->cfg.beta1; p.c2 = 1.0f - c->cfg.beta2;
   p.eps = c->cfg.eps;
@@ -354,18 +547,12 @@ int enqueue_step(qadam_adamw* c, const StepScalars& now, const StepScalars* coun
     p.keys.k[2 * i + 1] = (unsigned)(c->cfg.seed >> 32) + i * 0xBB67AE85u;
   }
   p.status = c->buf.status;
-  const int tensors = (int)c->geo.tensors.size(), tiles = (int)c->geo.tiles.size();
-  for (int s = 0; s < tensors; s += kManyPointers) {
-    const int count = std::min(kManyPointers, tensors - s);
-    p.tensor_base = s;
-    p.first = c->geo.tensors[s].first_tile;
-    const int grid = (s + count < tensors ? c->geo.tensors[s + count].first_tile : tiles) - p.first;
-    if (grid == 0) continue;
-    const bool few = count <= kFewPointers;
-    const int rc = c->cfg.state_bits == 8
-                       ? (few ? launch_adam<true, kFewPointers>(c, p, grid, count, st) : launch_adam<true, kManyPointers>(c, p, grid, count, st))
-                       : (few ? launch_adam<false, kFewPointers>(c, p, grid, count, st) : launch_adam<false, kManyPointers>(c, p, grid, count, st));
-    if (rc != QADAM_OK) return rc;
+  for (const AdamGeometry::Run& run : c->geo.runs) {
+    p.tensor_base = run.tensor_base;
+    p.first = run.first;
+    p.num_tiles = run.num;
+    if (!(run.tensors <= kFewPointers ? launch_adam<kFewPointers>(c, p, run, st) : launch_adam<kManyPointers>(c, p, run, st)))
+      return QADAM_ERR_CUDA;
   }
   return QADAM_OK;
 }
@@ -380,7 +567,7 @@ int qadam_adamw_query_sizes(const qadam_adamw_config* cfg, int64_t* D, int64_t* 
   if (rc != QADAM_OK) return rc;
   if (D) *D = g.D;
   if (off)
-    for (size_t s = 0; s < g.tensors.size(); ++s) off[s] = g.tensors[s].off;
+    std::copy(g.off.begin(), g.off.end(), off);
   if (workspace_bytes) *workspace_bytes = g.workspace_bytes;
   return QADAM_OK;
 } catch (const std::bad_alloc&) {
@@ -398,11 +585,11 @@ int qadam_adamw_create(const qadam_adamw_config* cfg, const qadam_adamw_buffers*
   if (!b->weights || !b->m || !b->v || !b->workspace || !b->status || !b->count || (cfg->master && !b->master) ||
       (eight && (!b->m_scale || !b->r_scale)))
     return QADAM_ERR_NULL;
-  for (size_t s = 0; s < g.tensors.size(); ++s) {
-    if (!b->weights[s] && g.tensors[s].len > 0) return QADAM_ERR_NULL;
-    if (!is_aligned(b->weights[s], type_bytes(g.tensors[s].wtype))) return QADAM_ERR_ALIGN;
-    g.tensors[s].w = b->weights[s];
+  for (size_t s = 0; s < g.len.size(); ++s) {
+    if (!b->weights[s] && g.len[s] > 0) return QADAM_ERR_NULL;
+    if (!is_aligned(b->weights[s], type_bytes(g.wtype[s]))) return QADAM_ERR_ALIGN;
   }
+  for (AdamTile& t : g.tiles) t.w = b->weights[t.seg];
   if (!is_aligned(b->m, 16) || !is_aligned(b->v, 16) || (cfg->master && !is_aligned(b->master, 16)) ||
       (eight && (!is_aligned(b->m_scale, 16) || !is_aligned(b->r_scale, 16))) || !is_aligned(b->count, 8) ||
       !is_aligned(b->status, 4) || !is_aligned(b->workspace, 256))
@@ -414,10 +601,9 @@ int qadam_adamw_create(const qadam_adamw_config* cfg, const qadam_adamw_buffers*
     return QADAM_ERR_CUDA;
   unsigned char* ws = static_cast<unsigned char*>(b->workspace);
   if (!g.tiles.empty() &&
-      !cuda_call(cudaMemcpy(ws, g.tiles.data(), g.tiles.size() * sizeof(Tile), cudaMemcpyHostToDevice)))
+      !cuda_call(cudaMemcpy(ws, g.tiles.data(), g.tiles.size() * sizeof(AdamTile), cudaMemcpyHostToDevice)))
     return QADAM_ERR_CUDA;
-  if (!cuda_call(cudaMemcpy(ws + g.off_tensors, g.tensors.data(), g.tensors.size() * sizeof(AdamTensor), cudaMemcpyHostToDevice)) ||
-      !cuda_call(cudaMemset(b->status, 0, sizeof(unsigned))) || !cuda_call(cudaStreamSynchronize(nullptr)))
+  if (!cuda_call(cudaMemset(b->status, 0, sizeof(unsigned))) || !cuda_call(cudaStreamSynchronize(nullptr)))
     return QADAM_ERR_CUDA;
   qadam_adamw* c = new qadam_adamw;
   c->cfg = *cfg;
@@ -436,9 +622,9 @@ int qadam_adamw_create(const qadam_adamw_config* cfg, const qadam_adamw_buffers*
 
 int qadam_adamw_bind(qadam_adamw* c, const void* const* grads) try {
   if (!c || !grads) return QADAM_ERR_NULL;
-  for (size_t s = 0; s < c->geo.tensors.size(); ++s)
-    if (!is_aligned(grads[s], type_bytes(c->geo.tensors[s].gtype))) return QADAM_ERR_ALIGN;
-  c->grads.assign(grads, grads + c->geo.tensors.size());
+  for (size_t s = 0; s < c->geo.len.size(); ++s)
+    if (!is_aligned(grads[s], type_bytes(c->geo.gtype[s]))) return QADAM_ERR_ALIGN;
+  c->grads.assign(grads, grads + c->geo.len.size());
   c->bound = true;
   return QADAM_OK;
 } catch (const std::bad_alloc&) {

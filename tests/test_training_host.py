@@ -53,7 +53,7 @@ def test_adamw_sizes_and_layout(lib):
     (dict(num_tensors=0), SIZE), (dict(num_tensors=(1 << 20) + 1), SIZE), (dict(reserved=1), SIZE), (dict(len=None), NULL),
     (dict(len=_i64(5, -1, 2)), SIZE), (dict(len=_i64(1 << 41, 1, 1)), SIZE), (dict(state_bits=16), TYPE), (dict(state_bits=0), TYPE),
     (dict(weight_type=_i32(0, 3, 0)), TYPE), (dict(grad_type=_i32(0, 0, -1)), TYPE), (dict(master=2), SIZE),
-    (dict(beta1=1.0), HYPER), (dict(beta1=float("nan")), HYPER), (dict(beta2=-0.1), HYPER), (dict(eps=0.0), HYPER),
+    (dict(beta1=1.0), HYPER), (dict(beta1=float("nan")), HYPER), (dict(beta2=-0.1), HYPER), (dict(eps=0.0), HYPER), (dict(eps=1e-31), HYPER),
     (dict(eps=float("inf")), HYPER), (dict(lr=-1.0), HYPER), (dict(lr=float("nan")), HYPER),
     (dict(decay=_f32(0.0, -1.0, 0.0)), HYPER), (dict(decay=_f32(0.0, float("inf"), 0.0)), HYPER),
 ])
