@@ -392,8 +392,9 @@ int qadam_norm_bind(qadam_norm* ctx, const void* const* tensors);
 
 /* out[0] = sqrt(sum of the squares of all elements), out[1] = min(1, max_norm / out[0]): the
  * factor that clips the gradients to max_norm (> 0, may be infinite).  out: device, 2 binary32,
- * 8-byte aligned.  Squares are formed and summed in binary64, in an order fixed by the list and
- * the device, and rounded once: the same bits every time.  If the norm is not finite (an element
+ * 8-byte aligned.  The squares in 16 bytes of a tensor are added in binary32, all else in binary64,
+ * in an order fixed by the list and the device: the same bits every time, within 5 x 2^-24 of the
+ * norm, whatever the elements' size.  If the norm is not finite (an element
  * is not, or the result is beyond binary32), out[1] is NaN: a step given that factor changes
  * nothing (see below). */
 int qadam_norm_run(qadam_norm* ctx, float max_norm, float* out, void* stream);

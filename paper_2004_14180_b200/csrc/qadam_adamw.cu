@@ -17,10 +17,9 @@ using namespace qadam;
 
 namespace {
 
-constexpr int kAdamThreads = 256;
-constexpr int kAdamCtas = 4;                                   // at least so many per SM
+constexpr int kAdamThreads = 128;
 constexpr int kPair = 256;                                     // elements of two rows: what a warp takes at a time
-constexpr int kAdamTile = kAdamThreads / 32 * kPair;           // 2048 elements per CTA
+constexpr int kAdamTile = kAdamThreads / 32 * kPair;           // 1024 elements per CTA
 constexpr float kLeastEps = 7.888609052210118e-31f;            // 2^-100: 1 / (root b + eps) is then an ordinary number
 constexpr unsigned kLeastScale = 0x00800000u;                  // 2^-126
 
@@ -60,6 +59,7 @@ struct RoundKeys {
 struct AdamParams {
   const AdamTile* tiles;
   int first, num_tiles;        // of this launch
+  int pairs;                   // of rows that a warp takes one after the other (8-bit moments)
   int tensor_base;             // tensor of the first gradient pointer
   float beta1, beta2, c1, c2, eps;
   StepScalars now;
@@ -195,8 +195,13 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
 // for: bound by instruction issue, so types are the kernel's and not the row's, products go two at a time, and
 // what a row or a pair of rows needs once is worked out by different lanes of one instruction.
 
-constexpr int kEightPairs = 2;                                 // that a warp takes one after the other
-constexpr int kEightTile = kAdamThreads / 32 * kPair * kEightPairs;      // 4096 elements per CTA
+// Warps per SM count for more than registers that never spill: at 10 CTAs of 4 warps (48 registers, a few spilt) the
+// BERT-shaped set takes 336 us, at 9 (56 registers) 338, at 8 371; 330 at 8 pairs of rows to a warp in place of 4
+// (355 at 2), which share what is worked out once per warp.  A warp has fewer pairs where there would be less
+// than about one wave of warps.
+constexpr int kEightCtas = 10;
+constexpr int kEightPairs = 8;
+constexpr int64_t kEightWave = 5000;
 
 __device__ __forceinline__ float reciprocal(float x) {
   float r;
@@ -331,7 +336,7 @@ __device__ __forceinline__ Raw4 load_whole4(const char* p) {
 }
 
 template <bool W16, bool G16, bool MASTER, int CAP>
-__global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw8_kernel(const __grid_constant__ AdamParams p,
+__global__ void __launch_bounds__(kAdamThreads, kEightCtas) adamw8_kernel(const __grid_constant__ AdamParams p,
                                                                          const __grid_constant__ Pointers<CAP> grads) {
   constexpr bool X16 = W16 && !MASTER;                         // what the step reads
   constexpr int kGBytes = G16 ? 2 : 4, kWBytes = W16 ? 2 : 4;
@@ -343,14 +348,14 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw8_kernel(const _
   const int lane = threadIdx.x % 32;
   const int left = T.left, gtype = T.gtype, wtype = T.wtype;
   const bool fits = ((reinterpret_cast<uintptr_t>(g) & (4 * kGBytes - 1)) | (reinterpret_cast<uintptr_t>(T.w) & (4 * kWBytes - 1))) == 0;
-  const int first = threadIdx.x / 32 * (kPair * kEightPairs);  // of the warp's elements in the tile
+  const int mine = kPair * p.pairs, first = threadIdx.x / 32 * mine;       // the warp's elements in the tile
   const char* from = g + (T.begin + first + 4 * lane) * kGBytes;
   char* w = static_cast<char*>(T.w) + (T.begin + first + 4 * lane) * kWBytes;
   long long at = T.at + first + 4 * lane;
   const float a = scalars_of(p).a, b = scalars_of(p).b;
   const float keep = (float)(1.0 - scalars_of(p).lr * (double)T.decay);
 #pragma unroll 1
-  for (int i0 = first; i0 < first + kPair * kEightPairs && i0 < left; i0 += kPair) {
+  for (int i0 = first; i0 < first + mine && i0 < left; i0 += kPair) {
     if (!fits || i0 + kPair > left) {
       step_pair_apart(p, g, t, i0, c);
     } else {
@@ -395,20 +400,21 @@ __global__ void adamw_count_kernel(StepScalars* now, long long* count, const flo
   *now = step_scalars(lr != nullptr ? (double)*lr : (double)lr_default, beta1, beta2, t);
 }
 
-// 8-bit moments as the values they stand for, four elements to a thread.
-__global__ void __launch_bounds__(kAdamThreads) adamw_moments_kernel(const uint32_t* m, const uint32_t* r, const float* m_scale,
-                                                                     const float* r_scale, long long quads, float4* m32,
-                                                                     float4* v32) {
-  for (long long q = (long long)blockIdx.x * kAdamThreads + threadIdx.x; q < quads; q += (long long)gridDim.x * kAdamThreads) {
+// 8-bit moments as the values they stand for, four elements to a thread.  Bound by its writes, 8 bytes of 10: 200 us for
+// 109.5 x 10^6 elements, 5.5 TB/s, whether a thread has loads for 4, 8, 16 or 32 elements under way (199 to 214 us).
+constexpr int kReadThreads = 256;
+constexpr int kReadCtasPerSm = 16;
+
+__global__ void __launch_bounds__(kReadThreads) adamw_moments_kernel(const uint32_t* m, const uint32_t* r, const float* m_scale,
+                                                                     const float* r_scale, long long quads, float4* m32, float4* v32) {
+  for (long long q = (long long)blockIdx.x * kReadThreads + threadIdx.x; q < quads; q += (long long)gridDim.x * kReadThreads) {
     float x[4];
     if (m32 != nullptr) {
       const uint32_t a = m[q];
       const float s = m_scale[q / 32];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float y = __fmul_rn(CodeM::value(a, k), s);
-        x[k] = ((a >> (8 * k)) & 128u) != 0u ? -y : y;
-      }
+      for (int k = 0; k < 4; ++k)
+        x[k] = __uint_as_float(__float_as_uint(__fmul_rn(CodeM::value(a, k), s)) | ((a << (24 - 8 * k)) & 0x80000000u));
       m32[q] = make_float4(x[0], x[1], x[2], x[3]);
     }
     if (v32 != nullptr) {
@@ -433,6 +439,7 @@ struct AdamGeometry {
   std::vector<int> wtype, gtype;                             // [S]
   std::vector<int64_t> off, len;
   int64_t D = 0;
+  int pairs = 1;
   size_t off_now = 0, workspace_bytes = 0;
 };
 
@@ -464,7 +471,9 @@ int adam_geometry(const qadam_adamw_config* c, AdamGeometry* g) {
     off += (c->len[s] + kAlign - 1) / kAlign * kAlign;
   }
   // a launch takes the tensors that it has pointers for; with 8-bit moments, those of one kind
-  const int64_t tile = c->state_bits == 8 ? kEightTile : kAdamTile;
+  if (c->state_bits == 8)
+    while (g->pairs < kEightPairs && off / (2 * g->pairs * kPair) >= kEightWave) g->pairs *= 2;
+  const int64_t tile = (int64_t)kAdamTile * g->pairs;
   for (size_t base = 0; base < S; base += kManyPointers) {
     const size_t end = std::min(S, base + kManyPointers);
     for (int kind = 0; kind < (c->state_bits == 8 ? 4 : 1); ++kind) {
@@ -538,6 +547,7 @@ int enqueue_step(qadam_adamw* c, const StepScalars& now, const StepScalars* coun
   p.eps = c->cfg.eps;
   p.now = now;
   p.counted = counted;
+  p.pairs = c->geo.pairs;
   p.grad_scale = grad_scale;
   p.master = c->buf.master;
   p.m = c->buf.m; p.v = c->buf.v;
@@ -664,8 +674,8 @@ int qadam_adamw_moments(qadam_adamw* c, float* m32, float* v32, void* stream) {
   if (quads == 0) return QADAM_OK;
   const OnDevice on(c->device);
   if (!on.ok()) return QADAM_ERR_CUDA;
-  const long long grid = std::min<long long>((quads + kAdamThreads - 1) / kAdamThreads, (long long)c->sm_count * 16);
-  adamw_moments_kernel<<<(int)grid, kAdamThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+  const long long grid = std::min<long long>((quads + kReadThreads - 1) / kReadThreads, (long long)c->sm_count * kReadCtasPerSm);
+  adamw_moments_kernel<<<(unsigned)grid, kReadThreads, 0, static_cast<cudaStream_t>(stream)>>>(
       static_cast<const uint32_t*>(c->buf.m), static_cast<const uint32_t*>(c->buf.v), c->buf.m_scale, c->buf.r_scale, quads,
       reinterpret_cast<float4*>(m32), reinterpret_cast<float4*>(v32));
   if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;

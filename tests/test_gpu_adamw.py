@@ -298,8 +298,9 @@ def test_norm(dtype, shift, lens):
     want = np.sqrt(sum(float((t.double() ** 2).sum()) for t in ts))
     for limit in (float("inf"), 0.25):
         n, f = norm(limit)
-        # binary64 sums of up to 10^5 squares, the root, one rounding to binary32
-        assert abs(float(n) - want) <= want * (2.0 ** -24 + 1e-11)
+        # at most 7 roundings of binary32 in a sum of squares (a half of that in its root), the rest in binary64, one
+        # rounding to binary32
+        assert abs(float(n) - want) <= want * (3.5 * 2.0 ** -24 + 2.0 ** -24 + 1e-11)
         assert float(f) == float(np.float32(min(1.0, np.float32(limit) / np.float32(float(n)))))
     first = norm(0.25)[0].clone()
     for _ in range(5):
@@ -312,7 +313,7 @@ def test_norm_of_squares_beyond_binary32(value):
     x = torch.full((70001,), value, device="cuda")
     n, f = qb.GradNorm([x])()
     want = float(x[0].double()) * np.sqrt(70001.0)
-    assert abs(float(n) - want) <= want * 2.0 ** -24 + 2.0 ** -150 and float(f) == 1.0
+    assert abs(float(n) - want) <= want * 2.0 ** -24 + 2.0 ** -149 and float(f) == 1.0
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
