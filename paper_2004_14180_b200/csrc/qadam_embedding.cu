@@ -99,10 +99,10 @@ int enqueue_lookup(LookupParams p, bool held, cudaStream_t st) {
 // (row, place) of every token, stable by row, so a row's tokens stay in the order of the batch.  The
 // launches that sort leave most of the GPU idle: further CTAs of theirs clear the gradient meanwhile.
 
-constexpr int kSortThreads = 1024;
+constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 8;                              // tokens per thread
-constexpr int kSortRun = kSortThreads * kSortItems;        // 8192 tokens per CTA
+constexpr int kSortRun = kSortThreads * kSortItems;        // 4096 tokens per CTA
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kDirectRuns = 256;                           // up to so many runs every CTA adds up the counts for itself
@@ -110,7 +110,7 @@ constexpr int kRankTokens = 8192;                          // up to so many toke
 constexpr int kRankThreads = 512;
 constexpr int kRankWarps = kRankThreads / 32;
 constexpr int kRankPer = 64;                               // tokens that a CTA ranks: 128 CTAs at the most
-constexpr int kClearThreads = 148 * 1024;                  // beside the CTAs that sort
+constexpr int kClearThreads = 147 * 1024;                  // beside the CTAs that sort
 
 struct ClearParams {
   void* grad;
@@ -130,7 +130,8 @@ struct SortParams {
   unsigned* out_places;
   unsigned* counts;            // [runs][digits]
   int count, runs;
-  int shift, digits;
+  int shift, digits;           // digits: 2^bits
+  int bits;
   int scanned;                 // counts are places already (scan_counts_kernel)
   unsigned rows;
   long long padding;
@@ -156,7 +157,8 @@ __device__ void clear_share(const ClearParams& c, int cta) {
   }
 }
 
-__global__ void __launch_bounds__(kRankThreads) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
+constexpr int kClearCta = 512;
+__global__ void __launch_bounds__(kClearCta) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
 
 // The sort's key of a token: its row, or `rows` for one that is left out.
 __device__ __forceinline__ unsigned key_of(const SortParams& p, long long id) {
@@ -242,6 +244,75 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
   p.out_places[n] = (unsigned)t;
 }
 
+// Lanes whose token has the same digit; a lane without a token has no peer but such lanes.  A ballot for each bit: a
+// match of the whole digit took several times as long.
+__device__ __forceinline__ unsigned peers_of(unsigned digit, int bits, bool live) {
+  unsigned peers = __ballot_sync(0xFFFFFFFFu, live);
+  if (!live) peers = ~peers;
+#pragma unroll
+  for (int b = 0; b < kDigitBits; ++b) {
+    if (b >= bits) break;
+    const unsigned with = __ballot_sync(0xFFFFFFFFu, ((digit >> b) & 1u) != 0u);
+    peers &= with ^ (((digit >> b) & 1u) - 1u);
+  }
+  return peers;
+}
+
+// A warp's tokens of a run, in order: each one's rank among the warp's tokens of its digit.  seen: the warp's count of
+// each digit, 0 before.
+template <int ITEMS>
+__device__ __forceinline__ void rank_tokens(const unsigned (&key)[ITEMS], const bool (&live)[ITEMS], int shift, int bits,
+                                            unsigned short* seen, unsigned short (&rank)[ITEMS]) {
+  const int lane = threadIdx.x % 32;
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    const unsigned d = (key[j] >> shift) & ((1u << bits) - 1u);
+    const unsigned peers = peers_of(d, bits, live[j]);
+    const int before = __popc(peers & ((1u << lane) - 1u));
+    const int had = seen[d];
+    __syncwarp();
+    if (live[j] && before == 0) seen[d] = (unsigned short)(had + __popc(peers));
+    __syncwarp();
+    rank[j] = (unsigned short)(had + before);
+  }
+}
+
+// The warps' counts of a digit to where their tokens begin among the run's of that digit; the run's count is returned.
+template <int WARPS>
+__device__ __forceinline__ unsigned spread_counts(unsigned short (*seen)[kDigits], int d) {
+  unsigned at = 0u;
+#pragma unroll
+  for (int w0 = 0; w0 < WARPS; w0 += 16) {
+    unsigned n[16];
+#pragma unroll
+    for (int w = 0; w < 16; ++w) n[w] = seen[w0 + w][d];
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      seen[w0 + w][d] = (unsigned short)at;
+      at += n[w];
+    }
+  }
+  return at;
+}
+
+// Exclusive running sum of one number per thread over the first `digits` threads.
+template <int WARPS>
+__device__ __forceinline__ unsigned scan_digits(unsigned x, unsigned* warp_total) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  unsigned upto = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned other = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+    if (lane >= o) upto += other;
+  }
+  if (lane == 31) warp_total[warp] = upto;
+  __syncthreads();
+  unsigned at = upto - x;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) at += w < warp ? warp_total[w] : 0u;
+  return at;
+}
+
 // Many tokens: at most 9 bits a pass, lowest first.  Counts of each digit in each CTA's run of tokens; then
 // every token to its place, behind all smaller digits and the same digit in earlier runs.
 __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid_constant__ SortParams p) {
@@ -263,49 +334,27 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid
   for (int d = threadIdx.x; d < p.digits; d += kSortThreads) p.counts[(size_t)blockIdx.x * p.digits + d] = n[d];
 }
 
-// Exclusive running sum over the digits, in place (shared memory), by the whole CTA: a digit to a thread.
-__device__ __forceinline__ void scan_digits(unsigned* total, int digits, unsigned* warp_total) {
-  static_assert(kDigits <= kSortThreads, "a digit to a thread");
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, d = threadIdx.x;
-  const unsigned x = d < digits ? total[d] : 0u;
-  unsigned upto = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned other = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-    if (lane >= o) upto += other;
-  }
-  if (lane == 31) warp_total[warp] = upto;
-  __syncthreads();
-  unsigned at = upto - x;
-  for (int w = 0; w < warp && d < digits; ++w) at += warp_total[w];
-  if (d < digits) total[d] = at;
-  __syncthreads();
-}
-
-// Counts to places for very many runs, by one CTA.
+// Counts to places for very many runs, by one CTA: a digit to a thread.
 __global__ void __launch_bounds__(kSortThreads) scan_counts_kernel(unsigned* counts, int runs, int digits) {
-  __shared__ unsigned total[kDigits], warp_total[kSortWarps];
-  for (int d = threadIdx.x; d < digits; d += kSortThreads) {
-    unsigned n = 0u;
+  static_assert(kDigits <= kSortThreads, "a digit to a thread");
+  __shared__ unsigned warp_total[kSortWarps];
+  const int d = threadIdx.x;
+  unsigned n = 0u;
+  if (d < digits) {
 #pragma unroll 8
     for (int r = 0; r < runs; ++r) n += counts[(size_t)r * digits + d];
-    total[d] = n;
   }
-  __syncthreads();
-  scan_digits(total, digits, warp_total);
-  for (int d = threadIdx.x; d < digits; d += kSortThreads) {
-    unsigned at = total[d];
+  unsigned at = scan_digits<kSortWarps>(n, warp_total);
+  if (d >= digits) return;
 #pragma unroll 8
-    for (int r = 0; r < runs; ++r) {
-      const unsigned n = counts[(size_t)r * digits + d];
-      counts[(size_t)r * digits + d] = at;
-      at += n;
-    }
+  for (int r = 0; r < runs; ++r) {
+    const unsigned c = counts[(size_t)r * digits + d];
+    counts[(size_t)r * digits + d] = at;
+    at += c;
   }
 }
 
 __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_constant__ SortParams p) {
-  // tokens of each digit that a warp has seen, then where the warp's tokens of that digit begin in the run
   __shared__ unsigned short seen[kSortWarps][kDigits];
   __shared__ unsigned start[kDigits], warp_total[kSortWarps];
   if ((int)blockIdx.x >= p.runs) {
@@ -314,20 +363,21 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   }
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   for (int i = threadIdx.x; i < kSortWarps * kDigits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(&seen[0][0])[i] = 0u;
-  unsigned key[kSortItems];
+  unsigned key[kSortItems], place[kSortItems];
+  bool live[kSortItems];
   unsigned short rank[kSortItems];
   const long long base = (long long)blockIdx.x * kSortRun + warp * (32 * kSortItems) + lane;
   load_keys<kSortItems>(p, base, 32, key);
-  unsigned place[kSortItems];
 #pragma unroll
-  for (int j = 0; j < kSortItems; ++j)
-    place[j] = p.places == nullptr ? (unsigned)(base + 32 * j) : base + 32 * j < p.count ? p.places[base + 32 * j] : 0u;
+  for (int j = 0; j < kSortItems; ++j) {
+    live[j] = base + 32 * j < p.count;
+    place[j] = p.places == nullptr ? (unsigned)(base + 32 * j) : live[j] ? p.places[base + 32 * j] : 0u;
+  }
   // this thread's digit in all runs, and in the runs before this one
   const int digit = threadIdx.x;
-  unsigned earlier = 0u;
+  unsigned earlier = 0u, all = 0u;
   if (digit < p.digits) {
     const unsigned* counts = p.counts + digit;
-    unsigned n = 0u;
     if (p.scanned) {
       earlier = counts[(size_t)blockIdx.x * p.digits];
     } else {
@@ -337,48 +387,21 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
         for (int j = 0; j < 32; ++j) x[j] = r0 + j < p.runs ? counts[(size_t)(r0 + j) * p.digits] : 0u;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          if (r0 + j == (int)blockIdx.x) earlier = n;
-          n += x[j];
+          if (r0 + j == (int)blockIdx.x) earlier = all;
+          all += x[j];
         }
       }
     }
-    start[digit] = n;
   }
+  const unsigned before = scan_digits<kSortWarps>(all, warp_total);          // (a barrier: `seen` is 0 everywhere)
+  if (digit < p.digits) start[digit] = before + earlier;
+  rank_tokens<kSortItems>(key, live, p.shift, p.bits, seen[warp], rank);
   __syncthreads();
-  scan_digits(start, p.digits, warp_total);
-  if (digit < p.digits) start[digit] += earlier;
-#pragma unroll
-  for (int j = 0; j < kSortItems; ++j) {
-    const bool live = base + 32 * j < p.count;
-    const unsigned d = live ? (key[j] >> p.shift) & (p.digits - 1) : (unsigned)p.digits + lane;   // nobody's peer
-    const unsigned peers = __match_any_sync(0xFFFFFFFFu, d);
-    const int before = __popc(peers & ((1u << lane) - 1u));
-    const int had = live ? seen[warp][d] : 0;
-    __syncwarp();
-    if (live && before == 0) seen[warp][d] = (unsigned short)(had + __popc(peers));
-    __syncwarp();
-    rank[j] = (unsigned short)(had + before);
-  }
-  __syncthreads();
-  for (int d = threadIdx.x; d < p.digits; d += kSortThreads) {
-    unsigned at = 0u;
-#pragma unroll
-    for (int w0 = 0; w0 < kSortWarps; w0 += 16) {
-      unsigned n[16];
-#pragma unroll
-      for (int w = 0; w < 16; ++w) n[w] = seen[w0 + w][d];
-#pragma unroll
-      for (int w = 0; w < 16; ++w) {
-        seen[w0 + w][d] = (unsigned short)at;
-        at += n[w];
-      }
-    }
-  }
+  if (digit < p.digits) spread_counts<kSortWarps>(seen, digit);
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kSortItems; ++j) {
-    const long long t = base + 32 * j;
-    if (t < p.count) {
+    if (live[j]) {
       const unsigned d = (key[j] >> p.shift) & (p.digits - 1);
       const unsigned to = start[d] + seen[warp][d] + rank[j];
       p.out_keys[to] = key[j];
@@ -713,7 +736,7 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
 
 // A chunk is 32 tokens, or fewer (down to 2) where that would leave SMs without enough warps to keep their loads in
 // flight: below `kWarps` warps over 512 bytes of columns.
-constexpr int64_t kWarps = 148 * 16;
+constexpr int64_t kWarps = 148 * 8;
 constexpr int kLeastChunk = 2;
 
 struct GradLayout {
@@ -876,13 +899,14 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
     c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearThreads / threads);
   };
   if (count == 0) {
-    share(kRankThreads);
+    share(kClearCta);
     if (c.ctas == 0) return QADAM_OK;
-    clear_kernel<<<c.ctas, kRankThreads, 0, st>>>(c);
+    clear_kernel<<<c.ctas, kClearCta, 0, st>>>(c);
     return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
   }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
-  s.padding = padding; s.status = status; s.digits = 1 << digit; s.scanned = scanned;
+  s.padding = padding; s.status = status; s.digits = 1 << digit; s.bits = digit;
+  s.scanned = scanned;
   s.counts = list(l.counts);
   s.joined = list(l.joined);
   s.counters = (long long)l.chunks * 3 * g.tiles;
