@@ -527,18 +527,37 @@ __device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, co
     if (c.first < p.width) finish_row_apart<COLS>(p, dst, c, sum);
     return;
   }
+  float x[COLS];
 #pragma unroll
-  for (int q = 0; q < COLS; q += 4) {
-    float x[4];
+  for (int k = 0; k < COLS; k += 2) {
+    const float2 r = mul2_rn(make_float2(sum.x[k], sum.x[k + 1]), make_float2(p.scale, p.scale));
+    x[k] = r.x;
+    x[k + 1] = r.y;
+  }
+  if (p.grad_type == QADAM_F32) {
+    float4* out = reinterpret_cast<float4*>(dst) + c.first / 4;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, sum.x[q + k]);
-    if (p.accumulate) {
-      float old[4];
-      to_floats(load_raw4(dst, p.grad_type, c.first + q, 0, true), p.grad_type, old);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(old[k], x[k]);
+    for (int q = 0; q < COLS / 4; ++q) {
+      float4 r = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+      if (p.accumulate) {
+        const float4 old = out[q];
+        r = make_float4(__fadd_rn(old.x, r.x), __fadd_rn(old.y, r.y), __fadd_rn(old.z, r.z), __fadd_rn(old.w, r.w));
+      }
+      out[q] = r;
     }
-    store_raw4(dst, p.grad_type, c.first + q, 0, true, from_floats(x, p.grad_type));
+  } else {
+#pragma unroll
+    for (int q = 0; q < COLS; q += 4) {
+      float y[4] = {x[q], x[q + 1], x[q + 2], x[q + 3]};
+      if (p.accumulate) {
+        float old[4];
+        to_floats(load_raw4(dst, p.grad_type, c.first + q, 0, true), p.grad_type, old);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = __fadd_rn(old[k], y[k]);
+      }
+      const Raw4 r = p.grad_type == QADAM_BF16 ? from_floats(y, QADAM_BF16) : from_floats(y, QADAM_F16);
+      reinterpret_cast<uint2*>(dst)[(c.first + q) / 4] = make_uint2(r.w[0], r.w[1]);
+    }
   }
 }
 
@@ -565,13 +584,13 @@ __device__ __forceinline__ int search(const unsigned* keys, unsigned key, int lo
 }
 
 // Counts a partial sum that this warp has left; true if it is the last of `of`, whose sums can then be read.
+// The lanes' stores come before the count of lane 0 (release), the sums that others counted before the reads (acquire).
 __device__ __forceinline__ bool left_last(unsigned* counter, int of) {
-  __threadfence();
   __syncwarp();
   unsigned n = 0u;
-  if (threadIdx.x % 32 == 0) n = atomicAdd(counter, 1u);
+  if (threadIdx.x % 32 == 0) asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(n) : "l"(counter) : "memory");
   n = __shfl_sync(0xFFFFFFFFu, n, 0);
-  __threadfence();
+  __syncwarp();
   return n == (unsigned)of - 1u;
 }
 
@@ -685,12 +704,15 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
   const bool together = c.together(p.width), some = c.first < p.width;
   const unsigned long long lane_bytes = (unsigned long long)c.first * (16 / COLS);
   const unsigned slot0 = (unsigned)__cvta_generic_to_shared(&ring[warp][0][lane]);
+  // all lanes with columns have 16 aligned bytes of them (a lane without any asks for the row's first)
+  const bool fast = __all_sync(0xFFFFFFFFu, together || !some);
+  const unsigned long long column = some ? lane_bytes : 0ull;
   auto ask = [&](unsigned i) {
-    if (i < (unsigned)to && some) {
+    if (i < (unsigned)to) {
       const unsigned long long row = address[warp][i];
-      if (together)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + i % kAhead * 512u), "l"(row + lane_bytes) : "memory");
-      else
+      if (fast)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + (i % kAhead << 9)), "l"(row + column) : "memory");
+      else if (some)
         ring[warp][i % kAhead][lane] = gather_row<COLS>(reinterpret_cast<const void*>(row), c, p.width);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -715,7 +737,11 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
     float x[COLS];
     row_floats<TYPE>(ring[warp][i % kAhead][lane], x);
 #pragma unroll
-    for (int k = 0; k < COLS; ++k) sum.x[k] = __fadd_rn(sum.x[k], x[k]);
+    for (int k = 0; k < COLS; k += 2) {
+      const float2 r = add2_rn(make_float2(sum.x[k], sum.x[k + 1]), make_float2(x[k], x[k + 1]));
+      sum.x[k] = r.x;
+      sum.x[k + 1] = r.y;
+    }
     ask(i + kAhead);
     if (((unsigned)ends & 1u) != 0u) {
       const bool goes_on = i + 1 == (unsigned)to && split_after;
