@@ -1,6 +1,8 @@
 // Rows of an embedding table and the table's gradient: qadam_embedding_*, qadam_held_lookup.
 #include "qadam.h"
 
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <cmath>
 
@@ -106,11 +108,16 @@ constexpr int kSortRun = kSortThreads * kSortItems;        // 4096 tokens per CT
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kDirectRuns = 256;                           // up to so many runs every CTA adds up the counts for itself
-constexpr int kRankTokens = 8192;                          // up to so many tokens are ranked by comparing all pairs
+constexpr int kRankTokens = 2048;                          // up to so many tokens are ranked by comparing all pairs
+constexpr int kCluster = 8;                                // CTAs that sort up to 8 x 4096 tokens through each other's shared memory
 constexpr int kRankThreads = 512;
 constexpr int kRankWarps = kRankThreads / 32;
-constexpr int kRankPer = 64;                               // tokens that a CTA ranks: 128 CTAs at the most
-constexpr int kClearThreads = 147 * 1024;                  // beside the CTAs that sort
+constexpr int kRankPer = 64;                               // tokens that a CTA ranks
+// Threads that clear beside the CTAs that sort: many for a sort that takes its time (8192 tokens, 94 MB: 31.8 us in all,
+// 40.1 with a quarter), few where the sums follow at once (64 tokens: 19.9 us, 22.9 with four times as many).
+constexpr int kClearThreads = 136 * 2048;
+constexpr int kClearThreadsFew = 136 * 512;
+constexpr int kFewTokens = 256;
 
 struct ClearParams {
   void* grad;
@@ -131,7 +138,8 @@ struct SortParams {
   unsigned* counts;            // [runs][digits]
   int count, runs;
   int shift, digits;           // digits: 2^bits
-  int bits;
+  int bits, passes;
+  int each;                    // log2 of a thread's tokens (sort_cluster_kernel)
   int scanned;                 // counts are places already (scan_counts_kernel)
   unsigned rows;
   long long padding;
@@ -311,6 +319,81 @@ __device__ __forceinline__ unsigned scan_digits(unsigned x, unsigned* warp_total
 #pragma unroll
   for (int w = 0; w < WARPS; ++w) at += w < warp ? warp_total[w] : 0u;
   return at;
+}
+
+// All passes in one launch, by a cluster: every CTA has a run of tokens in registers and sends them to where they
+// belong in the CTAs' shared memory.  Sorting leaves most of the GPU to what is cleared meanwhile, and costs
+// little more than its barriers: five launches of one after the other were three times as long.
+template <int ITEMS>
+__global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid_constant__ SortParams p) {
+  static_assert(kDigits <= kSortThreads, "a digit to a thread");
+  extern __shared__ uint2 exchange[];                      // [kSortThreads << each]
+  __shared__ unsigned short seen[kSortWarps][kDigits];
+  __shared__ unsigned counts[kDigits], start[kDigits], warp_total[kSortWarps];
+  if (blockIdx.x >= kCluster) {
+    clear_share(p.clear, blockIdx.x - kCluster);
+    return;
+  }
+  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int cta = (int)cluster.block_rank();
+  clear_counters(p, cta, kCluster);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int inside = (warp << (5 + p.each)) + lane, base = cta * (kSortThreads << p.each) + inside;
+  const unsigned mask = (kSortThreads << p.each) - 1, cta_bits = 31 - __clz(kSortThreads << p.each);
+  unsigned key[ITEMS], place[ITEMS];
+  bool live[ITEMS];
+  unsigned short rank[ITEMS];
+  load_keys<ITEMS>(p, base, 32, key);
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    live[j] = j < 1 << p.each && base + 32 * j < p.count;
+    place[j] = (unsigned)(base + 32 * j);
+  }
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * p.bits;
+    const bool last = pass + 1 == p.passes;
+    for (int i = threadIdx.x; i < kSortWarps * kDigits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(&seen[0][0])[i] = 0u;
+    __syncthreads();
+    if (pass > 0) {
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j)
+        if (live[j]) {
+          const uint2 e = exchange[inside + 32 * j];
+          key[j] = e.x;
+          place[j] = e.y;
+        }
+    }
+    rank_tokens<ITEMS>(key, live, shift, p.bits, seen[warp], rank);
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d < p.digits) counts[d] = spread_counts<kSortWarps>(seen, d);
+    cluster.sync();                                        // counts are there; all tokens have left `exchange`
+    unsigned all = 0u, earlier = 0u;
+    if (d < p.digits) {
+#pragma unroll
+      for (int c = 0; c < kCluster; ++c) {
+        const unsigned n = cluster.map_shared_rank(counts, c)[d];
+        if (c < cta) earlier += n;
+        all += n;
+      }
+    }
+    const unsigned before = scan_digits<kSortWarps>(all, warp_total);
+    if (d < p.digits) start[d] = before + earlier;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+      if (live[j]) {
+        const unsigned digit = (key[j] >> shift) & (p.digits - 1);
+        const unsigned to = start[digit] + seen[warp][digit] + rank[j];
+        if (last) {
+          p.out_keys[to] = key[j];
+          p.out_places[to] = place[j];
+        } else {
+          cluster.map_shared_rank(exchange, to >> cta_bits)[to & mask] = make_uint2(key[j], place[j]);
+        }
+      }
+    cluster.sync();                                        // tokens have arrived; counts have been read
+  }
 }
 
 // Many tokens: at most 9 bits a pass, lowest first.  Counts of each digit in each CTA's run of tokens; then
@@ -784,7 +867,7 @@ int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
   }
   if (l->chunk == kChunk) room = std::max<int64_t>(room, (count + kChunk - 1) / kChunk);
   l->chunks = (int)((count + l->chunk - 1) / l->chunk);
-  if (room * tiles > (int64_t)1 << 33) return QADAM_ERR_SIZE;
+  if (room * tiles > (int64_t)1 << 33) return QADAM_ERR_SIZE;      // (CTAs of one launch)
   size_t at = 0;
   const size_t list = round_up256((size_t)count * sizeof(unsigned));
   for (int i = 0; i < 2; ++i) {
@@ -905,6 +988,7 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   int place_bits = 0;
   while (((count - 1) >> place_bits) > 0) ++place_bits;
   const bool ranked = count <= kRankTokens && bits + place_bits <= 32;
+  const bool clustered = !ranked && count <= kCluster * kSortRun;
   const int passes = (bits + kDigitBits - 1) / kDigitBits, digit = (bits + passes - 1) / passes;
   const bool scanned = l.runs > kDirectRuns;
 
@@ -915,14 +999,14 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   c.dense = grad_stride == width && is_aligned(grad, 16) && rows * row_bytes % 16 == 0;
   // what there is to clear is dealt out evenly to the launches that sort
   const long long to_clear = accumulate ? 0 : c.dense ? rows * row_bytes / 16 : rows;
-  const int launches = count == 0 || ranked ? 1 : 2 * passes;
+  const int launches = count == 0 || ranked || clustered ? 1 : 2 * passes;
   int launch = 0;
   auto share = [&](int threads) {
     c.begin = to_clear * launch / launches;
     c.end = to_clear * (launch + 1) / launches;
     ++launch;
     const long long each = c.dense ? threads : 1;
-    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearThreads / threads);
+    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, (count <= kFewTokens ? kClearThreadsFew : kClearThreads) / threads);
   };
   if (count == 0) {
     share(kClearCta);
@@ -931,7 +1015,7 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
     return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
   }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
-  s.padding = padding; s.status = status; s.digits = 1 << digit; s.bits = digit;
+  s.padding = padding; s.status = status; s.digits = 1 << digit; s.bits = digit; s.passes = passes;
   s.scanned = scanned;
   s.counts = list(l.counts);
   s.joined = list(l.joined);
@@ -943,6 +1027,28 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
     share(kRankThreads);
     rank_kernel<<<((int)count + kRankPer - 1) / kRankPer + c.ctas, kRankThreads, (size_t)rank_quads((int)count) * kRankWarps * 16, st>>>(s);
     if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  } else if (clustered) {
+    while ((kCluster * kSortThreads << s.each) < count) ++s.each;
+    share(kSortThreads);
+    const auto kernel = s.each <= 1 ? sort_cluster_kernel<2> : sort_cluster_kernel<8>;
+    const size_t smem = passes > 1 ? (size_t)(kSortThreads << s.each) * sizeof(uint2) : 0;
+    // the limit of dynamic shared memory belongs to the kernel: every call that needs it raised sets the same
+    if (smem > 12 * 1024 &&
+        !cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortRun * (int)sizeof(uint2))))
+      return QADAM_ERR_CUDA;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3((unsigned)(kCluster + (c.ctas + kCluster - 1) / kCluster * kCluster));
+    c.ctas = (int)config.gridDim.x - kCluster;
+    config.blockDim = dim3(kSortThreads);
+    config.dynamicSmemBytes = smem;
+    config.stream = st;
+    cudaLaunchAttribute attribute;
+    attribute.id = cudaLaunchAttributeClusterDimension;
+    attribute.val.clusterDim.x = kCluster;
+    attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
+    config.attrs = &attribute;
+    config.numAttrs = 1;
+    if (!cuda_call(cudaLaunchKernelEx(&config, kernel, s))) return QADAM_ERR_CUDA;
   } else {
     for (int i = 0; i < passes; ++i) {
       s.shift = i * digit;
