@@ -18,14 +18,22 @@ __device__ __forceinline__ long long load_id(const void* ids, int id_bits, long 
 
 // ---------------------------------------------------------------- lookup
 
+//
+// Reads the rows that the batch names, writes a row per token: bound by HBM for long batches, by two trips to memory
+// (tokens, then rows) for short ones.  A CTA fetches its tokens first; a thread then has kLookAhead pieces of eight
+// columns under way.
+
 constexpr int kLookThreads = 256;
-constexpr int kLookQuads = 1024;            // quads of four columns a CTA covers
+constexpr int kLookAhead = 4;
+constexpr int kLookPieces = kLookThreads * kLookAhead;     // pieces a CTA covers
+constexpr int kDense = 0;                                  // else: 32-bit words that a piece of packed codes may touch
 
 struct LookupParams {
   const void* table;           // rows, or packed codes
   int type;
   long long rows, stride;
-  int width, quads;            // quads: of a row
+  int width, pieces;           // pieces: of a row
+  unsigned per_piece;          // 2^32 / pieces, rounded up: a division by a product
   const void* ids;
   int id_bits;
   long long count;
@@ -34,65 +42,170 @@ struct LookupParams {
   void* out;
   int out_type;
   long long out_stride;
+  int in_vector, out_vector;   // rows begin on 16 bytes
   unsigned* status;
   // packed codes
   int kx;
   long long first, words;
 };
 
-// Four elements from element e on of the packed weights: code q + 2^kx stands for q 2^-(kx + 1).
-__device__ __forceinline__ void held4(const LookupParams& p, long long e, float (&x)[4]) {
-  const uint32_t* w = static_cast<const uint32_t*>(p.table);
-  const int b = p.kx + 2;
-  const long long bit = e * b;
-  const long long at = bit >> 5;
-  const int shift = (int)(bit & 31);
-  const uint32_t w0 = w[at], w1 = w[min(at + 1, p.words - 1)], w2 = w[min(at + 2, p.words - 1)];
-  const unsigned long long low = (unsigned long long)w0 | ((unsigned long long)w1 << 32);
-  const unsigned long long bits = shift == 0 ? low : (low >> shift) | ((unsigned long long)w2 << (64 - shift));
-  const float step = exp2i(-(p.kx + 1));
+struct Piece {
+  uint32_t w[8];
+};
+
+// Eight elements of a dense row, as they lie in memory.
+__device__ __forceinline__ Piece load_piece(const char* row, int type, int col, int width, bool vector) {
+  Piece r = {};
+  if (vector && col + 8 <= width) {
+    const uint4 a = *reinterpret_cast<const uint4*>(row + (size_t)col * type_bytes(type));
+    r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+    if (type == QADAM_F32) {
+      const uint4 b = *reinterpret_cast<const uint4*>(row + (size_t)col * 4 + 16);
+      r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+    }
+  } else {
+    const Raw4 a = load_raw4(row, type, col, width, false), b = load_raw4(row, type, col + 4, width, false);
+    if (type == QADAM_F32) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) x[k] = __fmul_rn((float)((int)((bits >> (k * b)) & ((1u << b) - 1u)) - (1 << p.kx)), step);
+      for (int k = 0; k < 4; ++k) {
+        r.w[k] = a.w[k];
+        r.w[4 + k] = b.w[k];
+      }
+    } else {
+      r.w[0] = a.w[0]; r.w[1] = a.w[1]; r.w[2] = b.w[0]; r.w[3] = b.w[1];
+    }
+  }
+  return r;
 }
 
-template <bool HELD>
+__device__ __forceinline__ void piece_floats(const Piece& r, int type, float (&x)[8]) {
+  float a[4], b[4];
+  if (type == QADAM_F32) {
+    to_floats(Raw4{{r.w[0], r.w[1], r.w[2], r.w[3]}}, QADAM_F32, a);
+    to_floats(Raw4{{r.w[4], r.w[5], r.w[6], r.w[7]}}, QADAM_F32, b);
+  } else {
+    to_floats(Raw4{{r.w[0], r.w[1], 0u, 0u}}, type, a);
+    to_floats(Raw4{{r.w[2], r.w[3], 0u, 0u}}, type, b);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    x[k] = a[k];
+    x[4 + k] = b[k];
+  }
+}
+
+__device__ __forceinline__ void store_piece(char* row, int type, int col, int width, bool vector, const float (&x)[8]) {
+  const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
+  const Raw4 a = from_floats(lo, type), b = from_floats(hi, type);
+  if (vector && col + 8 <= width) {
+    uint4* out = reinterpret_cast<uint4*>(row + (size_t)col * type_bytes(type));
+    if (type == QADAM_F32) {
+      out[0] = make_uint4(a.w[0], a.w[1], a.w[2], a.w[3]);
+      out[1] = make_uint4(b.w[0], b.w[1], b.w[2], b.w[3]);
+    } else {
+      out[0] = make_uint4(a.w[0], a.w[1], b.w[0], b.w[1]);
+    }
+  } else {
+    store_raw4(row, type, col, width, false, a);
+    store_raw4(row, type, col + 4, width, false, b);
+  }
+}
+
+// The words that hold eight packed elements from element e on.
+template <int WORDS>
+__device__ __forceinline__ Piece load_codes(const LookupParams& p, long long e) {
+  const uint32_t* w = static_cast<const uint32_t*>(p.table);
+  const long long at = e * (p.kx + 2) >> 5;
+  Piece r = {};
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) r.w[k] = w[min(at + k, p.words - 1)];
+  return r;
+}
+
+// Code q + 2^kx stands for q 2^-(kx + 1).
+template <int WORDS>
+__device__ __forceinline__ void code_floats(const LookupParams& p, const Piece& r, long long e, float (&x)[8]) {
+  const int b = p.kx + 2, shift = (int)(e * b & 31);
+  const unsigned mask = (1u << b) - 1u;
+  const float step = exp2i(-(p.kx + 1));
+  unsigned v[4] = {0u, 0u, 0u, 0u};                        // 8 b bits
+#pragma unroll
+  for (int k = 0; k + 1 < WORDS; ++k) v[k] = __funnelshift_r(r.w[k], r.w[k + 1], shift);
+  const unsigned long long lo = (unsigned long long)v[1] << 32 | v[0], hi = (unsigned long long)v[3] << 32 | v[2];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int at = k * b;
+    unsigned code;
+    if constexpr (WORDS == 2) code = v[0] >> at;
+    else if constexpr (WORDS == 3) code = (unsigned)(lo >> at);
+    else code = at == 0 ? (unsigned)lo : at < 64 ? (unsigned)(lo >> at | hi << (64 - at)) : (unsigned)(hi >> (at - 64));
+    x[k] = __fmul_rn((float)((int)(code & mask) - (1 << p.kx)), step);
+  }
+}
+
+template <int WORDS>
 __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const __grid_constant__ LookupParams p) {
+  __shared__ long long ids[kLookPieces];
   const long long first = (long long)blockIdx.x * p.per_cta;
   const int tokens = (int)min((long long)p.per_cta, p.count - first);
-  const int column0 = blockIdx.y * kLookQuads;
-  const int quads = min(kLookQuads, p.quads - column0);
-  const bool out_fits = aligned4(p.out, p.out_type) && p.out_stride % 4 == 0;
-  const bool in_fits = !HELD && aligned4(p.table, p.type) && p.stride % 4 == 0;
-  for (int q = threadIdx.x; q < tokens * quads; q += kLookThreads) {
-    const long long t = first + q / quads;
-    const int col = 4 * (column0 + q % quads);
-    const long long id = load_id(p.ids, p.id_bits, t);
-    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (id >= 0 && id < p.rows) {
-      if constexpr (HELD) {
-        held4(p, p.first + id * p.width + col, x);
-      } else {
-        const char* row = static_cast<const char*>(p.table) + id * p.stride * type_bytes(p.type);
-        to_floats(load_raw4(row, p.type, col, p.width, in_fits && col + 4 <= p.width), p.type, x);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(p.scale, x[k]);
-    } else if (id >= p.rows && p.status != nullptr && col == 0) {
-      atomicOr(p.status, QADAM_ST_INDEX);
+  for (int t = threadIdx.x; t < tokens; t += kLookThreads) {
+    long long id = load_id(p.ids, p.id_bits, first + t);
+    if (id >= p.rows) {
+      if (p.status != nullptr) atomicOr(p.status, QADAM_ST_INDEX);
+      id = -1;
     }
-    char* row = static_cast<char*>(p.out) + t * p.out_stride * type_bytes(p.out_type);
-    store_raw4(row, p.out_type, col, p.width, out_fits && col + 4 <= p.width, from_floats(x, p.out_type));
+    ids[t] = id;
+  }
+  __syncthreads();
+  const int piece0 = blockIdx.y * kLookPieces, pieces = min(kLookPieces, p.pieces - piece0), all = tokens * pieces;
+  long long id[kLookAhead];
+  int token[kLookAhead], col[kLookAhead];
+  Piece raw[kLookAhead];
+#pragma unroll
+  for (int j = 0; j < kLookAhead; ++j) {
+    const int q = threadIdx.x + j * kLookThreads;
+    token[j] = gridDim.y > 1 ? 0 : (int)__umulhi((unsigned)q, p.per_piece);      // (a CTA of a very wide row has one token)
+    if (p.pieces == 1) token[j] = q;
+    col[j] = 8 * (piece0 + q - token[j] * pieces);
+    id[j] = q < all ? ids[token[j]] : -1;
+    raw[j] = Piece{};
+    if (id[j] >= 0) {
+      if constexpr (WORDS == kDense)
+        raw[j] = load_piece(static_cast<const char*>(p.table) + id[j] * p.stride * type_bytes(p.type), p.type, col[j], p.width, p.in_vector);
+      else
+        raw[j] = load_codes<WORDS>(p, p.first + id[j] * p.width + col[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kLookAhead; ++j) {
+    if (threadIdx.x + j * kLookThreads >= all) break;
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (id[j] >= 0) {
+      if constexpr (WORDS == kDense) piece_floats(raw[j], p.type, x);
+      else code_floats<WORDS>(p, raw[j], p.first + id[j] * p.width + col[j], x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
+    }
+    store_piece(static_cast<char*>(p.out) + (first + token[j]) * p.out_stride * type_bytes(p.out_type), p.out_type, col[j], p.width,
+                p.out_vector, x);
   }
 }
 
 int enqueue_lookup(LookupParams p, bool held, cudaStream_t st) {
-  p.quads = (p.width + 3) / 4;
-  const int across = (p.quads + kLookQuads - 1) / kLookQuads;
-  p.per_cta = std::max(1, kLookQuads / p.quads);
-  const long long grid = (p.count + p.per_cta - 1) / p.per_cta;
-  if (grid > 0x7FFFFFFF) return QADAM_ERR_SIZE;
-  if (held) lookup_kernel<true><<<dim3((unsigned)grid, across), kLookThreads, 0, st>>>(p);
-  else lookup_kernel<false><<<dim3((unsigned)grid, across), kLookThreads, 0, st>>>(p);
+  p.pieces = (p.width + 7) / 8;
+  p.per_piece = (unsigned)(((1ull << 32) + p.pieces - 1) / p.pieces);       // (not used for one piece, which it does not fit)
+  p.in_vector = !held && is_aligned(p.table, 16) && p.stride * type_bytes(p.type) % 16 == 0;
+  p.out_vector = is_aligned(p.out, 16) && p.out_stride * type_bytes(p.out_type) % 16 == 0;
+  const int across = (p.pieces + kLookPieces - 1) / kLookPieces;
+  p.per_cta = std::max(1, kLookPieces / p.pieces);
+  const long long ctas = (p.count + p.per_cta - 1) / p.per_cta;
+  if (ctas > 0x7FFFFFFF) return QADAM_ERR_SIZE;
+  const dim3 grid((unsigned)ctas, across);
+  const int bits = p.kx + 2;
+  if (!held) lookup_kernel<kDense><<<grid, kLookThreads, 0, st>>>(p);
+  else if (bits <= 4) lookup_kernel<2><<<grid, kLookThreads, 0, st>>>(p);
+  else if (bits <= 8) lookup_kernel<3><<<grid, kLookThreads, 0, st>>>(p);
+  else lookup_kernel<5><<<grid, kLookThreads, 0, st>>>(p);
   return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 

@@ -6,6 +6,7 @@ device that gets ST_INDEX if a token is not below the number of rows; the caller
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Optional
 
 import torch
@@ -54,6 +55,13 @@ def _out(shape, out, dtype, device):
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _grad_workspace(count: int, rows: int, width: int) -> int:
+    size = C.c_size_t()
+    _check(load_library().qadam_embedding_grad_query_sizes(count, rows, width, C.byref(size)), "qadam_embedding_grad_query_sizes")
+    return size.value
+
+
 def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
                      out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[..., :] = scale * table[ids[...], :], rounded once to out_dtype (the table's, if not given).
@@ -68,8 +76,10 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     n, width = table.shape
     shape = ids.shape + (width,)
     stride = _row_stride(table, "table", table.shape, device)
-    out = _out(shape, out, out_dtype if out_dtype is not None or out is not None else table.dtype, device)
-    out_stride = _row_stride(out, "out", shape, device)
+    if out is None:
+        out, out_stride = torch.empty(shape, dtype=out_dtype or table.dtype, device=device), width
+    else:
+        out, out_stride = _out(shape, out, out_dtype, device), _row_stride(out, "out", shape, device)
     with _Guard(device):
         _check(load_library().qadam_embedding_lookup(
             table.data_ptr(), element_type(table.dtype, "table"), n, width, stride, ids.data_ptr(), 8 * ids.element_size(),
@@ -91,8 +101,10 @@ def held_lookup(wcodes: torch.Tensor, kx: int, ids: torch.Tensor, rows: int, wid
     device = wcodes.device
     ids = _tokens(ids, device)
     shape = ids.shape + (width,)
-    out = _out(shape, out, None if out is not None else out_dtype, device)
-    out_stride = _row_stride(out, "out", shape, device)
+    if out is None:
+        out, out_stride = torch.empty(shape, dtype=out_dtype, device=device), width
+    else:
+        out_stride = _row_stride(out, "out", shape, device)
     with _Guard(device):
         _check(load_library().qadam_held_lookup(
             wcodes.data_ptr(), wcodes.numel(), kx, first, rows, width, ids.data_ptr(), 8 * ids.element_size(), ids.numel(), scale,
@@ -121,12 +133,11 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
     out = _out((rows, width), out, dtype if dtype is not None or out is not None else dy.dtype, device)
     dy_stride = _row_stride(dy, "dy", ids.shape + (width,), device)
     out_stride = _row_stride(out, "out", (rows, width), device)
-    L, size = load_library(), C.c_size_t()
-    _check(L.qadam_embedding_grad_query_sizes(count, rows, width, C.byref(size)), "qadam_embedding_grad_query_sizes")
+    size = _grad_workspace(count, rows, width)
     with _Guard(device):
-        scratch = torch.empty(size.value, dtype=torch.uint8, device=device)     # (torch's blocks are 512-byte aligned)
-        _check(L.qadam_embedding_grad(
+        scratch = torch.empty(size, dtype=torch.uint8, device=device)     # (torch's blocks are 512-byte aligned)
+        _check(load_library().qadam_embedding_grad(
             ids.data_ptr(), 8 * ids.element_size(), count, dy.data_ptr(), element_type(dy.dtype, "dy"), dy_stride, scale, padding,
-            out.data_ptr(), element_type(out.dtype, "out"), rows, width, out_stride, int(accumulate), scratch.data_ptr(), size.value,
+            out.data_ptr(), element_type(out.dtype, "out"), rows, width, out_stride, int(accumulate), scratch.data_ptr(), size,
             _status(status, device), stream_of(device)), "qadam_embedding_grad")
     return out
