@@ -20,19 +20,25 @@ __device__ __forceinline__ long long load_id(const void* ids, int id_bits, long 
 
 //
 // Reads the rows that the batch names, writes a row per token: bound by HBM for long batches, by two trips to memory
-// (tokens, then rows) for short ones.  A CTA fetches its tokens first; a thread then has kLookAhead pieces of eight
-// columns under way.
+// (tokens, then rows) for short ones.  A CTA fetches its tokens first; a thread then has AHEAD pieces of eight columns
+// under way.  Where rows do not begin on 16 bytes, a piece's columns are 32 apart, so that a warp's accesses are next to
+// each other.
 
 constexpr int kLookThreads = 256;
-constexpr int kLookAhead = 4;
-constexpr int kLookPieces = kLookThreads * kLookAhead;     // pieces a CTA covers
-constexpr int kDense = 0;                                  // else: 32-bit words that a piece of packed codes may touch
+constexpr int kLookPieces = 1024;                          // pieces a CTA covers, at the most
+// What the rows are: elements of 16 or 32 bits, or packed codes of KIND = 2 .. 16 bits.
+constexpr int kDense16 = 0, kDense32 = 1;
+template <int KIND>
+constexpr int kPieceWords = KIND == kDense32 ? 8 : KIND == kDense16 ? 4 : (8 * KIND + 31 + 31) / 32;
+template <int KIND>
+constexpr int kLookAhead = KIND == kDense32 ? 2 : 4;
 
 struct LookupParams {
   const void* table;           // rows, or packed codes
   int type;
   long long rows, stride;
   int width, pieces;           // pieces: of a row
+  int here;                    // of a row in one CTA, at the most
   unsigned per_piece;          // 2^32 / pieces, rounded up: a division by a product
   const void* ids;
   int id_bits;
@@ -42,109 +48,152 @@ struct LookupParams {
   void* out;
   int out_type;
   long long out_stride;
-  int in_vector, out_vector;   // rows begin on 16 bytes
+  int spread;                  // rows, of the table or of the result, do not begin on 16 bytes
   unsigned* status;
-  // packed codes
-  int kx;
-  long long first, words;
+  long long first, words;      // packed codes
 };
 
+// Columns of a piece: first + k step.
+__device__ __forceinline__ int piece_column(const LookupParams& p, int piece) {
+  return p.spread ? piece / 32 * 256 + piece % 32 : 8 * piece;
+}
+
+// Eight elements of a row as they lie in memory (a word each, if spread).
+template <int KIND>
 struct Piece {
+  uint32_t w[kPieceWords<KIND>];
+};
+struct SpreadPiece {
   uint32_t w[8];
 };
 
-// Eight elements of a dense row, as they lie in memory.
-__device__ __forceinline__ Piece load_piece(const char* row, int type, int col, int width, bool vector) {
-  Piece r = {};
-  if (vector && col + 8 <= width) {
-    const uint4 a = *reinterpret_cast<const uint4*>(row + (size_t)col * type_bytes(type));
-    r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
-    if (type == QADAM_F32) {
-      const uint4 b = *reinterpret_cast<const uint4*>(row + (size_t)col * 4 + 16);
-      r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
-    }
-  } else {
-    const Raw4 a = load_raw4(row, type, col, width, false), b = load_raw4(row, type, col + 4, width, false);
-    if (type == QADAM_F32) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        r.w[k] = a.w[k];
-        r.w[4 + k] = b.w[k];
+template <int KIND>
+__device__ __forceinline__ Piece<KIND> load_piece(const LookupParams& p, long long id, int col) {
+  Piece<KIND> r = {};
+  if constexpr (KIND == kDense16 || KIND == kDense32) {
+    constexpr int kBytes = KIND == kDense32 ? 4 : 2;
+    const char* row = static_cast<const char*>(p.table) + id * p.stride * kBytes;
+    if (col + 8 <= p.width) {
+      const uint4 a = *reinterpret_cast<const uint4*>(row + (size_t)col * kBytes);
+      r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+      if constexpr (KIND == kDense32) {
+        const uint4 b = *reinterpret_cast<const uint4*>(row + (size_t)col * 4 + 16);
+        r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
       }
     } else {
-      r.w[0] = a.w[0]; r.w[1] = a.w[1]; r.w[2] = b.w[0]; r.w[3] = b.w[1];
+      for (int k = 0; k < 8; ++k) {
+        if (col + k >= p.width) break;
+        if constexpr (KIND == kDense32) r.w[k] = reinterpret_cast<const uint32_t*>(row)[col + k];
+        else r.w[k / 2] |= (uint32_t) reinterpret_cast<const unsigned short*>(row)[col + k] << (16 * (k % 2));
+      }
+    }
+  } else {
+    const long long at = (p.first + id * p.width + col) * KIND >> 5;
+#pragma unroll
+    for (int k = 0; k < kPieceWords<KIND>; ++k) r.w[k] = static_cast<const uint32_t*>(p.table)[min(at + k, p.words - 1)];
+  }
+  return r;
+}
+
+// Code q + 2^kx stands for q 2^-(kx + 1).  The code becomes the last bits of 2^23 + code.
+template <int KIND>
+__device__ __forceinline__ float code_value(unsigned code) {
+  const float q = __fadd_rn(__uint_as_float(0x4B000000u | (code & ((1u << KIND) - 1u))), -(8388608.0f + (float)(1 << (KIND - 2))));
+  return __fmul_rn(q, 1.0f / (float)(1 << (KIND - 1)));
+}
+
+template <int KIND>
+__device__ __forceinline__ void piece_floats(const LookupParams& p, const Piece<KIND>& r, long long id, int col, float (&x)[8]) {
+  if constexpr (KIND == kDense32) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(r.w[k]);
+  } else if constexpr (KIND == kDense16) {
+    float a[4], b[4];
+    to_floats(Raw4{{r.w[0], r.w[1], 0u, 0u}}, p.type, a);
+    to_floats(Raw4{{r.w[2], r.w[3], 0u, 0u}}, p.type, b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[k] = a[k];
+      x[4 + k] = b[k];
+    }
+  } else {
+    const int shift = (int)((p.first + id * p.width + col) * KIND & 31);
+    unsigned v[kPieceWords<KIND>];                         // 8 KIND bits
+#pragma unroll
+    for (int k = 0; k < kPieceWords<KIND>; ++k) v[k] = k + 1 < kPieceWords<KIND> ? __funnelshift_r(r.w[k], r.w[k + 1], shift) : r.w[k] >> shift;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int at = k * KIND, w = at / 32, bit = at % 32;
+      unsigned code = v[w] >> bit;
+      if (bit + KIND > 32) code |= v[w + 1] << (32 - bit);
+      x[k] = code_value<KIND>(code);
+    }
+  }
+}
+
+template <int KIND>
+__device__ __forceinline__ SpreadPiece load_spread(const LookupParams& p, long long id, int col) {
+  SpreadPiece r = {};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int at = col + 32 * k;
+    if (at >= p.width) break;
+    if constexpr (KIND == kDense32) {
+      r.w[k] = static_cast<const uint32_t*>(p.table)[id * p.stride + at];
+    } else if constexpr (KIND == kDense16) {
+      r.w[k] = static_cast<const unsigned short*>(p.table)[id * p.stride + at];
+    } else {
+      // 32 bits from the 16 that the code begins in: it ends in them
+      const long long half = (p.first + id * p.width + at) * KIND >> 4;
+      const unsigned short* h = static_cast<const unsigned short*>(p.table);
+      r.w[k] = h[half] | (uint32_t)h[min(half + 1, 2 * p.words - 1)] << 16;
     }
   }
   return r;
 }
 
-__device__ __forceinline__ void piece_floats(const Piece& r, int type, float (&x)[8]) {
-  float a[4], b[4];
-  if (type == QADAM_F32) {
-    to_floats(Raw4{{r.w[0], r.w[1], r.w[2], r.w[3]}}, QADAM_F32, a);
-    to_floats(Raw4{{r.w[4], r.w[5], r.w[6], r.w[7]}}, QADAM_F32, b);
-  } else {
-    to_floats(Raw4{{r.w[0], r.w[1], 0u, 0u}}, type, a);
-    to_floats(Raw4{{r.w[2], r.w[3], 0u, 0u}}, type, b);
-  }
+template <int KIND>
+__device__ __forceinline__ void spread_floats(const LookupParams& p, const SpreadPiece& r, long long id, int col, float (&x)[8]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    x[k] = a[k];
-    x[4 + k] = b[k];
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (KIND == kDense32) {
+      x[k] = __uint_as_float(r.w[k]);
+    } else if constexpr (KIND == kDense16) {
+      x[k] = p.type == QADAM_BF16 ? __uint_as_float(r.w[k] << 16) : half_bits_to_float(r.w[k]);
+    } else {
+      x[k] = code_value<KIND>(r.w[k] >> (int)((p.first + id * p.width + col + 32 * k) * KIND & 15));
+    }
   }
 }
 
-__device__ __forceinline__ void store_piece(char* row, int type, int col, int width, bool vector, const float (&x)[8]) {
+__device__ __forceinline__ void store_piece(const LookupParams& p, long long t, int col, const float (&x)[8]) {
   const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
-  const Raw4 a = from_floats(lo, type), b = from_floats(hi, type);
-  if (vector && col + 8 <= width) {
-    uint4* out = reinterpret_cast<uint4*>(row + (size_t)col * type_bytes(type));
-    if (type == QADAM_F32) {
+  const Raw4 a = from_floats(lo, p.out_type), b = from_floats(hi, p.out_type);
+  char* row = static_cast<char*>(p.out) + t * p.out_stride * type_bytes(p.out_type);
+  if (!p.spread && col + 8 <= p.width) {
+    uint4* out = reinterpret_cast<uint4*>(row + (size_t)col * type_bytes(p.out_type));
+    if (p.out_type == QADAM_F32) {
       out[0] = make_uint4(a.w[0], a.w[1], a.w[2], a.w[3]);
       out[1] = make_uint4(b.w[0], b.w[1], b.w[2], b.w[3]);
     } else {
       out[0] = make_uint4(a.w[0], a.w[1], b.w[0], b.w[1]);
     }
-  } else {
-    store_raw4(row, type, col, width, false, a);
-    store_raw4(row, type, col + 4, width, false, b);
+    return;
   }
-}
-
-// The words that hold eight packed elements from element e on.
-template <int WORDS>
-__device__ __forceinline__ Piece load_codes(const LookupParams& p, long long e) {
-  const uint32_t* w = static_cast<const uint32_t*>(p.table);
-  const long long at = e * (p.kx + 2) >> 5;
-  Piece r = {};
-#pragma unroll
-  for (int k = 0; k < WORDS; ++k) r.w[k] = w[min(at + k, p.words - 1)];
-  return r;
-}
-
-// Code q + 2^kx stands for q 2^-(kx + 1).
-template <int WORDS>
-__device__ __forceinline__ void code_floats(const LookupParams& p, const Piece& r, long long e, float (&x)[8]) {
-  const int b = p.kx + 2, shift = (int)(e * b & 31);
-  const unsigned mask = (1u << b) - 1u;
-  const float step = exp2i(-(p.kx + 1));
-  unsigned v[4] = {0u, 0u, 0u, 0u};                        // 8 b bits
-#pragma unroll
-  for (int k = 0; k + 1 < WORDS; ++k) v[k] = __funnelshift_r(r.w[k], r.w[k + 1], shift);
-  const unsigned long long lo = (unsigned long long)v[1] << 32 | v[0], hi = (unsigned long long)v[3] << 32 | v[2];
+  const int step = p.spread ? 32 : 1;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int at = k * b;
-    unsigned code;
-    if constexpr (WORDS == 2) code = v[0] >> at;
-    else if constexpr (WORDS == 3) code = (unsigned)(lo >> at);
-    else code = at == 0 ? (unsigned)lo : at < 64 ? (unsigned)(lo >> at | hi << (64 - at)) : (unsigned)(hi >> (at - 64));
-    x[k] = __fmul_rn((float)((int)(code & mask) - (1 << p.kx)), step);
+    const int at = col + k * step;
+    if (at >= p.width) break;
+    const Raw4& r = k < 4 ? a : b;
+    if (p.out_type == QADAM_F32) reinterpret_cast<uint32_t*>(row)[at] = r.w[k % 4];
+    else reinterpret_cast<unsigned short*>(row)[at] = (unsigned short)(r.w[k % 4 / 2] >> (16 * (k % 2)));
   }
 }
 
-template <int WORDS>
-__global__ void __launch_bounds__(kLookThreads) lookup_kernel(const __grid_constant__ LookupParams p) {
+template <int KIND>
+__global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_constant__ LookupParams p) {
+  constexpr int AHEAD = kLookAhead<KIND>;
   __shared__ long long ids[kLookPieces];
   const long long first = (long long)blockIdx.x * p.per_cta;
   const int tokens = (int)min((long long)p.per_cta, p.count - first);
@@ -157,55 +206,70 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const __grid_const
     ids[t] = id;
   }
   __syncthreads();
-  const int piece0 = blockIdx.y * kLookPieces, pieces = min(kLookPieces, p.pieces - piece0), all = tokens * pieces;
-  long long id[kLookAhead];
-  int token[kLookAhead], col[kLookAhead];
-  Piece raw[kLookAhead];
+  const int piece0 = blockIdx.y * p.here, pieces = min(p.here, p.pieces - piece0), all = tokens * pieces;
+  // piece q of the CTA's: its token (there is one where a row has more pieces than a CTA) and column
+  auto token_of = [&](int q) { return gridDim.y > 1 ? 0 : p.pieces == 1 ? q : (int)__umulhi((unsigned)q, p.per_piece); };
+  auto column_of = [&](int q, int token) { return piece_column(p, piece0 + q - token * pieces); };
+  if (p.spread) {
+    for (int q = threadIdx.x; q < all; q += kLookThreads) {
+      const int token = token_of(q), col = column_of(q, token);
+      const long long id = ids[token];
+      float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (id >= 0) {
+        spread_floats<KIND>(p, load_spread<KIND>(p, id, col), id, col, x);
 #pragma unroll
-  for (int j = 0; j < kLookAhead; ++j) {
-    const int q = threadIdx.x + j * kLookThreads;
-    token[j] = gridDim.y > 1 ? 0 : (int)__umulhi((unsigned)q, p.per_piece);      // (a CTA of a very wide row has one token)
-    if (p.pieces == 1) token[j] = q;
-    col[j] = 8 * (piece0 + q - token[j] * pieces);
-    id[j] = q < all ? ids[token[j]] : -1;
-    raw[j] = Piece{};
-    if (id[j] >= 0) {
-      if constexpr (WORDS == kDense)
-        raw[j] = load_piece(static_cast<const char*>(p.table) + id[j] * p.stride * type_bytes(p.type), p.type, col[j], p.width, p.in_vector);
-      else
-        raw[j] = load_codes<WORDS>(p, p.first + id[j] * p.width + col[j]);
+        for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
+      }
+      store_piece(p, first + token, col, x);
     }
+    return;
   }
+  for (int q0 = threadIdx.x; q0 < all; q0 += AHEAD * kLookThreads) {
+    Piece<KIND> raw[AHEAD];
 #pragma unroll
-  for (int j = 0; j < kLookAhead; ++j) {
-    if (threadIdx.x + j * kLookThreads >= all) break;
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (id[j] >= 0) {
-      if constexpr (WORDS == kDense) piece_floats(raw[j], p.type, x);
-      else code_floats<WORDS>(p, raw[j], p.first + id[j] * p.width + col[j], x);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
+    for (int j = 0; j < AHEAD; ++j) {
+      const int q = q0 + j * kLookThreads;
+      raw[j] = Piece<KIND>{};
+      if (q < all) {
+        const int token = token_of(q);
+        const long long id = ids[token];
+        if (id >= 0) raw[j] = load_piece<KIND>(p, id, column_of(q, token));
+      }
     }
-    store_piece(static_cast<char*>(p.out) + (first + token[j]) * p.out_stride * type_bytes(p.out_type), p.out_type, col[j], p.width,
-                p.out_vector, x);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int q = q0 + j * kLookThreads;
+      if (q >= all) break;
+      const int token = token_of(q), col = column_of(q, token);
+      const long long id = ids[token];
+      float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (id >= 0) {
+        piece_floats<KIND>(p, raw[j], id, col, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
+      }
+      store_piece(p, first + token, col, x);
+    }
   }
 }
 
-int enqueue_lookup(LookupParams p, bool held, cudaStream_t st) {
-  p.pieces = (p.width + 7) / 8;
+template <int KIND>
+void launch_lookup(const LookupParams& p, const dim3& grid, int kind, cudaStream_t st) {
+  if (kind == KIND) lookup_kernel<KIND><<<grid, kLookThreads, 0, st>>>(p);
+  else if constexpr (KIND < 16) launch_lookup<KIND + 1>(p, grid, kind, st);
+}
+
+int enqueue_lookup(LookupParams p, int kind, cudaStream_t st) {
+  const bool in_fits = kind > kDense32 || (is_aligned(p.table, 16) && p.stride * type_bytes(p.type) % 16 == 0);
+  p.spread = !in_fits || !is_aligned(p.out, 16) || p.out_stride * type_bytes(p.out_type) % 16 != 0;
+  p.pieces = p.spread ? (p.width + 255) / 256 * 32 : (p.width + 7) / 8;
   p.per_piece = (unsigned)(((1ull << 32) + p.pieces - 1) / p.pieces);       // (not used for one piece, which it does not fit)
-  p.in_vector = !held && is_aligned(p.table, 16) && p.stride * type_bytes(p.type) % 16 == 0;
-  p.out_vector = is_aligned(p.out, 16) && p.out_stride * type_bytes(p.out_type) % 16 == 0;
+  p.here = std::min(p.pieces, kLookPieces);
   const int across = (p.pieces + kLookPieces - 1) / kLookPieces;
   p.per_cta = std::max(1, kLookPieces / p.pieces);
   const long long ctas = (p.count + p.per_cta - 1) / p.per_cta;
   if (ctas > 0x7FFFFFFF) return QADAM_ERR_SIZE;
-  const dim3 grid((unsigned)ctas, across);
-  const int bits = p.kx + 2;
-  if (!held) lookup_kernel<kDense><<<grid, kLookThreads, 0, st>>>(p);
-  else if (bits <= 4) lookup_kernel<2><<<grid, kLookThreads, 0, st>>>(p);
-  else if (bits <= 8) lookup_kernel<3><<<grid, kLookThreads, 0, st>>>(p);
-  else lookup_kernel<5><<<grid, kLookThreads, 0, st>>>(p);
+  launch_lookup<kDense16>(p, dim3((unsigned)ctas, across), kind, st);
   return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
@@ -1037,7 +1101,7 @@ int qadam_embedding_lookup(const void* table, int32_t type, int64_t rows, int64_
   p.table = table; p.type = type; p.rows = rows; p.stride = stride; p.width = (int)width;
   p.ids = ids; p.id_bits = id_bits; p.count = count; p.scale = scale;
   p.out = out; p.out_type = out_type; p.out_stride = out_stride; p.status = status;
-  return enqueue_lookup(p, false, static_cast<cudaStream_t>(stream));
+  return enqueue_lookup(p, type == QADAM_F32 ? kDense32 : kDense16, static_cast<cudaStream_t>(stream));
 }
 
 int qadam_held_lookup(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t rows, int64_t width,
@@ -1055,8 +1119,8 @@ int qadam_held_lookup(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_
   p.table = wcodes; p.rows = rows; p.width = (int)width;
   p.ids = ids; p.id_bits = id_bits; p.count = count; p.scale = scale;
   p.out = out; p.out_type = out_type; p.out_stride = out_stride; p.status = status;
-  p.kx = kx; p.first = first; p.words = (long long)(wcode_bytes / 4);
-  return enqueue_lookup(p, true, static_cast<cudaStream_t>(stream));
+  p.first = first; p.words = (long long)(wcode_bytes / 4);
+  return enqueue_lookup(p, kx + 2, static_cast<cudaStream_t>(stream));
 }
 
 int qadam_embedding_grad_query_sizes(int64_t count, int64_t rows, int64_t width, size_t* workspace_bytes) {

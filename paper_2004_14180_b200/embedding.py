@@ -77,7 +77,7 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     shape = ids.shape + (width,)
     stride = _row_stride(table, "table", table.shape, device)
     if out is None:
-        out, out_stride = torch.empty(shape, dtype=out_dtype or table.dtype, device=device), width
+        out, out_stride = torch.empty(*shape, dtype=out_dtype or table.dtype, device=device), width
     else:
         out, out_stride = _out(shape, out, out_dtype, device), _row_stride(out, "out", shape, device)
     with _Guard(device):
@@ -102,7 +102,7 @@ def held_lookup(wcodes: torch.Tensor, kx: int, ids: torch.Tensor, rows: int, wid
     ids = _tokens(ids, device)
     shape = ids.shape + (width,)
     if out is None:
-        out, out_stride = torch.empty(shape, dtype=out_dtype, device=device), width
+        out, out_stride = torch.empty(*shape, dtype=out_dtype, device=device), width
     else:
         out_stride = _row_stride(out, "out", shape, device)
     with _Guard(device):
