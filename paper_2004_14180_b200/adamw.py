@@ -186,8 +186,7 @@ class AdamW:
             self.m_scale, self.r_scale = (z(room // 128 + 4)[:self.D // 128], z(room // 128 + 4)[:self.D // 128]) if eight else (None, None)
             self.master = z(room)[:self.D] if master else None
             if master:
-                for w, o, k in zip(self.weights, self.off, self._lens):
-                    self.master[o:o + k].copy_(w.reshape(-1))
+                torch._foreach_copy_([self.master[o:o + k] for o, k in zip(self.off, self._lens)], [w.view(-1) for w in self.weights])
             self.count = torch.zeros(1, dtype=torch.int64, device=self.device)
             self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
             self._scratch = _Scratch(size.value, self.device)

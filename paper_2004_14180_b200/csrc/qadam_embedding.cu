@@ -679,7 +679,7 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
 // groups': in the order of the tokens, whoever it is.
 
 constexpr int kChunk = 32;
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 128;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr int kAhead = 8;                                  // rows a warp has asked for
 constexpr int kGroup = 32;                                 // chunks
@@ -696,7 +696,7 @@ struct GradParams {
   int grad_type;
   long long rows, grad_stride;
   int width, tiles;            // tiles: of 512 bytes of dy
-  int vector, grad_vector;     // rows of dy are aligned to 16 bytes, of the gradient to four elements
+  int vector, grad_vector;     // rows of dy are aligned to 16 bytes; of the gradient to four elements (1), to 16 bytes (2)
   int accumulate;
   float* partial;              // [chunks][2][tiles * columns]: of the row that began in an earlier chunk, of the one that goes on
   unsigned* joined;            // [3 chunks][tiles]: partial sums left in the group that begins there (2), groups
@@ -783,7 +783,7 @@ __device__ __noinline__ void finish_row_apart(const GradParams& p, char* dst, Co
 template <int COLS>
 __device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, const Columns<COLS>& c, const Sum<COLS>& sum) {
   char* dst = grad_row(p, row);
-  if (!p.grad_vector || !c.together(p.width)) {
+  if (p.grad_vector == 0 || !c.together(p.width)) {
     if (c.first < p.width) finish_row_apart<COLS>(p, dst, c, sum);
     return;
   }
@@ -805,19 +805,27 @@ __device__ __forceinline__ void finish_row(const GradParams& p, unsigned row, co
       }
       out[q] = r;
     }
+    return;
+  }
+  uint32_t w[COLS / 2];
+#pragma unroll
+  for (int q = 0; q < COLS; q += 4) {
+    float y[4] = {x[q], x[q + 1], x[q + 2], x[q + 3]};
+    if (p.accumulate) {
+      float old[4];
+      to_floats(load_raw4(dst, p.grad_type, c.first + q, 0, true), p.grad_type, old);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = __fadd_rn(old[k], y[k]);
+    }
+    const Raw4 r = p.grad_type == QADAM_BF16 ? from_floats(y, QADAM_BF16) : from_floats(y, QADAM_F16);
+    w[q / 2] = r.w[0];
+    w[q / 2 + 1] = r.w[1];
+  }
+  if (COLS == 8 && p.grad_vector == 2) {
+    *reinterpret_cast<uint4*>(dst + (size_t)c.first * 2) = make_uint4(w[0], w[1], w[COLS / 2 - 2], w[COLS / 2 - 1]);
   } else {
 #pragma unroll
-    for (int q = 0; q < COLS; q += 4) {
-      float y[4] = {x[q], x[q + 1], x[q + 2], x[q + 3]};
-      if (p.accumulate) {
-        float old[4];
-        to_floats(load_raw4(dst, p.grad_type, c.first + q, 0, true), p.grad_type, old);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = __fadd_rn(old[k], y[k]);
-      }
-      const Raw4 r = p.grad_type == QADAM_BF16 ? from_floats(y, QADAM_BF16) : from_floats(y, QADAM_F16);
-      reinterpret_cast<uint2*>(dst)[(c.first + q) / 4] = make_uint2(r.w[0], r.w[1]);
-    }
+    for (int q = 0; q < COLS; q += 4) reinterpret_cast<uint2*>(dst)[(c.first + q) / 4] = make_uint2(w[q / 2], w[q / 2 + 1]);
   }
 }
 
@@ -870,7 +878,7 @@ __device__ __forceinline__ void add_left(const GradParams& p, int chunk, bool be
 // This chunk's part of a split row.  Its group's chunks of the row: those that begin with the row, and the one before
 // them if it ends with it.
 template <int COLS>
-__device__ __noinline__ void leave_part(const GradParams& p, unsigned row, int chunk, int tile, Columns<COLS> c, Sum<COLS> sum) {
+__device__ __forceinline__ void leave_part(const GradParams& p, unsigned row, int chunk, int tile, Columns<COLS> c, Sum<COLS> sum) {
   const int lane = threadIdx.x % 32, group = chunk / kGroup * kGroup;
   const long long head = (long long)(group + lane) * p.chunk;
   const bool with = group + lane < p.chunks && p.keys[head] == row;              // chunk `group + lane` begins with the row
@@ -918,10 +926,11 @@ __device__ __noinline__ void leave_part(const GradParams& p, unsigned row, int c
 // worked out once per chunk.  Rows arrive through shared memory (cp.async), so that the ring of rows under way takes
 // no registers.
 template <int TYPE>
-__global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid_constant__ GradParams p) {
+__global__ void __launch_bounds__(kSumThreads, 7) sum_chunks_kernel(const __grid_constant__ GradParams p) {
   constexpr int COLS = kCols<TYPE>;
   __shared__ uint4 ring[kSumWarps][kAhead][32];
   __shared__ unsigned long long address[kSumWarps][2 * kChunk];
+  __shared__ unsigned rows[kSumWarps][2 * kChunk];
   const long long unit = (long long)blockIdx.x * kSumWarps + threadIdx.x / 32;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   if (unit >= (long long)p.chunks * p.tiles) return;
@@ -938,6 +947,8 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
   const long long row_bytes = p.dy_stride * (16 / COLS);
   address[warp][lane] = reinterpret_cast<unsigned long long>(p.dy) + (unsigned long long)(place0 * row_bytes);
   address[warp][32 + lane] = reinterpret_cast<unsigned long long>(p.dy) + (unsigned long long)(place1 * row_bytes);
+  rows[warp][lane] = key0;
+  rows[warp][32 + lane] = key1;
   const unsigned first = __shfl_sync(0xFFFFFFFFu, key0, 0);
   if (first == none) return;
   // bit i: token i is the last of its row in the window
@@ -967,13 +978,15 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
   // all lanes with columns have 16 aligned bytes of them (a lane without any asks for the row's first)
   const bool fast = __all_sync(0xFFFFFFFFu, together || !some);
   const unsigned long long column = some ? lane_bytes : 0ull;
-  auto ask = [&](unsigned i) {
-    if (i < (unsigned)to) {
-      const unsigned long long row = address[warp][i];
+  const unsigned long long* const where = address[warp];
+  uint4* const slots = &ring[warp][0][lane];
+  auto ask = [&](int i, unsigned slot) {
+    if (i < to) {
+      const unsigned long long row = where[i];
       if (fast)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + (i % kAhead << 9)), "l"(row + column) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + slot * 512u), "l"(row + column) : "memory");
       else if (some)
-        ring[warp][i % kAhead][lane] = gather_row<COLS>(reinterpret_cast<const void*>(row), c, p.width);
+        slots[slot * 32] = gather_row<COLS>(reinterpret_cast<const void*>(row), c, p.width);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -981,34 +994,36 @@ __global__ void __launch_bounds__(kSumThreads, 4) sum_chunks_kernel(const __grid
     // rows that will be added to are brought near while those of dy arrive
     for (int i = from; i < to; ++i)
       if (((ends >> i) & 1ull) != 0)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(grad_row(p, p.keys[begin + i]) + (size_t)c.first * type_bytes(p.grad_type)));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(grad_row(p, rows[warp][i]) + (size_t)c.first * type_bytes(p.grad_type)));
   }
 #pragma unroll 1
-  for (unsigned i = from; i < (unsigned)from + kAhead; ++i) ask(i);
+  for (int i = 0; i < kAhead; ++i) ask(from + i, i);
   Sum<COLS> sum;
 #pragma unroll
   for (int k = 0; k < COLS; ++k) sum.x[k] = 0.0f;
   bool leaves = split_before;                                        // the row's sum is a partial one
   // bit 0: this token ends its row, or what this warp has of it
   ends = (ends | 1ull << (to - 1)) >> from;
+  unsigned slot = 0u;
 #pragma unroll 1
-  for (unsigned i = from; i < (unsigned)to; ++i) {
+  for (int i = from; i < to; ++i) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
     float x[COLS];
-    row_floats<TYPE>(ring[warp][i % kAhead][lane], x);
+    row_floats<TYPE>(slots[slot * 32], x);
 #pragma unroll
     for (int k = 0; k < COLS; k += 2) {
       const float2 r = add2_rn(make_float2(sum.x[k], sum.x[k + 1]), make_float2(x[k], x[k + 1]));
       sum.x[k] = r.x;
       sum.x[k + 1] = r.y;
     }
-    ask(i + kAhead);
+    ask(i + kAhead, slot);
+    slot = (slot + 1) % kAhead;
     if (((unsigned)ends & 1u) != 0u) {
-      const bool goes_on = i + 1 == (unsigned)to && split_after;
+      const bool goes_on = i + 1 == to && split_after;
       if (leaves || goes_on) {
-        leave_part<COLS>(p, p.keys[begin + i], chunk, tile, c, sum);
+        leave_part<COLS>(p, rows[warp][i], chunk, tile, c, sum);
       } else {
-        finish_row<COLS>(p, p.keys[begin + i], c, sum);
+        finish_row<COLS>(p, rows[warp][i], c, sum);
       }
       leaves = false;
 #pragma unroll
@@ -1246,7 +1261,8 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   g.partial = reinterpret_cast<float*>(ws + l.partial);
   g.joined = s.joined;
   g.vector = is_aligned(dy, 16) && dy_stride % cols == 0;
-  g.grad_vector = is_aligned(grad, 4 * type_bytes(grad_type)) && grad_stride % 4 == 0;
+  g.grad_vector = !is_aligned(grad, 4 * type_bytes(grad_type)) || grad_stride % 4 != 0 ? 0
+                  : is_aligned(grad, 16) && grad_stride * type_bytes(grad_type) % 16 == 0 ? 2 : 1;
   const long long units = (long long)l.chunks * g.tiles;
   const unsigned grid = (unsigned)((units + kSumWarps - 1) / kSumWarps);
   if (dy_type == QADAM_F32) sum_chunks_kernel<QADAM_F32><<<grid, kSumThreads, 0, st>>>(g);
