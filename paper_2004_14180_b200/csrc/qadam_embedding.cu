@@ -300,8 +300,9 @@ struct ClearParams {
   void* grad;
   int type, width;
   long long rows, stride;
-  long long begin, end;        // this launch's share: 16-byte words where rows touch, else rows
-  int dense;                   // rows touch and begin on 16 bytes
+  long long begin, end;        // this launch's share: aligned 16-byte words where rows touch, else rows
+  int dense;                   // rows touch
+  int head, tail;              // 2-byte pieces before and behind the words, cleared with the first of them
   int ctas;                    // CTAs of the launch that clear
 };
 
@@ -328,7 +329,13 @@ struct SortParams {
 
 __device__ void clear_share(const ClearParams& c, int cta) {
   if (c.dense) {
-    uint4* w = static_cast<uint4*>(c.grad);
+    unsigned short* edge = static_cast<unsigned short*>(c.grad);
+    uint4* w = reinterpret_cast<uint4*>(edge + c.head);
+    if (c.begin == 0 && cta == 0 && threadIdx.x < 8) {
+      if ((int)threadIdx.x < c.head) edge[threadIdx.x] = 0;
+      unsigned short* end = edge + c.rows * c.width * (type_bytes(c.type) / 2) - c.tail;
+      if ((int)threadIdx.x < c.tail) end[threadIdx.x] = 0;
+    }
     for (long long i = c.begin + (long long)cta * blockDim.x + threadIdx.x; i < c.end; i += (long long)c.ctas * blockDim.x)
       w[i] = make_uint4(0u, 0u, 0u, 0u);
   } else {
@@ -741,17 +748,31 @@ __device__ __forceinline__ void row_floats(const uint4& r, float (&x)[kCols<TYPE
   }
 }
 
-// A lane's part of a row that is not 16 aligned bytes.
+// A lane's parts of up to kGather rows that are not 16 aligned bytes, into its slots: all loads are under way before the
+// first is stored.
+constexpr int kGather = 4;
 template <int COLS>
-__device__ __noinline__ uint4 gather_row(const void* row, Columns<COLS> c, int width) {
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
+__device__ __noinline__ void gather_rows(uint4* slots, unsigned slot, const unsigned long long* where, int rows, Columns<COLS> c, int width) {
+  // columns and rows that are not there take the last one's place: what becomes of them is not used
+  unsigned v[kGather][COLS];
 #pragma unroll
-  for (int k = 0; k < COLS; ++k) {
-    if (c.at(k) >= width) break;
-    if constexpr (COLS == 4) w[k] = static_cast<const uint32_t*>(row)[c.at(k)];
-    else w[k / 2] |= (uint32_t) static_cast<const unsigned short*>(row)[c.at(k)] << (16 * (k % 2));
+  for (int r = 0; r < kGather; ++r) {
+    const void* row = reinterpret_cast<const void*>(where[min(r, rows - 1)]);
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) {
+      const int at = min(c.at(k), width - 1);
+      if constexpr (COLS == 4) v[r][k] = static_cast<const uint32_t*>(row)[at];
+      else v[r][k] = static_cast<const unsigned short*>(row)[at];
+    }
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+  for (int r = 0; r < kGather; ++r) {
+    if (r >= rows) break;
+    uint4 w;
+    if constexpr (COLS == 4) w = make_uint4(v[r][0], v[r][1], v[r][2], v[r][3]);
+    else w = make_uint4(v[r][0] | v[r][1] << 16, v[r][2] | v[r][3] << 16, v[r][4] | v[r][5] << 16, v[r][6] | v[r][7] << 16);
+    slots[(slot + r) * 32] = w;
+  }
 }
 
 __device__ __forceinline__ char* grad_row(const GradParams& p, unsigned row) {
@@ -981,13 +1002,8 @@ __global__ void __launch_bounds__(kSumThreads, 7) sum_chunks_kernel(const __grid
   const unsigned long long* const where = address[warp];
   uint4* const slots = &ring[warp][0][lane];
   auto ask = [&](int i, unsigned slot) {
-    if (i < to) {
-      const unsigned long long row = where[i];
-      if (fast)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + slot * 512u), "l"(row + column) : "memory");
-      else if (some)
-        slots[slot * 32] = gather_row<COLS>(reinterpret_cast<const void*>(row), c, p.width);
-    }
+    if (i < to && fast)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot0 + slot * 512u), "l"(where[i] + column) : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (p.accumulate && some) {
@@ -1008,6 +1024,7 @@ __global__ void __launch_bounds__(kSumThreads, 7) sum_chunks_kernel(const __grid
 #pragma unroll 1
   for (int i = from; i < to; ++i) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    if (!fast && some && slot % kGather == 0u) gather_rows<COLS>(slots, slot, where + i, min(to - i, kGather), c, p.width);
     float x[COLS];
     row_floats<TYPE>(slots[slot * 32], x);
 #pragma unroll
@@ -1017,7 +1034,7 @@ __global__ void __launch_bounds__(kSumThreads, 7) sum_chunks_kernel(const __grid
       sum.x[k + 1] = r.y;
     }
     ask(i + kAhead, slot);
-    slot = (slot + 1) % kAhead;
+    slot = (slot + 1) % kAhead;                            // (a multiple of kGather)
     if (((unsigned)ends & 1u) != 0u) {
       const bool goes_on = i + 1 == to && split_after;
       if (leaves || goes_on) {
@@ -1188,9 +1205,13 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   ClearParams& c = s.clear;
   c.grad = grad; c.type = grad_type; c.width = (int)width; c.rows = rows; c.stride = grad_stride;
   const int64_t row_bytes = width * type_bytes(grad_type);
-  c.dense = grad_stride == width && is_aligned(grad, 16) && rows * row_bytes % 16 == 0;
+  // rows that touch and have a whole aligned word between them are one run of words with an edge at either end
+  const int64_t to_word = -(int64_t)(reinterpret_cast<uintptr_t>(grad)) & 15, run = rows * row_bytes - to_word;
+  c.dense = grad_stride == width && run >= 16;
+  c.head = (int)(to_word / 2);
+  c.tail = (int)(run % 16 / 2);
   // what there is to clear is dealt out evenly to the launches that sort
-  const long long to_clear = accumulate ? 0 : c.dense ? rows * row_bytes / 16 : rows;
+  const long long to_clear = accumulate ? 0 : c.dense ? run / 16 : rows;
   const int launches = count == 0 || ranked || clustered ? 1 : 2 * passes;
   int launch = 0;
   auto share = [&](int threads) {

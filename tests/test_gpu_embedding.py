@@ -120,7 +120,7 @@ def _check_grad(got, ids, dy, rows, scale, out, old=None, padding=-1):
 
 
 SIZES = [(1, 1, 1), (1, 5, 768), (2, 2, 3), (31, 7, 127), (32, 7, 128), (33, 7, 129), (64, 1, 64), (65, 40, 4), (300, 513, 100),
-         (1025, 512, 257), (4096, 30522, 64), (4097, 2, 260), (8192, 1, 9), (8193, 600000, 5), (100, 2000000, 2), (9001, 300000, 12),
+         (1025, 512, 257), (4096, 30522, 64), (4097, 2, 260), (8192, 1, 9), (8193, 600000, 5), (100, 2000000, 2), (1500, 5000000, 1), (9001, 300000, 12),
          (20000, 50, 40), (40001, 700, 300), (90000, 30, 20), (1100000, 1000, 3)]
 
 
