@@ -361,7 +361,8 @@ int qadam_destroy(qadam_ctx* ctx);
  *  - calls of one context, and calls that share a workspace, must be ordered by the caller (one
  *    stream, or events between streams): they use the same scratch.  That goes for graphs that
  *    captured such calls too.  Everything but the create, query and poll calls may be captured;
- *  - a tensor may start at any multiple of its element's size (16-byte alignment is faster).
+ *  - a tensor may start at any multiple of its element's size (16-byte alignment is faster);
+ *  - outputs do not overlap inputs or scratch.
  * =========================================================================================== */
 
 enum { QADAM_F32 = 0, QADAM_BF16 = 1, QADAM_F16 = 2 };       /* element types */
@@ -415,7 +416,7 @@ int qadam_norm_destroy(qadam_norm* ctx);
  *
  * Layout: moments and master weights are in the padded layout: tensor s starts at off[s], the
  * running sum of lengths rounded up to 128; pads are 0 and stay 0.  Weights and gradients are
- * the caller's own tensors, each contiguous and anywhere.
+ * the caller's own tensors, each contiguous and anywhere; no weight overlaps another buffer.
  *
  * Weights of 16 bits are rounded to nearest after each step, which loses a step smaller than half
  * of a weight's last place; with master = 1 the step reads and writes binary32 master weights
@@ -521,7 +522,7 @@ int qadam_embedding_grad_query_sizes(int64_t count, int64_t rows, int64_t width,
  * a token become 0.  accumulate = 1: round(grad[i][:] + scale * sum) for rows with a token, the others
  * are left as they are.  dy: device, [count][dy_stride >= width]; grad: device, [rows][grad_stride >=
  * width], only its first `width` columns are written.  Sums are binary32, over tokens sorted by id, in an
- * order that depends on the sizes alone: the same bits every time.  Tokens that are negative or equal to `padding`
+ * order that depends on ids and sizes alone: the same bits every time.  Tokens that are negative or equal to `padding`
  * (-1: none) are left out; ids >= rows are left out and set QADAM_ST_INDEX in *status (device, may be
  * NULL).  count <= 2^30, rows < 2^31 - 1, width <= 2^22, count * width <= 2^44. */
 int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const void* dy, int32_t dy_type,

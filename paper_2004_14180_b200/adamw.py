@@ -148,6 +148,7 @@ class AdamW:
     master: keep float32 master weights (`self.master`, padded layout; set from `weights` here).
     weight_decay: one factor, or one for each tensor.
     Moments are `m`, `v` ([D] float32, padded layout) or `m`, `r` ([D] uint8) with `m_scale`, `r_scale`.
+    Weights are updated in place, where they are now.  Steps run on the current stream; keep the holder until they are done.
     """
 
     ctx = None
@@ -166,6 +167,11 @@ class AdamW:
         if not all(w.is_contiguous() for w in self.weights):
             raise ValueError("weights must be contiguous")
         self._types = [element_type((g if g is not None else w).dtype, "grads") for g, w in zip(grads, self.weights)]
+        end = 0
+        for first, size in sorted((w.data_ptr(), w.numel() * w.element_size()) for w in self.weights if w.numel()):
+            if first < end:
+                raise ValueError("weights overlap: a tensor may be listed once only")
+            end = first + size
         decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
         if len(decay) != n:
             raise ValueError(f"{len(decay)} weight decays for {n} weights")

@@ -450,7 +450,8 @@ class QAdam:
         return qadam_poll_status(self.ctx)
 
     def lookup(self, segment: int, width: int, ids: torch.Tensor, scale: float = 1.0, out_dtype=torch.bfloat16, **kw):
-        """Rows of a tensor as the workers hold it (the broadcast of the last step), see `held_lookup`."""
+        """Rows of a tensor as the workers hold it (the broadcast of the last step), see `held_lookup`.  Runs on the current
+        stream: if the context was given another one, the two have to be ordered."""
         from .embedding import held_lookup
         if self.kx < 0:
             raise ValueError("nothing is broadcast in packed form with kx = -1: look the rows up in x")

@@ -128,9 +128,39 @@ def _run(lens, w, g, bits, master, steps=3, shift=0, scale=None, decay=0.01, mis
 
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("w,g,master", [("f32", "f32", False), ("f32", "bf16", False), ("bf16", "bf16", True), ("bf16", "f32", True),
-                                        ("f16", "f16", True), ("bf16", "bf16", False), ("f16", "f32", False), ("f32", "f16", True)])
+                                        ("f16", "f16", True), ("f32", "f32", True), ("bf16", "bf16", False), ("f16", "f32", False), ("f32", "f16", True)])
 def test_step_is_the_plain_statement(bits, w, g, master):
     _run(RAGGED, DTYPES[w], DTYPES[g], bits, master)
+
+
+@pytest.mark.parametrize("large,master", [(2_700_001, False), (5_300_000, True), (10_600_130, False)])
+def test_several_pairs_of_rows_to_a_warp(large, master):
+    # from 2.56, 5.12 and 10.24 x 10^6 elements on a warp takes 2, 4 and 8 pairs; compared: small tensors around a large one,
+    # and parts of that one (a tensor's random bits go by its offset: a part that begins at a multiple of 256 is one of its own)
+    lens = [700, large, 129, 4000]
+    gen = torch.Generator(device="cuda").manual_seed(large)
+    wtype = torch.bfloat16 if master else torch.float32
+    w = [(torch.randn(n, device="cuda", generator=gen) * 0.05).to(wtype) for n in lens]
+    g = [(torch.randn(n, device="cuda", generator=gen) * 0.01).to(wtype) for n in lens]
+    opt = qb.AdamW(w, g, state_bits=8, master=master, seed=77, **HYPER)
+    x0 = [(opt.view(opt.master, i) if master else t).clone() for i, t in enumerate(w)]
+    opt.step(1)
+    k = adamw_constants(HYPER["beta1"], HYPER["beta2"], HYPER["lr"], 0.0, 1)
+    last = (large // 4096 - 1) * 4096
+    parts = [(0, 0, 700), (1, 0, 8192), (1, 1 << 20, (1 << 20) + 9000), (1, last, large), (2, 0, 129), (3, 0, 4000)]
+    for i, lo, hi in parts:
+        off, gp = opt.off[i] + lo, _pad(_np(g[i][lo:hi]))
+        z, s = np.zeros(gp.size, np.uint8), np.zeros(gp.size // 128, np.float32)
+        x, cm, sm, cr, sr = adamw8(_pad(_np(x0[i][lo:hi])), z, s, z, s, gp, k, HYPER["eps"], off, 1, 77)
+        # whole rows of the part: a row that goes on behind it has another largest value
+        n = hi - lo if hi == lens[i] else (hi - lo) // 128 * 128
+        live = slice(off, off + n)
+        rows = slice(off // 128, off // 128 + n // 128)
+        assert np.array_equal(opt.m[live].cpu().numpy(), cm[:n]) and np.array_equal(opt.r[live].cpu().numpy(), cr[:n]), (i, lo)
+        assert _same(_np(opt.m_scale[rows]), sm[:n // 128]) and _same(_np(opt.r_scale[rows]), sr[:n // 128])
+        got = _np((opt.view(opt.master, i) if master else w[i])[lo:lo + n])
+        # the step is at most lr (1 + 2^-10) at t = 1; its quotient is off by 1.5 x 2^-22, x by a rounding on either side
+        assert np.all(np.abs(got - x[:n]) <= 1.1e-3 * 1.5 * 2.0 ** -22 + 2.0 ** -23 * np.abs(x[:n]))
 
 
 @pytest.mark.parametrize("bits", [32, 8])
@@ -395,6 +425,32 @@ def test_step_runs_on_the_current_stream():
         got = w.clone()
     s.synchronize()
     assert bool((got != 0).all()) and abs(float(opt.m[0]) - 0.1) < 1e-6      # g = 20 * 0.05, m = 0.1 g
+
+
+def test_refusals_of_the_holders():
+    w, g = torch.zeros(100, device="cuda"), torch.zeros(100, device="cuda")
+    for bad in (lambda: qb.AdamW([w], []), lambda: qb.AdamW([], []), lambda: qb.AdamW([w, w[50:]], [g, g[50:]]), lambda: qb.AdamW([w, w], [g, g]),
+                lambda: qb.AdamW([w.double()], [g]), lambda: qb.AdamW([w], [g.int()]), lambda: qb.AdamW([w], [g[:99]]),
+                lambda: qb.AdamW([w.view(10, 10).t()], [g]), lambda: qb.AdamW([w], [g], weight_decay=[0.1, 0.1]),
+                lambda: qb.AdamW([w], [g.cpu()]), lambda: qb.GradNorm([]), lambda: qb.GradNorm([g.view(10, 10)[:, :3]]),
+                lambda: qb.GradNorm([g])(1.0, out=torch.zeros(3, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: qb.AdamW([w], [g], state_bits=16), lambda: qb.AdamW([w], [g], beta1=1.0), lambda: qb.AdamW([w], [g], eps=0.0),
+                lambda: qb.GradNorm([g])(0.0), lambda: qb.GradNorm([g])(float("nan"))):
+        with pytest.raises(qb.QAdamError):
+            bad()
+    opt = qb.AdamW([w], [g])
+    for bad in (lambda: opt.bind([g.bfloat16()]), lambda: opt.bind([]), lambda: opt.step(1, lr=-1.0), lambda: opt.step(1, lr=float("nan")),
+                lambda: opt.step(1, grad_scale=torch.zeros(2, device="cuda")), lambda: opt.step(1, grad_scale=torch.zeros(1)),
+                lambda: opt.moments(out=(w, g))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(qb.QAdamError):
+        opt.step(0)
+    opt.close()
+    with pytest.raises(qb.QAdamError):
+        opt.step(1)
 
 
 def test_resume_from_saved_buffers():

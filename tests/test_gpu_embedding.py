@@ -203,9 +203,32 @@ def test_gradient_against_differences(count, rows):
     assert abs(slope - want) <= size * (count + 2) * 2.0 ** -24 + 1e-9
 
 
-def test_captured_and_replayed_with_new_tokens():
+def test_refusals():
+    t, ids, dy = torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, 8, device="cuda")
+    codes = torch.zeros(160, dtype=torch.uint8, device="cuda")
+    for bad in (lambda: qb.embedding_lookup(t, ids.float()), lambda: qb.embedding_lookup(t, ids.cpu()), lambda: qb.embedding_lookup(t.t(), ids),
+                lambda: qb.embedding_lookup(t.double(), ids), lambda: qb.embedding_lookup(t[0], ids),
+                lambda: qb.embedding_lookup(t, ids, out=torch.zeros(4, 7, device="cuda")),
+                lambda: qb.embedding_lookup(t, ids, out=torch.zeros(4, 8, device="cuda"), out_dtype=torch.bfloat16),
+                lambda: qb.embedding_lookup(t, ids, out=torch.zeros(8, 4, device="cuda").t()),
+                lambda: qb.embedding_lookup(t, ids, status=torch.zeros(1, device="cuda")),
+                lambda: qb.held_lookup(codes.int(), 6, ids, 10, 16), lambda: qb.held_lookup(codes[::2], 6, ids, 5, 16),
+                lambda: qb.embedding_grad(ids, dy[:3], 10), lambda: qb.embedding_grad(ids, dy, 10, accumulate=True),
+                lambda: qb.embedding_grad(ids, dy, 10, out=torch.zeros(9, 8, device="cuda")), lambda: qb.embedding_grad(ids, dy.double(), 10),
+                lambda: qb.embedding_grad(ids, dy[:1].expand(4, 8), 10), lambda: qb.embedding_grad(ids, dy, 10, dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: qb.held_lookup(codes, 15, ids, 10, 16), lambda: qb.held_lookup(codes, 6, ids, 11, 16),
+                lambda: qb.held_lookup(codes[:150], 6, ids, 9, 16), lambda: qb.embedding_lookup(t, ids, scale=float("nan")),
+                lambda: qb.embedding_grad(ids, dy, 10, scale=float("inf"))):
+        with pytest.raises(qb.QAdamError):
+            bad()
+
+
+@pytest.mark.parametrize("count", [2000, 5000, 40000])
+def test_captured_and_replayed_with_new_tokens(count):
     gen = _gen(6)
-    ids, dy = _ids(gen, 2000, 300), torch.randn(2000, 96, generator=gen, device="cuda")
+    ids, dy = _ids(gen, count, 300), torch.randn(count, 96, generator=gen, device="cuda")
     table, out = torch.randn(300, 96, generator=gen, device="cuda"), torch.empty(300, 96, device="cuda")
     qb.embedding_grad(ids, dy, 300, out=out)
     qb.embedding_lookup(table, ids)
@@ -215,7 +238,7 @@ def test_captured_and_replayed_with_new_tokens():
         rows = qb.embedding_lookup(table, ids, scale=2.0)
         qb.embedding_grad(ids, rows, 300, out=out)
     for _ in range(3):
-        ids.copy_(_ids(gen, 2000, 300))
+        ids.copy_(_ids(gen, count, 300))
         graph.replay()
         fresh = qb.embedding_lookup(table, ids, scale=2.0)
         assert torch.equal(rows, fresh) and torch.equal(out, qb.embedding_grad(ids, fresh, 300))
