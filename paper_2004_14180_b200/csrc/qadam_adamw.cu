@@ -143,6 +143,7 @@ __device__ __forceinline__ bool gradient_factor(const AdamParams& p, float& c) {
 template <int CAP>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamParams p,
                                                              const __grid_constant__ Pointers<CAP> grads) {
+  wait_for_previous_launch();
   const AdamTile T = p.tiles[p.first + blockIdx.x];
   const void* g = grads.at[T.seg - p.tensor_base];
   float c;
@@ -338,6 +339,7 @@ __device__ __forceinline__ Raw4 load_whole4(const char* p) {
 template <bool W16, bool G16, bool MASTER, int CAP>
 __global__ void __launch_bounds__(kAdamThreads, kEightCtas) adamw8_kernel(const __grid_constant__ AdamParams p,
                                                                          const __grid_constant__ Pointers<CAP> grads) {
+  wait_for_previous_launch();
   constexpr bool X16 = W16 && !MASTER;                         // what the step reads
   constexpr int kGBytes = G16 ? 2 : 4, kWBytes = W16 ? 2 : 4;
   const int t = p.first + blockIdx.x;
@@ -395,6 +397,7 @@ __global__ void __launch_bounds__(kAdamThreads, kEightCtas) adamw8_kernel(const 
 // The scalars of the next step, from the device's own count and step size.
 __global__ void adamw_count_kernel(StepScalars* now, long long* count, const float* lr, float lr_default, float beta1,
                                    float beta2, const float* grad_scale) {
+  wait_for_previous_launch();
   const long long t = *count + 1;
   if (grad_scale == nullptr || finite(*grad_scale)) *count = t;
   *now = step_scalars(lr != nullptr ? (double)*lr : (double)lr_default, beta1, beta2, t);
@@ -407,6 +410,7 @@ constexpr int kReadCtasPerSm = 16;
 
 __global__ void __launch_bounds__(kReadThreads) adamw_moments_kernel(const uint32_t* m, const uint32_t* r, const float* m_scale,
                                                                      const float* r_scale, long long quads, float4* m32, float4* v32) {
+  wait_for_previous_launch();
   for (long long q = (long long)blockIdx.x * kReadThreads + threadIdx.x; q < quads; q += (long long)gridDim.x * kReadThreads) {
     float x[4];
     if (m32 != nullptr) {
@@ -512,8 +516,7 @@ namespace {
 
 template <bool W16, bool G16, bool MASTER, int CAP>
 bool launch_eight(const AdamParams& p, const Pointers<CAP>& grads, cudaStream_t st) {
-  adamw8_kernel<W16, G16, MASTER, CAP><<<p.num_tiles, kAdamThreads, 0, st>>>(p, grads);
-  return cuda_call(cudaGetLastError());
+  return launch(adamw8_kernel<W16, G16, MASTER, CAP>, p.num_tiles, kAdamThreads, 0, 0, st, p, grads);
 }
 
 template <int CAP>
@@ -522,10 +525,7 @@ bool launch_adam(qadam_adamw* c, const AdamParams& p, const AdamGeometry::Run& r
   Pointers<CAP> grads;
   std::copy(c->grads.begin() + run.tensor_base, c->grads.begin() + run.tensor_base + run.tensors, grads.at);
   c->launches += 1;
-  if (c->cfg.state_bits == 32) {
-    adamw_kernel<CAP><<<p.num_tiles, kAdamThreads, 0, st>>>(p, grads);
-    return cuda_call(cudaGetLastError());
-  }
+  if (c->cfg.state_bits == 32) return launch(adamw_kernel<CAP>, p.num_tiles, kAdamThreads, 0, 0, st, p, grads);
   switch (run.kind + (p.master != nullptr ? 4 : 0)) {
     case 0: return launch_eight<false, false, false>(p, grads, st);
     case 1: return launch_eight<false, true, false>(p, grads, st);
@@ -659,9 +659,9 @@ int qadam_adamw_step_counted(qadam_adamw* c, const float* lr, const float* grad_
   if (!on.ok()) return QADAM_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   StepScalars* now = reinterpret_cast<StepScalars*>(static_cast<unsigned char*>(c->buf.workspace) + c->geo.off_now);
-  adamw_count_kernel<<<1, 1, 0, st>>>(now, reinterpret_cast<long long*>(c->buf.count), lr, c->cfg.lr, c->cfg.beta1,
-                                      c->cfg.beta2, grad_scale);
-  if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  if (!launch(adamw_count_kernel, 1, 1, 0, 0, st, now, reinterpret_cast<long long*>(c->buf.count), lr, c->cfg.lr, c->cfg.beta1,
+              c->cfg.beta2, grad_scale))
+    return QADAM_ERR_CUDA;
   c->launches += 1;
   return enqueue_step(c, StepScalars{}, now, grad_scale, st);
 }
@@ -675,10 +675,10 @@ int qadam_adamw_moments(qadam_adamw* c, float* m32, float* v32, void* stream) {
   const OnDevice on(c->device);
   if (!on.ok()) return QADAM_ERR_CUDA;
   const long long grid = std::min<long long>((quads + kReadThreads - 1) / kReadThreads, (long long)c->sm_count * kReadCtasPerSm);
-  adamw_moments_kernel<<<(unsigned)grid, kReadThreads, 0, static_cast<cudaStream_t>(stream)>>>(
-      static_cast<const uint32_t*>(c->buf.m), static_cast<const uint32_t*>(c->buf.v), c->buf.m_scale, c->buf.r_scale, quads,
-      reinterpret_cast<float4*>(m32), reinterpret_cast<float4*>(v32));
-  if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  if (!launch(adamw_moments_kernel, grid, kReadThreads, 0, 0, static_cast<cudaStream_t>(stream), static_cast<const uint32_t*>(c->buf.m),
+              static_cast<const uint32_t*>(c->buf.v), static_cast<const float*>(c->buf.m_scale), static_cast<const float*>(c->buf.r_scale),
+              quads, reinterpret_cast<float4*>(m32), reinterpret_cast<float4*>(v32)))
+    return QADAM_ERR_CUDA;
   c->launches += 1;
   return QADAM_OK;
 }

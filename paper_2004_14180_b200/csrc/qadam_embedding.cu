@@ -38,7 +38,7 @@ struct LookupParams {
   int type;
   long long rows, stride;
   int width, pieces;           // pieces: of a row
-  int here;                    // of a row in one CTA, at the most
+  int here, across;            // of a row in one CTA, at the most; CTAs of a row
   unsigned per_piece;          // 2^32 / pieces, rounded up: a division by a product
   const void* ids;
   int id_bits;
@@ -193,9 +193,10 @@ __device__ __forceinline__ void store_piece(const LookupParams& p, long long t, 
 
 template <int KIND>
 __global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_constant__ LookupParams p) {
+  wait_for_previous_launch();
   constexpr int AHEAD = kLookAhead<KIND>;
   __shared__ long long ids[kLookPieces];
-  const long long first = (long long)blockIdx.x * p.per_cta;
+  const long long first = (long long)(blockIdx.x / p.across) * p.per_cta;
   const int tokens = (int)min((long long)p.per_cta, p.count - first);
   for (int t = threadIdx.x; t < tokens; t += kLookThreads) {
     long long id = load_id(p.ids, p.id_bits, first + t);
@@ -206,9 +207,9 @@ __global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_co
     ids[t] = id;
   }
   __syncthreads();
-  const int piece0 = blockIdx.y * p.here, pieces = min(p.here, p.pieces - piece0), all = tokens * pieces;
+  const int piece0 = (int)(blockIdx.x % p.across) * p.here, pieces = min(p.here, p.pieces - piece0), all = tokens * pieces;
   // piece q of the CTA's: its token (there is one where a row has more pieces than a CTA) and column
-  auto token_of = [&](int q) { return gridDim.y > 1 ? 0 : p.pieces == 1 ? q : (int)__umulhi((unsigned)q, p.per_piece); };
+  auto token_of = [&](int q) { return p.across > 1 ? 0 : p.pieces == 1 ? q : (int)__umulhi((unsigned)q, p.per_piece); };
   auto column_of = [&](int q, int token) { return piece_column(p, piece0 + q - token * pieces); };
   if (p.spread) {
     for (int q = threadIdx.x; q < all; q += kLookThreads) {
@@ -254,9 +255,10 @@ __global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_co
 }
 
 template <int KIND>
-void launch_lookup(const LookupParams& p, const dim3& grid, int kind, cudaStream_t st) {
-  if (kind == KIND) lookup_kernel<KIND><<<grid, kLookThreads, 0, st>>>(p);
-  else if constexpr (KIND < 16) launch_lookup<KIND + 1>(p, grid, kind, st);
+bool launch_lookup(const LookupParams& p, long long grid, int kind, cudaStream_t st) {
+  if (kind == KIND) return launch(lookup_kernel<KIND>, grid, kLookThreads, 0, 0, st, p);
+  if constexpr (KIND < 16) return launch_lookup<KIND + 1>(p, grid, kind, st);
+  return false;
 }
 
 int enqueue_lookup(LookupParams p, int kind, cudaStream_t st) {
@@ -265,12 +267,11 @@ int enqueue_lookup(LookupParams p, int kind, cudaStream_t st) {
   p.pieces = p.spread ? (p.width + 255) / 256 * 32 : (p.width + 7) / 8;
   p.per_piece = (unsigned)(((1ull << 32) + p.pieces - 1) / p.pieces);       // (not used for one piece, which it does not fit)
   p.here = std::min(p.pieces, kLookPieces);
-  const int across = (p.pieces + kLookPieces - 1) / kLookPieces;
   p.per_cta = std::max(1, kLookPieces / p.pieces);
   const long long ctas = (p.count + p.per_cta - 1) / p.per_cta;
-  if (ctas > 0x7FFFFFFF) return QADAM_ERR_SIZE;
-  launch_lookup<kDense16>(p, dim3((unsigned)ctas, across), kind, st);
-  return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
+  p.across = (p.pieces + kLookPieces - 1) / kLookPieces;
+  if (ctas > 0x7FFFFFFF / p.across) return QADAM_ERR_SIZE;
+  return launch_lookup<kDense16>(p, ctas * p.across, kind, st) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
 // ---------------------------------------------------------------- gradient: tokens sorted by id
@@ -388,6 +389,7 @@ __host__ __device__ inline int rank_quads(int count) { return (count + 4 * kRank
 // Few tokens: a token's place is the number of tokens before it, by row and place in one number (`shift` bits
 // of place).  T^2 comparisons of a cycle or two on all lanes.
 __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constant__ SortParams p) {
+  wait_for_previous_launch();
   extern __shared__ uint4 ranked[];                        // p.count numbers, filled up with the largest
   __shared__ unsigned before[kRankWarps][kRankPer];
   const int ctas = (p.count + kRankPer - 1) / kRankPer;
@@ -510,6 +512,7 @@ __device__ __forceinline__ unsigned scan_digits(unsigned x, unsigned* warp_total
 // little more than its barriers: five launches of one after the other were three times as long.
 template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid_constant__ SortParams p) {
+  wait_for_previous_launch();
   static_assert(kDigits <= kSortThreads, "a digit to a thread");
   extern __shared__ uint2 exchange[];                      // [kSortThreads << each]
   __shared__ unsigned short seen[kSortWarps][kDigits];
@@ -583,6 +586,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid
 // Many tokens: at most 9 bits a pass, lowest first.  Counts of each digit in each CTA's run of tokens; then
 // every token to its place, behind all smaller digits and the same digit in earlier runs.
 __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid_constant__ SortParams p) {
+  wait_for_previous_launch();
   __shared__ unsigned n[kDigits];
   if ((int)blockIdx.x >= p.runs) {
     clear_share(p.clear, blockIdx.x - p.runs);
@@ -603,6 +607,7 @@ __global__ void __launch_bounds__(kSortThreads) count_digits_kernel(const __grid
 
 // Counts to places for very many runs, by one CTA: a digit to a thread.
 __global__ void __launch_bounds__(kSortThreads) scan_counts_kernel(unsigned* counts, int runs, int digits) {
+  wait_for_previous_launch();
   static_assert(kDigits <= kSortThreads, "a digit to a thread");
   __shared__ unsigned warp_total[kSortWarps];
   const int d = threadIdx.x;
@@ -622,6 +627,7 @@ __global__ void __launch_bounds__(kSortThreads) scan_counts_kernel(unsigned* cou
 }
 
 __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_constant__ SortParams p) {
+  wait_for_previous_launch();
   __shared__ unsigned short seen[kSortWarps][kDigits];
   __shared__ unsigned start[kDigits], warp_total[kSortWarps];
   if ((int)blockIdx.x >= p.runs) {
@@ -948,6 +954,7 @@ __device__ __forceinline__ void leave_part(const GradParams& p, unsigned row, in
 // no registers.
 template <int TYPE>
 __global__ void __launch_bounds__(kSumThreads, 7) sum_chunks_kernel(const __grid_constant__ GradParams p) {
+  wait_for_previous_launch();
   constexpr int COLS = kCols<TYPE>;
   __shared__ uint4 ring[kSumWarps][kAhead][32];
   __shared__ unsigned long long address[kSumWarps][2 * kChunk];
@@ -1076,7 +1083,7 @@ int grad_layout(int64_t count, int64_t rows, int64_t width, GradLayout* l) {
   }
   if (l->chunk == kChunk) room = std::max<int64_t>(room, (count + kChunk - 1) / kChunk);
   l->chunks = (int)((count + l->chunk - 1) / l->chunk);
-  if (room * tiles > (int64_t)1 << 33) return QADAM_ERR_SIZE;      // (CTAs of one launch)
+  if (room * tiles > (int64_t)1 << 32) return QADAM_ERR_SIZE;      // (CTAs of one launch)
   size_t at = 0;
   const size_t list = round_up256((size_t)count * sizeof(unsigned));
   for (int i = 0; i < 2; ++i) {
@@ -1213,19 +1220,18 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   // what there is to clear is dealt out evenly to the launches that sort
   const long long to_clear = accumulate ? 0 : c.dense ? run / 16 : rows;
   const int launches = count == 0 || ranked || clustered ? 1 : 2 * passes;
-  int launch = 0;
+  int turn = 0;
   auto share = [&](int threads) {
-    c.begin = to_clear * launch / launches;
-    c.end = to_clear * (launch + 1) / launches;
-    ++launch;
+    c.begin = to_clear * turn / launches;
+    c.end = to_clear * (turn + 1) / launches;
+    ++turn;
     const long long each = c.dense ? threads : 1;
     c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, (count <= kFewTokens ? kClearThreadsFew : kClearThreads) / threads);
   };
   if (count == 0) {
     share(kClearCta);
     if (c.ctas == 0) return QADAM_OK;
-    clear_kernel<<<c.ctas, kClearCta, 0, st>>>(c);
-    return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
+    return launch(clear_kernel, c.ctas, kClearCta, 0, 0, st, c) ? QADAM_OK : QADAM_ERR_CUDA;
   }
   s.ids = ids; s.id_bits = id_bits; s.count = (int)count; s.runs = l.runs; s.rows = (unsigned)rows;
   s.padding = padding; s.status = status; s.digits = 1 << digit; s.bits = digit; s.passes = passes;
@@ -1238,8 +1244,9 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   if (ranked) {
     s.shift = place_bits;
     share(kRankThreads);
-    rank_kernel<<<((int)count + kRankPer - 1) / kRankPer + c.ctas, kRankThreads, (size_t)rank_quads((int)count) * kRankWarps * 16, st>>>(s);
-    if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+    if (!launch(rank_kernel, ((int)count + kRankPer - 1) / kRankPer + c.ctas, kRankThreads, (size_t)rank_quads((int)count) * kRankWarps * 16,
+                0, st, s))
+      return QADAM_ERR_CUDA;
   } else if (clustered) {
     while ((kCluster * kSortThreads << s.each) < count) ++s.each;
     share(kSortThreads);
@@ -1249,19 +1256,8 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
     if (smem > 12 * 1024 &&
         !cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortRun * (int)sizeof(uint2))))
       return QADAM_ERR_CUDA;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3((unsigned)(kCluster + (c.ctas + kCluster - 1) / kCluster * kCluster));
-    c.ctas = (int)config.gridDim.x - kCluster;
-    config.blockDim = dim3(kSortThreads);
-    config.dynamicSmemBytes = smem;
-    config.stream = st;
-    cudaLaunchAttribute attribute;
-    attribute.id = cudaLaunchAttributeClusterDimension;
-    attribute.val.clusterDim.x = kCluster;
-    attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
-    config.attrs = &attribute;
-    config.numAttrs = 1;
-    if (!cuda_call(cudaLaunchKernelEx(&config, kernel, s))) return QADAM_ERR_CUDA;
+    c.ctas = (c.ctas + kCluster - 1) / kCluster * kCluster;
+    if (!launch(kernel, kCluster + c.ctas, kSortThreads, smem, kCluster, st, s)) return QADAM_ERR_CUDA;
   } else {
     for (int i = 0; i < passes; ++i) {
       s.shift = i * digit;
@@ -1270,11 +1266,10 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
       s.out_keys = list(l.keys[i % 2]);
       s.out_places = list(l.places[i % 2]);
       share(kSortThreads);
-      count_digits_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
-      if (scanned) scan_counts_kernel<<<1, kSortThreads, 0, st>>>(s.counts, l.runs, s.digits);
+      if (!launch(count_digits_kernel, l.runs + c.ctas, kSortThreads, 0, 0, st, s)) return QADAM_ERR_CUDA;
+      if (scanned && !launch(scan_counts_kernel, 1, kSortThreads, 0, 0, st, s.counts, l.runs, s.digits)) return QADAM_ERR_CUDA;
       share(kSortThreads);
-      place_kernel<<<l.runs + c.ctas, kSortThreads, 0, st>>>(s);
-      if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+      if (!launch(place_kernel, l.runs + c.ctas, kSortThreads, 0, 0, st, s)) return QADAM_ERR_CUDA;
     }
   }
   g.keys = s.out_keys;
@@ -1285,11 +1280,11 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
   g.grad_vector = !is_aligned(grad, 4 * type_bytes(grad_type)) || grad_stride % 4 != 0 ? 0
                   : is_aligned(grad, 16) && grad_stride * type_bytes(grad_type) % 16 == 0 ? 2 : 1;
   const long long units = (long long)l.chunks * g.tiles;
-  const unsigned grid = (unsigned)((units + kSumWarps - 1) / kSumWarps);
-  if (dy_type == QADAM_F32) sum_chunks_kernel<QADAM_F32><<<grid, kSumThreads, 0, st>>>(g);
-  else if (dy_type == QADAM_BF16) sum_chunks_kernel<QADAM_BF16><<<grid, kSumThreads, 0, st>>>(g);
-  else sum_chunks_kernel<QADAM_F16><<<grid, kSumThreads, 0, st>>>(g);
-  return cuda_call(cudaGetLastError()) ? QADAM_OK : QADAM_ERR_CUDA;
+  const long long grid = (units + kSumWarps - 1) / kSumWarps;
+  const bool ok = dy_type == QADAM_F32    ? launch(sum_chunks_kernel<QADAM_F32>, grid, kSumThreads, 0, 0, st, g)
+                  : dy_type == QADAM_BF16 ? launch(sum_chunks_kernel<QADAM_BF16>, grid, kSumThreads, 0, 0, st, g)
+                                          : launch(sum_chunks_kernel<QADAM_F16>, grid, kSumThreads, 0, 0, st, g);
+  return ok ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
 }  // extern "C"

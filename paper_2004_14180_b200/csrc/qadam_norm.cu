@@ -121,6 +121,7 @@ __device__ __forceinline__ double block_sum(double s, double* shared) {
 template <int CAP>
 __global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(const __grid_constant__ NormParams p,
                                                                             const __grid_constant__ Pointers<CAP> ptrs) {
+  wait_for_previous_launch();
   __shared__ double shared[kNormThreads / 32];
   __shared__ bool last;
   double sum = 0.0;
@@ -182,6 +183,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(cons
 }
 
 __global__ void norm_of_nothing_kernel(float* out) {
+  wait_for_previous_launch();
   out[0] = 0.0f;
   out[1] = 1.0f;
 }
@@ -241,8 +243,7 @@ int launch_norm(qadam_norm* c, NormParams p, int grid, int tensors, cudaStream_t
   static_assert(sizeof(Pointers<CAP>) + sizeof(NormParams) <= 32764, "kernel parameters");
   Pointers<CAP> ptrs;
   std::copy(c->ptrs.begin() + p.tensor_base, c->ptrs.begin() + p.tensor_base + tensors, ptrs.at);
-  norm_kernel<CAP><<<grid, kNormThreads, 0, st>>>(p, ptrs);
-  if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+  if (!launch(norm_kernel<CAP>, grid, kNormThreads, 0, 0, st, p, ptrs)) return QADAM_ERR_CUDA;
   c->launches += 1;
   return QADAM_OK;
 }
@@ -310,8 +311,7 @@ int qadam_norm_run(qadam_norm* c, float max_norm, float* out, void* stream) {
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int tensors = (int)c->geo.type.size(), tiles = (int)c->geo.tiles.size();
   if (tiles == 0) {
-    norm_of_nothing_kernel<<<1, 1, 0, st>>>(out);
-    if (!cuda_call(cudaGetLastError())) return QADAM_ERR_CUDA;
+    if (!launch(norm_of_nothing_kernel, 1, 1, 0, 0, st, out)) return QADAM_ERR_CUDA;
     c->launches += 1;
     return QADAM_OK;
   }

@@ -48,6 +48,31 @@ __host__ __device__ inline int type_bytes(int t) { return t == QADAM_F32 ? 4 : 2
 inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t round_up256(size_t v) { return (v + 255) / 256 * 256; }
 
+// Launches `kernel` so that it may be brought up while what is before it in the stream ends (every kernel that is launched
+// so begins with wait_for_previous_launch).  The kernels before it say nothing early, so what is gained is the launch
+// alone: 2 us of 14 (norm of 11.7 x 10^6 elements), 11 us of 161 over the five launches of a long embedding gradient.
+// Saying so early gained nothing more.  cluster > 0: CTAs of a cluster.
+template <typename... P, typename... A>
+inline bool launch(void (*kernel)(P...), long long grid, int block, size_t smem, int cluster, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3((unsigned)grid);
+  config.blockDim = dim3((unsigned)block);
+  config.dynamicSmemBytes = smem;
+  config.stream = st;
+  cudaLaunchAttribute attributes[2];
+  attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attributes[0].val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = attributes;
+  config.numAttrs = 1;
+  if (cluster > 0) {
+    attributes[1].id = cudaLaunchAttributeClusterDimension;
+    attributes[1].val.clusterDim.x = (unsigned)cluster;
+    attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
+    config.numAttrs = 2;
+  }
+  return cuda_call(cudaLaunchKernelEx(&config, kernel, args...));
+}
+
 // The tensors that one launch reads through pointers that may change from call to call.  They
 // travel as kernel parameters, so a call needs no copy to the device, two calls never share a table
 // that one of them is still reading, and a captured launch keeps its own.  4 KB of parameters
