@@ -89,8 +89,15 @@ __device__ __forceinline__ Piece<KIND> load_piece(const LookupParams& p, long lo
     }
   } else {
     const long long at = (p.first + id * p.width + col) * KIND >> 5;
+    const uint32_t* w = static_cast<const uint32_t*>(p.table) + at;
+    if (at + kPieceWords<KIND> <= p.words) {
 #pragma unroll
-    for (int k = 0; k < kPieceWords<KIND>; ++k) r.w[k] = static_cast<const uint32_t*>(p.table)[min(at + k, p.words - 1)];
+      for (int k = 0; k < kPieceWords<KIND>; ++k) r.w[k] = w[k];
+    } else {
+      const int last = (int)(p.words - 1 - at);              // (codes end in a word before the piece's last)
+#pragma unroll
+      for (int k = 0; k < kPieceWords<KIND>; ++k) r.w[k] = w[min(k, last)];
+    }
   }
   return r;
 }

@@ -86,17 +86,21 @@ __device__ __forceinline__ void add_squares16(const uint4& r, int type, double& 
     return;
   }
   float x[8];
+  if (type == QADAM_BF16) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (type == QADAM_BF16) {
+    for (int k = 0; k < 4; ++k) {
       x[2 * k] = __uint_as_float(w[k] << 16);
       x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    } else {
+    }
+    add_squares<8>(x, sum);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
       x[2 * k] = half_bits_to_float(w[k] & 0xFFFFu);
       x[2 * k + 1] = half_bits_to_float(w[k] >> 16);
     }
+    add_squares<8>(x, sum);
   }
-  add_squares<8>(x, sum);
 }
 
 __device__ __forceinline__ double warp_sum(double s) {
@@ -156,8 +160,16 @@ __global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(cons
         ask(tile, raw[h ^ 1]);
         if (now + 2 * step < p.last) tile = p.tiles[now + 2 * step];
       }
+      if (type[h] == QADAM_F32) {
 #pragma unroll
-      for (int k = 0; k < kNormLoads; ++k) add_squares16(raw[h][k], type[h], sum);
+        for (int k = 0; k < kNormLoads; ++k) add_squares16(raw[h][k], QADAM_F32, sum);
+      } else if (type[h] == QADAM_BF16) {
+#pragma unroll
+        for (int k = 0; k < kNormLoads; ++k) add_squares16(raw[h][k], QADAM_BF16, sum);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kNormLoads; ++k) add_squares16(raw[h][k], QADAM_F16, sum);
+      }
     }
   }
   sum = block_sum(sum, shared);
