@@ -25,7 +25,8 @@ __device__ __forceinline__ long long load_id(const void* ids, int id_bits, long 
 // each other.
 
 constexpr int kLookThreads = 256;
-constexpr int kLookPieces = 1024;                          // pieces a CTA covers, at the most
+constexpr int kLookRounds = 4;                             // tokens that a thread takes
+constexpr int kLookTokens = kLookThreads * kLookRounds;
 // What the rows are: elements of 16 or 32 bits, or packed codes of KIND = 2 .. 16 bits.
 constexpr int kDense16 = 0, kDense32 = 1;
 template <int KIND>
@@ -39,7 +40,7 @@ struct LookupParams {
   long long rows, stride;
   int width, pieces;           // pieces: of a row
   int here, across;            // of a row in one CTA, at the most; CTAs of a row
-  unsigned per_piece;          // 2^32 / pieces, rounded up: a division by a product
+  int at_once;                 // tokens that a CTA's threads take at a time
   const void* ids;
   int id_bits;
   long long count;
@@ -202,10 +203,10 @@ template <int KIND>
 __global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_constant__ LookupParams p) {
   wait_for_previous_launch();
   constexpr int AHEAD = kLookAhead<KIND>;
-  __shared__ long long ids[kLookPieces];
+  __shared__ long long ids[kLookTokens];
   const long long first = (long long)(blockIdx.x / p.across) * p.per_cta;
   const int tokens = (int)min((long long)p.per_cta, p.count - first);
-  for (int t = threadIdx.x; t < tokens; t += kLookThreads) {
+  for (int t = threadIdx.x; t < tokens; t += blockDim.x) {
     long long id = load_id(p.ids, p.id_bits, first + t);
     if (id >= p.rows) {
       if (p.status != nullptr) atomicOr(p.status, QADAM_ST_INDEX);
@@ -214,56 +215,51 @@ __global__ void __launch_bounds__(kLookThreads, 6) lookup_kernel(const __grid_co
     ids[t] = id;
   }
   __syncthreads();
-  const int piece0 = (int)(blockIdx.x % p.across) * p.here, pieces = min(p.here, p.pieces - piece0), all = tokens * pieces;
-  // piece q of the CTA's: its token (there is one where a row has more pieces than a CTA) and column
-  auto token_of = [&](int q) { return p.across > 1 ? 0 : p.pieces == 1 ? q : (int)__umulhi((unsigned)q, p.per_piece); };
-  auto column_of = [&](int q, int token) { return piece_column(p, piece0 + q - token * pieces); };
+  // a thread keeps its columns and goes from token to token
+  const int row = threadIdx.x / p.here, piece = (int)(blockIdx.x % p.across) * p.here + (threadIdx.x - row * p.here);
+  if (piece >= p.pieces) return;
+  const int col = piece_column(p, piece), step = p.at_once;
   if (p.spread) {
-    for (int q = threadIdx.x; q < all; q += kLookThreads) {
-      const int token = token_of(q), col = column_of(q, token);
-      const long long id = ids[token];
+    for (int t = row; t < tokens; t += step) {
+      const long long id = ids[t];
       float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if (id >= 0) {
         spread_floats<KIND>(p, load_spread<KIND>(p, id, col), id, col, x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
       }
-      store_piece(p, first + token, col, x);
+      store_piece(p, first + t, col, x);
     }
     return;
   }
-  for (int q0 = threadIdx.x; q0 < all; q0 += AHEAD * kLookThreads) {
+  for (int t0 = row; t0 < tokens; t0 += AHEAD * step) {
     Piece<KIND> raw[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int q = q0 + j * kLookThreads;
+      const int t = t0 + j * step;
+      const long long id = t < tokens ? ids[t] : -1;
       raw[j] = Piece<KIND>{};
-      if (q < all) {
-        const int token = token_of(q);
-        const long long id = ids[token];
-        if (id >= 0) raw[j] = load_piece<KIND>(p, id, column_of(q, token));
-      }
+      if (id >= 0) raw[j] = load_piece<KIND>(p, id, col);
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int q = q0 + j * kLookThreads;
-      if (q >= all) break;
-      const int token = token_of(q), col = column_of(q, token);
-      const long long id = ids[token];
+      const int t = t0 + j * step;
+      if (t >= tokens) break;
+      const long long id = ids[t];
       float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if (id >= 0) {
         piece_floats<KIND>(p, raw[j], id, col, x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(p.scale, x[k]);
       }
-      store_piece(p, first + token, col, x);
+      store_piece(p, first + t, col, x);
     }
   }
 }
 
 template <int KIND>
 bool launch_lookup(const LookupParams& p, long long grid, int kind, cudaStream_t st) {
-  if (kind == KIND) return launch(lookup_kernel<KIND>, grid, kLookThreads, 0, 0, st, p);
+  if (kind == KIND) return launch(lookup_kernel<KIND>, grid, p.here * p.at_once, 0, 0, st, p);
   if constexpr (KIND < 16) return launch_lookup<KIND + 1>(p, grid, kind, st);
   return false;
 }
@@ -272,11 +268,11 @@ int enqueue_lookup(LookupParams p, int kind, cudaStream_t st) {
   const bool in_fits = kind > kDense32 || (is_aligned(p.table, 16) && p.stride * type_bytes(p.type) % 16 == 0);
   p.spread = !in_fits || !is_aligned(p.out, 16) || p.out_stride * type_bytes(p.out_type) % 16 != 0;
   p.pieces = p.spread ? (p.width + 255) / 256 * 32 : (p.width + 7) / 8;
-  p.per_piece = (unsigned)(((1ull << 32) + p.pieces - 1) / p.pieces);       // (not used for one piece, which it does not fit)
-  p.here = std::min(p.pieces, kLookPieces);
-  p.per_cta = std::max(1, kLookPieces / p.pieces);
+  p.here = std::min(p.pieces, kLookThreads);
+  p.across = (p.pieces + p.here - 1) / p.here;
+  p.at_once = kLookThreads / p.here;
+  p.per_cta = p.at_once * kLookRounds;
   const long long ctas = (p.count + p.per_cta - 1) / p.per_cta;
-  p.across = (p.pieces + kLookPieces - 1) / kLookPieces;
   if (ctas > 0x7FFFFFFF / p.across) return QADAM_ERR_SIZE;
   return launch_lookup<kDense16>(p, ctas * p.across, kind, st) ? QADAM_OK : QADAM_ERR_CUDA;
 }
