@@ -27,21 +27,6 @@ def stream_of(device: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-class _Guard:
-    """torch.cuda.device(device), which costs 3 us, where the device is not the current one already."""
-
-    def __init__(self, device: torch.device):
-        self.other = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *what):
-        if self.other is not None:
-            self.other.__exit__(*what)
-
-
 def _device_of(tensors: Sequence[Optional[torch.Tensor]], what: str) -> torch.device:
     devices = {t.device for t in tensors if t is not None}
     if len(devices) != 1 or next(iter(devices)).type != "cuda":

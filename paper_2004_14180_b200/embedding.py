@@ -11,8 +11,18 @@ from typing import Optional
 
 import torch
 
-from .adamw import _Guard, _need_cuda, element_type, stream_of
+from .adamw import TYPES, _need_cuda, element_type, stream_of
 from .binding import _check, load_library
+
+
+def _elsewhere(device: torch.device) -> bool:
+    """Whether another device than `device` is the current one (torch.cuda.device(device) costs 3 us when it is not)."""
+    return torch.cuda.current_device() != device.index
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    ty = TYPES.get(t.dtype)
+    return ty if ty is not None else element_type(t.dtype, what)
 
 
 def _tokens(ids: torch.Tensor, device: torch.device) -> torch.Tensor:
@@ -72,19 +82,23 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
         _need_cuda()
         raise ValueError("table: a CUDA tensor [rows, width] is needed; there is no CPU path")
     device = table.device
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return embedding_lookup(table, ids, scale, out_dtype, out, status)
     ids = _tokens(ids, device)
     n, width = table.shape
     shape = ids.shape + (width,)
-    stride = _row_stride(table, "table", table.shape, device)
+    stride = width if table.is_contiguous() else _row_stride(table, "table", table.shape, device)
     if out is None:
         out, out_stride = torch.empty(*shape, dtype=out_dtype or table.dtype, device=device), width
     else:
         out, out_stride = _out(shape, out, out_dtype, device), _row_stride(out, "out", shape, device)
-    with _Guard(device):
-        _check(load_library().qadam_embedding_lookup(
-            table.data_ptr(), element_type(table.dtype, "table"), n, width, stride, ids.data_ptr(), 8 * ids.element_size(),
-            ids.numel(), scale, out.data_ptr(), element_type(out.dtype, "out"), out_stride, _status(status, device),
-            stream_of(device)), "qadam_embedding_lookup")
+    rc = load_library().qadam_embedding_lookup(
+        table.data_ptr(), _type(table, "table"), n, width, stride, ids.data_ptr(), 64 if ids.dtype is torch.int64 else 32,
+        ids.numel(), scale, out.data_ptr(), _type(out, "out"), out_stride, None if status is None else _status(status, device),
+        stream_of(device))
+    if rc:
+        _check(rc, "qadam_embedding_lookup")
     return out
 
 
@@ -99,17 +113,20 @@ def held_lookup(wcodes: torch.Tensor, kx: int, ids: torch.Tensor, rows: int, wid
     if not wcodes.is_cuda or wcodes.dtype != torch.uint8 or not wcodes.is_contiguous():
         raise ValueError("wcodes: a contiguous CUDA tensor of uint8 is needed; there is no CPU path")
     device = wcodes.device
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return held_lookup(wcodes, kx, ids, rows, width, scale, out_dtype, first, out, status)
     ids = _tokens(ids, device)
     shape = ids.shape + (width,)
     if out is None:
         out, out_stride = torch.empty(*shape, dtype=out_dtype, device=device), width
     else:
         out_stride = _row_stride(out, "out", shape, device)
-    with _Guard(device):
-        _check(load_library().qadam_held_lookup(
-            wcodes.data_ptr(), wcodes.numel(), kx, first, rows, width, ids.data_ptr(), 8 * ids.element_size(), ids.numel(), scale,
-            out.data_ptr(), element_type(out.dtype, "out"), out_stride, _status(status, device), stream_of(device)),
-            "qadam_held_lookup")
+    rc = load_library().qadam_held_lookup(
+        wcodes.data_ptr(), wcodes.numel(), kx, first, rows, width, ids.data_ptr(), 64 if ids.dtype is torch.int64 else 32, ids.numel(),
+        scale, out.data_ptr(), _type(out, "out"), out_stride, None if status is None else _status(status, device), stream_of(device))
+    if rc:
+        _check(rc, "qadam_held_lookup")
     return out
 
 
@@ -126,6 +143,9 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
         _need_cuda()
         raise ValueError("dy: a CUDA tensor [..., width] is needed; there is no CPU path")
     device, width = dy.device, dy.shape[-1]
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return embedding_grad(ids, dy, rows, scale, dtype, out, accumulate, padding, status)
     ids = _tokens(ids, device)
     count = ids.numel()
     if accumulate and out is None:
@@ -134,10 +154,11 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
     dy_stride = _row_stride(dy, "dy", ids.shape + (width,), device)
     out_stride = _row_stride(out, "out", (rows, width), device)
     size = _grad_workspace(count, rows, width)
-    with _Guard(device):
-        scratch = torch.empty(size, dtype=torch.uint8, device=device)     # (torch's blocks are 512-byte aligned)
-        _check(load_library().qadam_embedding_grad(
-            ids.data_ptr(), 8 * ids.element_size(), count, dy.data_ptr(), element_type(dy.dtype, "dy"), dy_stride, scale, padding,
-            out.data_ptr(), element_type(out.dtype, "out"), rows, width, out_stride, int(accumulate), scratch.data_ptr(), size,
-            _status(status, device), stream_of(device)), "qadam_embedding_grad")
+    scratch = torch.empty(size, dtype=torch.uint8, device=device)     # (torch's blocks are 512-byte aligned)
+    rc = load_library().qadam_embedding_grad(
+        ids.data_ptr(), 64 if ids.dtype is torch.int64 else 32, count, dy.data_ptr(), _type(dy, "dy"), dy_stride, scale, padding,
+        out.data_ptr(), _type(out, "out"), rows, width, out_stride, int(accumulate), scratch.data_ptr(), size,
+        None if status is None else _status(status, device), stream_of(device))
+    if rc:
+        _check(rc, "qadam_embedding_grad")
     return out
