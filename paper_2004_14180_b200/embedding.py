@@ -2,6 +2,7 @@
 
 All calls run on the current stream of the table's device.  `status`, where given, is one int32 on the
 device that gets ST_INDEX if a token is not below the number of rows; the caller clears and reads it.
+None of them is recorded by autograd: the gradient of a lookup is embedding_grad.
 """
 from __future__ import annotations
 
