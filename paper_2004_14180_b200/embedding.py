@@ -136,6 +136,7 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
                    status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of embedding_lookup(table, ids, scale) with respect to the table, for the gradient dy of its rows.
 
+    dy: [..., width], rows at equal distances that do not overlap (make an expanded gradient contiguous first).
     -> [rows, width] of `dtype` (dy's, if not given), or `out`: overwritten, or added to where accumulate is true (rows
     without a token are then not touched).  `out` may be a part of a larger buffer, such as a worker's gradient of one tensor
     in the padded layout.  Tokens that are negative or equal to `padding` have no gradient; one that is not below `rows` has

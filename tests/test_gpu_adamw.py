@@ -471,3 +471,32 @@ def test_resume_from_saved_buffers():
         b.grads[0].copy_(gs[t - 1])
         b.step(t)
     assert torch.equal(a.weights[0], b.weights[0]) and torch.equal(a.master, b.master) and torch.equal(a.r, b.r)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_beyond_32_bits(bits):
+    """A tensor of more than 2^32 elements, and one behind it: their last elements are stepped, and count in the norm.
+    (8.6 GB for each of weight and gradient, 17 GB a moment.)"""
+    large, tail = (1 << 32) + 4105, 1300
+    first = large - tail - (large - tail) % 1024
+    gen = torch.Generator(device="cuda").manual_seed(bits)
+    w = [torch.zeros(large, device="cuda", dtype=torch.bfloat16), torch.randn(700, device="cuda", generator=gen)]
+    g = [torch.zeros(large, device="cuda", dtype=torch.bfloat16), torch.randn(700, device="cuda", generator=gen)]
+    w[0][first:] = torch.randn(large - first, device="cuda", generator=gen)
+    g[0][first:] = torch.randn(large - first, device="cuda", generator=gen)
+    ends = [w[0][first:].clone(), w[1].clone()]
+    opt = qb.AdamW(w, g, state_bits=bits, seed=5, **HYPER)
+    # the same elements as tensors of their own; a step's weights do not depend on the random bits
+    small = qb.AdamW(ends, [g[0][first:].clone(), g[1]], state_bits=bits, seed=5, **HYPER)
+    opt.step(1)
+    small.step(1)
+    assert torch.equal(w[0][first:], ends[0]) and torch.equal(w[1], ends[1])
+    assert not bool(w[0][first - 4096:first].any()) and not bool(w[0][:4096].any())
+    scale, m = (1, lambda o: o.m) if bits == 32 else (128, lambda o: o.m_scale)
+    end = opt.off[1] + 700 if bits == 32 else opt.off[1] + 768
+    ours, its = m(opt)[first // scale:end // scale], m(small)[:(end - first) // scale]
+    assert torch.equal(ours, its) and bool(ours.any())
+    norm, _ = opt.grad_norm()
+    want = float(torch.sqrt(g[0][first:].double().square().sum() + g[1].double().square().sum()))
+    # eight squares at a time are off by at most 7 x 2^-24, the norm by half of that and its own rounding
+    assert abs(float(norm) - want) <= want * 5 * 2.0 ** -24

@@ -242,3 +242,61 @@ def test_captured_and_replayed_with_new_tokens(count):
         graph.replay()
         fresh = qb.embedding_lookup(table, ids, scale=2.0)
         assert torch.equal(rows, fresh) and torch.equal(out, qb.embedding_grad(ids, fresh, 300))
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, tokens and packed codes whose elements lie 2^32 and more behind the first: 8.6 GB at a time."""
+    gen = _gen(8)
+    rows, width = 4_300_007, 1000
+    assert (rows - 100) * width > 2 ** 32
+    table = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    table[-100:] = torch.randn(100, width, generator=gen, device="cuda")
+    ids = torch.tensor([rows - 1, 3, rows - 100, rows - 57, rows - 1], device="cuda")
+    got = qb.embedding_lookup(table, ids)
+    assert torch.equal(got, table[ids])
+    # its gradient: the whole table is cleared, from the last row to the first
+    table.fill_(7.0)
+    dy = torch.randn(5, width, generator=gen, device="cuda").bfloat16()
+    qb.embedding_grad(ids, dy, rows, out=table)
+    assert torch.equal(table[3], dy[1]) and torch.equal(table[rows - 100], dy[2]) and torch.equal(table[rows - 57], dy[3])
+    assert torch.equal(table[-1], (dy[0].float() + dy[4].float()).bfloat16())
+    for i in (3, rows - 100, rows - 57, rows - 1):
+        table[i] = 0
+    assert not any(bool(part.any()) for part in table.split(1 << 19))
+    # as many tokens: all but the last few have no gradient
+    many = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    many[-4:] = torch.tensor([2, 0, 2, 1], dtype=torch.int32, device="cuda")
+    table[-4:] = dy[:4]
+    got = qb.embedding_grad(many, table, 5, dtype=torch.float32)
+    assert torch.equal(got[0], dy[1].float()) and torch.equal(got[1], dy[3].float()) and not bool(got[3:].any())
+    assert torch.equal(got[2], dy[0].float() + dy[2].float())
+    # and a row for each of them: the last tokens' rows of the result
+    source = torch.randn(3, width, generator=gen, device="cuda").bfloat16()
+    qb.embedding_lookup(source, many, out=table)
+    assert torch.equal(table[-4], source[2]) and torch.equal(table[-3], source[0]) and not bool(table[0].any())
+    # packed codes, 8 bits each
+    codes = table.view(-1).view(torch.uint8)
+    codes[-8000:] = torch.randint(0, 129, (8000,), generator=gen, device="cuda").to(torch.uint8)
+    codes = codes[:codes.numel() // 16 * 16]
+    first = codes.numel() - 5000
+    assert first > 2 ** 32
+    got = qb.held_lookup(codes, 6, torch.tensor([4, 0], device="cuda"), 5, 1000, out_dtype=torch.float32, first=first)
+    want = ((codes[first:].double() - 64) / 128).view(5, 1000)
+    assert torch.equal(got.double(), want[[4, 0]])
+
+
+def test_a_batch_without_tokens_waits_for_what_is_before_it():
+    gen = _gen(9)
+    big = torch.randn(4096, 4096, generator=gen, device="cuda")
+    for _ in range(20):
+        out = torch.mm(big, big)                               # a long kernel that writes `out` to its end
+        got = qb.embedding_grad(torch.empty(0, dtype=torch.int64, device="cuda"), big[:0], 4096, out=out)
+        assert not bool(got.any())
+
+
+def test_an_expanded_gradient_is_refused():
+    ids = torch.tensor([0, 1, 2], device="cuda")
+    for dy in (torch.ones(1, 8, device="cuda").expand(3, 8), torch.ones(3, 1, device="cuda").expand(3, 8)):
+        with pytest.raises(ValueError, match="dy"):
+            qb.embedding_grad(ids, dy, 4)
+        assert bool((qb.embedding_grad(ids, dy.contiguous(), 4)[:3] == 1).all())
