@@ -356,7 +356,10 @@ __device__ void clear_share(const ClearParams& c, int cta) {
 }
 
 constexpr int kClearCta = 512;
-__global__ void __launch_bounds__(kClearCta) clear_kernel(const __grid_constant__ ClearParams c) { clear_share(c, blockIdx.x); }
+__global__ void __launch_bounds__(kClearCta) clear_kernel(const __grid_constant__ ClearParams c) {
+  wait_for_previous_launch();
+  clear_share(c, blockIdx.x);
+}
 
 // The sort's key of a token: its row, or `rows` for one that is left out.
 __device__ __forceinline__ unsigned key_of(const SortParams& p, long long id) {
