@@ -323,7 +323,7 @@ struct SortParams {
   int count, runs;
   int shift, digits;           // digits: 2^bits
   int bits, passes;
-  int each;                    // log2 of a thread's tokens (sort_cluster_kernel)
+  int each;                    // a thread's tokens (sort_cluster_kernel)
   int scanned;                 // counts are places already (scan_counts_kernel)
   unsigned rows;
   long long padding;
@@ -522,7 +522,7 @@ template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid_constant__ SortParams p) {
   wait_for_previous_launch();
   static_assert(kDigits <= kSortThreads, "a digit to a thread");
-  extern __shared__ uint2 exchange[];                      // [kSortThreads << each]
+  extern __shared__ uint2 exchange[];                      // [kSortThreads * each]
   __shared__ unsigned short seen[kSortWarps][kDigits];
   __shared__ unsigned counts[kDigits], start[kDigits], warp_total[kSortWarps];
   if (blockIdx.x >= kCluster) {
@@ -533,15 +533,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid
   const int cta = (int)cluster.block_rank();
   clear_counters(p, cta, kCluster);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int inside = (warp << (5 + p.each)) + lane, base = cta * (kSortThreads << p.each) + inside;
-  const unsigned mask = (kSortThreads << p.each) - 1, cta_bits = 31 - __clz(kSortThreads << p.each);
+  const unsigned slots = kSortThreads * p.each;
+  const int inside = warp * 32 * p.each + lane, base = cta * (int)slots + inside;
+  // x / slots is the high word of x over, as x (over slots - 2^32) < x slots < 2^32
+  const unsigned over = 0xFFFFFFFFu / slots + 1u;
   unsigned key[ITEMS], place[ITEMS];
   bool live[ITEMS];
   unsigned short rank[ITEMS];
   load_keys<ITEMS>(p, base, 32, key);
 #pragma unroll
   for (int j = 0; j < ITEMS; ++j) {
-    live[j] = j < 1 << p.each && base + 32 * j < p.count;
+    live[j] = j < p.each && base + 32 * j < p.count;
     place[j] = (unsigned)(base + 32 * j);
   }
   for (int pass = 0; pass < p.passes; ++pass) {
@@ -584,7 +586,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid
           p.out_keys[to] = key[j];
           p.out_places[to] = place[j];
         } else {
-          cluster.map_shared_rank(exchange, to >> cta_bits)[to & mask] = make_uint2(key[j], place[j]);
+          const unsigned there = __umulhi(to, over);
+          cluster.map_shared_rank(exchange, there)[to - there * slots] = make_uint2(key[j], place[j]);
         }
       }
     cluster.sync();                                        // tokens have arrived; counts have been read
@@ -1257,10 +1260,11 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
                 0, st, s))
       return QADAM_ERR_CUDA;
   } else if (clustered) {
-    while ((kCluster * kSortThreads << s.each) < count) ++s.each;
+    // no more than the batch needs (20000 tokens: 5 each 33.5 us, 8 each 35.5)
+    s.each = (int)((count + kCluster * kSortThreads - 1) / (kCluster * kSortThreads));
     share(kSortThreads);
-    const auto kernel = s.each <= 1 ? sort_cluster_kernel<2> : sort_cluster_kernel<8>;
-    const size_t smem = passes > 1 ? (size_t)(kSortThreads << s.each) * sizeof(uint2) : 0;
+    const auto kernel = s.each <= 2 ? sort_cluster_kernel<2> : sort_cluster_kernel<kSortItems>;
+    const size_t smem = passes > 1 ? (size_t)kSortThreads * s.each * sizeof(uint2) : 0;
     // the limit of dynamic shared memory belongs to the kernel: every call that needs it raised sets the same
     if (smem > 12 * 1024 &&
         !cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortRun * (int)sizeof(uint2))))

@@ -300,3 +300,19 @@ def test_an_expanded_gradient_is_refused():
         with pytest.raises(ValueError, match="dy"):
             qb.embedding_grad(ids, dy, 4)
         assert bool((qb.embedding_grad(ids, dy.contiguous(), 4)[:3] == 1).all())
+
+
+@pytest.mark.parametrize("each", range(1, 9))
+def test_batches_around_what_a_cluster_sorts(each):
+    """Whole and nearly whole clusters of 8 x 512 threads with 1 to 8 tokens each, over one, two and three digits."""
+    for rows in (300, 30522, 300000):
+        for count in (4096 * each - 1, 4096 * each, 4096 * each + 1):
+            ids = torch.randint(0, rows, (count,), generator=_gen(count, rows), device="cuda")
+            ids[::3] = rows - 1
+            dy = torch.arange(count, device="cuda").remainder(2048).float().view(-1, 1)
+            got = qb.embedding_grad(ids, dy, rows)
+            # sums of whole numbers: exact in binary32 while below 2^24
+            want = torch.zeros(rows, dtype=torch.float64, device="cuda").index_add_(0, ids, dy[:, 0].double())
+            exact = want < 2 ** 24
+            assert torch.equal(got[exact, 0].double(), want[exact])
+            assert bool(((got[:, 0].double() - want).abs() <= want * (count + 1) * 2.0 ** -24).all())
