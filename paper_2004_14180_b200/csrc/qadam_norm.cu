@@ -5,7 +5,7 @@
 // One read of the tensors: bound by HBM, as long as an element costs few instructions.  The squares of what a thread has
 // in 16 bytes are added in binary32 (4 products and sums, or 8 exact products of 16-bit numbers: the sum of squares
 // is off by at most 7 x 2^-24, the norm by half of that), everything else in binary64: conversions of every element
-// to binary64 took half as long again (59 us in place of 37 for 109.5 x 10^6 bf16, 5.9 TB/s).  Squares that binary32 does not hold,
+// to binary64 took half as long again (59 us in place of 38 for 109.5 x 10^6 bf16, 5.7 TB/s).  Squares that binary32 does not hold,
 // of numbers below 1e-12 or above 1e19, are seen by their sum, and formed in binary64.
 #include "qadam.h"
 
