@@ -66,7 +66,7 @@ class GradNorm:
     """sqrt of the sum of squares over all tensors, and the factor that clips it.
 
     tensors: contiguous CUDA tensors of float32, bfloat16 or float16, of any lengths.  Calls of one holder
-    share scratch: order them (one stream, or events).
+    share scratch: order them (one stream, or events).  Keep the holder as long as a graph that captured one is replayed.
     """
 
     ctx = None
@@ -133,7 +133,8 @@ class AdamW:
     master: keep float32 master weights (`self.master`, padded layout; set from `weights` here).
     weight_decay: one factor, or one for each tensor.
     Moments are `m`, `v` ([D] float32, padded layout) or `m`, `r` ([D] uint8) with `m_scale`, `r_scale`.
-    Weights are updated in place, where they are now.  Steps run on the current stream; keep the holder until they are done.
+    Weights are updated in place, where they are now.  Steps run on the current stream; keep the holder until they are done, and as long
+    as a graph that captured them is replayed (with the gradients that were bound at its capture).
     """
 
     ctx = None
