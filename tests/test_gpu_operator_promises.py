@@ -1,0 +1,43 @@
+"""What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded."""
+import numpy as np
+import pytest
+import torch
+
+from _training import adamw_constants
+
+pytestmark = pytest.mark.gpu
+
+import paper_2004_14180_b200 as qb  # noqa: E402
+
+F = np.float32
+HYPER = dict(beta1=0.9, beta2=0.999, eps=1e-8, lr=1e-3)
+
+
+@pytest.mark.parametrize("eps", [1e-8, 0.05])
+@pytest.mark.parametrize("master", [False, True])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_eight_bit_weights_round_every_operation_but_the_quotient(shift, master, eps):
+    # Weights that a step nearly cancels show each rounding of x k - a q: the result has fewer bits than a q, so that
+    # it is one of those that the quotients within 3 units in the last place give (the reciprocal is off by at most one of its own,
+    # which is less than two of the quotient's; the product and the rounded quotient by half a unit each), or it is not.
+    n, decay = 5000, 0.3
+    rng = np.random.default_rng(7)
+    g = (rng.standard_normal(n) * 0.01).astype(F)
+    k = adamw_constants(HYPER["beta1"], HYPER["beta2"], HYPER["lr"], decay, 1)
+    m, v = k["c1"] * g, k["c2"] * (g * g)
+    q = m / (np.sqrt(v) * k["b"] + F(eps))
+    x = (k["a"] * q / k["keep"] * (1 + rng.standard_normal(n).astype(F) * F(2.0 ** -9))).astype(F)
+    room = torch.zeros(n + 8, device="cuda", dtype=torch.bfloat16 if master else torch.float32)
+    gt = torch.zeros(n + 8, device="cuda")
+    w, gt = room[shift:shift + n], gt[shift:shift + n]
+    gt.copy_(torch.from_numpy(g))
+    if not master:
+        w.copy_(torch.from_numpy(x))
+    opt = qb.AdamW([w], [gt], state_bits=8, master=master, weight_decay=decay, seed=1, **dict(HYPER, eps=eps))
+    if master:
+        opt.master[:n] = torch.from_numpy(x).cuda()
+    opt.step(1)
+    got = (opt.master[:n] if master else w).cpu().numpy()
+    near = [(q.view(np.int32) + j).view(F) for j in range(-3, 4)]
+    may = np.stack([x * k["keep"] - k["a"] * near_q for near_q in near])
+    assert np.all((may == got).any(axis=0))
