@@ -66,7 +66,8 @@ class GradNorm:
     """sqrt of the sum of squares over all tensors, and the factor that clips it.
 
     tensors: contiguous CUDA tensors of float32, bfloat16 or float16, of any lengths.  Calls of one holder
-    share scratch: order them (one stream, or events).  Keep the holder as long as a graph that captured one is replayed.
+    share scratch: order them (one stream, or events).  Keep the holder until its calls are done, and as long as a graph that
+    captured one is replayed.
     """
 
     ctx = None
@@ -89,7 +90,8 @@ class GradNorm:
             torch.cuda.current_stream(self.device).synchronize()      # its memory may still be in use there
             _check(L.qadam_norm_create(C.byref(spec), self._scratch.ptr, size.value, C.byref(ctx)), "qadam_norm_create")
         self.ctx = ctx.value
-        self.result = torch.zeros(2, dtype=torch.float32, device=self.device)
+        # (not filled: a fill here would run on this stream, after a first call on another)
+        self.result = torch.empty(2, dtype=torch.float32, device=self.device)
         self.bind(tensors)
 
     def bind(self, tensors: Sequence[Optional[torch.Tensor]]) -> None:

@@ -1,4 +1,5 @@
-"""What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded."""
+"""What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded, first
+calls on a stream of their own."""
 import numpy as np
 import pytest
 import torch
@@ -41,3 +42,27 @@ def test_eight_bit_weights_round_every_operation_but_the_quotient(shift, master,
     near = [(q.view(np.int32) + j).view(F) for j in range(-3, 4)]
     may = np.stack([x * k["keep"] - k["a"] * near_q for near_q in near])
     assert np.all((may == got).any(axis=0))
+
+
+def test_first_norm_on_another_stream(monkeypatch):
+    # nothing that a new holder has queued on the stream of its creation may reach its result after a call elsewhere
+    lib = qb.binding.load_library()
+    create, big = lib.qadam_norm_create, torch.ones(8192, 8192, device="cuda")
+
+    def create_then_be_busy(*args):
+        rc = create(*args)
+        for _ in range(20):
+            torch.mm(big, big)
+        return rc
+
+    x, s = torch.full((1000,), 2.0, device="cuda"), torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        qb.GradNorm([x])(1.0)                                    # (kernels are loaded by their first call)
+    torch.mm(big, big)
+    torch.cuda.synchronize()
+    monkeypatch.setattr(lib, "qadam_norm_create", create_then_be_busy)
+    norm = qb.GradNorm([x])
+    with torch.cuda.stream(s):
+        n, f = norm(1.0)
+    torch.cuda.synchronize()
+    assert abs(float(n) - 2 * np.sqrt(1000)) < 1e-3 and float(f) < 0.1
