@@ -77,10 +77,19 @@ class GradNorm:
         tensors = list(tensors)
         if not tensors:
             raise ValueError("no tensors")
-        self.device = _device_of(tensors, "tensors")
-        self._lens = [t.numel() for t in tensors]
-        self._types = [element_type(t.dtype, "tensors") for t in tensors]
-        n = len(tensors)
+        self._create([t.numel() for t in tensors], [element_type(t.dtype, "tensors") for t in tensors], _device_of(tensors, "tensors"))
+        self.bind(tensors)
+
+    @classmethod
+    def _of(cls, lens: Sequence[int], types: Sequence[int], device: torch.device) -> "GradNorm":
+        """One for tensors of these lengths and types, none of them bound."""
+        norm = cls.__new__(cls)
+        norm._create(lens, types, device)
+        return norm
+
+    def _create(self, lens: Sequence[int], types: Sequence[int], device: torch.device) -> None:
+        self.device, self._lens, self._types = device, list(lens), list(types)
+        n = len(self._lens)
         spec = TensorList(n, 0, (C.c_int64 * n)(*self._lens), (C.c_int32 * n)(*self._types))
         size, ctx = C.c_size_t(), C.c_void_p()
         L = load_library()
@@ -92,7 +101,6 @@ class GradNorm:
         self.ctx = ctx.value
         # (not filled: a fill here would run on this stream, after a first call on another)
         self.result = torch.empty(2, dtype=torch.float32, device=self.device)
-        self.bind(tensors)
 
     def bind(self, tensors: Sequence[Optional[torch.Tensor]]) -> None:
         """The tensors that later calls read, of the lengths and types given at creation; None counts as zero."""
@@ -207,9 +215,7 @@ class AdamW:
         """(norm of all bound gradients, factor that clips it to max_norm): see GradNorm.  The first call makes its context,
         so make it outside any stream capture."""
         if self._norm is None:
-            types = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
-            norm = GradNorm([g if g is not None else torch.empty(n, dtype=types[t], device=self.device)
-                             for g, n, t in zip(self.grads, self._lens, self._types)])
+            norm = GradNorm._of(self._lens, self._types, self.device)
             norm.bind(self.grads)
             self._norm = norm
         return self._norm(max_norm)

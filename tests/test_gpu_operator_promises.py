@@ -1,5 +1,5 @@
 """What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded, first
-calls on a stream of their own."""
+calls on a stream of their own, what is allocated."""
 import numpy as np
 import pytest
 import torch
@@ -66,3 +66,18 @@ def test_first_norm_on_another_stream(monkeypatch):
         n, f = norm(1.0)
     torch.cuda.synchronize()
     assert abs(float(n) - 2 * np.sqrt(1000)) < 1e-3 and float(f) < 0.1
+
+
+def test_norm_of_missing_gradients_takes_no_memory_for_them():
+    w = [torch.zeros(1 << 24, device="cuda"), torch.zeros(5, device="cuda", dtype=torch.bfloat16), torch.zeros(7, device="cuda")]
+    g = torch.full((7,), 2.0, device="cuda")
+    opt = qb.AdamW(w, [None, None, g])
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    n, _ = opt.grad_norm()
+    assert torch.cuda.max_memory_allocated() - before < 1 << 20
+    assert abs(float(n) - 2 * np.sqrt(7)) < 1e-5
+    g1 = torch.full((5,), 1.0, device="cuda", dtype=torch.bfloat16)
+    opt.bind([None, g1, None])
+    assert abs(float(opt.grad_norm()[0]) - np.sqrt(5)) < 1e-5
