@@ -477,7 +477,8 @@ int qadam_adamw_create(const qadam_adamw_config* cfg, const qadam_adamw_buffers*
 int qadam_adamw_bind(qadam_adamw* ctx, const void* const* grads);
 
 /* Step t = `step` >= 1 with step size lr (< 0: the configuration's).  grad_scale: device, one
- * binary32, or NULL.  If it is not finite, the step changes nothing and sets QADAM_ST_NONFINITE.
+ * binary32, or NULL.  If it is not finite, the step changes nothing and sets QADAM_ST_NONFINITE (a set
+ * without elements has nothing to launch and sets nothing).
  * Steps need not be in order: t only enters the bias corrections and the random stream.  A captured
  * call repeats its t and lr. */
 int qadam_adamw_step(qadam_adamw* ctx, int64_t step, float lr, const float* grad_scale, void* stream);

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   const AdamTile T = p.tiles[p.first + blockIdx.x];
   const void* g = grads.at[T.seg - p.tensor_base];
   float c;
-  if (g == nullptr || !gradient_factor(p, c)) return;
+  if (!gradient_factor(p, c) || g == nullptr) return;
   const int lane = threadIdx.x % 32;
   const int i0 = threadIdx.x / 32 * kPair;                   // of the warp's two rows, inside the tile
   const int rows = i0 >= T.left ? 0 : i0 + 128 >= T.left ? 1 : 2;
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(kAdamThreads, kEightCtas) adamw8_kernel(const 
   const AdamTile& T = p.tiles[t];
   const char* const g = static_cast<const char*>(grads.at[T.seg - p.tensor_base]);
   float c;
-  if (g == nullptr || !gradient_factor(p, c)) return;
+  if (!gradient_factor(p, c) || g == nullptr) return;
   const int lane = threadIdx.x % 32;
   const int left = T.left, gtype = T.gtype, wtype = T.wtype;
   const bool fits = ((reinterpret_cast<uintptr_t>(g) & (4 * kGBytes - 1)) | (reinterpret_cast<uintptr_t>(T.w) & (4 * kWBytes - 1))) == 0;

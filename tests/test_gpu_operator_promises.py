@@ -1,5 +1,6 @@
 """What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded, first
-calls on a stream of their own, what is allocated."""
+calls on a stream of their own, what is allocated,
+what a step without gradients tells."""
 import numpy as np
 import pytest
 import torch
@@ -81,3 +82,12 @@ def test_norm_of_missing_gradients_takes_no_memory_for_them():
     g1 = torch.full((5,), 1.0, device="cuda", dtype=torch.bfloat16)
     opt.bind([None, g1, None])
     assert abs(float(opt.grad_norm()[0]) - np.sqrt(5)) < 1e-5
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_factor_that_is_not_finite_is_told_without_gradients_too(bits):
+    opt = qb.AdamW([torch.ones(2000, device="cuda"), torch.ones(0, device="cuda")], [None, None], state_bits=bits)
+    opt.step(1, grad_scale=torch.ones(1, device="cuda"))
+    assert opt.poll_status() == 0
+    opt.step(1, grad_scale=torch.full((1,), float("nan"), device="cuda"))
+    assert opt.poll_status() == qb.ST_NONFINITE and bool((opt.weights[0] == 1).all())
