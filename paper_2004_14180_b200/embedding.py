@@ -2,7 +2,7 @@
 
 All calls run on the current stream of the table's device.  `status`, where given, is one int32 on the
 device that gets ST_INDEX if a token is not below the number of rows; the caller clears and reads it.
-None of them is recorded by autograd: the gradient of a lookup is embedding_grad.
+None of them is recorded by autograd: the gradient of a lookup is embedding_grad.  It is told that `out` is written.
 """
 from __future__ import annotations
 
@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-from .adamw import TYPES, _need_cuda, element_type, stream_of
+from .adamw import TYPES, _need_cuda, element_type, stream_of, written
 from .binding import _check, load_library
 
 
@@ -90,7 +90,8 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     n, width = table.shape
     shape = ids.shape + (width,)
     stride = width if table.is_contiguous() else _row_stride(table, "table", table.shape, device)
-    if out is None:
+    given = out is not None
+    if not given:
         out, out_stride = torch.empty(*shape, dtype=out_dtype or table.dtype, device=device), width
     else:
         out, out_stride = _out(shape, out, out_dtype, device), _row_stride(out, "out", shape, device)
@@ -100,6 +101,8 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
         stream_of(device))
     if rc:
         _check(rc, "qadam_embedding_lookup")
+    if given:
+        written(out)
     return out
 
 
@@ -119,7 +122,8 @@ def held_lookup(wcodes: torch.Tensor, kx: int, ids: torch.Tensor, rows: int, wid
             return held_lookup(wcodes, kx, ids, rows, width, scale, out_dtype, first, out, status)
     ids = _tokens(ids, device)
     shape = ids.shape + (width,)
-    if out is None:
+    given = out is not None
+    if not given:
         out, out_stride = torch.empty(*shape, dtype=out_dtype, device=device), width
     else:
         out_stride = _row_stride(out, "out", shape, device)
@@ -128,6 +132,8 @@ def held_lookup(wcodes: torch.Tensor, kx: int, ids: torch.Tensor, rows: int, wid
         scale, out.data_ptr(), _type(out, "out"), out_stride, None if status is None else _status(status, device), stream_of(device))
     if rc:
         _check(rc, "qadam_held_lookup")
+    if given:
+        written(out)
     return out
 
 
@@ -152,6 +158,7 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
     count = ids.numel()
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
+    given = out is not None
     out = _out((rows, width), out, dtype if dtype is not None or out is not None else dy.dtype, device)
     dy_stride = _row_stride(dy, "dy", ids.shape + (width,), device)
     out_stride = _row_stride(out, "out", (rows, width), device)
@@ -163,4 +170,6 @@ def embedding_grad(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float 
         None if status is None else _status(status, device), stream_of(device))
     if rc:
         _check(rc, "qadam_embedding_grad")
+    if given:
+        written(out)
     return out

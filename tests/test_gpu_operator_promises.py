@@ -1,6 +1,6 @@
-"""What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is rounded, first
-calls on a stream of their own, what is allocated,
-what a step without gradients tells."""
+"""What the operators around the quantized step promise beside their values: how each operation of the 8-bit step is
+rounded, first calls on a stream of their own, what is allocated, what a step without gradients tells, what autograd is told
+of writes."""
 import numpy as np
 import pytest
 import torch
@@ -91,3 +91,50 @@ def test_a_factor_that_is_not_finite_is_told_without_gradients_too(bits):
     assert opt.poll_status() == 0
     opt.step(1, grad_scale=torch.full((1,), float("nan"), device="cuda"))
     assert opt.poll_status() == qb.ST_NONFINITE and bool((opt.weights[0] == 1).all())
+
+
+# ---------------------------------------------------------------- what autograd is told
+
+@pytest.mark.parametrize("counted", [False, True])
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_backward_pass_through_stepped_weights_is_refused(packed, counted):
+    base = torch.ones(300, device="cuda")
+    w = [base[:100], base[100:300]] if packed else [torch.nn.Parameter(torch.ones(n, device="cuda")) for n in (100, 200)]
+    s = torch.ones(1, device="cuda", requires_grad=True)
+    opt = qb.AdamW(w, [torch.ones(n, device="cuda") for n in (100, 200)])
+    for used in w:
+        y = (s * used).sum()
+        opt.step_counted() if counted else opt.step(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+        (s * used).sum().backward()
+
+
+def test_weights_made_in_inference_mode_are_stepped():
+    with torch.inference_mode():
+        w, g = torch.ones(100, device="cuda"), torch.ones(100, device="cuda")
+        opt = qb.AdamW([w], [g])
+        opt.step(1)
+        out = torch.empty(2, device="cuda")
+        opt.grad_norm()
+        qb.GradNorm([g])(1.0, out=out)
+        rows = qb.embedding_lookup(w.view(10, 10), torch.tensor([3, 0], device="cuda"), out=torch.empty(2, 10, device="cuda"))
+    assert bool((w < 1).all()) and float(out[0]) == 10.0 and torch.equal(rows, w.view(10, 10)[[3, 0]])
+
+
+@pytest.mark.parametrize("call", ["lookup", "held", "grad", "norm", "own norm", "moments"])
+def test_a_backward_pass_through_an_overwritten_result_is_refused(call):
+    ids = torch.tensor([1, 0, 3], device="cuda")
+    table, codes = torch.ones(4, 8, device="cuda"), torch.zeros(32, dtype=torch.uint8, device="cuda")
+    s = torch.ones(1, device="cuda", requires_grad=True)
+    out = torch.empty((3, 8) if call in ("lookup", "held") else (4, 8) if call == "grad" else 2, device="cuda")
+    norm = qb.GradNorm([table])
+    opt = qb.AdamW([table], [table.clone()], state_bits=8)
+    pair = (torch.empty(128, device="cuda"), torch.empty(128, device="cuda"))
+    run = {"lookup": lambda: qb.embedding_lookup(table, ids, out=out), "held": lambda: qb.held_lookup(codes, 6, ids, 4, 8, out=out),
+           "grad": lambda: qb.embedding_grad(ids, table[:3], 4, out=out), "norm": lambda: norm(1.0, out=out)[1],
+           "own norm": lambda: norm(1.0)[1], "moments": lambda: opt.moments(out=pair)[1]}[call]
+    y = (s * run()).sum()
+    run()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
