@@ -296,11 +296,15 @@ constexpr int kCluster = 8;                                // CTAs that sort up 
 constexpr int kRankThreads = 512;
 constexpr int kRankWarps = kRankThreads / 32;
 constexpr int kRankPer = 64;                               // tokens that a CTA ranks
-// Threads that clear beside the CTAs that sort: many for a sort that takes its time (8192 tokens, 94 MB: 31.8 us in all,
-// 40.1 with a quarter), few where the sums follow at once (64 tokens: 19.9 us, 22.9 with four times as many).
-constexpr int kClearThreads = 136 * 2048;
-constexpr int kClearThreadsFew = 136 * 512;
-constexpr int kFewTokens = 256;
+// Threads that clear beside the CTAs that sort.  Whole calls with 16 / 256 / 2048 / 8192 / 32768 tokens, binary32 gradients of 768
+// columns, us:
+//                  1000 rows                      30522                          400000
+//   136 x  512     4.0   8.1                      18.0  20.2                     205   209
+//   136 x 2048     4.2   8.2  15.6  19.7  33.5    18.5  20.9  24.3  28.8  45.2    186   188   192   223   237
+//   136 x 4096     4.2   8.2  15.6  19.7  33.5    17.6  20.0  23.2  28.5  45.0    191   193   197   202   216
+//   136 x 8192     4.2   8.2  15.6  19.7  33.5    17.0  19.4  23.1  27.9  44.3    183   185   189   190   204
+// The last takes 8.3 us in place of 7.1 for 16 tokens and 8000 rows, and 82 in place of 79 for 10^5 tokens and 30522 rows.
+constexpr int kClearThreads = 136 * 4096;
 
 struct ClearParams {
   void* grad;
@@ -1238,7 +1242,7 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
     c.end = to_clear * (turn + 1) / launches;
     ++turn;
     const long long each = c.dense ? threads : 1;
-    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, (count <= kFewTokens ? kClearThreadsFew : kClearThreads) / threads);
+    c.ctas = (int)std::min<long long>((c.end - c.begin + each - 1) / each, kClearThreads / threads);
   };
   if (count == 0) {
     share(kClearCta);
