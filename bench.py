@@ -54,15 +54,15 @@ def ncu_traffic():
         return {}
 
 
-# What the kernels of the quantized step are made of (the host side and other operators apart).
-STEP_KERNELS = ("qadam_device.cuh", "qadam_kernels.cuh", "qadam_noalloc.cu", "qadam_server_pipe.cuh",
-                "qadam_worker_resident.cuh", "qadam_worker_stream.cuh")
+# Sources of the operators beside the quantized step: nothing of the step is made of them.
+OTHER_OPERATORS = ("qadam_adamw.cu", "qadam_embedding.cu", "qadam_norm.cu", "qadam_tensors.cuh")
 
 
 def csrc_digest() -> str:
+    """Of everything that the step's kernels and their launches are made of; a file that is not named above counts."""
     h = hashlib.sha256()
     base = os.path.join(ROOT, "paper_2004_14180_b200", "csrc")
-    for name in STEP_KERNELS:
+    for name in sorted(set(os.listdir(base)) - set(OTHER_OPERATORS)):
         with open(os.path.join(base, name), "rb") as f:
             h.update(name.encode())
             h.update(f.read())
