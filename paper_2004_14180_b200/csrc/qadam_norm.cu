@@ -4,9 +4,11 @@
 //
 // One read of the tensors: bound by HBM, as long as an element costs few instructions.  The squares of what a thread has
 // in 16 bytes are added in binary32 (4 products and sums, or 8 exact products of 16-bit numbers: the sum of squares
-// is off by at most 7 x 2^-24, the norm by half of that), everything else in binary64: conversions of every element
-// to binary64 took half as long again (59 us in place of 38 for 109.5 x 10^6 bf16, 5.7 TB/s).  Squares that binary32 does not hold,
-// of numbers below 1e-12 or above 1e19, are seen by their sum, and formed in binary64.
+// is off by at most 7 x 2^-24, the norm by half of that), everything else in binary64: with squares in binary64 this
+// kernel takes 53 us in place of 37 for 109.5 x 10^6 bf16 (5.9 TB/s) and 33.8 in place of 32.7 for 47 x 10^6 fp32.  Squares that
+// binary32 does not hold, of numbers below 1e-12 or above 1e19, are seen by their sum, and formed in binary64.  A short list
+// is bound by what does not depend on its length: 1000 elements take 3.6 us, 10^6 5.1, 11.7 x 10^6 12.0, and every further 10^6
+// 0.59 (6.8 TB/s).
 #include "qadam.h"
 
 #include <algorithm>
