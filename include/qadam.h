@@ -354,7 +354,7 @@ int qadam_destroy(qadam_ctx* ctx);
 
 /* ===========================================================================================
  * The training step around the quantized step: AdamW over many tensors, the norm of their
- * gradients, and the two operators at an embedding table.  They are contexts and calls of their
+ * gradients, the two operators at an embedding table, layer norm, and products in 8 bits.  They are contexts and calls of their
  * own and share nothing with a qadam_ctx but the conventions above, with these differences:
  *  - every call takes the stream that it enqueues on, which belongs to the context's device (to
  *    the current device where there is no context).  The device that is current stays current;
@@ -530,6 +530,77 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
                          int64_t dy_stride, float scale, int64_t padding, void* grad, int32_t grad_type,
                          int64_t rows, int64_t width, int64_t grad_stride, int32_t accumulate,
                          void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
+
+/* ---- layer norm --------------------------------------------------------------------------- */
+
+/* For each of `rows` rows h of `width` elements (h = x, or h = round(x + residual) in `type`, which is then written to sum):
+ *     mean = sum h / width,  rstd = 1 / sqrt(sum (h - mean)^2 / width + eps),  y = (h - mean) rstd weight + bias
+ * in binary32; out = round(y).  x, residual, sum, out: device, rows a stride (in elements, >= width) apart, all of `type`.
+ * weight, bias: device, [width], each of a type of its own, or NULL (1, 0).  mean, rstd: device, [rows], or NULL.
+ * q (NULL: none): y before its rounding, in 8 bits, with scale and sums as qadam_quantize_rows writes them.  Of out, q, mean and
+ * rstd at least one is needed; sum goes with residual.  rows = 0 is allowed; rows < 2^31, width <= 2^24. */
+int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                     int32_t weight_type, const void* bias, int32_t bias_type, int64_t rows, int64_t width, float eps, void* sum,
+                     int64_t sum_stride, void* out, int64_t out_stride, float* mean, float* rstd, int8_t* q, int64_t q_stride,
+                     float* scale, int32_t* sums, void* stream);
+
+/* Scratch of qadam_layer_norm_grad. */
+int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes);
+
+/* Gradients of the norm of x (of h, if there was a residual), from dy, the gradient of out, and the mean and rstd that the norm
+ * has written.  With xhat = (x - mean) rstd and g = dy weight:
+ *     dx = round(rstd (g - sum g / width - xhat sum(g xhat) / width) + dsum)
+ *     dweight = sum over rows of dy xhat,  dbias = sum over rows of dy
+ * in binary32; the sums over rows in an order that the sizes alone fix: the same bits every time.  dsum: the gradient that
+ * reaches h by other ways, or NULL; dx is then the gradient of x and of residual both.  dy, x, dsum, dx are of `type`.  dweight, dbias: device,
+ * [width] of grad_type, either may be NULL; accumulate = 1 adds to what is there.  rows = 0: the sums are zero.
+ * workspace: 256-byte aligned, needed for dweight or dbias. */
+int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const void* x, int64_t x_stride, const float* mean,
+                          const float* rstd, const void* weight, int32_t weight_type, const void* dsum, int64_t dsum_stride,
+                          int64_t rows, int64_t width, void* dx, int64_t dx_stride, void* dweight, void* dbias, int32_t grad_type,
+                          int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- products in 8 bits -------------------------------------------------------------------
+ * A row in 8 bits is q[k], -127 .. 127, each worth `scale`: with a = max(max |x[k]|, 2^-100),
+ *     q[k] = x[k] * (127 / a) rounded to the nearest whole number, ties to even;  scale = a / 127
+ * (quotients and product rounded to binary32).  A row with a value that is not finite has scale NaN and zeros.
+ * Rows of q are a multiple of 16 bytes apart and begin on 16 bytes; bytes between them are not read. */
+
+/* Rows of x[][k] columns[k] (columns: device, [width], or NULL: 1; one binary32 product) in 8 bits.  sums: device, [rows], or
+ * NULL: gets sum_k q[k].  rows = 0 is allowed; rows < 2^31, width <= 2^24. */
+int qadam_quantize_rows(const void* x, int32_t type, int64_t x_stride, const float* columns, int64_t rows, int64_t width, int8_t* q,
+                        int64_t q_stride, float* scale, int32_t* sums, void* stream);
+
+/* The columns of x [rows][width] as rows in 8 bits: q is [width][q_stride], q_stride >= rows rounded up to 16 (the bytes up to
+ * there are written), scale [width].  rows >= 1. */
+int qadam_quantize_columns_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes);
+int qadam_quantize_columns(const void* x, int32_t type, int64_t x_stride, int64_t rows, int64_t width, int8_t* q, int64_t q_stride, float* scale,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Elements [first, first + rows * width) of the packed broadcast Q_x(x) (see qadam_held_lookup; kx = 0 .. 6) as rows in 8 bits:
+ * q = level, -2^kx .. 2^kx, worth 2^-(kx + 1).  q_stride >= width rounded up to 16 (the bytes up to there are written). */
+int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t rows, int64_t width, int8_t* q,
+                    int64_t q_stride, void* stream);
+
+/* out[m][n] = round(a_scale[m] b_scale[n] sum_k a[m][k] B[k][n] + bias[n]), m < rows, n < channels, k < depth; accumulate = 1:
+ * round(out[m][n] + the same).  The sum is exact (depth <= 131072), the rest binary32.
+ * transposed = 0: B[k][n] = b[n][k], b is [channels][b_stride >= depth] and b_scale [channels], as a layer's output needs it.
+ * transposed = 1: B[k][n] = b[k][n], b is [depth][b_stride >= channels], as the gradient of a layer's input needs it; b_scale is
+ * not read (the scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
+ * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
+ * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
+int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
+                      const float* b_scale, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type, void* out,
+                      int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream);
+
+/* The same with the weights that a worker holds in codes of one byte (kx = 6, QADAM_ERR_LEVEL otherwise): b is a table of the elements from
+ * `first` on, [channels][depth], or [depth][channels] if transposed, read as it lies in wcodes; b_scale is 2^-7.  a_sums: the
+ * sums of a's rows.  QADAM_ERR_ALIGN unless wcodes, first and the table's width are multiples of 16: take qadam_held_rows then,
+ * and for other kx. */
+int qadam_held_product(const int8_t* a, int64_t a_stride, const float* a_scale, const int32_t* a_sums, int64_t rows, int64_t depth,
+                       const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t channels, int32_t transposed,
+                       const void* bias, int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, int32_t accumulate,
+                       uint32_t* status, void* stream);
 
 const char* qadam_strerror(int err);
 

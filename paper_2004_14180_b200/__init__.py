@@ -1,5 +1,5 @@
 """Quantized Adam with error feedback: one parameter-server step on a B200, and the
-training step around it (AdamW, gradient norm, embedding rows and their gradient).
+training step around it (AdamW, gradient norm, embedding rows and their gradient, layer norm, products in 8 bits).
 
 Thin Python binding over the C interface of include/qadam.h (libqadam.so, built
 from csrc/ by build.py).  Every step of the method runs in the library's CUDA
@@ -22,3 +22,5 @@ from .binding import (  # noqa: F401
 )
 from .adamw import AdamW, GradNorm  # noqa: F401
 from .embedding import embedding_grad, embedding_lookup, held_lookup  # noqa: F401
+from .norm import Normed, layer_norm, layer_norm_grad  # noqa: F401
+from .int8 import Int8Rows, held_matmul, held_rows, int8_matmul, quantize_columns, quantize_rows  # noqa: F401

@@ -34,6 +34,9 @@ exported_symbols = (
     "qadam_adamw_launch_count", "qadam_adamw_destroy",
     "qadam_embedding_lookup", "qadam_held_lookup", "qadam_embedding_grad_query_sizes",
     "qadam_embedding_grad",
+    "qadam_layer_norm", "qadam_layer_norm_grad_query_sizes", "qadam_layer_norm_grad",
+    "qadam_quantize_rows", "qadam_quantize_columns_query_sizes", "qadam_quantize_columns",
+    "qadam_held_rows", "qadam_row_product", "qadam_held_product",
 )
 
 SERVER_AUTO, SERVER_PLAIN = 0, 1
@@ -177,6 +180,15 @@ def load_library():
         "held_lookup": [vp, size, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp, vp],
         "embedding_grad_query_sizes": [i64, i64, i64, C.POINTER(size)],
         "embedding_grad": [vp, i32, i64, vp, i32, i64, f32, i64, vp, i32, i64, i64, i64, i32, vp, size, vp, vp],
+        "layer_norm": [vp, i32, i64, vp, i64, vp, i32, vp, i32, i64, i64, f32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp],
+        "layer_norm_grad_query_sizes": [i64, i64, C.POINTER(size)],
+        "layer_norm_grad": [vp, i32, i64, vp, i64, vp, vp, vp, i32, vp, i64, i64, i64, vp, i64, vp, vp, i32, i32, vp, size, vp],
+        "quantize_rows": [vp, i32, i64, vp, i64, i64, vp, i64, vp, vp, vp],
+        "quantize_columns_query_sizes": [i64, i64, C.POINTER(size)],
+        "quantize_columns": [vp, i32, i64, i64, i64, vp, i64, vp, vp, size, vp],
+        "held_rows": [vp, size, i32, i64, i64, i64, vp, i64, vp],
+        "row_product": [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
+        "held_product": [vp, i64, vp, vp, i64, i64, vp, size, i32, i64, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
     }.items():
         fn = getattr(L, "qadam_" + name)
         fn.restype, fn.argtypes = C.c_int, args
@@ -459,6 +471,17 @@ class QAdam:
             raise ValueError(f"segment {segment} of {self.seg_len[segment]} elements has no rows of {width}")
         return held_lookup(self.wcodes[:self.wcode_bytes], self.kx, ids, self.seg_len[segment] // width, width, scale=scale,
                            out_dtype=out_dtype, first=self.seg_off[segment], **kw)
+
+    def matmul(self, segment: int, width: int, a, transpose: bool = False, **kw):
+        """8-bit rows times a tensor as the workers hold it, see `held_matmul`: the tensor's rows are `width` long.  Runs on the
+        current stream, as `lookup` does."""
+        from .int8 import held_matmul
+        if self.kx < 0:
+            raise ValueError("nothing is broadcast in packed form with kx = -1: quantize the rows of x")
+        if width < 1 or self.seg_len[segment] % width:
+            raise ValueError(f"segment {segment} of {self.seg_len[segment]} elements has no rows of {width}")
+        return held_matmul(a, self.wcodes[:self.wcode_bytes], self.kx, self.seg_len[segment] // width, width, first=self.seg_off[segment],
+                           transpose=transpose, **kw)
 
     def set_moment_rates(self, beta_t: float, theta_t: float) -> None:
         """beta_t, theta_t of Algorithm 1 for the steps that follow."""

@@ -10,11 +10,13 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libqadam.so")
 SOURCES = [os.path.join(CSRC, "qadam_api.cu"), os.path.join(CSRC, "qadam_noalloc.cu"), os.path.join(CSRC, "qadam_norm.cu"),
-           os.path.join(CSRC, "qadam_adamw.cu"), os.path.join(CSRC, "qadam_embedding.cu")]
+           os.path.join(CSRC, "qadam_adamw.cu"), os.path.join(CSRC, "qadam_embedding.cu"),
+           os.path.join(CSRC, "qadam_layer.cu"), os.path.join(CSRC, "qadam_product.cu")]
 HEADERS = [os.path.join(CSRC, "qadam_device.cuh"), os.path.join(CSRC, "qadam_kernels.cuh"),
            os.path.join(CSRC, "qadam_server_pipe.cuh"),
            os.path.join(CSRC, "qadam_worker_resident.cuh"), os.path.join(CSRC, "qadam_worker_stream.cuh"),
            os.path.join(CSRC, "qadam_host.h"), os.path.join(CSRC, "qadam_tensors.cuh"),
+           os.path.join(CSRC, "qadam_rows.cuh"),
            os.path.join(_ROOT, "include", "qadam.h")]
 
 NVCC_FLAGS = [

@@ -1,0 +1,393 @@
+// Products of rows in 8 bits with weights in 8 bits: qadam_row_product, qadam_held_product.
+//
+//   out[m][n] = round( a_scale[m] b_scale[n] (sum_k a[m][k] b[n][k] - zero a_sums[m]) + bias[n] (+ out[m][n]) )
+//
+// The sums are whole numbers of 32 bits, exact.  A packed weight of 8 bits is its code, 0 .. 128, level + 64: the codes go to
+// the tensor cores as they lie in memory, as unsigned bytes, and 64 sum_k a[m][k] is taken off at the end.
+#include "qadam.h"
+
+#include <cuda.h>
+#include <cooperative_groups.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "qadam_rows.cuh"
+
+using namespace qadam;
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int kChannels = 128;             // of a tile: the rows of the tensor cores' result
+constexpr int kDepth = 128;                // bytes of a row in a stage
+constexpr int kMaxTokens = 256;            // of a tile: the columns of the result
+constexpr int kProductThreads = 192;       // a warp that loads, one that multiplies, four for the end
+constexpr int kMaxStages = 8;
+constexpr int kMaxSplit = 8;
+constexpr unsigned kPolls = 1u << 21;      // of a wait, each suspended for up to a microsecond
+
+struct ProductParams {
+  const float* a_scale;
+  const int* a_sums;
+  const float* b_scale;
+  float worth;                             // of a weight, where there is no b_scale
+  int zero;
+  const void* bias;
+  int bias_type;
+  char* out;
+  int out_type;
+  long long out_stride;
+  int accumulate;
+  long long rows, channels;
+  int blocks;                              // of kDepth along the sum
+  int tokens;                              // of a tile
+  int channel_tiles;
+  int transposed;
+  int b_signed;
+  int stages;
+  unsigned* status;
+};
+
+__device__ __forceinline__ unsigned shared_at(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint64_t* bar, unsigned count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_at(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_at(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint64_t* bar, unsigned parity) {
+  unsigned ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(shared_at(bar)), "r"(parity), "r"(1000u)
+      : "memory");
+  return ok != 0;
+}
+// Gives up after kPolls polls, or once another thread has.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, volatile int* gave_up) {
+  for (unsigned i = 0; i < kPolls; ++i) {
+    if (barrier_try(bar, parity)) return true;
+    if (*gave_up) return false;
+  }
+  *gave_up = 1;
+  return false;
+}
+
+__device__ __forceinline__ void load_tile(void* to, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(shared_at(to)),
+      "l"(map), "r"(x), "r"(y), "r"(shared_at(bar))
+      : "memory");
+}
+
+// Where an operand lies in shared memory: rows of 128 bytes, swizzled in groups of eight (1024 bytes apart).
+__device__ __forceinline__ uint64_t operand(unsigned at) {
+  return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)(16384u >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+__device__ __forceinline__ void multiply(unsigned result, uint64_t a, uint64_t b, unsigned kind, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(result),
+      "l"(a), "l"(b), "r"(kind), "r"((unsigned)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_at(bar)) : "memory");
+}
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Sixteen columns of the result, of the warp's 32 rows.
+__device__ __forceinline__ void read_columns(unsigned from, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(from)
+      : "memory");
+}
+
+struct ProductShared {
+  uint64_t full[kMaxStages], empty[kMaxStages], done;
+  unsigned result;                         // in tensor memory
+  int gave_up;
+};
+
+// What a thread knows of its channel.
+struct Channel {
+  long long at;
+  float worth, bias;
+  bool in;
+};
+__device__ __forceinline__ Channel channel_of(const ProductParams& p, long long at) {
+  Channel c;
+  c.at = at;
+  c.in = at < p.channels;
+  c.worth = c.in && p.b_scale ? p.b_scale[at] : p.worth;
+  c.bias = c.in && p.bias ? load_one_of(p.bias, p.bias_type, at) : 0.0f;
+  return c;
+}
+__device__ __forceinline__ void finish(const ProductParams& p, const Channel& c, long long row, uint32_t sum) {
+  if (p.a_sums) sum -= (uint32_t)p.zero * (uint32_t)p.a_sums[row];
+  float y = fmaf((float)(int)sum * p.a_scale[row], c.worth, c.bias);
+  const long long i = row * p.out_stride + c.at;
+  if (p.accumulate) y += load_one_of(p.out, p.out_type, i);
+  store_one_of(p.out, p.out_type, i, y);
+}
+
+// One tile of kChannels x tokens to a cluster; its CTAs share the sum's blocks and add up in each other's shared memory.
+__global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                                                                  const __grid_constant__ ProductParams p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ ProductShared s;
+  uint8_t* ring = raw + (1024u - (shared_at(raw) & 1023u)) % 1024u;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const unsigned b_bytes = kChannels * kDepth, a_bytes = (unsigned)p.tokens * kDepth, stage_bytes = a_bytes + b_bytes;
+  const long long tile = blockIdx.x / split;
+  const long long channel = tile % p.channel_tiles * kChannels, row = tile / p.channel_tiles * p.tokens;
+  const int from = (int)((long long)p.blocks * rank / split), to = (int)((long long)p.blocks * (rank + 1) / split);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.stages; ++i) {
+      barrier_init(&s.full[i], 1);
+      barrier_init(&s.empty[i], 1);
+    }
+    barrier_init(&s.done, 1);
+    s.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  unsigned columns = 32;
+  while ((int)columns < p.tokens) columns *= 2;
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_at(&s.result)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const unsigned result = s.result;
+  wait_for_previous_launch();
+
+  int loaded = 0;                          // stages' fills asked for (warp 0)
+  if (warp == 0 && lane == 0) {
+    for (int i = from; i < to; ++i, ++loaded) {
+      const int st = loaded % p.stages;
+      if (!barrier_wait(&s.empty[st], (unsigned)(loaded / p.stages & 1) ^ 1u, &s.gave_up)) break;
+      uint8_t* b = ring + st * stage_bytes;
+      barrier_expect(&s.full[st], stage_bytes);
+      if (p.transposed) load_tile(b, &b_map, (int)channel, i * kDepth, &s.full[st]);
+      else load_tile(b, &b_map, i * kDepth, (int)channel, &s.full[st]);
+      load_tile(b + b_bytes, &a_map, i * kDepth, (int)row, &s.full[st]);
+    }
+  } else if (warp == 1 && lane == 0) {
+    // result 32 bits signed; first operand by its type; second signed; sizes in eights and sixteens
+    const unsigned kind = 2u << 4 | (unsigned)p.b_signed << 7 | 1u << 10 | (unsigned)p.transposed << 15 | (unsigned)(p.tokens / 8) << 17 |
+                          (unsigned)(kChannels / 16) << 24;
+    const unsigned step = p.transposed ? 32 * 128 / 16 : 32 / 16;
+    int n = 0;
+    for (int i = from; i < to; ++i, ++n) {
+      const int st = n % p.stages;
+      if (!barrier_wait(&s.full[st], (unsigned)(n / p.stages & 1), &s.gave_up)) break;
+      after_sync();
+      const unsigned b = shared_at(ring + st * stage_bytes);
+      const uint64_t wd = operand(b), td = operand(b + b_bytes);
+#pragma unroll
+      for (int k = 0; k < kDepth / 32; ++k) multiply(result, wd + (uint64_t)(k * step), td + (uint64_t)(k * 2), kind, n > 0 || k > 0);
+      commit(&s.empty[st]);
+    }
+    commit(&s.done);
+  }
+  __syncwarp();
+  const bool ok = barrier_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0;
+  after_sync();
+  const long long left = p.rows - row;
+  const int live = left < p.tokens ? (int)left : p.tokens;
+  if (split == 1) {
+    if (warp >= 2 && ok) {
+      const int quarter = warp % 4;        // a warp can read the rows of the result that its number names
+      const Channel c = channel_of(p, channel + quarter * 32 + lane);
+      for (int t = 0; t < live; t += 16) {
+        uint32_t v[16];
+        read_columns(result + (unsigned)(quarter * 32) * 65536u + (unsigned)t, v);
+        if (c.in) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            if (t + k < live) finish(p, c, row + t + k, v[k]);
+        }
+      }
+    }
+  } else {
+    int* mine = reinterpret_cast<int*>(ring);          // [tokens][kChannels]; nothing is on its way into the ring any more
+    __syncthreads();
+    if (warp >= 2 && ok) {
+      const int quarter = warp % 4;
+      for (int t = 0; t < live; t += 16) {
+        uint32_t v[16];
+        read_columns(result + (unsigned)(quarter * 32) * 65536u + (unsigned)t, v);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) mine[(t + k) * kChannels + quarter * 32 + lane] = (int)v[k];
+      }
+    }
+    cluster.sync();
+    if (warp >= 2) {
+      const Channel c = channel_of(p, channel + warp % 4 * 32 + lane);
+      bool all = true;
+      for (int r = 0; r < split; ++r) all &= *cluster.map_shared_rank(&s.gave_up, r) == 0;
+      if (all && c.in) {
+        for (int t = rank; t < live; t += split) {
+          uint32_t sum = 0;
+          for (int r = 0; r < split; ++r) sum += (uint32_t)cluster.map_shared_rank(mine, r)[t * kChannels + warp % 4 * 32 + lane];
+          finish(p, c, row + t, sum);
+        }
+      }
+    }
+    cluster.sync();
+  }
+  if (s.gave_up && warp == 0 && lane == 0) {
+    // what was asked for has to land before this CTA's memory is anyone else's
+    for (int i = loaded > p.stages ? loaded - p.stages : 0; i < loaded; ++i)
+      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[i % p.stages], (unsigned)(i / p.stages & 1)); ++n) {}
+    if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
+  }
+  before_sync();
+  __syncthreads();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(columns));
+}
+
+// ---------------------------------------------------------------- launches
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static std::atomic<Encode> known{nullptr};
+  Encode e = known.load();
+  if (e) return e;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (!cuda_call(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found)) || found != cudaDriverEntryPointSuccess) return nullptr;
+  e = reinterpret_cast<Encode>(fn);
+  known.store(e);
+  return e;
+}
+
+// A matrix of bytes [rows][stride], of which a copy takes boxes of 128 x `box_rows`; what lies beyond it reads as zero.
+bool byte_map(CUtensorMap* map, const void* p, int64_t width, int64_t rows, int64_t stride, int box_rows) {
+  const Encode encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)stride};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, unit[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// CTAs of a cluster wait for one another while they hold tensor memory, so no SM may be given more of them than its 512 columns
+// serve.  Their shared memory sees to it: a sum is split for tiles of at most 64 tokens only, with two stages of 24 KB for
+// 64 columns, or one of 18 KB and more for 32.
+constexpr int kRingBytes = 208 * 1024;
+
+// Once for each device: how much shared memory the kernel may take.
+bool allow_shared_memory() {
+  static std::atomic<uint64_t> done{0};
+  int device = 0;
+  if (!cuda_call(cudaGetDevice(&device))) return false;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (done.load() & bit) return true;
+  if (!cuda_call(cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024))) return false;
+  done.fetch_or(bit);
+  return true;
+}
+
+constexpr int kSms = 148;
+
+int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t depth, const void* b, int64_t b_stride, cudaStream_t st) {
+  p.blocks = (int)((depth + kDepth - 1) / kDepth);
+  p.channel_tiles = (int)((p.channels + kChannels - 1) / kChannels);
+  int tokens = 16;
+  while (tokens < kMaxTokens && tokens < p.rows) tokens *= 2;
+  while (tokens > 64 && (int64_t)p.channel_tiles * ((p.rows + tokens - 1) / tokens) < kSms) tokens /= 2;
+  p.tokens = tokens;
+  const int64_t tiles = (int64_t)p.channel_tiles * ((p.rows + tokens - 1) / tokens);
+  int split = 1;
+  while (split < kMaxSplit && tokens <= 64 && tiles * split * 2 <= 2 * kSms && p.blocks >= split * 4) split *= 2;
+  const int stage = (kChannels + tokens) * kDepth;
+  const int needed = (p.blocks + split - 1) / split;
+  p.stages = std::min({kMaxStages, kRingBytes / stage, std::max(needed, (tokens * kChannels * 4 + stage - 1) / stage)});
+  if (tiles * split >= (int64_t)1 << 31) return QADAM_ERR_SIZE;
+  CUtensorMap a_map, b_map;
+  const bool maps = byte_map(&a_map, a, depth, p.rows, a_stride, tokens) &&
+                    (p.transposed ? byte_map(&b_map, b, p.channels, depth, b_stride, kDepth) : byte_map(&b_map, b, depth, p.channels, b_stride, kChannels));
+  if (!maps || !allow_shared_memory()) return QADAM_ERR_CUDA;
+  return launch(product_kernel, tiles * split, kProductThreads, (size_t)p.stages * stage + 1024, split, st, a_map, b_map, p) ? QADAM_OK : QADAM_ERR_CUDA;
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 31, kMostDepth = 131072;
+
+int check_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, int64_t channels, const void* bias,
+                  int32_t bias_type, const void* out, int32_t out_type, int64_t out_stride, int32_t transposed, int32_t accumulate,
+                  const uint32_t* status) {
+  if (rows < 0 || rows >= kMostRows || channels < 1 || channels >= kMostRows || depth < 1 || depth > kMostDepth) return QADAM_ERR_SIZE;
+  if ((transposed != 0 && transposed != 1) || (accumulate != 0 && accumulate != 1)) return QADAM_ERR_SIZE;
+  if (!known_type(out_type) || (bias && !known_type(bias_type))) return QADAM_ERR_TYPE;
+  if (rows > 0 && (!a || !a_scale || !out)) return QADAM_ERR_NULL;
+  if (a_stride < depth || a_stride >= (int64_t)1 << 40 || out_stride < channels || out_stride > (int64_t)1 << 40) return QADAM_ERR_SIZE;
+  if (!is_aligned(a, 16) || a_stride % 16 != 0 || !is_aligned(a_scale, 4) || (bias && !is_aligned(bias, type_bytes(bias_type))) ||
+      !is_aligned(out, type_bytes(out_type)) || !is_aligned(status, 4))
+    return QADAM_ERR_ALIGN;
+  return QADAM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
+                      const float* b_scale, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type, void* out,
+                      int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream) {
+  const int rc = check_product(a, a_stride, a_scale, rows, depth, channels, bias, bias_type, out, out_type, out_stride, transposed, accumulate, status);
+  if (rc != QADAM_OK) return rc;
+  if (rows > 0 && (!b || (!transposed && !b_scale))) return QADAM_ERR_NULL;
+  if (b_stride < (transposed ? channels : depth) || b_stride >= (int64_t)1 << 40) return QADAM_ERR_SIZE;
+  if (!is_aligned(b, 16) || b_stride % 16 != 0 || !is_aligned(b_scale, 4)) return QADAM_ERR_ALIGN;
+  if (rows == 0) return QADAM_OK;
+  ProductParams p = {};
+  p.a_scale = a_scale; p.b_scale = transposed ? nullptr : b_scale; p.worth = 1.0f;
+  p.bias = bias; p.bias_type = bias_type;
+  p.out = static_cast<char*>(out); p.out_type = out_type; p.out_stride = out_stride; p.accumulate = accumulate;
+  p.rows = rows; p.channels = channels; p.transposed = transposed; p.b_signed = 1; p.status = status;
+  return enqueue_product(p, a, a_stride, depth, b, b_stride, static_cast<cudaStream_t>(stream));
+}
+
+int qadam_held_product(const int8_t* a, int64_t a_stride, const float* a_scale, const int32_t* a_sums, int64_t rows, int64_t depth,
+                       const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t channels, int32_t transposed,
+                       const void* bias, int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, int32_t accumulate,
+                       uint32_t* status, void* stream) {
+  const int rc = check_product(a, a_stride, a_scale, rows, depth, channels, bias, bias_type, out, out_type, out_stride, transposed, accumulate, status);
+  if (rc != QADAM_OK) return rc;
+  if (kx != 6) return QADAM_ERR_LEVEL;
+  if (!wcodes || (rows > 0 && !a_sums)) return QADAM_ERR_NULL;
+  const int64_t width = transposed ? channels : depth, table = transposed ? depth : channels;
+  if (!is_aligned(wcodes, 16) || first % 16 != 0 || width % 16 != 0 || !is_aligned(a_sums, 4)) return QADAM_ERR_ALIGN;
+  if (first < 0 || first > (int64_t)1 << 44 || wcode_bytes / 2 > (size_t)1 << 44) return QADAM_ERR_SIZE;
+  if (first > (int64_t)wcode_bytes || table > ((int64_t)wcode_bytes - first) / width) return QADAM_ERR_SIZE;
+  if (rows == 0) return QADAM_OK;
+  ProductParams p = {};
+  p.a_scale = a_scale; p.a_sums = a_sums; p.zero = 64; p.worth = 1.0f / 128.0f;
+  p.bias = bias; p.bias_type = bias_type;
+  p.out = static_cast<char*>(out); p.out_type = out_type; p.out_stride = out_stride; p.accumulate = accumulate;
+  p.rows = rows; p.channels = channels; p.transposed = transposed; p.b_signed = 0; p.status = status;
+  return enqueue_product(p, a, a_stride, depth, static_cast<const uint8_t*>(wcodes) + first, width, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,137 @@
+"""Layer norm of token rows and its gradients (include/qadam.h).
+
+Calls run on the current stream of x's device.  Neither is recorded by autograd: the gradients are layer_norm_grad.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+from typing import NamedTuple, Optional, Tuple
+
+import torch
+
+from .adamw import _need_cuda, stream_of, written
+from .binding import _check, load_library
+from .embedding import _elsewhere, _row_stride, _type
+from .int8 import Int8Rows, empty_rows
+
+
+class Normed(NamedTuple):
+    """out: the normed rows (None if not asked for); sum: x + residual, rounded (x itself without a residual); mean, rstd: of the
+    rows, float32, flat; rows: out in 8 bits before its rounding (None if not asked for)."""
+    out: Optional[torch.Tensor]
+    sum: torch.Tensor
+    mean: torch.Tensor
+    rstd: torch.Tensor
+    rows: Optional[Int8Rows]
+
+
+def _parameter(t: Optional[torch.Tensor], what: str, width: int, device: torch.device):
+    if t is None:
+        return None, 0
+    if t.device != device or t.shape != (width,) or not t.is_contiguous():
+        raise ValueError(f"{what}: {width} contiguous elements on {device} are needed")
+    return t.data_ptr(), _type(t, what)
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               residual: Optional[torch.Tensor] = None, dense: bool = True, int8: bool = False) -> Normed:
+    """Layer norm over the last dimension of x [..., width] (float32, bfloat16 or float16; rows at equal distances), of x + residual if
+    a residual is given (x's shape and type).
+
+    weight, bias: [width], of any of the three types each.  dense: give `out`, of x's type; int8: give `rows`, for a product in 8 bits."""
+    if not x.is_cuda or x.dim() < 1:
+        _need_cuda()
+        raise ValueError("x: a CUDA tensor [..., width] is needed; there is no CPU path")
+    device, width = x.device, x.shape[-1]
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return layer_norm(x, weight, bias, eps, residual, dense, int8)
+    if width < 1:
+        raise ValueError("x: rows of no elements")
+    n = x.numel() // width
+    kind = _type(x, "x")
+    stride = _row_stride(x, "x", x.shape, device)
+    weight_at, weight_type = _parameter(weight, "weight", width, device)
+    bias_at, bias_type = _parameter(bias, "bias", width, device)
+    total, residual_at, residual_stride = x, None, 0
+    if residual is not None:
+        if residual.dtype != x.dtype:
+            raise ValueError(f"residual is {residual.dtype}, x {x.dtype}")
+        residual_at, residual_stride = residual.data_ptr(), _row_stride(residual, "residual", x.shape, device)
+        total = torch.empty(x.shape, dtype=x.dtype, device=device)
+    out = torch.empty(x.shape, dtype=x.dtype, device=device) if dense else None
+    mean, rstd = torch.empty(2, n, dtype=torch.float32, device=device).unbind()
+    rows = None
+    if int8:
+        rows = Int8Rows(empty_rows(n, width, device), torch.empty(n, dtype=torch.float32, device=device),
+                        torch.empty(n, dtype=torch.int32, device=device))
+    if n:
+        rc = load_library().qadam_layer_norm(
+            x.data_ptr(), kind, stride, residual_at, residual_stride, weight_at, weight_type, bias_at, bias_type, n, width, eps,
+            None if residual is None else total.data_ptr(), width, None if out is None else out.data_ptr(), width, mean.data_ptr(),
+            rstd.data_ptr(), None if rows is None else rows.q.data_ptr(), (width + 15) // 16 * 16,
+            None if rows is None else rows.scale.data_ptr(), None if rows is None else rows.sums.data_ptr(), stream_of(device))
+        if rc:
+            _check(rc, "qadam_layer_norm")
+    return Normed(out, total, mean, rstd, rows)
+
+
+@functools.lru_cache(maxsize=256)
+def _grad_workspace(rows: int, width: int) -> int:
+    size = C.c_size_t()
+    _check(load_library().qadam_layer_norm_grad_query_sizes(rows, width, C.byref(size)), "qadam_layer_norm_grad_query_sizes")
+    return size.value
+
+
+def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                    dsum: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                    accumulate: bool = False, grad_dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """-> (dx, dweight, dbias) from dy, the gradient of layer_norm's out; x: what was normed (`sum`); mean, rstd: as it gave them.
+
+    dsum: the gradient that reaches `sum` by other ways: dx is then the gradient of x and of the residual both.  dy, x and dsum have one
+    type and one shape.  dweight, dbias: buffers ([width], contiguous, of one type) to overwrite, or to add to with accumulate, such as a
+    worker's gradient of one tensor in the padded layout; made here, of grad_dtype, if not given (accumulate needs both).  The
+    sums over rows are binary32 and the same bits every time."""
+    if not x.is_cuda or x.dim() < 1:
+        _need_cuda()
+        raise ValueError("x: a CUDA tensor [..., width] is needed; there is no CPU path")
+    device, width = x.device, x.shape[-1]
+    if _elsewhere(device):
+        with torch.cuda.device(device):
+            return layer_norm_grad(dy, x, mean, rstd, weight, dsum, dweight, dbias, accumulate, grad_dtype)
+    if width < 1:
+        raise ValueError("x: rows of no elements")
+    n = x.numel() // width
+    kind = _type(x, "x")
+    for t, what in ((dy, "dy"), (dsum, "dsum")):
+        if t is not None and t.dtype != x.dtype:
+            raise ValueError(f"{what} is {t.dtype}, x {x.dtype}")
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        if t.device != device or t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what}: {n} contiguous float32 on {device} are needed")
+    if accumulate and (dweight is None or dbias is None):
+        raise ValueError("accumulate needs dweight and dbias")
+    given = [t for t in (dweight, dbias) if t is not None]
+    if given:
+        grad_dtype = given[0].dtype
+    dweight = torch.empty(width, dtype=grad_dtype, device=device) if dweight is None else dweight
+    dbias = torch.empty(width, dtype=grad_dtype, device=device) if dbias is None else dbias
+    dw_at, dw_type = _parameter(dweight, "dweight", width, device)
+    db_at, db_type = _parameter(dbias, "dbias", width, device)
+    if dw_type != db_type:
+        raise ValueError(f"dweight is {dweight.dtype}, dbias {dbias.dtype}")
+    weight_at, weight_type = _parameter(weight, "weight", width, device)
+    x_stride, dy_stride = _row_stride(x, "x", x.shape, device), _row_stride(dy, "dy", x.shape, device)
+    ds_at, ds_stride = (None, 0) if dsum is None else (dsum.data_ptr(), _row_stride(dsum, "dsum", x.shape, device))
+    dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+    size = _grad_workspace(n, width)
+    scratch = torch.empty(size, dtype=torch.uint8, device=device)
+    rc = load_library().qadam_layer_norm_grad(
+        dy.data_ptr(), kind, dy_stride, x.data_ptr(), x_stride, mean.data_ptr(), rstd.data_ptr(), weight_at, weight_type, ds_at, ds_stride,
+        n, width, dx.data_ptr(), width, dw_at, db_at, dw_type, int(accumulate), scratch.data_ptr(), size, stream_of(device))
+    if rc:
+        _check(rc, "qadam_layer_norm_grad")
+    for t in given:
+        written(t)
+    return dx, dweight, dbias
