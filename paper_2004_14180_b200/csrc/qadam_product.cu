@@ -264,6 +264,284 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(columns));
 }
 
+// ---------------------------------------------------------------- many tokens
+
+// Tiles of 256 tokens x up to 256 channels to a pair of CTAs on two SMs, which multiply together: each has 128 tokens, half of the
+// channels' weights in its shared memory, and the results of its 128 tokens in its tensor memory.  That halves the weights'
+// way into shared memory.  The pairs go from tile to tile; results have two places, so that the end of a tile (eight warps: numbers of
+// 32 bits times scales, rounded, through shared memory and out in boxes) runs beside the next one's products.
+constexpr int kPairThreads = 384;          // a warp that loads, one that multiplies, one for tensor memory, one idle, eight for the end
+constexpr int kPairTokens = 256;
+constexpr int kPairStages = 5;
+constexpr int kOperandBytes = 128 * kDepth;
+constexpr int kPairStageBytes = 2 * kOperandBytes;
+constexpr int kEndWarps = 8;
+constexpr int kBoxBytes = 32 * 128;        // of 32 tokens, 128 bytes each
+constexpr int kEndChannels = 128;          // of a tile, that a warp sees at most
+constexpr int kPairBytes = kPairStages * kPairStageBytes + kEndWarps * (kBoxBytes + kEndChannels * 8);
+constexpr int kTokenGroup = 8;             // tiles of so many token blocks lie next to each other in time: what they read stays in L2
+
+struct PairParams {
+  const float* a_scale;
+  const int* a_sums;
+  const float* b_scale;
+  float worth;
+  int zero;
+  const void* bias;
+  int bias_type;
+  char* out;
+  long long out_stride;
+  int accumulate;
+  long long rows, channels;
+  int blocks;
+  int half;                                // channels of a tile that a CTA's shared memory has the weights of: 32, 64, 96 or 128
+  int token_tiles, channel_tiles;
+  int transposed, b_signed;
+  unsigned* status;
+};
+
+struct PairShared {
+  uint64_t full[kPairStages], empty[kPairStages], result_full[2], result_empty[2];
+  unsigned result;
+  int gave_up;
+};
+
+__device__ __forceinline__ unsigned of_first(unsigned at) {                // the same place in the pair's first CTA
+  unsigned r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(at));
+  return r;
+}
+__device__ __forceinline__ void pair_load(void* to, const CUtensorMap* map, int x, int y, unsigned bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          shared_at(to)),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_multiply(unsigned result, uint64_t a, uint64_t b, unsigned kind, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(result),
+      "l"(a), "l"(b), "r"(kind), "r"((unsigned)add)
+      : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {               // arrives in both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_at(bar)),
+               "h"((unsigned short)3)
+               : "memory");
+}
+__device__ __forceinline__ void arrive_at(unsigned bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void read_columns32(unsigned from, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+        "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+        "=r"(v[31])
+      : "r"(from)
+      : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap* map, const void* from, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(shared_at(from))
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+struct PairTile {
+  int token, channel;                      // tiles
+};
+__device__ __forceinline__ PairTile pair_tile(const PairParams& p, long long t) {
+  const long long group = t / ((long long)kTokenGroup * p.channel_tiles);
+  const int first = (int)group * kTokenGroup, tall = min(kTokenGroup, p.token_tiles - first);
+  const long long in = t - group * kTokenGroup * p.channel_tiles;
+  return {first + (int)(in % tall), (int)(in / tall)};
+}
+
+// OUT: type of the result.  BOXES: it is written in boxes; else (rows that do not begin on 16 bytes, or a result to be added
+// to) from shared memory element by element, 32 channels of a token at a time.
+template <int OUT, bool BOXES>
+__global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                                                               const __grid_constant__ CUtensorMap out_map, const __grid_constant__ PairParams p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ PairShared s;
+  uint8_t* ring = raw + (1024u - (shared_at(raw) & 1023u)) % 1024u;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank();
+  const long long tiles = (long long)p.token_tiles * p.channel_tiles, step = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kPairStages; ++i) {
+      barrier_init(&s.full[i], 1);
+      barrier_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(&s.result_full[i], 1);
+      barrier_init(&s.result_empty[i], 2 * kEndWarps);
+    }
+    s.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_at(&s.result)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
+  before_sync();
+  cluster.sync();
+  after_sync();
+  const unsigned result = s.result;
+  wait_for_previous_launch();
+
+  const unsigned b_bytes = p.transposed ? kOperandBytes : (unsigned)p.half * kDepth;
+  long long loaded = 0;
+  if (warp == 0 && lane == 0) {
+    bool ok = true;
+    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step) {
+      const PairTile tile = pair_tile(p, t);
+      const int row = tile.token * kPairTokens + rank * 128, channel = tile.channel * 2 * p.half + rank * p.half;
+      for (int i = 0; i < p.blocks; ++i, ++loaded) {
+        const int st = (int)(loaded % kPairStages);
+        ok = barrier_wait(&s.empty[st], (unsigned)(loaded / kPairStages & 1) ^ 1u, &s.gave_up);
+        if (!ok) break;
+        uint8_t* a = ring + st * kPairStageBytes;
+        const unsigned bar = of_first(shared_at(&s.full[st]));
+        if (rank == 0) barrier_expect(&s.full[st], 2 * (kOperandBytes + b_bytes));
+        pair_load(a, &a_map, i * kDepth, row, bar);
+        if (p.transposed) pair_load(a + kOperandBytes, &b_map, channel, i * kDepth, bar);
+        else pair_load(a + kOperandBytes, &b_map, i * kDepth, channel, bar);
+      }
+    }
+  } else if (warp == 1 && lane == 0 && rank == 0) {
+    // result 32 bits signed; first operand signed, second by its type; sizes in eights and sixteens
+    const unsigned kind = 2u << 4 | 1u << 7 | (unsigned)p.b_signed << 10 | (unsigned)p.transposed << 16 | (unsigned)(2 * p.half / 8) << 17 |
+                          (unsigned)(kPairTokens / 16) << 24;
+    const unsigned b_step = p.transposed ? 32 * 128 / 16 : 32 / 16;
+    long long n = 0;
+    int turn = 0;
+    bool ok = true;
+    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step, ++turn) {
+      ok = barrier_wait(&s.result_empty[turn & 1], (unsigned)(turn / 2 & 1) ^ 1u, &s.gave_up);
+      if (!ok) break;
+      after_sync();
+      const unsigned at = result + (unsigned)(turn & 1) * 256u;
+      for (int i = 0; i < p.blocks; ++i, ++n) {
+        const int st = (int)(n % kPairStages);
+        ok = barrier_wait(&s.full[st], (unsigned)(n / kPairStages & 1), &s.gave_up);
+        if (!ok) break;
+        after_sync();
+        const unsigned a = shared_at(ring + st * kPairStageBytes);
+        const uint64_t ad = operand(a), bd = operand(a + kOperandBytes);
+#pragma unroll
+        for (int k = 0; k < kDepth / 32; ++k) pair_multiply(at, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * b_step), kind, i > 0 || k > 0);
+        pair_commit(&s.empty[st]);
+      }
+      if (ok) pair_commit(&s.result_full[turn & 1]);
+    }
+  } else if (warp >= 4) {
+    const int end = warp - 4, quarter = warp % 4, side = end / 4;
+    uint8_t* box = ring + kPairStages * kPairStageBytes + end * kBoxBytes;
+    float2* about = reinterpret_cast<float2*>(ring + kPairStages * kPairStageBytes + kEndWarps * kBoxBytes) + end * kEndChannels;   // scale, bias
+    constexpr int kBox = BOXES && OUT != QADAM_F32 ? 64 : 32;                // channels of a box
+    int turn = 0;
+    for (long long t = blockIdx.x / 2; t < tiles; t += step, ++turn) {
+      const PairTile tile = pair_tile(p, t);
+      const long long row0 = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32, row = row0 + lane;
+      const long long channel0 = (long long)tile.channel * 2 * p.half;
+      const int wide = (int)min((long long)2 * p.half, p.channels - channel0);
+      const float a_scale = row < p.rows ? p.a_scale[row] : 0.0f;
+      const int less = row < p.rows && p.a_sums ? p.zero * p.a_sums[row] : 0;
+      __syncwarp();
+      // this warp's channels: every other box of the tile
+      for (int i = lane; i < kEndChannels; i += 32) {
+        const int c = (i / kBox * 2 + side) * kBox + i % kBox;
+        float2 f = make_float2(p.worth, 0.0f);
+        if (c < wide) {
+          if (p.b_scale) f.x = p.b_scale[channel0 + c];
+          if (p.bias) f.y = load_one_of(p.bias, p.bias_type, channel0 + c);
+        }
+        about[i] = f;
+      }
+      __syncwarp();
+      if (!barrier_wait(&s.result_full[turn & 1], (unsigned)(turn / 2 & 1), &s.gave_up)) break;
+      after_sync();
+      const unsigned at = result + (unsigned)(turn & 1) * 256u + (unsigned)(quarter * 32) * 65536u;
+      for (int j = 0; (j * 2 + side) * kBox < wide; ++j) {
+        const int c0 = (j * 2 + side) * kBox;
+        if constexpr (BOXES) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < kBox / 32; ++h) {
+          uint32_t v[32];
+          read_columns32(at + (unsigned)(c0 + h * 32), v);
+          const float4* f = reinterpret_cast<const float4*>(about + j * kBox + h * 32);
+          uint8_t* line = box + lane * 128;
+          float y[32];
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            const float4 g = f[k / 2];
+            y[k] = fmaf((float)((int)v[k] - less) * a_scale, g.x, g.y);
+            y[k + 1] = fmaf((float)((int)v[k + 1] - less) * a_scale, g.z, g.w);
+          }
+          if constexpr (kBox == 64) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+              const float e[8] = {y[k], y[k + 1], y[k + 2], y[k + 3], y[k + 4], y[k + 5], y[k + 6], y[k + 7]};
+              store_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(line + (((h * 4 + k / 8) ^ (lane & 7)) << 4), floats_to_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(e));
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)
+              *reinterpret_cast<float4*>(line + (((k / 4) ^ (lane & 7)) << 4)) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+          }
+        }
+        if constexpr (BOXES) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && row0 < p.rows) store_box(&out_map, box, (int)(channel0 + c0), (int)row0);
+        } else {
+          __syncwarp();
+          const int live = (int)min((long long)32, p.rows - row0);
+          const bool in = c0 + lane < wide;
+          const long long first = row0 * p.out_stride + channel0 + c0 + lane;
+#pragma unroll 8
+          for (int r = 0; r < 32; ++r) {
+            const float y = *reinterpret_cast<const float*>(box + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + lane % 4 * 4);
+            if (in && r < live) {
+              const long long i = first + r * p.out_stride;
+              store_one<OUT>(p.out, i, p.accumulate ? load_one<OUT>(p.out, i) + y : y);
+            }
+          }
+        }
+      }
+      before_sync();
+      __syncwarp();
+      if (lane == 0) arrive_at(of_first(shared_at(&s.result_empty[turn & 1])));
+    }
+    if constexpr (BOXES) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+  }
+  __syncwarp();
+  if (s.gave_up && warp == 0 && lane == 0) {
+    // what was asked for has to land before these CTAs' memory is anyone else's
+    if (rank == 0)
+      for (long long i = loaded > kPairStages ? loaded - kPairStages : 0; i < loaded; ++i)
+        for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[i % kPairStages], (unsigned)(i / kPairStages & 1)); ++n) {}
+    if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
+  }
+  before_sync();
+  cluster.sync();
+  after_sync();
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(512));
+}
+
 // ---------------------------------------------------------------- launches
 
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -279,6 +557,18 @@ Encode encoder() {
   e = reinterpret_cast<Encode>(fn);
   known.store(e);
   return e;
+}
+
+// A matrix of results, written in boxes of 32 rows of 128 bytes.
+bool box_map(CUtensorMap* map, void* p, int type, int64_t channels, int64_t rows, int64_t stride) {
+  const Encode encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)channels, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(stride * type_bytes(type))};
+  const cuuint32_t box[2] = {type == QADAM_F32 ? 32u : 64u, 32u}, unit[2] = {1, 1};
+  return encode(map, type == QADAM_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == QADAM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                2, p, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // A matrix of bytes [rows][stride], of which a copy takes boxes of 128 x `box_rows`; what lies beyond it reads as zero.
@@ -297,22 +587,82 @@ bool byte_map(CUtensorMap* map, const void* p, int64_t width, int64_t rows, int6
 // 64 columns, or one of 18 KB and more for 32.
 constexpr int kRingBytes = 208 * 1024;
 
-// Once for each device: how much shared memory the kernel may take.
-bool allow_shared_memory() {
-  static std::atomic<uint64_t> done{0};
+using PairKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, PairParams);
+constexpr PairKernel kPairKernels[3][2] = {{pair_kernel<QADAM_F32, false>, pair_kernel<QADAM_F32, true>},
+                                           {pair_kernel<QADAM_BF16, false>, pair_kernel<QADAM_BF16, true>},
+                                           {pair_kernel<QADAM_F16, false>, pair_kernel<QADAM_F16, true>}};
+
+// Once for each device: how much shared memory the kernels may take; the pairs of SMs that there are.
+constexpr int kDevices = 64;
+int pairs_of_device() {
+  static std::atomic<int> known[kDevices];
   int device = 0;
-  if (!cuda_call(cudaGetDevice(&device))) return false;
-  const uint64_t bit = (uint64_t)1 << (device & 63);
-  if (done.load() & bit) return true;
-  if (!cuda_call(cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024))) return false;
-  done.fetch_or(bit);
-  return true;
+  if (!cuda_call(cudaGetDevice(&device))) return 0;
+  std::atomic<int>& pairs = known[device % kDevices];
+  if (const int n = pairs.load()) return n;
+  if (!cuda_call(cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + 1024))) return 0;
+  for (const auto& of_type : kPairKernels)
+    for (const PairKernel kernel : of_type)
+      if (!cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairBytes + 1024))) return 0;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(2);
+  config.blockDim = dim3(kPairThreads);
+  config.dynamicSmemBytes = kPairBytes + 1024;
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = 2;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  config.attrs = &cluster;
+  config.numAttrs = 1;
+  int n = 0;
+  if (!cuda_call(cudaOccupancyMaxActiveClusters(&n, kPairKernels[0][0], &config)) || n < 1) return 0;
+  pairs.store(n);
+  return n;
 }
 
 constexpr int kSms = 148;
+constexpr int kFewTokens = 128;
+
+// Channels of a pair's tile: the time of the pairs' rounds, in cycles of the tensor cores (a block of 128 bytes takes twice a tile's
+// channels) and what a tile costs besides, is to be least.
+int pair_half(int64_t token_tiles, int64_t channels, int blocks, int pairs) {
+  int best = 128;
+  int64_t least = INT64_MAX;
+  for (int half = 128; half >= 32; half -= 32) {             // (whole boxes of results)
+    const int64_t tiles = token_tiles * ((channels + 2 * half - 1) / (2 * half));
+    const int64_t cost = (tiles + pairs - 1) / pairs * ((int64_t)blocks * 4 * half + 1500);
+    if (cost < least) {
+      least = cost;
+      best = half;
+    }
+  }
+  return best;
+}
+
+int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int64_t depth, const void* b, int64_t b_stride, int pairs, cudaStream_t st) {
+  PairParams p = {};
+  p.a_scale = q.a_scale; p.a_sums = q.a_sums; p.b_scale = q.b_scale; p.worth = q.worth; p.zero = q.zero; p.bias = q.bias; p.bias_type = q.bias_type;
+  p.out = q.out; p.out_stride = q.out_stride; p.accumulate = q.accumulate; p.rows = q.rows; p.channels = q.channels; p.blocks = q.blocks;
+  p.transposed = q.transposed; p.b_signed = q.b_signed; p.status = q.status;
+  p.token_tiles = (int)((p.rows + kPairTokens - 1) / kPairTokens);
+  p.half = pair_half(p.token_tiles, p.channels, p.blocks, pairs);
+  p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
+  const bool boxes = !p.accumulate && is_aligned(p.out, 16) && p.out_stride * type_bytes(q.out_type) % 16 == 0;
+  CUtensorMap a_map, b_map, out_map = {};
+  const bool maps = byte_map(&a_map, a, depth, p.rows, a_stride, 128) &&
+                    (p.transposed ? byte_map(&b_map, b, p.channels, depth, b_stride, kDepth) : byte_map(&b_map, b, depth, p.channels, b_stride, p.half)) &&
+                    (!boxes || box_map(&out_map, p.out, q.out_type, p.channels, p.rows, p.out_stride));
+  if (!maps) return QADAM_ERR_CUDA;
+  const int64_t tiles = (int64_t)p.token_tiles * p.channel_tiles;
+  return launch(kPairKernels[q.out_type][boxes], 2 * std::min<int64_t>(tiles, pairs), kPairThreads, kPairBytes + 1024, 2, st, a_map, b_map, out_map, p)
+             ? QADAM_OK : QADAM_ERR_CUDA;
+}
 
 int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t depth, const void* b, int64_t b_stride, cudaStream_t st) {
   p.blocks = (int)((depth + kDepth - 1) / kDepth);
+  const int pairs = pairs_of_device();
+  if (pairs == 0) return QADAM_ERR_CUDA;
+  if (p.rows > kFewTokens) return enqueue_pairs(p, a, a_stride, depth, b, b_stride, pairs, st);
   p.channel_tiles = (int)((p.channels + kChannels - 1) / kChannels);
   int tokens = 16;
   while (tokens < kMaxTokens && tokens < p.rows) tokens *= 2;
@@ -328,7 +678,7 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
   CUtensorMap a_map, b_map;
   const bool maps = byte_map(&a_map, a, depth, p.rows, a_stride, tokens) &&
                     (p.transposed ? byte_map(&b_map, b, p.channels, depth, b_stride, kDepth) : byte_map(&b_map, b, depth, p.channels, b_stride, kChannels));
-  if (!maps || !allow_shared_memory()) return QADAM_ERR_CUDA;
+  if (!maps) return QADAM_ERR_CUDA;
   return launch(product_kernel, tiles * split, kProductThreads, (size_t)p.stages * stage + 1024, split, st, a_map, b_map, p) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 

@@ -31,7 +31,7 @@ def check(got, a, b, b_scale, bias, kind, before=None):
 
 
 SIZES = [(1, 1, 1), (1, 16, 8), (1, 4096, 512), (2, 100, 130), (3, 128, 128), (16, 768, 768), (17, 769, 129), (33, 1000, 257), (64, 2048, 1000),
-         (65, 64, 3000), (128, 130, 640), (129, 768, 2304), (300, 257, 1537), (513, 768, 768), (1000, 48, 4097), (2049, 1536, 700)]
+         (65, 64, 3000), (128, 130, 640), (129, 768, 2304), (300, 257, 1537), (513, 768, 768), (1000, 48, 4097), (2049, 1536, 700), (4099, 300, 2500), (6000, 130, 1537)]
 
 
 @pytest.mark.parametrize("m,k,n", SIZES)
