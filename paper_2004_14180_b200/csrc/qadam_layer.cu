@@ -13,8 +13,11 @@ namespace {
 
 constexpr int kWarpRowThreads = 128;                       // rows of at most 1024 elements: a warp each, four to a CTA
 constexpr int kWarpRowWidth = 1024;
-constexpr int kBlockRowWidth = 32768;                      // a CTA each, in registers; beyond, it reads the row again
+constexpr int kGroupRowWidth = 16384;                      // a group of warps for a row, in registers; beyond, a CTA reads the row again
+constexpr int kGroupMostThreads = 768;                     // of an SM, that go from row to row
 constexpr int kWideThreads = 1024;
+constexpr int kSms = 148;
+constexpr int kRingBytes = 220 * 1024;                     // of an SM's shared memory, for rows under way
 
 struct RowParams {
   const char* x;
@@ -43,186 +46,152 @@ struct RowParams {
 
 // ---------------------------------------------------------------- rows in registers
 
-// One pass: a row is read once, held in registers for mean, sum of squares around it and largest value, and written once.
-// Bound by HBM.  VEC: a thread has pieces of eight consecutive elements; else elements one by one, a group's width apart.
-template <int TY, int NV, bool VEC, bool CTA>
-__global__ void __launch_bounds__(CTA ? 1024 : kWarpRowThreads) row_kernel(const __grid_constant__ RowParams p) {
-  __shared__ RowShared shared;
-  wait_for_previous_launch();
-  constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
-  RowGroup<CTA> group(&shared);
-  const int threads = CTA ? blockDim.x : 32;
-  const int t = CTA ? threadIdx.x : threadIdx.x % 32;
-  const long long row = CTA ? (long long)blockIdx.x : (long long)blockIdx.x * (kWarpRowThreads / 32) + threadIdx.x / 32;
-  if (row >= p.rows) return;                               // (a warp, or the whole CTA)
-  const char* x = p.x + row * p.x_stride * kBytes;
-  float h[NV][8];
-  if constexpr (VEC) {
-    Raw8<TY> raw[NV] = {};
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * threads + t) * 8;
-      if (col < p.width) raw[v] = load_raw8<TY>(x + (size_t)col * kBytes);
-    }
-    if (p.r) {
-      const char* r = p.r + row * p.r_stride * kBytes;
-      char* sum = p.sum + row * p.sum_stride * kBytes;
-      Raw8<TY> more[NV] = {};
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int col = (v * threads + t) * 8;
-        if (col < p.width) more[v] = load_raw8<TY>(r + (size_t)col * kBytes);
-      }
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int col = (v * threads + t) * 8;
-        float a[8], b[8];
-        raw8_to_floats<TY>(raw[v], a);
-        raw8_to_floats<TY>(more[v], b);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] += b[k];
-        raw[v] = floats_to_raw8<TY>(a);
-        if (col < p.width) store_raw8<TY>(sum + (size_t)col * kBytes, raw[v]);
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) raw8_to_floats<TY>(raw[v], h[v]);
-  } else {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = (v * 8 + k) * threads + t;
-        h[v][k] = col < p.width ? load_one<TY>(x, col) : 0.0f;
-      }
-    if (p.r) {
-      const char* r = p.r + row * p.r_stride * kBytes;
-      char* sum = p.sum + row * p.sum_stride * kBytes;
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int col = (v * 8 + k) * threads + t;
-          if (col < p.width) {
-            h[v][k] = rounded<TY>(h[v][k] + load_one<TY>(r, col));
-            store_one<TY>(sum, col, h[v][k]);
-          }
-        }
-    }
-  }
+// What becomes of a row h, dealt out to a group's threads: normed, scaled, written, in 8 bits.
+template <int TY, int NV, bool VEC, bool MANY>
+__device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY, NV, VEC>& part, RowGroup<MANY>& group, long long row, float2 (&h)[4 * NV]) {
+  using Part = RowPart<TY, NV, VEC>;
   if (p.normed) {
-    float s = 0.0f;
+    float2 s = h[0];
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int i = 1; i < Part::kPairs; ++i) s = add2_rn(s, h[i]);
+    const float mean = group.add(s.x + s.y) / (float)p.width;
+    const float2 less = make_float2(-mean, -mean);
+    s = make_float2(0.0f, 0.0f);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += h[v][k];
-    const float mean = group.add(s) / (float)p.width;
-    s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = VEC ? (v * threads + t) * 8 : (v * 8 + k) * threads + t;
-        h[v][k] -= mean;
-        if (col < p.width) s = fmaf(h[v][k], h[v][k], s);
+    for (int i = 0; i < Part::kPairs; ++i) {
+      h[i] = add2_rn(h[i], less);
+      if constexpr (VEC) {
+        if (!part.has(Part::piece_of(2 * i))) h[i] = make_float2(0.0f, 0.0f);
+      } else {
+        if (!part.has(2 * i)) h[i].x = 0.0f;
+        if (!part.has(2 * i + 1)) h[i].y = 0.0f;
       }
-    const float rstd = 1.0f / sqrtf(group.add(s) / (float)p.width + p.eps);
-    if (t == 0) {
+      s = fma2_rn(h[i], h[i], s);
+    }
+    const float rstd = 1.0f / sqrtf(group.add(s.x + s.y) / (float)p.width + p.eps);
+    if (part.t == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
     }
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) h[v][k] *= rstd;
+    for (int i = 0; i < Part::kPairs; ++i) h[i] = mul2_rn(h[i], make_float2(rstd, rstd));
   }
   if (p.w || p.b) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if constexpr (VEC) {
-        const int col = (v * threads + t) * 8;
-        float w[8], b[8];
-        if (col < p.width) {
-          if (p.w) {
-            load_eight_of(p.w, p.w_type, col, p.w_vec, w);
-          }
-          if (p.b) {
-            load_eight_of(p.b, p.b_type, col, p.b_vec, b);
-          }
+    for (int q = 0; q < Part::kPieces; q += Part::kStep) {
+      float2 w[Part::kStepPairs], b[Part::kStepPairs];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) h[v][k] = fmaf(h[v][k], p.w ? w[k] : 1.0f, p.b ? b[k] : 0.0f);
-        }
-      } else {
+      for (int k = 0; k < Part::kStepPairs; ++k) w[k] = b[k] = make_float2(0.0f, 0.0f);               // (beyond the row: zero)
+      if (p.w) part.read_parameters(p.w, p.w_type, p.w_vec, q, w);
+      if (p.b) part.read_parameters(p.b, p.b_type, p.b_vec, q, b);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int col = (v * 8 + k) * threads + t;
-          if (col < p.width)
-            h[v][k] = fmaf(h[v][k], p.w ? load_one_of(p.w, p.w_type, col) : 1.0f, p.b ? load_one_of(p.b, p.b_type, col) : 0.0f);
-        }
+      for (int k = 0; k < Part::kStepPairs; ++k) {
+        float2& y = h[q / Part::kStep * Part::kStepPairs + k];
+        y = p.w ? p.b ? fma2_rn(y, w[k], b[k]) : mul2_rn(y, w[k]) : add2_rn(y, b[k]);
       }
     }
   }
-  if (p.out) {
-    char* out = p.out + row * p.out_stride * kBytes;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if constexpr (VEC) {
-        const int col = (v * threads + t) * 8;
-        if (col < p.width) store_raw8<TY>(out + (size_t)col * kBytes, floats_to_raw8<TY>(h[v]));
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int col = (v * 8 + k) * threads + t;
-          if (col < p.width) store_one<TY>(out, col, h[v][k]);
-        }
-      }
-    }
-  }
+  if (p.out) part.store(p.out + row * p.out_stride * Part::kBytes, h);
   if (p.q) {
-    uint32_t largest = 0u;
+    float largest = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = VEC ? (v * threads + t) * 8 : (v * 8 + k) * threads + t;
-        if (col < p.width) largest = max(largest, abs_bits(h[v][k]));
-      }
-    const ByteScale s = byte_scale(group.max(largest));
+    for (int i = 0; i < Part::kPairs; ++i) largest = largest_of(largest, h[i].x, h[i].y);
+    const ByteScale s = byte_scale(group.max(abs_bits(largest)));
     signed char* q = p.q + row * p.q_stride;
+    const uint32_t finite = s.per > 0.0f ? 0xFFFFFFFFu : 0u;
     int sum = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      int c[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = VEC ? (v * threads + t) * 8 : (v * 8 + k) * threads + t;
-        c[k] = to_byte(h[v][k], s.per);
-        if (col < p.width) {
-          sum += c[k];
-          if constexpr (!VEC) q[col] = (signed char)c[k];
-        }
-      }
+    for (int i = 0; i < Part::kPairs; i += 2) {
+      const uint32_t c = to_bytes(h[i], h[i + 1], s.per) & finite;
+      sum = __dp4a((int)c, 0x01010101, sum);               // (beyond the row: zeros)
       if constexpr (VEC) {
-        const int col = (v * threads + t) * 8;
-        if (col < p.width)
-          *reinterpret_cast<uint2*>(q + col) = make_uint2(four_bytes(c[0], c[1], c[2], c[3]), four_bytes(c[4], c[5], c[6], c[7]));
+        constexpr int kWords = Part::kPiece / 4;           // of a piece
+        if (part.has(i / (2 * kWords))) *reinterpret_cast<uint32_t*>(q + part.column(i / (2 * kWords)) + i / 2 % kWords * 4) = c;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (part.has(2 * i + k)) q[part.column(2 * i + k)] = (signed char)(c >> (8 * k));
       }
     }
     if (p.sums) sum = group.add(sum);
-    if (t == 0) {
+    if (part.t == 0) {
       p.scale[row] = s.worth;
       if (p.sums) p.sums[row] = sum;
     }
   }
 }
 
+// One pass: a row is read once, held in registers for mean, sum of squares around it and largest value, and written once.
+// Bound by HBM.  There is a warp for each row: enough of them are on an SM to keep its share of the loads under way.
+template <int TY, int NV, bool VEC>
+__global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_constant__ RowParams p) {
+  wait_for_previous_launch();
+  using Part = RowPart<TY, NV, VEC>;
+  RowGroup<false> group(nullptr, 1, 0);
+  const Part part(p.width, 32, threadIdx.x % 32);
+  const long long row = (long long)blockIdx.x * (kWarpRowThreads / 32) + threadIdx.x / 32;
+  if (row >= p.rows) return;
+  typename Part::Row h;
+  part.read(p.x + row * p.x_stride * Part::kBytes, h);
+  if (p.r) {
+    typename Part::Row r;
+    part.read(p.r + row * p.r_stride * Part::kBytes, r);
+#pragma unroll
+    for (int i = 0; i < Part::kPairs; ++i) h[i] = add2_rn(h[i], r[i]);
+    part.store_rounded(p.sum + row * p.sum_stride * Part::kBytes, h);
+  }
+  finish_row(p, part, group, row, h);
+}
+
+// Wider rows: a group of warps goes from row to row, with the next ones under way.
+constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
+template <int TY, int NV, bool VEC, int MOST>
+__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages) {
+  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][1 or 2][a row]
+  __shared__ GroupShared shared[kGroupWarps];
+  wait_for_previous_launch();
+  using Part = RowPart<TY, NV, VEC>;
+  const int threads = warps * 32, number = (int)threadIdx.x / threads;
+  const int groups = blockDim.x / threads;
+  const Part part(p.width, threads, (int)threadIdx.x % threads);
+  RowGroup<true> group(&shared[number], warps, number);
+  const int each = Part::slot_bytes(p.width), both = p.r ? 2 * each : each;
+  uint8_t* ring = slots + number * stages * both;
+  const long long first = (long long)blockIdx.x * groups + number, step = (long long)gridDim.x * groups;
+  const auto fetch = [&](long long row, int stage) {
+    if (row < p.rows) {
+      part.fetch(ring + stage * both, p.x + row * p.x_stride * Part::kBytes);
+      if (p.r) part.fetch(ring + stage * both + each, p.r + row * p.r_stride * Part::kBytes);
+    }
+    fetched();
+  };
+  for (int i = 0; i + 1 < stages; ++i) fetch(first + i * step, i);
+  int stage = 0;
+  for (long long row = first; row < p.rows; row += step) {
+    wait_fetched(stages - 2);
+    if constexpr (!VEC) group.sync();                      // (what others have copied; what the row before has left)
+    fetch(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+    typename Part::Row h;
+    part.read_slot(ring + stage * both, p.x + row * p.x_stride * Part::kBytes, h);
+    if (p.r) {
+      typename Part::Row r;
+      part.read_slot(ring + stage * both + each, p.r + row * p.r_stride * Part::kBytes, r);
+#pragma unroll
+      for (int i = 0; i < Part::kPairs; ++i) h[i] = add2_rn(h[i], r[i]);
+      part.store_rounded(p.sum + row * p.sum_stride * Part::kBytes, h);
+    }
+    finish_row(p, part, group, row, h);
+    stage = stage + 1 == stages ? 0 : stage + 1;
+  }
+}
+
 // Rows too wide for a CTA's registers: read again for each thing that is known only at the row's end.
 template <int TY>
 __global__ void __launch_bounds__(kWideThreads) wide_row_kernel(const __grid_constant__ RowParams p) {
-  __shared__ RowShared shared;
+  __shared__ GroupShared shared;
   wait_for_previous_launch();
   constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
-  RowGroup<true> group(&shared);
+  RowGroup<true> group(&shared, kWideThreads / 32, 0);
   const long long row = blockIdx.x;
   const char* x = p.x + row * p.x_stride * kBytes;
   const char* r = p.r ? p.r + row * p.r_stride * kBytes : nullptr;
@@ -272,23 +241,55 @@ __global__ void __launch_bounds__(kWideThreads) wide_row_kernel(const __grid_con
   }
 }
 
-template <int TY, int NV, bool CTA>
-bool launch_rows(const RowParams& p, bool vec, int threads, cudaStream_t st) {
-  const long long grid = CTA ? p.rows : (p.rows + kWarpRowThreads / 32 - 1) / (kWarpRowThreads / 32);
-  return vec ? launch(row_kernel<TY, NV, true, CTA>, grid, threads, 0, 0, st, p)
-             : launch(row_kernel<TY, NV, false, CTA>, grid, threads, 0, 0, st, p);
+template <int TY, int NV>
+bool launch_warp_rows(const RowParams& p, bool vec, cudaStream_t st) {
+  const long long grid = (p.rows + kWarpRowThreads / 32 - 1) / (kWarpRowThreads / 32);
+  return vec ? launch(warp_row_kernel<TY, NV, true>, grid, kWarpRowThreads, 0, 0, st, p) : launch(warp_row_kernel<TY, NV, false>, grid, kWarpRowThreads, 0, 0, st, p);
+}
+
+// CTAs of `threads` threads that an SM has at a time (of most_threads), and stages of `bytes` that each of them has then: 2 or 3,
+// or none if two do not fit.
+struct Residents {
+  int per_sm, stages;
+};
+Residents residents(int threads, int most_threads, int bytes) {
+  const int per_sm = std::max(1, std::min(most_threads / threads, kRingBytes / (2 * bytes + 2048)));
+  const int stages = std::min(3, (kRingBytes / per_sm - 2048) / bytes);
+  return {per_sm, stages < 2 ? 0 : stages};
+}
+
+// The limit of dynamic shared memory belongs to the kernel: it is raised to the same for every launch that needs it.
+template <typename K>
+bool allow_ring(K kernel, size_t bytes) {
+  return bytes <= 40 * 1024 || cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes));
+}
+
+template <int TY, int NV, bool VEC>
+bool launch_group_rows(const RowParams& p, cudaStream_t st) {
+  const int warps = (p.width + 256 * NV - 1) / (256 * NV), groups = std::max(1, kGroupWarps / warps);
+  const int threads = warps * groups * 32, bytes = RowPart<TY, NV, VEC>::slot_bytes(p.width) * (p.r ? 2 : 1) * groups;
+  const Residents r = residents(threads, kGroupMostThreads, bytes);
+  if (r.stages == 0) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
+  const auto kernel = threads <= 256 ? group_row_kernel<TY, NV, VEC, 256> : group_row_kernel<TY, NV, VEC, 512>;
+  return allow_ring(kernel, (size_t)r.stages * bytes) &&
+         launch(kernel, std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm), threads, (size_t)r.stages * bytes, 0, st, p, warps,
+                r.stages);
+}
+template <int TY, int NV>
+bool launch_group_rows(const RowParams& p, bool vec, cudaStream_t st) {
+  return vec ? launch_group_rows<TY, NV, true>(p, st) : launch_group_rows<TY, NV, false>(p, st);
 }
 
 template <int TY>
 bool enqueue_rows_of(const RowParams& p, bool vec, cudaStream_t st) {
-  if (p.width <= 256) return launch_rows<TY, 1, false>(p, vec, kWarpRowThreads, st);
-  if (p.width <= 512) return launch_rows<TY, 2, false>(p, vec, kWarpRowThreads, st);
-  if (p.width <= 768) return launch_rows<TY, 3, false>(p, vec, kWarpRowThreads, st);
-  if (p.width <= kWarpRowWidth) return launch_rows<TY, 4, false>(p, vec, kWarpRowThreads, st);
-  if (p.width > kBlockRowWidth) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
-  // (two pieces a thread, while there are threads for it)
-  if (p.width <= 16384) return launch_rows<TY, 2, true>(p, vec, (p.width + 511) / 512 * 32, st);
-  return launch_rows<TY, 4, true>(p, vec, (p.width + 1023) / 1024 * 32, st);
+  if (p.width <= 256) return launch_warp_rows<TY, 1>(p, vec, st);
+  if (p.width <= 512) return launch_warp_rows<TY, 2>(p, vec, st);
+  if (p.width <= 768) return launch_warp_rows<TY, 3>(p, vec, st);
+  if (p.width <= kWarpRowWidth) return launch_warp_rows<TY, 4>(p, vec, st);
+  if (p.width > kGroupRowWidth) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
+  // 24 or 32 elements to a thread, whichever leaves fewer threads without
+  const int three = (p.width + 767) / 768 * 768, four = (p.width + 1023) / 1024 * 1024;
+  return three < four && three <= 16 * 768 ? launch_group_rows<TY, 3>(p, vec, st) : launch_group_rows<TY, 4>(p, vec, st);
 }
 
 int enqueue_rows(const RowParams& p, int type, bool vec, cudaStream_t st) {
@@ -299,9 +300,8 @@ int enqueue_rows(const RowParams& p, int type, bool vec, cudaStream_t st) {
 
 // ---------------------------------------------------------------- gradients
 
-constexpr int kGradThreads = 128;
-constexpr int kGradBlockWidth = 8192;                      // in registers up to here
-constexpr int kMaxPartials = 1024;
+constexpr int kGradWarps = 12;                             // of a CTA, in groups, or one group of up to 32
+constexpr int kGradGroupWidth = 8192;                      // beyond, rows are read again, and the columns' sums are a pass of their own
 
 struct GradParams {
   const char* dy;
@@ -321,136 +321,114 @@ struct GradParams {
   int width;
 };
 
-template <int TY, int NV, bool VEC, bool CTA>
-__global__ void __launch_bounds__(CTA ? 512 : kGradThreads) row_grad_kernel(const __grid_constant__ GradParams p) {
-  extern __shared__ float columns[];                       // [2][width], warps' rows only
-  __shared__ RowShared shared;
+// A group of warps, eight elements to a thread, goes from row to row, with the next ones under way, and adds up its rows' part of the
+// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  One read, one write: bound by HBM.
+template <int TY, bool VEC, int MOST>
+__global__ void __launch_bounds__(MOST, MOST <= kGradWarps * 32 ? 2 : 1) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
+  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][2 or 3][a row]; at the end the groups' sums [groups][2][width]
+  __shared__ GroupShared shared[kGradWarps];
   wait_for_previous_launch();
-  constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
-  RowGroup<CTA> group(&shared);
-  const int threads = CTA ? blockDim.x : 32;
-  const int t = CTA ? threadIdx.x : threadIdx.x % 32;
-  const int here = CTA ? 1 : kGradThreads / 32;
-  const int mine = CTA ? 0 : threadIdx.x / 32;
+  using Part = RowPart<TY, 1, VEC>;
+  constexpr int kBytes = Part::kBytes;
+  const int threads = warps * 32, number = (int)threadIdx.x / threads;
+  const int groups = blockDim.x / threads;
+  const Part part(p.width, threads, (int)threadIdx.x % threads);
+  RowGroup<true> group(&shared[number], warps, number);
+  const int each = Part::slot_bytes(p.width), all_of = p.ds ? 3 * each : 2 * each;
+  uint8_t* ring = slots + number * stages * all_of;
   const float per = 1.0f / (float)p.width;
-  float dw[NV][8] = {}, db[NV][8] = {};
-  for (long long row = (long long)blockIdx.x * here + mine; row < p.rows; row += (long long)gridDim.x * here) {
-    const char* x = p.x + row * p.x_stride * kBytes;
-    const char* dy = p.dy + row * p.dy_stride * kBytes;
-    float h[NV][8], g[NV][8];
-    if constexpr (VEC) {
-      Raw8<TY> a[NV] = {}, b[NV] = {};
+  const long long first = (long long)blockIdx.x * groups + number, step = (long long)gridDim.x * groups;
+  const auto fetch = [&](long long row, int stage) {
+    if (row < p.rows) {
+      uint8_t* to = ring + stage * all_of;
+      part.fetch(to, p.x + row * p.x_stride * kBytes);
+      part.fetch(to + each, p.dy + row * p.dy_stride * kBytes);
+      if (p.ds) part.fetch(to + 2 * each, p.ds + row * p.ds_stride * kBytes);
+    }
+    fetched();
+  };
+  for (int i = 0; i + 1 < stages; ++i) fetch(first + i * step, i);
+  typename Part::Row dw, db, w;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int col = (v * threads + t) * 8;
-        if (col < p.width) {
-          a[v] = load_raw8<TY>(x + (size_t)col * kBytes);
-          b[v] = load_raw8<TY>(dy + (size_t)col * kBytes);
-        }
-      }
+  for (int i = 0; i < Part::kPairs; ++i) {
+    dw[i] = db[i] = make_float2(0.0f, 0.0f);
+    w[i] = make_float2(1.0f, 1.0f);
+  }
+  if (p.w) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        raw8_to_floats<TY>(a[v], h[v]);
-        raw8_to_floats<TY>(b[v], g[v]);
-      }
+    for (int q = 0; q < Part::kPieces; q += Part::kStep) part.read_parameters(p.w, p.w_type, p.w_vec, q, &w[q / Part::kStep * Part::kStepPairs]);
+  }
+  int stage = 0;
+  for (long long row = first; row < p.rows; row += step) {
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    wait_fetched(stages - 2);
+    if constexpr (!VEC) group.sync();                      // (what others have copied; what the row before has left)
+    fetch(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+    const uint8_t* from = ring + stage * all_of;
+    const float2 less = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
+    typename Part::Row h, g;
+    part.read_slot(from, p.x + row * p.x_stride * kBytes, h);
+    part.read_slot(from + each, p.dy + row * p.dy_stride * kBytes, g);
+    float2 along2 = make_float2(0.0f, 0.0f), all2 = along2;
+#pragma unroll
+    for (int i = 0; i < Part::kPairs; ++i) {               // (beyond the row g is zero)
+      h[i] = mul2_rn(add2_rn(h[i], less), times);
+      dw[i] = fma2_rn(g[i], h[i], dw[i]);
+      db[i] = add2_rn(db[i], g[i]);
+      g[i] = mul2_rn(g[i], w[i]);
+      along2 = fma2_rn(g[i], h[i], along2);
+      all2 = add2_rn(all2, g[i]);
+    }
+    float along = along2.x + along2.y, all = all2.x + all2.y;
+    group.add2(along, all);
+    along *= -per;
+    all *= -per;
+    typename Part::Row s;
+    if (p.ds) {
+      part.read_slot(from + 2 * each, p.ds + row * p.ds_stride * kBytes, s);
     } else {
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int col = (v * 8 + k) * threads + t;
-          const bool in = col < p.width;
-          h[v][k] = in ? load_one<TY>(x, col) : 0.0f;
-          g[v][k] = in ? load_one<TY>(dy, col) : 0.0f;
-        }
+      for (int i = 0; i < Part::kPairs; ++i) s[i] = make_float2(0.0f, 0.0f);
     }
-    const float mean = p.mean[row], rstd = p.rstd[row];
-    float along = 0.0f, all = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float w[8];
-      if constexpr (VEC) {
-        const int col = (v * threads + t) * 8;
-        if (p.w && col < p.width) load_eight_of(p.w, p.w_type, col, p.w_vec, w);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = VEC ? (v * threads + t) * 8 : (v * 8 + k) * threads + t;
-        if (col < p.width) {
-          h[v][k] = (h[v][k] - mean) * rstd;
-          dw[v][k] = fmaf(g[v][k], h[v][k], dw[v][k]);
-          db[v][k] += g[v][k];
-          if (p.w) g[v][k] *= VEC ? w[k] : load_one_of(p.w, p.w_type, col);
-          along = fmaf(g[v][k], h[v][k], along);
-          all += g[v][k];
-        }
-      }
-    }
-    group.add2(along, all);
-    along *= per;
-    all *= per;
-    char* dx = p.dx + row * p.dx_stride * kBytes;
-    const char* ds = p.ds ? p.ds + row * p.ds_stride * kBytes : nullptr;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if constexpr (VEC) {
-        const int col = (v * threads + t) * 8;
-        if (col < p.width) {
-          float s[8] = {};
-          if (ds) raw8_to_floats<TY>(load_raw8<TY>(ds + (size_t)col * kBytes), s);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s[k] = fmaf(rstd, (g[v][k] - all) - h[v][k] * along, s[k]);
-          store_raw8<TY>(dx + (size_t)col * kBytes, floats_to_raw8<TY>(s));
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int col = (v * 8 + k) * threads + t;
-          if (col < p.width) store_one<TY>(dx, col, fmaf(rstd, (g[v][k] - all) - h[v][k] * along, ds ? load_one<TY>(ds, col) : 0.0f));
-        }
-      }
-    }
+    for (int i = 0; i < Part::kPairs; ++i)
+      s[i] = fma2_rn(times, fma2_rn(h[i], make_float2(along, along), add2_rn(g[i], make_float2(all, all))), s[i]);
+    part.store(p.dx + row * p.dx_stride * kBytes, s);
+    stage = stage + 1 == stages ? 0 : stage + 1;
   }
   if (!p.partial) return;
-  float* part = p.partial + (size_t)blockIdx.x * 2 * p.width;
-  if constexpr (CTA) {
+  float* sums = p.partial + (size_t)blockIdx.x * 2 * p.width;
+  float* to = groups == 1 ? sums : reinterpret_cast<float*>(slots) + (size_t)number * 2 * p.width;
+  if (groups > 1) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+  }
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int col = VEC ? (v * threads + t) * 8 + k : (v * 8 + k) * threads + t;
-        if (col < p.width) {
-          part[col] = dw[v][k];
-          part[p.width + col] = db[v][k];
-        }
-      }
-  } else {
-    for (int turn = 0; turn < here; ++turn) {
-      if (mine == turn) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int col = VEC ? (v * threads + t) * 8 + k : (v * 8 + k) * threads + t;
-            if (col < p.width) {
-              columns[col] = turn ? columns[col] + dw[v][k] : dw[v][k];
-              columns[p.width + col] = turn ? columns[p.width + col] + db[v][k] : db[v][k];
-            }
-          }
-      }
-      __syncthreads();
+  for (int e = 0; e < 8; ++e) {
+    if (part.has(Part::piece_of(e))) {
+      const int col = part.column(Part::piece_of(e)) + e % Part::kPiece;
+      to[col] = e % 2 ? dw[e / 2].y : dw[e / 2].x;
+      to[p.width + col] = e % 2 ? db[e / 2].y : db[e / 2].x;
     }
-    for (int i = threadIdx.x; i < 2 * p.width; i += kGradThreads) part[i] = columns[i];
+  }
+  if (groups > 1) {
+    __syncthreads();
+    const float* each_of = reinterpret_cast<const float*>(slots);
+    for (int i = threadIdx.x; i < 2 * p.width; i += blockDim.x) {
+      float s = each_of[i];
+      for (int n = 1; n < groups; ++n) s += each_of[n * 2 * p.width + i];
+      sums[i] = s;
+    }
   }
 }
 
 // Rows too wide for registers: the rows' gradient by reading twice, the columns' sums by another pass.
 template <int TY>
 __global__ void __launch_bounds__(kWideThreads) wide_row_grad_kernel(const __grid_constant__ GradParams p) {
-  __shared__ RowShared shared;
+  __shared__ GroupShared shared;
   wait_for_previous_launch();
   constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
-  RowGroup<true> group(&shared);
+  RowGroup<true> group(&shared, kWideThreads / 32, 0);
   const long long row = blockIdx.x;
   const char* x = p.x + row * p.x_stride * kBytes;
   const char* dy = p.dy + row * p.dy_stride * kBytes;
@@ -493,7 +471,7 @@ __global__ void __launch_bounds__(256) wide_column_grad_kernel(const __grid_cons
 }
 
 // The CTAs' sums joined, in an order that the sizes fix: 32 columns to a CTA, the partial sums dealt out to its warps.
-constexpr int kJoinWarps = 16;
+constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float* partial, int parts, int width, void* dw, void* db, int type,
                                                                    int accumulate) {
   __shared__ float sum[kJoinWarps][2][32];
@@ -521,32 +499,38 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float*
   store_one_of(to, type, col, accumulate ? load_one_of(to, type, col) + s : s);
 }
 
-int grad_threads(int width) { return width <= kWarpRowWidth ? kGradThreads : (width + 511) / 512 * 32; }
-
-// CTAs of the gradient, and so partial sums: as many as find room on the device's SMs, at most one to a row (four rows).
-constexpr int kGradSms = 148;
+// CTAs of the gradient, and so partial sums: as many as are on the device's SMs at a time, at most one to the rows of its groups.
+struct GradShape {
+  int warps, groups, threads, most, per_sm;                // most: threads of an SM that there are registers for
+};
+GradShape grad_shape(int width) {
+  GradShape g;
+  g.warps = (width + 255) / 256;
+  g.groups = std::max(1, kGradWarps / g.warps);
+  g.threads = g.warps * g.groups * 32;
+  g.most = g.warps <= kGradWarps ? 2 * kGradWarps * 32 : 1024;
+  g.per_sm = g.most / g.threads;
+  return g;
+}
 int grad_parts(long long rows, int width) {
-  if (width > kGradBlockWidth) return (int)std::min<long long>(rows, std::max(1, 4 * kGradSms * 256 / width));
-  const long long units = width <= kWarpRowWidth ? (rows + 3) / 4 : rows;
-  const int resident = std::max(1, 512 / grad_threads(width));
-  return (int)std::min<long long>(units, std::min(kMaxPartials, resident * kGradSms));
+  if (width > kGradGroupWidth) return (int)std::min<long long>(rows, std::max(1, 4 * kSms * 256 / width));
+  const GradShape g = grad_shape(width);
+  return (int)std::min<long long>((rows + g.groups - 1) / g.groups, g.per_sm * kSms);
 }
 
-template <int TY, int NV, bool CTA>
-bool launch_grad(const GradParams& p, int parts, bool vec, cudaStream_t st) {
-  const size_t smem = CTA || !p.partial ? 0 : (size_t)2 * p.width * sizeof(float);
-  const int threads = grad_threads(p.width);
-  return vec ? launch(row_grad_kernel<TY, NV, true, CTA>, parts, threads, smem, 0, st, p)
-             : launch(row_grad_kernel<TY, NV, false, CTA>, parts, threads, smem, 0, st, p);
+template <int TY, bool VEC>
+bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
+  const GradShape g = grad_shape(p.width);
+  const int bytes = RowPart<TY, 1, VEC>::slot_bytes(p.width) * (p.ds ? 3 : 2) * g.groups;
+  const Residents r = residents(g.threads, g.most, bytes);       // (at least two stages: 3 x 32 KB at the most)
+  const size_t smem = std::max((size_t)r.stages * bytes, g.groups == 1 ? 0 : (size_t)g.groups * 2 * p.width * sizeof(float));
+  const auto kernel = g.warps <= kGradWarps ? row_grad_kernel<TY, VEC, kGradWarps * 32> : row_grad_kernel<TY, VEC, 1024>;
+  return allow_ring(kernel, smem) && launch(kernel, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
 }
 
 template <int TY>
 bool enqueue_grad_of(const GradParams& p, int parts, bool vec, cudaStream_t st) {
-  if (p.width <= 256) return launch_grad<TY, 1, false>(p, parts, vec, st);
-  if (p.width <= 512) return launch_grad<TY, 2, false>(p, parts, vec, st);
-  if (p.width <= 768) return launch_grad<TY, 3, false>(p, parts, vec, st);
-  if (p.width <= kWarpRowWidth) return launch_grad<TY, 4, false>(p, parts, vec, st);
-  if (p.width <= kGradBlockWidth) return launch_grad<TY, 2, true>(p, parts, vec, st);
+  if (p.width <= kGradGroupWidth) return vec ? launch_grad<TY, true>(p, parts, st) : launch_grad<TY, false>(p, parts, st);
   if (!launch(wide_row_grad_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p)) return false;
   return !p.partial || launch(wide_column_grad_kernel<TY>, (long long)(p.width + 255) / 256 * parts, 256, 0, 0, st, p, parts);
 }
@@ -662,7 +646,7 @@ __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_
 
 int column_chunks(long long rows, long long width) {
   const long long strips = (width + 255) / 256;
-  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 32, 4 * kGradSms / strips}));
+  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 32, 4 * kSms / strips}));
 }
 
 template <int TY, bool VEC>
@@ -721,6 +705,7 @@ constexpr int64_t kMostRows = (int64_t)1 << 31, kMostWidth = (int64_t)1 << 24;
 
 bool bad_rows(int64_t rows, int64_t width) { return rows < 0 || rows >= kMostRows || width < 1 || width > kMostWidth; }
 bool bad_stride(int64_t stride, int64_t width) { return stride < width || stride > (int64_t)1 << 40; }
+bool whole(int64_t width, int type) { return width * type_bytes(type) % 16 == 0; }               // pieces of 16 bytes
 bool on16(const void* p, int64_t stride, int type) { return is_aligned(p, 16) && stride * type_bytes(type) % 16 == 0; }
 
 }  // namespace
@@ -754,7 +739,7 @@ int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* 
   p.mean = mean; p.rstd = rstd;
   p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride; p.scale = scale; p.sums = sums;
   p.rows = rows; p.width = (int)width; p.normed = 1; p.eps = eps;
-  const bool vec = width % 8 == 0 && on16(x, x_stride, type) && (!residual || (on16(residual, residual_stride, type) && on16(sum, sum_stride, type))) &&
+  const bool vec = whole(width, type) && on16(x, x_stride, type) && (!residual || (on16(residual, residual_stride, type) && on16(sum, sum_stride, type))) &&
                    (!out || on16(out, out_stride, type));
   return enqueue_rows(p, type, vec, static_cast<cudaStream_t>(stream));
 }
@@ -773,7 +758,7 @@ int qadam_quantize_rows(const void* x, int32_t type, int64_t x_stride, const flo
   p.w = columns; p.w_type = QADAM_F32; p.w_vec = is_aligned(columns, 16);
   p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride; p.scale = scale; p.sums = sums;
   p.rows = rows; p.width = (int)width;
-  return enqueue_rows(p, type, width % 8 == 0 && on16(x, x_stride, type), static_cast<cudaStream_t>(stream));
+  return enqueue_rows(p, type, whole(width, type) && on16(x, x_stride, type), static_cast<cudaStream_t>(stream));
 }
 
 int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes) {
@@ -811,7 +796,7 @@ int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const
     p.w = weight; p.w_type = weight_type; p.w_vec = is_aligned(weight, 16);
     p.partial = sums ? static_cast<float*>(workspace) : nullptr;
     p.rows = rows; p.width = (int)width;
-    const bool vec = width % 8 == 0 && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&
+    const bool vec = whole(width, type) && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&
                      (!dsum || on16(dsum, dsum_stride, type));
     const bool ok = type == QADAM_F32 ? enqueue_grad_of<QADAM_F32>(p, parts, vec, st)
                     : type == QADAM_BF16 ? enqueue_grad_of<QADAM_BF16>(p, parts, vec, st) : enqueue_grad_of<QADAM_F16>(p, parts, vec, st);

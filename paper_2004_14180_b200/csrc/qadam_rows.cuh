@@ -120,68 +120,231 @@ __device__ __forceinline__ float warp_add(float v) {
   return v;
 }
 
-// Reductions over the threads of a row: a warp, or (CTA) a whole block of whole warps.  A block's reductions take turns with
-// two buffers, so one barrier each is enough: a buffer is written again only behind the barrier of the reduction between.
-struct RowShared {
+// Reductions over the threads that share a row: a warp, or (MANY) up to 32 warps of a CTA, that have a barrier of their own.  Reductions
+// take turns with two buffers, so one barrier each is enough: a buffer is written again only behind the barrier of the reduction
+// between.
+struct GroupShared {
   float f[2][32][2];
-  uint32_t u[2][32];
 };
 
-template <bool CTA>
+template <bool MANY>
 class RowGroup {
  public:
-  __device__ explicit RowGroup(RowShared* s) : s_(s) {}
+  // warps: of the group; number: of the group in its CTA, which is its barrier's too (from 1 on)
+  __device__ RowGroup(GroupShared* s, int warps, int number) : s_(s), warps_(warps), barrier_(number + 1) {}
 
+  __device__ __forceinline__ void sync() {
+    if constexpr (MANY) asm volatile("bar.sync %0, %1;" ::"r"(barrier_), "r"(warps_ * 32) : "memory");
+    else __syncwarp();
+  }
   __device__ __forceinline__ float add(float v) {
     v = warp_add(v);
-    if constexpr (CTA) {
-      if (threadIdx.x % 32 == 0) s_->f[turn_][threadIdx.x / 32][0] = v;
-      __syncthreads();
-      v = warp_add(lane_in_use() ? s_->f[turn_][threadIdx.x % 32][0] : 0.0f);
+    if constexpr (MANY) {
+      put(v, 0);
+      sync();
+      v = warp_add(got(0));
       turn_ ^= 1;
     }
     return v;
   }
+  // Two sums at the price of one: the warp's lower half adds up a, its upper half b.
   __device__ __forceinline__ void add2(float& a, float& b) {
-    a = warp_add(a);
-    b = warp_add(b);
-    if constexpr (CTA) {
-      if (threadIdx.x % 32 == 0) {
-        s_->f[turn_][threadIdx.x / 32][0] = a;
-        s_->f[turn_][threadIdx.x / 32][1] = b;
-      }
-      __syncthreads();
-      a = warp_add(lane_in_use() ? s_->f[turn_][threadIdx.x % 32][0] : 0.0f);
-      b = warp_add(lane_in_use() ? s_->f[turn_][threadIdx.x % 32][1] : 0.0f);
+    const bool upper = threadIdx.x % 32 >= 16;
+    float mine = upper ? b : a;
+    mine += __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+    mine = half_add(mine);
+    if constexpr (MANY) {
+      const int lane = threadIdx.x % 16;
+      if (lane == 0) s_->f[turn_][warp()][upper] = mine;
+      sync();
+      mine = lane < warps_ ? s_->f[turn_][lane][upper] : 0.0f;
+      if (warps_ > 16) mine += lane + 16 < warps_ ? s_->f[turn_][lane + 16][upper] : 0.0f;
+      mine = half_add(mine);
       turn_ ^= 1;
     }
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, mine, 16);
+    a = upper ? other : mine;
+    b = upper ? mine : other;
   }
   __device__ __forceinline__ uint32_t max(uint32_t v) {
     v = __reduce_max_sync(0xFFFFFFFFu, v);
-    if constexpr (CTA) {
-      if (threadIdx.x % 32 == 0) s_->u[turn_][threadIdx.x / 32] = v;
-      __syncthreads();
-      v = __reduce_max_sync(0xFFFFFFFFu, lane_in_use() ? s_->u[turn_][threadIdx.x % 32] : 0u);
+    if constexpr (MANY) {
+      put(__uint_as_float(v), 0);
+      sync();
+      v = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(got(0)));
       turn_ ^= 1;
     }
     return v;
   }
   __device__ __forceinline__ int add(int v) {
     v = __reduce_add_sync(0xFFFFFFFFu, v);
-    if constexpr (CTA) {
-      if (threadIdx.x % 32 == 0) s_->u[turn_][threadIdx.x / 32] = (uint32_t)v;
-      __syncthreads();
-      v = __reduce_add_sync(0xFFFFFFFFu, lane_in_use() ? (int)s_->u[turn_][threadIdx.x % 32] : 0);
+    if constexpr (MANY) {
+      put(__int_as_float(v), 0);
+      sync();
+      v = __reduce_add_sync(0xFFFFFFFFu, __float_as_int(got(0)));
       turn_ ^= 1;
     }
     return v;
   }
 
  private:
-  __device__ __forceinline__ bool lane_in_use() const { return threadIdx.x % 32 < blockDim.x / 32; }
-  RowShared* s_;
-  int turn_ = 0;
+  __device__ static __forceinline__ float half_add(float v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+  }
+  __device__ __forceinline__ int warp() const { return (int)(threadIdx.x / 32) % warps_; }
+  __device__ __forceinline__ void put(float v, int i) {
+    if (threadIdx.x % 32 == 0) s_->f[turn_][warp()][i] = v;
+  }
+  __device__ __forceinline__ float got(int i) const { return (int)(threadIdx.x % 32) < warps_ ? s_->f[turn_][threadIdx.x % 32][i] : 0.0f; }
+  GroupShared* s_;
+  int warps_, barrier_, turn_ = 0;
 };
+
+// How a row's elements are dealt out, 8 NV to each of a group's threads, in pairs.  VEC: in pieces of 16 bytes; else one by one, a
+// group's width apart.  An element beyond the row reads as zero.
+template <int TY, int NV, bool VEC>
+struct RowPart {
+  static constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
+  static constexpr int kPiece = VEC ? 16 / kBytes : 1;     // consecutive elements
+  static constexpr int kPieces = 8 * NV / kPiece;
+  static constexpr int kPairs = 4 * NV;
+  using Row = float2[kPairs];
+
+  int width, threads, t;
+  unsigned live;                                           // bits of the pieces that are in the row
+  __device__ __forceinline__ RowPart(int w, int n, int i) : width(w), threads(n), t(i), live(0u) {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) live |= (unsigned)(column(q) < w) << q;
+  }
+  __device__ __forceinline__ int column(int q) const { return (q * threads + t) * kPiece; }           // a piece's first
+  __device__ __forceinline__ bool has(int q) const { return live >> q & 1u; }
+  __device__ __forceinline__ static constexpr int piece_of(int e) { return e / kPiece; }
+
+  // from global or shared memory
+  __device__ __forceinline__ void read(const void* row, Row& x) const {
+    if constexpr (VEC) {
+      uint4 r[kPieces];
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) r[q] = has(q) ? static_cast<const uint4*>(row)[q * threads + t] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) unpack(r[q], &x[q * kPiece / 2]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        x[i].x = has(2 * i) ? load_one<TY>(row, column(2 * i)) : 0.0f;
+        x[i].y = has(2 * i + 1) ? load_one<TY>(row, column(2 * i + 1)) : 0.0f;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(void* row, const Row& x) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        if (has(q)) static_cast<uint4*>(row)[q * threads + t] = packed(&x[q * kPiece / 2]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        if (has(2 * i)) store_one<TY>(row, column(2 * i), x[i].x);
+        if (has(2 * i + 1)) store_one<TY>(row, column(2 * i + 1), x[i].y);
+      }
+    }
+  }
+  // x becomes what is stored.
+  __device__ __forceinline__ void store_rounded(void* row, Row& x) const {
+    store(row, x);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) x[i] = make_float2(rounded<TY>(x[i].x), rounded<TY>(x[i].y));
+  }
+  // Parameters of any type; on16: they begin on 16 bytes.
+  __device__ __forceinline__ void read_parameters(const void* p, int type, bool on16, int q, float2* x) const {
+    if constexpr (VEC) {
+      if (!has(q)) return;
+      const int col = column(q);
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 4) {
+        float y[4];
+        if (!on16) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = load_one_of(p, type, col + k + i);
+        } else if (type == QADAM_F32) {
+          const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + col + k);
+          y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const unsigned short*>(p) + col + k);
+          to_floats(Raw4{{v.x, v.y, 0u, 0u}}, type, y);
+        }
+        x[k / 2] = make_float2(y[0], y[1]);
+        x[k / 2 + 1] = make_float2(y[2], y[3]);
+      }
+    } else {                                               // two pieces: a pair
+      if (has(q)) x[0].x = load_one_of(p, type, column(q));
+      if (has(q + 1)) x[0].y = load_one_of(p, type, column(q + 1));
+    }
+  }
+  static constexpr int kStep = VEC ? 1 : 2;                // pieces that hold whole pairs
+  static constexpr int kStepPairs = VEC ? kPiece / 2 : 1;
+
+  // ---- a row in shared memory: its bytes, as far from 16 as in memory
+  __host__ __device__ static constexpr int slot_bytes(int width) { return (width * kBytes + 15) / 16 * 16 + (VEC ? 0 : 16); }
+
+  // Copies a row behind the threads' backs: what is whole pieces of 16 bytes in memory asynchronously, what is left at its ends
+  // by the first threads' own hands.  VEC: a thread copies what it will read.
+  __device__ __forceinline__ void fetch(uint8_t* slot, const char* row) const {
+    const unsigned at = (unsigned)__cvta_generic_to_shared(slot);
+    if constexpr (VEC) {
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) {
+        const unsigned piece = (unsigned)(q * threads + t) * 16u;
+        if (has(q)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + piece), "l"(row + piece) : "memory");
+      }
+    } else {
+      const int bytes = width * kBytes, phase = (int)(reinterpret_cast<uintptr_t>(row) & 15u);
+      const int head = min((16 - phase) & 15, bytes), body = (bytes - head) >> 4, tail = bytes - head - body * 16;
+      for (int i = t; i < body; i += threads)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (unsigned)(phase + head + i * 16)), "l"(row + head + i * 16) : "memory");
+      if (t < (head + tail) / kBytes) {
+        const int i = t < head / kBytes ? t : t + body * (16 / kBytes);
+        if constexpr (TY == QADAM_F32) *reinterpret_cast<uint32_t*>(slot + phase + i * 4) = reinterpret_cast<const uint32_t*>(row)[i];
+        else *reinterpret_cast<unsigned short*>(slot + phase + i * 2) = reinterpret_cast<const unsigned short*>(row)[i];
+      }
+    }
+  }
+  __device__ __forceinline__ void read_slot(const uint8_t* slot, const char* row, Row& x) const {
+    read(VEC ? slot : slot + (reinterpret_cast<uintptr_t>(row) & 15u), x);
+  }
+
+ private:
+  __device__ static __forceinline__ void unpack(const uint4& r, float2* x) {
+    if constexpr (TY == QADAM_F32) {
+      x[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y));
+      x[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
+    } else {
+      const Raw8<TY> h = {{r.x, r.y, r.z, r.w}};
+      float y[8];
+      raw8_to_floats<TY>(h, y);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = make_float2(y[2 * k], y[2 * k + 1]);
+    }
+  }
+  __device__ static __forceinline__ uint4 packed(const float2* x) {
+    if constexpr (TY == QADAM_F32) {
+      return make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
+    } else {
+      const float y[8] = {x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
+      const Raw8<TY> h = floats_to_raw8<TY>(y);
+      return make_uint4(h.w[0], h.w[1], h.w[2], h.w[3]);
+    }
+  }
+};
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the youngest `left` fetches (0 .. 2) are there.
+__device__ __forceinline__ void wait_fetched(int left) {
+  if (left == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
 
 // Rows in 8 bits: a = max(largest |x|, 2^-100), q = rne(x fl(127 / a)), worth a / 127.  `largest`: the bits of the largest
 // |x|, which a NaN exceeds.  A row with a value that is not finite is worth NaN.
@@ -192,6 +355,20 @@ __device__ __forceinline__ ByteScale byte_scale(uint32_t largest) {
   if (largest >= 0x7F800000u) return {0.0f, __uint_as_float(0x7FC00000u)};
   const float a = fmaxf(__uint_as_float(largest), 7.888609052210118e-31f);
   return {__fdiv_rn(127.0f, a), __fdiv_rn(a, 127.0f)};
+}
+// The largest magnitude of three, NaN if one is.
+__device__ __forceinline__ float largest_of(float m, float a, float b) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(a), "f"(b));
+  return r;
+}
+// Four quotients as bytes: 1.5 x 2^23 added to a product of at most 2^22 leaves it rounded, ties to even, in the last bits.
+// (The products one by one: a packed product and a packed sum were compiled into one operation with one rounding.)
+__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b, float per) {
+  const float2 magic = make_float2(12582912.0f, 12582912.0f);
+  a = add2_rn(make_float2(__fmul_rn(a.x, per), __fmul_rn(a.y, per)), magic);
+  b = add2_rn(make_float2(__fmul_rn(b.x, per), __fmul_rn(b.y, per)), magic);
+  return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
 }
 __device__ __forceinline__ int to_byte(float x, float per) { return __float2int_rn(__fmul_rn(x, per)); }      // (a NaN gives 0)
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
