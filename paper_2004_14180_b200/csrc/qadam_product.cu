@@ -61,10 +61,10 @@ __device__ __forceinline__ bool barrier_try(uint64_t* bar, unsigned parity) {
   unsigned ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
-      : "r"(shared_at(bar)), "r"(parity), "r"(1000u)
+      : "r"(shared_at(bar)), "r"(parity)
       : "memory");
   return ok != 0;
 }
@@ -115,6 +115,37 @@ __device__ __forceinline__ void read_columns(unsigned from, uint32_t (&v)[16]) {
       : "memory");
 }
 
+// One lane of a warp whose lanes are all here.  What that lane alone issues stands in code that the warp runs as one, with values that
+// are the same in all lanes: in a branch that lane 0 takes, a product cost 68 cycles to issue and a block of the sum 350 more.
+__device__ __forceinline__ bool elected() {
+  unsigned p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xFFFFFFFF;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int warp_of_thread() { return __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x / 32), 0); }
+
+// The stages of a ring, one after the other, and the phase of their barriers.
+struct RingPlace {
+  int stage = 0;
+  unsigned phase = 0;
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1u;
+    }
+  }
+  __device__ __forceinline__ void back(int stages) {
+    if (--stage < 0) {
+      stage = stages - 1;
+      phase ^= 1u;
+    }
+  }
+};
+
 struct ProductShared {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
   unsigned result;                         // in tensor memory
@@ -149,7 +180,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   extern __shared__ uint8_t raw[];
   __shared__ ProductShared s;
   uint8_t* ring = raw + (1024u - (shared_at(raw) & 1023u)) % 1024u;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_of_thread(), lane = threadIdx.x % 32;
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const unsigned b_bytes = kChannels * kDepth, a_bytes = (unsigned)p.tokens * kDepth, stage_bytes = a_bytes + b_bytes;
@@ -178,36 +209,40 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   const unsigned result = s.result;
   wait_for_previous_launch();
 
+  RingPlace at;
   int loaded = 0;                          // stages' fills asked for (warp 0)
-  if (warp == 0 && lane == 0) {
-    for (int i = from; i < to; ++i, ++loaded) {
-      const int st = loaded % p.stages;
-      if (!barrier_wait(&s.empty[st], (unsigned)(loaded / p.stages & 1) ^ 1u, &s.gave_up)) break;
-      uint8_t* b = ring + st * stage_bytes;
-      barrier_expect(&s.full[st], stage_bytes);
-      if (p.transposed) load_tile(b, &b_map, (int)channel, i * kDepth, &s.full[st]);
-      else load_tile(b, &b_map, i * kDepth, (int)channel, &s.full[st]);
-      load_tile(b + b_bytes, &a_map, i * kDepth, (int)row, &s.full[st]);
+  if (warp == 0) {
+    for (int i = from; i < to; ++i, ++loaded, at.next(p.stages)) {
+      if (!barrier_wait(&s.empty[at.stage], at.phase ^ 1u, &s.gave_up)) break;
+      if (elected()) {
+        uint8_t* b = ring + at.stage * stage_bytes;
+        barrier_expect(&s.full[at.stage], stage_bytes);
+        if (p.transposed) load_tile(b, &b_map, (int)channel, i * kDepth, &s.full[at.stage]);
+        else load_tile(b, &b_map, i * kDepth, (int)channel, &s.full[at.stage]);
+        load_tile(b + b_bytes, &a_map, i * kDepth, (int)row, &s.full[at.stage]);
+      }
+      __syncwarp();
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     // result 32 bits signed; first operand by its type; second signed; sizes in eights and sixteens
     const unsigned kind = 2u << 4 | (unsigned)p.b_signed << 7 | 1u << 10 | (unsigned)p.transposed << 15 | (unsigned)(p.tokens / 8) << 17 |
                           (unsigned)(kChannels / 16) << 24;
     const unsigned step = p.transposed ? 32 * 128 / 16 : 32 / 16;
-    int n = 0;
-    for (int i = from; i < to; ++i, ++n) {
-      const int st = n % p.stages;
-      if (!barrier_wait(&s.full[st], (unsigned)(n / p.stages & 1), &s.gave_up)) break;
+    for (int i = from; i < to; ++i, at.next(p.stages)) {
+      if (!barrier_wait(&s.full[at.stage], at.phase, &s.gave_up)) break;
       after_sync();
-      const unsigned b = shared_at(ring + st * stage_bytes);
+      const unsigned b = shared_at(ring) + (unsigned)at.stage * stage_bytes;
       const uint64_t wd = operand(b), td = operand(b + b_bytes);
+      if (elected()) {
 #pragma unroll
-      for (int k = 0; k < kDepth / 32; ++k) multiply(result, wd + (uint64_t)(k * step), td + (uint64_t)(k * 2), kind, n > 0 || k > 0);
-      commit(&s.empty[st]);
+        for (int k = 0; k < kDepth / 32; ++k) multiply(result, wd + (uint64_t)(k * step), td + (uint64_t)(k * 2), kind, i > from || k > 0);
+        commit(&s.empty[at.stage]);
+      }
+      __syncwarp();
     }
-    commit(&s.done);
+    if (elected()) commit(&s.done);
+    __syncwarp();
   }
-  __syncwarp();
   const bool ok = barrier_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0;
   after_sync();
   const long long left = p.rows - row;
@@ -255,8 +290,10 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   }
   if (s.gave_up && warp == 0 && lane == 0) {
     // what was asked for has to land before this CTA's memory is anyone else's
-    for (int i = loaded > p.stages ? loaded - p.stages : 0; i < loaded; ++i)
-      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[i % p.stages], (unsigned)(i / p.stages & 1)); ++n) {}
+    for (int i = 0; i < loaded && i < p.stages; ++i) {
+      at.back(p.stages);
+      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[at.stage], at.phase); ++n) {}
+    }
     if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
   }
   before_sync();
@@ -370,7 +407,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   extern __shared__ uint8_t raw[];
   __shared__ PairShared s;
   uint8_t* ring = raw + (1024u - (shared_at(raw) & 1023u)) % 1024u;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_of_thread(), lane = threadIdx.x % 32;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
   const long long tiles = (long long)p.token_tiles * p.channel_tiles, step = gridDim.x / 2;
@@ -398,57 +435,62 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   wait_for_previous_launch();
 
   const unsigned b_bytes = p.transposed ? kOperandBytes : (unsigned)p.half * kDepth;
-  long long loaded = 0;
-  if (warp == 0 && lane == 0) {
+  RingPlace place;
+  int loaded = 0;                          // stages' fills asked for, up to all of them
+  if (warp == 0) {
     bool ok = true;
     for (long long t = blockIdx.x / 2; t < tiles && ok; t += step) {
       const PairTile tile = pair_tile(p, t);
       const int row = tile.token * kPairTokens + rank * 128, channel = tile.channel * 2 * p.half + rank * p.half;
-      for (int i = 0; i < p.blocks; ++i, ++loaded) {
-        const int st = (int)(loaded % kPairStages);
-        ok = barrier_wait(&s.empty[st], (unsigned)(loaded / kPairStages & 1) ^ 1u, &s.gave_up);
+      for (int i = 0; i < p.blocks; ++i, place.next(kPairStages)) {
+        ok = barrier_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up);
         if (!ok) break;
-        uint8_t* a = ring + st * kPairStageBytes;
-        const unsigned bar = of_first(shared_at(&s.full[st]));
-        if (rank == 0) barrier_expect(&s.full[st], 2 * (kOperandBytes + b_bytes));
-        pair_load(a, &a_map, i * kDepth, row, bar);
-        if (p.transposed) pair_load(a + kOperandBytes, &b_map, channel, i * kDepth, bar);
-        else pair_load(a + kOperandBytes, &b_map, i * kDepth, channel, bar);
+        if (elected()) {
+          uint8_t* a = ring + place.stage * kPairStageBytes;
+          const unsigned bar = of_first(shared_at(&s.full[place.stage]));
+          if (rank == 0) barrier_expect(&s.full[place.stage], 2 * (kOperandBytes + b_bytes));
+          pair_load(a, &a_map, i * kDepth, row, bar);
+          if (p.transposed) pair_load(a + kOperandBytes, &b_map, channel, i * kDepth, bar);
+          else pair_load(a + kOperandBytes, &b_map, i * kDepth, channel, bar);
+        }
+        __syncwarp();
+        loaded = min(loaded + 1, kPairStages);
       }
     }
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     // result 32 bits signed; first operand signed, second by its type; sizes in eights and sixteens
     const unsigned kind = 2u << 4 | 1u << 7 | (unsigned)p.b_signed << 10 | (unsigned)p.transposed << 16 | (unsigned)(2 * p.half / 8) << 17 |
                           (unsigned)(kPairTokens / 16) << 24;
     const unsigned b_step = p.transposed ? 32 * 128 / 16 : 32 / 16;
-    long long n = 0;
-    int turn = 0;
+    RingPlace turn;
     bool ok = true;
-    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step, ++turn) {
-      ok = barrier_wait(&s.result_empty[turn & 1], (unsigned)(turn / 2 & 1) ^ 1u, &s.gave_up);
+    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step, turn.next(2)) {
+      ok = barrier_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up);
       if (!ok) break;
       after_sync();
-      const unsigned at = result + (unsigned)(turn & 1) * 256u;
-      for (int i = 0; i < p.blocks; ++i, ++n) {
-        const int st = (int)(n % kPairStages);
-        ok = barrier_wait(&s.full[st], (unsigned)(n / kPairStages & 1), &s.gave_up);
+      const unsigned at = result + (unsigned)turn.stage * 256u;
+      for (int i = 0; i < p.blocks; ++i, place.next(kPairStages)) {
+        ok = barrier_wait(&s.full[place.stage], place.phase, &s.gave_up);
         if (!ok) break;
         after_sync();
-        const unsigned a = shared_at(ring + st * kPairStageBytes);
+        const unsigned a = shared_at(ring) + (unsigned)place.stage * kPairStageBytes;
         const uint64_t ad = operand(a), bd = operand(a + kOperandBytes);
+        if (elected()) {
 #pragma unroll
-        for (int k = 0; k < kDepth / 32; ++k) pair_multiply(at, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * b_step), kind, i > 0 || k > 0);
-        pair_commit(&s.empty[st]);
+          for (int k = 0; k < kDepth / 32; ++k) pair_multiply(at, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * b_step), kind, i > 0 || k > 0);
+          pair_commit(&s.empty[place.stage]);
+          if (i + 1 == p.blocks) pair_commit(&s.result_full[turn.stage]);
+        }
+        __syncwarp();
       }
-      if (ok) pair_commit(&s.result_full[turn & 1]);
     }
   } else if (warp >= 4) {
     const int end = warp - 4, quarter = warp % 4, side = end / 4;
     uint8_t* box = ring + kPairStages * kPairStageBytes + end * kBoxBytes;
     float2* about = reinterpret_cast<float2*>(ring + kPairStages * kPairStageBytes + kEndWarps * kBoxBytes) + end * kEndChannels;   // scale, bias
     constexpr int kBox = BOXES && OUT != QADAM_F32 ? 64 : 32;                // channels of a box
-    int turn = 0;
-    for (long long t = blockIdx.x / 2; t < tiles; t += step, ++turn) {
+    RingPlace turn;
+    for (long long t = blockIdx.x / 2; t < tiles; t += step, turn.next(2)) {
       const PairTile tile = pair_tile(p, t);
       const long long row0 = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32, row = row0 + lane;
       const long long channel0 = (long long)tile.channel * 2 * p.half;
@@ -467,9 +509,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
         about[i] = f;
       }
       __syncwarp();
-      if (!barrier_wait(&s.result_full[turn & 1], (unsigned)(turn / 2 & 1), &s.gave_up)) break;
+      if (!barrier_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up)) break;
       after_sync();
-      const unsigned at = result + (unsigned)(turn & 1) * 256u + (unsigned)(quarter * 32) * 65536u;
+      const unsigned at = result + (unsigned)turn.stage * 256u + (unsigned)(quarter * 32) * 65536u;
       for (int j = 0; (j * 2 + side) * kBox < wide; ++j) {
         const int c0 = (j * 2 + side) * kBox;
         if constexpr (BOXES) {
@@ -522,7 +564,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       }
       before_sync();
       __syncwarp();
-      if (lane == 0) arrive_at(of_first(shared_at(&s.result_empty[turn & 1])));
+      if (lane == 0) arrive_at(of_first(shared_at(&s.result_empty[turn.stage])));
     }
     if constexpr (BOXES) {
       if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -531,9 +573,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   __syncwarp();
   if (s.gave_up && warp == 0 && lane == 0) {
     // what was asked for has to land before these CTAs' memory is anyone else's
-    if (rank == 0)
-      for (long long i = loaded > kPairStages ? loaded - kPairStages : 0; i < loaded; ++i)
-        for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[i % kPairStages], (unsigned)(i / kPairStages & 1)); ++n) {}
+    for (int i = 0; rank == 0 && i < loaded; ++i) {
+      place.back(kPairStages);
+      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[place.stage], place.phase); ++n) {}
+    }
     if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
   }
   before_sync();
