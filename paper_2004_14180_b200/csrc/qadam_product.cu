@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kChannels = 128;             // of a tile: the rows of the tensor cores' result
 constexpr int kDepth = 128;                // bytes of a row in a stage
-constexpr int kMaxTokens = 256;            // of a tile: the columns of the result
+constexpr int kFewTokens = 32;             // of a tile at most: the columns of the result; more tokens take the kernel below
 constexpr int kProductThreads = 192;       // a warp that loads, one that multiplies, four for the end
 constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
@@ -152,26 +152,39 @@ struct ProductShared {
   int gave_up;
 };
 
-// What a thread knows of its channel.
-struct Channel {
-  long long at;
-  float worth, bias;
-  bool in;
+// The end of the sums of a channel and up to N tokens, `step` apart from t on, of which those below `live` are there.
+struct EndShared {
+  float scale[kFewTokens];
+  int less[kFewTokens];
 };
-__device__ __forceinline__ Channel channel_of(const ProductParams& p, long long at) {
-  Channel c;
-  c.at = at;
-  c.in = at < p.channels;
-  c.worth = c.in && p.b_scale ? p.b_scale[at] : p.worth;
-  c.bias = c.in && p.bias ? load_one_of(p.bias, p.bias_type, at) : 0.0f;
-  return c;
-}
-__device__ __forceinline__ void finish(const ProductParams& p, const Channel& c, long long row, uint32_t sum) {
-  if (p.a_sums) sum -= (uint32_t)p.zero * (uint32_t)p.a_sums[row];
-  float y = fmaf((float)(int)sum * p.a_scale[row], c.worth, c.bias);
-  const long long i = row * p.out_stride + c.at;
-  if (p.accumulate) y += load_one_of(p.out, p.out_type, i);
-  store_one_of(p.out, p.out_type, i, y);
+template <int N>
+__device__ __forceinline__ void finish(const ProductParams& p, const EndShared& e, float worth, float bias, long long row, long long channel, int t,
+                                       int step, int live, const uint32_t (&sum)[N]) {
+  float y[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int i = t + k * step < live ? t + k * step : t;
+    y[k] = fmaf((float)(int)(sum[k] - (uint32_t)e.less[i]) * e.scale[i], worth, bias);
+  }
+  const long long first = (row + t) * p.out_stride + channel, next = (long long)step * p.out_stride;
+  if (p.accumulate) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t + k * step < live) y[k] += load_one_of(p.out, p.out_type, first + k * next);
+  }
+  if (p.out_type == QADAM_F32) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t + k * step < live) store_one<QADAM_F32>(p.out, first + k * next, y[k]);
+  } else if (p.out_type == QADAM_BF16) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t + k * step < live) store_one<QADAM_BF16>(p.out, first + k * next, y[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t + k * step < live) store_one<QADAM_F16>(p.out, first + k * next, y[k]);
+  }
 }
 
 // One tile of kChannels x tokens to a cluster; its CTAs share the sum's blocks and add up in each other's shared memory.
@@ -179,6 +192,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
                                                                   const __grid_constant__ ProductParams p) {
   extern __shared__ uint8_t raw[];
   __shared__ ProductShared s;
+  __shared__ EndShared about;
   uint8_t* ring = raw + (1024u - (shared_at(raw) & 1023u)) % 1024u;
   const int warp = warp_of_thread(), lane = threadIdx.x % 32;
   cg::cluster_group cluster = cg::this_cluster();
@@ -197,8 +211,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     s.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  unsigned columns = 32;
-  while ((int)columns < p.tokens) columns *= 2;
+  constexpr unsigned columns = 32;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_at(&s.result)), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -243,46 +256,57 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     if (elected()) commit(&s.done);
     __syncwarp();
   }
-  const bool ok = barrier_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0;
-  after_sync();
   const long long left = p.rows - row;
   const int live = left < p.tokens ? (int)left : p.tokens;
+  const long long mine = channel + warp % 4 * 32 + lane;     // a warp can read the rows of the result that its number names
+  const bool in = warp >= 2 && mine < p.channels;
+  float worth = p.worth, bias = 0.0f;
+  if (warp >= 2) {                         // what the end needs is here when the sums are
+    for (int i = threadIdx.x - 64; i < live; i += 128) {
+      about.scale[i] = p.a_scale[row + i];
+      about.less[i] = p.a_sums ? p.zero * p.a_sums[row + i] : 0;
+    }
+    if (in && p.b_scale) worth = p.b_scale[mine];
+    if (in && p.bias) bias = load_one_of(p.bias, p.bias_type, mine);
+  }
+  __syncthreads();
+  const bool ok = barrier_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0;
+  after_sync();
+  const unsigned from_result = result + (unsigned)(warp % 4 * 32) * 65536u;
   if (split == 1) {
     if (warp >= 2 && ok) {
-      const int quarter = warp % 4;        // a warp can read the rows of the result that its number names
-      const Channel c = channel_of(p, channel + quarter * 32 + lane);
       for (int t = 0; t < live; t += 16) {
         uint32_t v[16];
-        read_columns(result + (unsigned)(quarter * 32) * 65536u + (unsigned)t, v);
-        if (c.in) {
-#pragma unroll
-          for (int k = 0; k < 16; ++k)
-            if (t + k < live) finish(p, c, row + t + k, v[k]);
-        }
+        read_columns(from_result + (unsigned)t, v);
+        if (in) finish(p, about, worth, bias, row, mine, t, 1, live, v);
       }
     }
   } else {
-    int* mine = reinterpret_cast<int*>(ring);          // [tokens][kChannels]; nothing is on its way into the ring any more
-    __syncthreads();
+    int* sums = reinterpret_cast<int*>(ring);              // [tokens][kChannels]; nothing is on its way into the ring any more
+    const int of_warp = warp % 4 * 32 + lane;
     if (warp >= 2 && ok) {
-      const int quarter = warp % 4;
       for (int t = 0; t < live; t += 16) {
         uint32_t v[16];
-        read_columns(result + (unsigned)(quarter * 32) * 65536u + (unsigned)t, v);
+        read_columns(from_result + (unsigned)t, v);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) mine[(t + k) * kChannels + quarter * 32 + lane] = (int)v[k];
+        for (int k = 0; k < 16; ++k) sums[(t + k) * kChannels + of_warp] = (int)v[k];
       }
     }
     cluster.sync();
     if (warp >= 2) {
-      const Channel c = channel_of(p, channel + warp % 4 * 32 + lane);
       bool all = true;
       for (int r = 0; r < split; ++r) all &= *cluster.map_shared_rank(&s.gave_up, r) == 0;
-      if (all && c.in) {
-        for (int t = rank; t < live; t += split) {
-          uint32_t sum = 0;
-          for (int r = 0; r < split; ++r) sum += (uint32_t)cluster.map_shared_rank(mine, r)[t * kChannels + warp % 4 * 32 + lane];
-          finish(p, c, row + t, sum);
+      if (all && in) {
+        for (int t = rank; t < live; t += 2 * split) {     // two tokens at a time
+          uint32_t v[2] = {0u, 0u};
+          const bool two = t + split < live;
+#pragma unroll 8
+          for (int r = 0; r < split; ++r) {
+            const int* of = cluster.map_shared_rank(sums, r) + of_warp;
+            v[0] += (uint32_t)of[t * kChannels];
+            if (two) v[1] += (uint32_t)of[(t + split) * kChannels];
+          }
+          finish(p, about, worth, bias, row, mine, t, split, live, v);
         }
       }
     }
@@ -309,13 +333,20 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
 // 32 bits times scales, rounded, through shared memory and out in boxes) runs beside the next one's products.
 constexpr int kPairThreads = 384;          // a warp that loads, one that multiplies, one for tensor memory, one idle, eight for the end
 constexpr int kPairTokens = 256;
-constexpr int kPairStages = 5;
+constexpr int kPairMaxStages = 5;
 constexpr int kOperandBytes = 128 * kDepth;
 constexpr int kPairStageBytes = 2 * kOperandBytes;
 constexpr int kEndWarps = 8;
 constexpr int kBoxBytes = 32 * 128;        // of 32 tokens, 128 bytes each
+constexpr int kUnit = 64;                  // channels that a warp takes at a time
 constexpr int kEndChannels = 128;          // of a tile, that a warp sees at most
-constexpr int kPairBytes = kPairStages * kPairStageBytes + kEndWarps * (kBoxBytes + kEndChannels * 8);
+// Shared memory: stages, boxes of results on their way out, what the end knows of its channels.  Five stages and one box a warp, or four and
+// two: for sums of 8192 (8192 x 8192 results of 16 bits) five stages take 337 us and four 357, for sums of 768 (8192 x 768) two boxes
+// take 9.9 us and one 10.7.  (Sixteen warps for the end in place of eight: no gain at 16 bits, 32 us against 25 for 8192 x 2304 fp32.)
+constexpr int pair_bytes(int stages, int boxes) { return stages * kPairStageBytes + kEndWarps * (boxes * kBoxBytes + kEndChannels * 8); }
+constexpr int kPairBytes = pair_bytes(4, 2);
+static_assert(kPairBytes >= pair_bytes(5, 1), "");
+constexpr int kLongSum = 16;               // blocks from which five stages are taken
 constexpr int kTokenGroup = 8;             // tiles of so many token blocks lie next to each other in time: what they read stays in L2
 
 struct PairParams {
@@ -334,11 +365,12 @@ struct PairParams {
   int half;                                // channels of a tile that a CTA's shared memory has the weights of: 32, 64, 96 or 128
   int token_tiles, channel_tiles;
   int transposed, b_signed;
+  int stages, boxes;
   unsigned* status;
 };
 
 struct PairShared {
-  uint64_t full[kPairStages], empty[kPairStages], result_full[2], result_empty[2];
+  uint64_t full[kPairMaxStages], empty[kPairMaxStages], result_full[2], result_empty[2];
   unsigned result;
   int gave_up;
 };
@@ -371,32 +403,35 @@ __device__ __forceinline__ void pair_commit(uint64_t* bar) {               // ar
 __device__ __forceinline__ void arrive_at(unsigned bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void read_columns32(unsigned from, uint32_t (&v)[32]) {
+__device__ __forceinline__ void read_unit(unsigned from, uint32_t (&v)[kUnit]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+      "%26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, "
+      "%50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
         "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
         "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
-        "=r"(v[31])
+        "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]),
+        "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]),
+        "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]),
+        "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
       : "r"(from)
       : "memory");
 }
 __device__ __forceinline__ void store_box(const CUtensorMap* map, const void* from, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(shared_at(from))
                : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 struct PairTile {
   int token, channel;                      // tiles
 };
-__device__ __forceinline__ PairTile pair_tile(const PairParams& p, long long t) {
-  const long long group = t / ((long long)kTokenGroup * p.channel_tiles);
-  const int first = (int)group * kTokenGroup, tall = min(kTokenGroup, p.token_tiles - first);
-  const long long in = t - group * kTokenGroup * p.channel_tiles;
-  return {first + (int)(in % tall), (int)(in / tall)};
+__device__ __forceinline__ PairTile pair_tile(const PairParams& p, int t) {
+  const int group = t / (kTokenGroup * p.channel_tiles);
+  const int first = group * kTokenGroup, tall = min(kTokenGroup, p.token_tiles - first);
+  const int in = t - first * p.channel_tiles;
+  return {first + in % tall, in / tall};
 }
 
 // OUT: type of the result.  BOXES: it is written in boxes; else (rows that do not begin on 16 bytes, or a result to be added
@@ -410,10 +445,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   const int warp = warp_of_thread(), lane = threadIdx.x % 32;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
-  const long long tiles = (long long)p.token_tiles * p.channel_tiles, step = gridDim.x / 2;
+  const int tiles = p.token_tiles * p.channel_tiles, step = gridDim.x / 2;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kPairStages; ++i) {
+    for (int i = 0; i < p.stages; ++i) {
       barrier_init(&s.full[i], 1);
       barrier_init(&s.empty[i], 1);
     }
@@ -439,10 +474,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   int loaded = 0;                          // stages' fills asked for, up to all of them
   if (warp == 0) {
     bool ok = true;
-    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step) {
+    for (int t = blockIdx.x / 2; t < tiles && ok; t += step) {
       const PairTile tile = pair_tile(p, t);
       const int row = tile.token * kPairTokens + rank * 128, channel = tile.channel * 2 * p.half + rank * p.half;
-      for (int i = 0; i < p.blocks; ++i, place.next(kPairStages)) {
+      for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
         ok = barrier_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up);
         if (!ok) break;
         if (elected()) {
@@ -454,7 +489,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
           else pair_load(a + kOperandBytes, &b_map, i * kDepth, channel, bar);
         }
         __syncwarp();
-        loaded = min(loaded + 1, kPairStages);
+        loaded = min(loaded + 1, p.stages);
       }
     }
   } else if (warp == 1 && rank == 0) {
@@ -464,12 +499,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
     const unsigned b_step = p.transposed ? 32 * 128 / 16 : 32 / 16;
     RingPlace turn;
     bool ok = true;
-    for (long long t = blockIdx.x / 2; t < tiles && ok; t += step, turn.next(2)) {
+    for (int t = blockIdx.x / 2; t < tiles && ok; t += step, turn.next(2)) {
       ok = barrier_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up);
       if (!ok) break;
       after_sync();
       const unsigned at = result + (unsigned)turn.stage * 256u;
-      for (int i = 0; i < p.blocks; ++i, place.next(kPairStages)) {
+      for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
         ok = barrier_wait(&s.full[place.stage], place.phase, &s.gave_up);
         if (!ok) break;
         after_sync();
@@ -486,80 +521,108 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
     }
   } else if (warp >= 4) {
     const int end = warp - 4, quarter = warp % 4, side = end / 4;
-    uint8_t* box = ring + kPairStages * kPairStageBytes + end * kBoxBytes;
-    float2* about = reinterpret_cast<float2*>(ring + kPairStages * kPairStageBytes + kEndWarps * kBoxBytes) + end * kEndChannels;   // scale, bias
-    constexpr int kBox = BOXES && OUT != QADAM_F32 ? 64 : 32;                // channels of a box
-    RingPlace turn;
-    for (long long t = blockIdx.x / 2; t < tiles; t += step, turn.next(2)) {
+    uint8_t* boxes = ring + p.stages * kPairStageBytes + end * p.boxes * kBoxBytes;
+    float2* about = reinterpret_cast<float2*>(ring + p.stages * kPairStageBytes + kEndWarps * p.boxes * kBoxBytes) + end * kEndChannels;   // scale, bias
+    constexpr bool kWide = BOXES && OUT != QADAM_F32;                        // a box has 64 channels of 16 bits, or 32 of 32 bits
+    // what the end of a tile needs to know is asked for while the tile before it is at its end
+    float2 channels[kEndChannels / 32];
+    float a_scale = 0.0f;
+    int less = 0;
+    const auto ask = [&](int t) {
+      if (t >= tiles) return;
       const PairTile tile = pair_tile(p, t);
-      const long long row0 = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32, row = row0 + lane;
+      const long long row = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32 + lane;
+      a_scale = row < p.rows ? p.a_scale[row] : 0.0f;
+      less = row < p.rows && p.a_sums ? p.a_sums[row] : 0;
+#pragma unroll
+      for (int i = 0; i < kEndChannels / 32; ++i) {                          // this warp's: every other unit of the tile
+        const int n = i * 32 + lane, c = (n / kUnit * 2 + side) * kUnit + n % kUnit;
+        const long long at = (long long)tile.channel * 2 * p.half + c;
+        channels[i] = make_float2(p.worth, 0.0f);
+        if (c < 2 * p.half && at < p.channels) {
+          if (p.b_scale) channels[i].x = p.b_scale[at];
+          if (p.bias) channels[i].y = load_one_of(p.bias, p.bias_type, at);
+        }
+      }
+    };
+    ask(blockIdx.x / 2);
+    RingPlace turn;
+    int flip = 0;
+    for (int t = blockIdx.x / 2; t < tiles; t += step, turn.next(2)) {
+      const PairTile tile = pair_tile(p, t);
+      const long long row0 = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32;
       const long long channel0 = (long long)tile.channel * 2 * p.half;
       const int wide = (int)min((long long)2 * p.half, p.channels - channel0);
-      const float a_scale = row < p.rows ? p.a_scale[row] : 0.0f;
-      const int less = row < p.rows && p.a_sums ? p.zero * p.a_sums[row] : 0;
       __syncwarp();
-      // this warp's channels: every other box of the tile
-      for (int i = lane; i < kEndChannels; i += 32) {
-        const int c = (i / kBox * 2 + side) * kBox + i % kBox;
-        float2 f = make_float2(p.worth, 0.0f);
-        if (c < wide) {
-          if (p.b_scale) f.x = p.b_scale[channel0 + c];
-          if (p.bias) f.y = load_one_of(p.bias, p.bias_type, channel0 + c);
-        }
-        about[i] = f;
-      }
+#pragma unroll
+      for (int i = 0; i < kEndChannels / 32; ++i) about[i * 32 + lane] = channels[i];
+      const float times = a_scale;
+      const int off = less * p.zero;
       __syncwarp();
       if (!barrier_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up)) break;
       after_sync();
+      ask(t + step);
       const unsigned at = result + (unsigned)turn.stage * 256u + (unsigned)(quarter * 32) * 65536u;
-      for (int j = 0; (j * 2 + side) * kBox < wide; ++j) {
-        const int c0 = (j * 2 + side) * kBox;
-        if constexpr (BOXES) {
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      for (int j = 0; (j * 2 + side) * kUnit < wide; ++j) {
+        const int c0 = (j * 2 + side) * kUnit;
+        uint8_t* box = boxes + (kWide ? flip * kBoxBytes : 0);
+        uint32_t v[kUnit];
+        read_unit(at + (unsigned)c0, v);
+        if constexpr (BOXES) {             // (this one's box has been read)
+          if (kWide && p.boxes == 2) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            flip ^= 1;
+          } else {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          }
         }
         __syncwarp();
+        const float4* f = reinterpret_cast<const float4*>(about + j * kUnit);
+        uint8_t* line = box + lane * 128;
 #pragma unroll
-        for (int h = 0; h < kBox / 32; ++h) {
-          uint32_t v[32];
-          read_columns32(at + (unsigned)(c0 + h * 32), v);
-          const float4* f = reinterpret_cast<const float4*>(about + j * kBox + h * 32);
-          uint8_t* line = box + lane * 128;
-          float y[32];
+        for (int k = 0; k < kUnit; k += 8) {
+          float y[8];
 #pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            const float4 g = f[k / 2];
-            y[k] = fmaf((float)((int)v[k] - less) * a_scale, g.x, g.y);
-            y[k + 1] = fmaf((float)((int)v[k + 1] - less) * a_scale, g.z, g.w);
+          for (int i = 0; i < 8; i += 2) {
+            const float4 g = f[(k + i) / 2];
+            y[i] = fmaf((float)((int)v[k + i] - off) * times, g.x, g.y);
+            y[i + 1] = fmaf((float)((int)v[k + i + 1] - off) * times, g.z, g.w);
           }
-          if constexpr (kBox == 64) {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-              const float e[8] = {y[k], y[k + 1], y[k + 2], y[k + 3], y[k + 4], y[k + 5], y[k + 6], y[k + 7]};
-              store_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(line + (((h * 4 + k / 8) ^ (lane & 7)) << 4), floats_to_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(e));
-            }
+          if constexpr (kWide) {
+            store_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(line + (((k / 8) ^ (lane & 7)) << 4), floats_to_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(y));
           } else {
 #pragma unroll
-            for (int k = 0; k < 32; k += 4)
-              *reinterpret_cast<float4*>(line + (((k / 4) ^ (lane & 7)) << 4)) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+            for (int i = 0; i < 8; i += 4)
+              *reinterpret_cast<float4*>(line + (k / 32) * kBoxBytes + ((((k + i) / 4 % 8) ^ (lane & 7)) << 4)) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
           }
         }
         if constexpr (BOXES) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0 && row0 < p.rows) store_box(&out_map, box, (int)(channel0 + c0), (int)row0);
+          if (lane == 0) {
+            if (row0 < p.rows) {
+              store_box(&out_map, box, (int)(channel0 + c0), (int)row0);
+              if (!kWide && c0 + 32 < wide) store_box(&out_map, box + kBoxBytes, (int)(channel0 + c0 + 32), (int)row0);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
         } else {
           __syncwarp();
           const int live = (int)min((long long)32, p.rows - row0);
-          const bool in = c0 + lane < wide;
-          const long long first = row0 * p.out_stride + channel0 + c0 + lane;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const bool in = c0 + h * 32 + lane < wide;
+            const long long first = row0 * p.out_stride + channel0 + c0 + h * 32 + lane;
 #pragma unroll 8
-          for (int r = 0; r < 32; ++r) {
-            const float y = *reinterpret_cast<const float*>(box + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + lane % 4 * 4);
-            if (in && r < live) {
-              const long long i = first + r * p.out_stride;
-              store_one<OUT>(p.out, i, p.accumulate ? load_one<OUT>(p.out, i) + y : y);
+            for (int r = 0; r < 32; ++r) {
+              const float y = *reinterpret_cast<const float*>(box + h * kBoxBytes + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + lane % 4 * 4);
+              if (in && r < live) {
+                const long long i = first + r * p.out_stride;
+                store_one<OUT>(p.out, i, p.accumulate ? load_one<OUT>(p.out, i) + y : y);
+              }
             }
           }
+          __syncwarp();
         }
       }
       before_sync();
@@ -574,7 +637,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   if (s.gave_up && warp == 0 && lane == 0) {
     // what was asked for has to land before these CTAs' memory is anyone else's
     for (int i = 0; rank == 0 && i < loaded; ++i) {
-      place.back(kPairStages);
+      place.back(p.stages);
       for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[place.stage], place.phase); ++n) {}
     }
     if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
@@ -626,8 +689,7 @@ bool byte_map(CUtensorMap* map, const void* p, int64_t width, int64_t rows, int6
 }
 
 // CTAs of a cluster wait for one another while they hold tensor memory, so no SM may be given more of them than its 512 columns
-// serve.  Their shared memory sees to it: a sum is split for tiles of at most 64 tokens only, with two stages of 24 KB for
-// 64 columns, or one of 18 KB and more for 32.
+// serve.  Their shared memory sees to it: tiles of few tokens hold 32 columns and 18 KB or more, pairs 512 columns and 200 KB.
 constexpr int kRingBytes = 208 * 1024;
 
 using PairKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, PairParams);
@@ -664,7 +726,6 @@ int pairs_of_device() {
 }
 
 constexpr int kSms = 148;
-constexpr int kFewTokens = 128;
 
 // Channels of a pair's tile: the time of the pairs' rounds, in cycles of the tensor cores (a block of 128 bytes takes twice a tile's
 // channels) and what a tile costs besides, is to be least.
@@ -691,12 +752,15 @@ int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int
   p.half = pair_half(p.token_tiles, p.channels, p.blocks, pairs);
   p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
   const bool boxes = !p.accumulate && is_aligned(p.out, 16) && p.out_stride * type_bytes(q.out_type) % 16 == 0;
+  p.boxes = boxes && q.out_type != QADAM_F32 && p.blocks >= kLongSum ? 1 : 2;
+  p.stages = p.boxes == 1 ? 5 : 4;
   CUtensorMap a_map, b_map, out_map = {};
   const bool maps = byte_map(&a_map, a, depth, p.rows, a_stride, 128) &&
                     (p.transposed ? byte_map(&b_map, b, p.channels, depth, b_stride, kDepth) : byte_map(&b_map, b, depth, p.channels, b_stride, p.half)) &&
                     (!boxes || box_map(&out_map, p.out, q.out_type, p.channels, p.rows, p.out_stride));
   if (!maps) return QADAM_ERR_CUDA;
   const int64_t tiles = (int64_t)p.token_tiles * p.channel_tiles;
+  if (tiles >= (int64_t)1 << 30) return QADAM_ERR_SIZE;
   return launch(kPairKernels[q.out_type][boxes], 2 * std::min<int64_t>(tiles, pairs), kPairThreads, kPairBytes + 1024, 2, st, a_map, b_map, out_map, p)
              ? QADAM_OK : QADAM_ERR_CUDA;
 }
@@ -707,13 +771,11 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
   if (pairs == 0) return QADAM_ERR_CUDA;
   if (p.rows > kFewTokens) return enqueue_pairs(p, a, a_stride, depth, b, b_stride, pairs, st);
   p.channel_tiles = (int)((p.channels + kChannels - 1) / kChannels);
-  int tokens = 16;
-  while (tokens < kMaxTokens && tokens < p.rows) tokens *= 2;
-  while (tokens > 64 && (int64_t)p.channel_tiles * ((p.rows + tokens - 1) / tokens) < kSms) tokens /= 2;
+  const int tokens = p.rows <= 16 ? 16 : 32;
   p.tokens = tokens;
-  const int64_t tiles = (int64_t)p.channel_tiles * ((p.rows + tokens - 1) / tokens);
+  const int64_t tiles = p.channel_tiles;
   int split = 1;
-  while (split < kMaxSplit && tokens <= 64 && tiles * split * 2 <= 2 * kSms && p.blocks >= split * 4) split *= 2;
+  while (split < kMaxSplit && tiles * split * 2 <= 2 * kSms && p.blocks >= split * 4) split *= 2;
   const int stage = (kChannels + tokens) * kDepth;
   const int needed = (p.blocks + split - 1) / split;
   p.stages = std::min({kMaxStages, kRingBytes / stage, std::max(needed, (tokens * kChannels * 4 + stage - 1) / stage)});
