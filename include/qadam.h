@@ -578,9 +578,10 @@ int qadam_quantize_columns(const void* x, int32_t type, int64_t x_stride, int64_
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* Elements [first, first + rows * width) of the packed broadcast Q_x(x) (see qadam_held_lookup; kx = 0 .. 6) as rows in 8 bits:
- * q = level, -2^kx .. 2^kx, worth 2^-(kx + 1).  q_stride >= width rounded up to 16 (the bytes up to there are written). */
+ * q = level, -2^kx .. 2^kx, worth 2^-(kx + 1), which goes to scale ([rows], or NULL).  q_stride >= width rounded up to 16 (the
+ * bytes up to there are written). */
 int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t rows, int64_t width, int8_t* q,
-                    int64_t q_stride, void* stream);
+                    int64_t q_stride, float* scale, void* stream);
 
 /* out[m][n] = round(a_scale[m] b_scale[n] sum_k a[m][k] B[k][n] + bias[n]), m < rows, n < channels, k < depth; accumulate = 1:
  * round(out[m][n] + the same).  The sum is exact (depth <= 131072), the rest binary32.

@@ -667,6 +667,7 @@ struct HeldParams {
   int width, pieces;                                       // pieces of 16 elements in a row
   signed char* q;
   long long q_stride;
+  float* scale;
 };
 
 // A thread decodes 16 consecutive codes: (16 BITS + 31) / 32 + 1 words at most, one store of 16 bytes.
@@ -697,6 +698,7 @@ __global__ void __launch_bounds__(256) held_rows_kernel(const __grid_constant__ 
     packed[k / 4] |= (uint32_t)(level & 255) << (8 * (k % 4));
   }
   *reinterpret_cast<uint4*>(p.q + row * p.q_stride + col) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+  if (p.scale && col == 0) p.scale[row] = 1.0f / (float)(1 << (BITS - 1));
 }
 
 // ---------------------------------------------------------------- arguments
@@ -839,11 +841,11 @@ int qadam_quantize_columns(const void* x, int32_t type, int64_t x_stride, int64_
 }
 
 int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t rows, int64_t width, int8_t* q,
-                    int64_t q_stride, void* stream) {
+                    int64_t q_stride, float* scale, void* stream) {
   if (bad_rows(rows, width) || bad_stride(q_stride, (width + 15) / 16 * 16)) return QADAM_ERR_SIZE;
   if (kx < 0 || kx > 6) return QADAM_ERR_LEVEL;
   if (!wcodes || (rows > 0 && !q)) return QADAM_ERR_NULL;
-  if (!is_aligned(wcodes, 16) || !is_aligned(q, 16) || q_stride % 16 != 0) return QADAM_ERR_ALIGN;
+  if (!is_aligned(wcodes, 16) || !is_aligned(q, 16) || q_stride % 16 != 0 || !is_aligned(scale, 4)) return QADAM_ERR_ALIGN;
   if (first < 0 || first > (int64_t)1 << 44 || wcode_bytes % 16 != 0 || wcode_bytes / 2 > (size_t)1 << 44) return QADAM_ERR_SIZE;
   const int64_t held = (int64_t)(wcode_bytes * 8 / (size_t)(kx + 2));
   if (first > held || rows > (held - first) / width) return QADAM_ERR_SIZE;
@@ -851,7 +853,7 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
   HeldParams p = {};
   p.codes = static_cast<const uint32_t*>(wcodes); p.words = (long long)(wcode_bytes / 4); p.first = first;
   p.rows = rows; p.width = (int)width; p.pieces = (int)((width + 15) / 16);
-  p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride;
+  p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride; p.scale = scale;
   const long long grid = (rows * p.pieces + 255) / 256;
   if (grid >= kMostRows) return QADAM_ERR_SIZE;
   using Kernel = void (*)(HeldParams);

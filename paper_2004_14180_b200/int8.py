@@ -13,27 +13,83 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-from typing import NamedTuple, Optional
+from typing import Optional
 
 import torch
 
-from .adamw import TYPES, _need_cuda, element_type, stream_of, written
+from .adamw import _need_cuda, stream_of, written
 from .binding import _check, load_library
 from .embedding import _elsewhere, _row_stride, _status, _type
 
 
-class Int8Rows(NamedTuple):
-    """Rows in 8 bits: q[i, k] is worth scale[i]; sums[i] (if there) is the sum of q[i, :].
+class Int8Rows:
+    """Rows in 8 bits: q[i, k] is worth scale[i]; sums[i] (None if not known) is the sum of q[i, :].
 
     q: [rows, width] int8 whose rows begin on 16 bytes, a multiple of 16 bytes apart; scale: [rows] float32; sums: [rows] int32.
-    What quantize_rows, quantize_columns, held_rows and layer_norm give is so; q of one's own may be laid out by `empty_rows`."""
-    q: torch.Tensor
-    scale: torch.Tensor
-    sums: Optional[torch.Tensor] = None
+    What quantize_rows, quantize_columns, held_rows and layer_norm give is so (one allocation; the three are views of it, made when
+    they are asked for); q of one's own may be laid out by `empty_rows`."""
+
+    __slots__ = ("rows", "width", "stride", "device", "q_at", "scale_at", "sums_at", "_q", "_scale", "_sums", "_buffer")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, sums: Optional[torch.Tensor] = None):
+        if not q.is_cuda or q.dim() != 2 or q.dtype is not torch.int8:
+            _need_cuda()
+            raise ValueError("q must be a CUDA tensor [rows, width] of int8; there is no CPU path")
+        self.rows, self.width = q.shape
+        self.device = q.device
+        if scale.device != q.device or scale.dtype is not torch.float32 or scale.shape != (self.rows,) or not scale.is_contiguous():
+            raise ValueError(f"scale must be {self.rows} contiguous float32 on {q.device}")
+        if sums is not None and (sums.device != q.device or sums.dtype is not torch.int32 or sums.shape != (self.rows,) or
+                                 not sums.is_contiguous()):
+            raise ValueError(f"sums must be {self.rows} contiguous int32 on {q.device}")
+        row, column = q.stride()
+        if self.width > 1 and column != 1:
+            raise ValueError("a row's elements must be next to each other")
+        self.stride = row if self.rows > 1 else (self.width + 15) // 16 * 16
+        self.q_at = q.data_ptr()
+        if self.stride % 16 or self.stride < self.width or self.q_at % 16:
+            raise ValueError("rows must begin on 16 bytes, a multiple of 16 bytes apart (empty_rows lays them out so)")
+        self.scale_at, self.sums_at = scale.data_ptr(), None if sums is None else sums.data_ptr()
+        self._q, self._scale, self._sums, self._buffer = q, scale, sums, None
+
+    @classmethod
+    def _make(cls, rows: int, width: int, device: torch.device, sums: bool) -> "Int8Rows":
+        """Room for so many rows, in one allocation: [q, rows on 16 bytes][scale][sums]."""
+        self = cls.__new__(cls)
+        self.rows, self.width, self.device = rows, width, device
+        self.stride = stride = (width + 15) // 16 * 16
+        self._buffer = buffer = torch.empty(rows * (stride + (8 if sums else 4)), dtype=torch.uint8, device=device)
+        self.q_at = at = buffer.data_ptr()
+        self.scale_at = at + rows * stride
+        self.sums_at = self.scale_at + 4 * rows if sums else None
+        self._q = self._scale = self._sums = None
+        return self
+
+    @property
+    def q(self) -> torch.Tensor:
+        if self._q is None:
+            self._q = self._buffer[:self.rows * self.stride].view(torch.int8).view(self.rows, self.stride)[:, :self.width]
+        return self._q
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if self._scale is None:
+            first = self.rows * self.stride
+            self._scale = self._buffer[first:first + 4 * self.rows].view(torch.float32)
+        return self._scale
+
+    @property
+    def sums(self) -> Optional[torch.Tensor]:
+        if self._sums is None and self.sums_at is not None:
+            self._sums = self._buffer[self.rows * (self.stride + 4):].view(torch.int32)
+        return self._sums
 
     def values(self) -> torch.Tensor:
         """What the rows stand for, float32 (by torch's operations)."""
         return self.q.float() * self.scale[:, None]
+
+    def __repr__(self) -> str:
+        return f"Int8Rows({self.rows} x {self.width} on {self.device})"
 
 
 def empty_rows(rows: int, width: int, device: torch.device) -> torch.Tensor:
@@ -41,23 +97,6 @@ def empty_rows(rows: int, width: int, device: torch.device) -> torch.Tensor:
     pitch = (width + 15) // 16 * 16
     q = torch.empty(rows, pitch, dtype=torch.int8, device=device)
     return q if pitch == width else q[:, :width]
-
-
-def _rows_of(a: Int8Rows, what: str):
-    """-> rows, width, stride of a.q, all checked but for the alignment, which the library looks at."""
-    q, scale = a.q, a.scale
-    if not q.is_cuda or q.dim() != 2 or q.dtype != torch.int8:
-        _need_cuda()
-        raise ValueError(f"{what}: q must be a CUDA tensor [rows, width] of int8; there is no CPU path")
-    rows, width = q.shape
-    if scale.device != q.device or scale.dtype != torch.float32 or scale.shape != (rows,) or not scale.is_contiguous():
-        raise ValueError(f"{what}: scale must be {rows} contiguous float32 on {q.device}")
-    if width > 1 and q.stride(1) != 1:
-        raise ValueError(f"{what}: a row's elements must be next to each other")
-    stride = q.stride(0) if rows > 1 else (width + 15) // 16 * 16
-    if stride % 16 or stride < width or (rows and q.data_ptr() % 16):
-        raise ValueError(f"{what}: rows must begin on 16 bytes, a multiple of 16 bytes apart (empty_rows lays them out so)")
-    return rows, width, stride
 
 
 def quantize_rows(x: torch.Tensor, columns: Optional[torch.Tensor] = None, sums: bool = True) -> Int8Rows:
@@ -73,20 +112,17 @@ def quantize_rows(x: torch.Tensor, columns: Optional[torch.Tensor] = None, sums:
             return quantize_rows(x, columns, sums)
     if width < 1:
         raise ValueError("x: rows of no elements")
-    if columns is not None and (columns.device != device or columns.dtype != torch.float32 or columns.shape != (width,) or
+    if columns is not None and (columns.device != device or columns.dtype is not torch.float32 or columns.shape != (width,) or
                                 not columns.is_contiguous()):
         raise ValueError(f"columns: {width} contiguous float32 on {device} are needed")
-    stride = _row_stride(x, "x", x.shape, device)
+    stride = width if x.is_contiguous() else _row_stride(x, "x", x.shape, device)
     rows = x.numel() // width
-    q = empty_rows(rows, width, device)
-    scale = torch.empty(rows, dtype=torch.float32, device=device)
-    total = torch.empty(rows, dtype=torch.int32, device=device) if sums else None
-    rc = load_library().qadam_quantize_rows(
-        x.data_ptr(), _type(x, "x"), stride, None if columns is None else columns.data_ptr(), rows, width, q.data_ptr(),
-        (width + 15) // 16 * 16, scale.data_ptr(), None if total is None else total.data_ptr(), stream_of(device))
+    r = Int8Rows._make(rows, width, device, sums)
+    rc = load_library().qadam_quantize_rows(x.data_ptr(), _type(x, "x"), stride, None if columns is None else columns.data_ptr(), rows, width,
+                                            r.q_at, r.stride, r.scale_at, r.sums_at, stream_of(device))
     if rc:
         _check(rc, "qadam_quantize_rows")
-    return Int8Rows(q, scale, total)
+    return r
 
 
 @functools.lru_cache(maxsize=256)
@@ -107,17 +143,16 @@ def quantize_columns(x: torch.Tensor) -> Int8Rows:
             return quantize_columns(x)
     if x.numel() == 0:
         raise ValueError("x: no elements")
-    stride = _row_stride(x, "x", x.shape, device)
+    stride = width if x.is_contiguous() else _row_stride(x, "x", x.shape, device)
     rows = x.numel() // width
-    q = empty_rows(width, rows, device)
-    scale = torch.empty(width, dtype=torch.float32, device=device)
+    r = Int8Rows._make(width, rows, device, False)
     size = _column_workspace(rows, width)
     scratch = torch.empty(size, dtype=torch.uint8, device=device)
-    rc = load_library().qadam_quantize_columns(x.data_ptr(), _type(x, "x"), stride, rows, width, q.data_ptr(), (rows + 15) // 16 * 16,
-                                               scale.data_ptr(), scratch.data_ptr(), size, stream_of(device))
+    rc = load_library().qadam_quantize_columns(x.data_ptr(), _type(x, "x"), stride, rows, width, r.q_at, r.stride, r.scale_at,
+                                               scratch.data_ptr(), size, stream_of(device))
     if rc:
         _check(rc, "qadam_quantize_columns")
-    return Int8Rows(q, scale)
+    return r
 
 
 def _check_codes(wcodes: torch.Tensor) -> None:
@@ -137,12 +172,12 @@ def held_rows(wcodes: torch.Tensor, kx: int, rows: int, width: int, first: int =
             return held_rows(wcodes, kx, rows, width, first)
     if rows < 0 or width < 1:
         raise ValueError(f"no table of {rows} rows of {width}")
-    q = empty_rows(rows, width, device)
-    rc = load_library().qadam_held_rows(wcodes.data_ptr(), wcodes.numel(), kx, first, rows, width, q.data_ptr(), (width + 15) // 16 * 16,
+    r = Int8Rows._make(rows, width, device, False)
+    rc = load_library().qadam_held_rows(wcodes.data_ptr(), wcodes.numel(), kx, first, rows, width, r.q_at, r.stride, r.scale_at,
                                         stream_of(device))
     if rc:
         _check(rc, "qadam_held_rows")
-    return Int8Rows(q, torch.full((rows,), 2.0 ** -(kx + 1), dtype=torch.float32, device=device))
+    return r
 
 
 def _output(rows, channels, out, out_dtype, accumulate, bias, device):
@@ -170,21 +205,19 @@ def int8_matmul(a: Int8Rows, b: Int8Rows, bias: Optional[torch.Tensor] = None, o
     The sums over the common width (at most 131072) are exact.  transpose: a b instead, [rows of a, width of b]; b's scales belong
     to the axis that is then summed over and are not applied: quantize a with columns=b.scale.
     status: one int32 on the device that gets ST_TIMEOUT if a wait inside the kernel gives up."""
-    rows, depth, a_stride = _rows_of(a, "a")
-    device = a.q.device
+    device, rows, depth = a.device, a.rows, a.width
     if _elsewhere(device):
         with torch.cuda.device(device):
             return int8_matmul(a, b, bias, out_dtype, out, accumulate, transpose, status)
-    b_rows, b_width, b_stride = _rows_of(b, "b")
-    if b.q.device != device:
-        raise ValueError(f"a on {device}, b on {b.q.device}")
-    if depth != (b_rows if transpose else b_width):
-        raise ValueError(f"a [{rows}, {depth}] and b [{b_rows}, {b_width}] have no common axis{' (transposed)' if transpose else ''}")
-    channels = b_width if transpose else b_rows
+    if b.device != device:
+        raise ValueError(f"a on {device}, b on {b.device}")
+    common, channels = (b.rows, b.width) if transpose else (b.width, b.rows)
+    if depth != common:
+        raise ValueError(f"a [{rows}, {depth}] and b [{b.rows}, {b.width}] have no common axis{' (transposed)' if transpose else ''}")
     given = out is not None
     out, out_stride, bias_at, bias_type = _output(rows, channels, out, out_dtype, accumulate, bias, device)
     rc = load_library().qadam_row_product(
-        a.q.data_ptr(), a_stride, a.scale.data_ptr(), rows, depth, b.q.data_ptr(), b_stride, b.scale.data_ptr(), channels, int(transpose),
+        a.q_at, a.stride, a.scale_at, rows, depth, b.q_at, b.stride, b.scale_at, channels, int(transpose),
         bias_at, bias_type, out.data_ptr(), _type(out, "out"), out_stride, int(accumulate),
         None if status is None else _status(status, device), stream_of(device))
     if rc:
@@ -202,9 +235,8 @@ def held_matmul(a: Int8Rows, wcodes: torch.Tensor, kx: int, rows: int, width: in
 
     Codes of one byte (kx = 6) whose rows begin on 16 bytes are multiplied as they lie; others are laid out as rows in 8 bits
     first, by a launch that writes rows * width bytes."""
-    a_rows, depth, a_stride = _rows_of(a, "a")
+    device, a_rows, depth = a.device, a.rows, a.width
     _check_codes(wcodes)
-    device = a.q.device
     if wcodes.device != device:
         raise ValueError(f"a on {device}, wcodes on {wcodes.device}")
     if _elsewhere(device):
@@ -215,16 +247,15 @@ def held_matmul(a: Int8Rows, wcodes: torch.Tensor, kx: int, rows: int, width: in
     if kx != 6 or width % 16 or first % 16 or wcodes.data_ptr() % 16:
         w = held_rows(wcodes, kx, rows, width, first)
         if transpose:              # the weights' worth is the same for all: it goes to a
-            a = Int8Rows(a.q, a.scale * 2.0 ** -(kx + 1))
+            a = Int8Rows(a.q, a.scale * 2.0 ** -(kx + 1))          # (a power of two)
         return int8_matmul(a, w, bias, out_dtype, out, accumulate, transpose, status)
-    sums = a.sums
-    if sums is None or sums.device != device or sums.dtype != torch.int32 or sums.shape != (a_rows,) or not sums.is_contiguous():
-        raise ValueError(f"a: sums ({a_rows} contiguous int32 on {device}) are needed")
+    if a.sums_at is None:
+        raise ValueError("a: the sums of its rows are needed")
     channels = width if transpose else rows
     given = out is not None
     out, out_stride, bias_at, bias_type = _output(a_rows, channels, out, out_dtype, accumulate, bias, device)
     rc = load_library().qadam_held_product(
-        a.q.data_ptr(), a_stride, a.scale.data_ptr(), sums.data_ptr(), a_rows, depth, wcodes.data_ptr(), wcodes.numel(), kx, first,
+        a.q_at, a.stride, a.scale_at, a.sums_at, a_rows, depth, wcodes.data_ptr(), wcodes.numel(), kx, first,
         channels, int(transpose), bias_at, bias_type, out.data_ptr(), _type(out, "out"), out_stride, int(accumulate),
         None if status is None else _status(status, device), stream_of(device))
     if rc:

@@ -13,7 +13,7 @@ import torch
 from .adamw import _need_cuda, stream_of, written
 from .binding import _check, load_library
 from .embedding import _elsewhere, _row_stride, _type
-from .int8 import Int8Rows, empty_rows
+from .int8 import Int8Rows
 
 
 class Normed(NamedTuple):
@@ -24,6 +24,11 @@ class Normed(NamedTuple):
     mean: torch.Tensor
     rstd: torch.Tensor
     rows: Optional[Int8Rows]
+
+
+def _like(x: torch.Tensor, whole: bool) -> torch.Tensor:
+    """A contiguous tensor of x's shape and type (empty_like of a contiguous one is: 1.3 us, not 3.5)."""
+    return torch.empty_like(x) if whole else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _parameter(t: Optional[torch.Tensor], what: str, width: int, device: torch.device):
@@ -51,7 +56,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         raise ValueError("x: rows of no elements")
     n = x.numel() // width
     kind = _type(x, "x")
-    stride = _row_stride(x, "x", x.shape, device)
+    whole = x.is_contiguous()
+    stride = width if whole else _row_stride(x, "x", x.shape, device)
     weight_at, weight_type = _parameter(weight, "weight", width, device)
     bias_at, bias_type = _parameter(bias, "bias", width, device)
     total, residual_at, residual_stride = x, None, 0
@@ -59,19 +65,17 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         if residual.dtype != x.dtype:
             raise ValueError(f"residual is {residual.dtype}, x {x.dtype}")
         residual_at, residual_stride = residual.data_ptr(), _row_stride(residual, "residual", x.shape, device)
-        total = torch.empty(x.shape, dtype=x.dtype, device=device)
-    out = torch.empty(x.shape, dtype=x.dtype, device=device) if dense else None
-    mean, rstd = torch.empty(2, n, dtype=torch.float32, device=device).unbind()
-    rows = None
-    if int8:
-        rows = Int8Rows(empty_rows(n, width, device), torch.empty(n, dtype=torch.float32, device=device),
-                        torch.empty(n, dtype=torch.int32, device=device))
+        total = _like(x, whole)
+    out = _like(x, whole) if dense else None
+    mean = torch.empty(n, dtype=torch.float32, device=device)
+    rstd = torch.empty(n, dtype=torch.float32, device=device)
+    rows = Int8Rows._make(n, width, device, True) if int8 else None
     if n:
         rc = load_library().qadam_layer_norm(
             x.data_ptr(), kind, stride, residual_at, residual_stride, weight_at, weight_type, bias_at, bias_type, n, width, eps,
             None if residual is None else total.data_ptr(), width, None if out is None else out.data_ptr(), width, mean.data_ptr(),
-            rstd.data_ptr(), None if rows is None else rows.q.data_ptr(), (width + 15) // 16 * 16,
-            None if rows is None else rows.scale.data_ptr(), None if rows is None else rows.sums.data_ptr(), stream_of(device))
+            rstd.data_ptr(), None if rows is None else rows.q_at, 0 if rows is None else rows.stride,
+            None if rows is None else rows.scale_at, None if rows is None else rows.sums_at, stream_of(device))
         if rc:
             _check(rc, "qadam_layer_norm")
     return Normed(out, total, mean, rstd, rows)
@@ -122,9 +126,10 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd:
     if dw_type != db_type:
         raise ValueError(f"dweight is {dweight.dtype}, dbias {dbias.dtype}")
     weight_at, weight_type = _parameter(weight, "weight", width, device)
-    x_stride, dy_stride = _row_stride(x, "x", x.shape, device), _row_stride(dy, "dy", x.shape, device)
+    whole = x.is_contiguous()
+    x_stride, dy_stride = width if whole else _row_stride(x, "x", x.shape, device), _row_stride(dy, "dy", x.shape, device)
     ds_at, ds_stride = (None, 0) if dsum is None else (dsum.data_ptr(), _row_stride(dsum, "dsum", x.shape, device))
-    dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+    dx = _like(x, whole)
     size = _grad_workspace(n, width)
     scratch = torch.empty(size, dtype=torch.uint8, device=device)
     rc = load_library().qadam_layer_norm_grad(

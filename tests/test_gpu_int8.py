@@ -16,6 +16,10 @@ def int8_rows(gen, rows, width, full=False):
     return qb.Int8Rows(q, torch.exp2(randn(gen, rows)), q.sum(1, dtype=torch.int32))
 
 
+def scaled(a, scale):
+    return qb.Int8Rows(a.q, scale, a.sums)
+
+
 def check(got, a, b, b_scale, bias, kind, before=None):
     """got = sa sb (a b^T) + bias (+ before): the sum is rounded once, two products, a sum, perhaps another sum."""
     whole = a.q.double() @ b.double().T                        # (exact: below 2^53)
@@ -45,8 +49,8 @@ def test_product(m, k, n):
             got = got.float().clamp(-65504, 65504)
             fits = (a.q.double() @ b.q.double().T * a.scale.double()[:, None] * b.scale.double() + more.double()).abs() < 65000
             assert got.shape == (m, n)
-            small = qb.int8_matmul(a._replace(scale=a.scale * 2.0 ** -10), b, out_dtype=torch.float16)
-            check(small.clamp(-65504, 65504)[:, :1], a._replace(scale=a.scale * 2.0 ** -10), b.q[:1], b.scale[:1], None, kind) if bool(fits.all()) else None
+            small = qb.int8_matmul(scaled(a, a.scale * 2.0 ** -10), b, out_dtype=torch.float16)
+            check(small.clamp(-65504, 65504)[:, :1], scaled(a, a.scale * 2.0 ** -10), b.q[:1], b.scale[:1], None, kind) if bool(fits.all()) else None
         else:
             check(got, a, b.q, b.scale, more, kind)
     # transposed: the scales of b's rows are left to a
@@ -58,16 +62,16 @@ def test_sums_at_the_ends_of_their_range():
     gen = gen_of(5)
     k = 131072
     a, b = int8_rows(gen, 2, k, full=True), int8_rows(gen, 130, k, full=True)
-    b.q[1::2] = -128
+    b.q[1::2] = -128                                           # (a's sums hold, b's are not looked at)
     one = torch.ones(2, device="cuda")
-    a = a._replace(scale=one)
-    b = b._replace(scale=torch.ones(130, device="cuda"))
+    a = scaled(a, one)
+    b = scaled(b, torch.ones(130, device="cuda"))
     got = qb.int8_matmul(a, b, out_dtype=torch.float32)
     want = torch.tensor([127.0 * 127 * k, -127.0 * 128 * k] * 65, dtype=torch.float64).float().cuda()
     assert torch.equal(got, want.expand(2, 130))
     codes = torch.full((130 * k,), 128, dtype=torch.uint8, device="cuda")
     codes[k:2 * k] = 0
-    got = qb.held_matmul(a._replace(sums=a.q.sum(1, dtype=torch.int32)), codes, 6, 130, k, out_dtype=torch.float32)
+    got = qb.held_matmul(a, codes, 6, 130, k, out_dtype=torch.float32)
     want = torch.full((2, 130), 127 * k / 2, device="cuda")
     want[:, 1] *= -1
     assert torch.equal(got, want)
@@ -100,7 +104,7 @@ def test_strides_accumulation_and_what_lies_around():
         room = randn(gen, m + 2, n + 7).to(DTYPES[kind])
         before = room.clone()
         out = room[1:1 + m, 3:3 + n]
-        small = a._replace(scale=a.scale * 2.0 ** -16)
+        small = scaled(a, a.scale * 2.0 ** -16)
         assert qb.int8_matmul(small, b, out=out, accumulate=True) is out
         check(out, small, b.q, b.scale, None, kind, before[1:1 + m, 3:3 + n])
         keep = torch.ones_like(room, dtype=torch.bool)
