@@ -25,9 +25,10 @@ struct RowParams {
   const char* r;
   long long r_stride;
   const void* w;
-  int w_type, w_vec;
+  int w_type;
   const void* b;
-  int b_type, b_vec;
+  int b_type;
+  int alike;                                               // the type of w and b (of w, if there is no b), or -1, see kAnyType
   char* sum;
   long long sum_stride;
   char* out;
@@ -46,9 +47,39 @@ struct RowParams {
 
 // ---------------------------------------------------------------- rows in registers
 
+// h w + b; PT: the type of both, w's alone where there is no b, or kAnyType: w and b of types of their own, anywhere, each there or not.
+constexpr int kAnyType = -1, kShared = 3;                  // kShared: binary32 of both in shared memory
+template <int PT, int TY, int NV, bool VEC>
+__device__ __forceinline__ void scale_and_shift(const RowParams& p, const RowPart<TY, NV, VEC>& part, const float* shared, float2 (&h)[4 * NV]) {
+  using Part = RowPart<TY, NV, VEC>;
+#pragma unroll
+  for (int q = 0; q < Part::kPieces; q += Part::kStep) {
+    float2 w[Part::kStepPairs], b[Part::kStepPairs];
+#pragma unroll
+    for (int k = 0; k < Part::kStepPairs; ++k) w[k] = b[k] = make_float2(0.0f, 0.0f);                 // (beyond the row: zero)
+    if constexpr (PT == kShared) {
+      part.read_shared(shared, q, w);
+      part.read_shared(shared + part.threads * 8 * NV, q, b);
+    } else if constexpr (PT != kAnyType) {
+      part.template read_parameters<PT>(p.w, q, w);
+      if (p.b) part.template read_parameters<PT>(p.b, q, b);
+    } else {
+      if (p.w) part.read_any(p.w, p.w_type, q, w);
+      if (p.b) part.read_any(p.b, p.b_type, q, b);
+    }
+#pragma unroll
+    for (int k = 0; k < Part::kStepPairs; ++k) {
+      float2& y = h[q / Part::kStep * Part::kStepPairs + k];
+      if (PT != kAnyType || p.w) y = fma2_rn(y, w[k], b[k]);
+      else y = add2_rn(y, b[k]);
+    }
+  }
+}
+
 // What becomes of a row h, dealt out to a group's threads: normed, scaled, written, in 8 bits.
 template <int TY, int NV, bool VEC, bool MANY>
-__device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY, NV, VEC>& part, RowGroup<MANY>& group, long long row, float2 (&h)[4 * NV]) {
+__device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY, NV, VEC>& part, RowGroup<MANY>& group, long long row,
+                                           const float* shared, float2 (&h)[4 * NV]) {
   using Part = RowPart<TY, NV, VEC>;
   if (p.normed) {
     float2 s = h[0];
@@ -77,17 +108,14 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
     for (int i = 0; i < Part::kPairs; ++i) h[i] = mul2_rn(h[i], make_float2(rstd, rstd));
   }
   if (p.w || p.b) {
-#pragma unroll
-    for (int q = 0; q < Part::kPieces; q += Part::kStep) {
-      float2 w[Part::kStepPairs], b[Part::kStepPairs];
-#pragma unroll
-      for (int k = 0; k < Part::kStepPairs; ++k) w[k] = b[k] = make_float2(0.0f, 0.0f);               // (beyond the row: zero)
-      if (p.w) part.read_parameters(p.w, p.w_type, p.w_vec, q, w);
-      if (p.b) part.read_parameters(p.b, p.b_type, p.b_vec, q, b);
-#pragma unroll
-      for (int k = 0; k < Part::kStepPairs; ++k) {
-        float2& y = h[q / Part::kStep * Part::kStepPairs + k];
-        y = p.w ? p.b ? fma2_rn(y, w[k], b[k]) : mul2_rn(y, w[k]) : add2_rn(y, b[k]);
+    if (MANY && shared) {
+      scale_and_shift<kShared>(p, part, shared, h);
+    } else {
+      switch (p.alike) {                                   // (told apart once, not for each element)
+        case QADAM_F32: scale_and_shift<QADAM_F32>(p, part, nullptr, h); break;
+        case QADAM_BF16: scale_and_shift<QADAM_BF16>(p, part, nullptr, h); break;
+        case QADAM_F16: scale_and_shift<QADAM_F16>(p, part, nullptr, h); break;
+        default: scale_and_shift<kAnyType>(p, part, nullptr, h);
       }
     }
   }
@@ -100,18 +128,25 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
     signed char* q = p.q + row * p.q_stride;
     const uint32_t finite = s.per > 0.0f ? 0xFFFFFFFFu : 0u;
     int sum = 0;
+    signed char* to = q + part.first;
+    uint32_t c[Part::kPairs / 2];
 #pragma unroll
     for (int i = 0; i < Part::kPairs; i += 2) {
-      const uint32_t c = to_bytes(h[i], h[i + 1], s.per) & finite;
-      sum = __dp4a((int)c, 0x01010101, sum);               // (beyond the row: zeros)
-      if constexpr (VEC) {
-        constexpr int kWords = Part::kPiece / 4;           // of a piece
-        if (part.has(i / (2 * kWords))) *reinterpret_cast<uint32_t*>(q + part.column(i / (2 * kWords)) + i / 2 % kWords * 4) = c;
-      } else {
+      c[i / 2] = to_bytes(h[i], h[i + 1], s.per) & finite;
+      sum = __dp4a((int)c[i / 2], 0x01010101, sum);        // (beyond the row: zeros)
+    }
+    if constexpr (VEC) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (part.has(2 * i + k)) q[part.column(2 * i + k)] = (signed char)(c >> (8 * k));
+      for (int n = 0; n < Part::kPieces; ++n) {
+        if (part.has(n)) {
+          if constexpr (Part::kPiece == 8) *reinterpret_cast<uint2*>(to + n * 256) = make_uint2(c[2 * n], c[2 * n + 1]);
+          else *reinterpret_cast<uint32_t*>(to + n * 128) = c[n];
+        }
       }
+    } else {
+#pragma unroll
+      for (int n = 0; n < Part::kPieces; ++n)
+        if (part.has(n)) to[n * 32] = (signed char)(c[n / 4] >> (8 * (n % 4)));
     }
     if (p.sums) sum = group.add(sum);
     if (part.t == 0) {
@@ -140,14 +175,14 @@ __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_
     for (int i = 0; i < Part::kPairs; ++i) h[i] = add2_rn(h[i], r[i]);
     part.store_rounded(p.sum + row * p.sum_stride * Part::kBytes, h);
   }
-  finish_row(p, part, group, row, h);
+  finish_row(p, part, group, row, nullptr, h);
 }
 
 // Wider rows: a group of warps goes from row to row, with the next ones under way.
 constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
 template <int TY, int NV, bool VEC, int MOST>
-__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages) {
-  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][1 or 2][a row]
+__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages, int with_parameters) {
+  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][1 or 2][a row]; with_parameters: then w, b
   __shared__ GroupShared shared[kGroupWarps];
   wait_for_previous_launch();
   using Part = RowPart<TY, NV, VEC>;
@@ -155,8 +190,15 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(co
   const int groups = blockDim.x / threads;
   const Part part(p.width, threads, (int)threadIdx.x % threads);
   RowGroup<true> group(&shared[number], warps, number);
-  const int each = Part::slot_bytes(p.width), both = p.r ? 2 * each : each;
+  const int each = Part::slot_bytes(threads), both = p.r ? 2 * each : each;
   uint8_t* ring = slots + number * stages * both;
+  float* parameters = with_parameters ? reinterpret_cast<float*>(slots + groups * stages * both) : nullptr;
+  clear_shared(slots, groups * stages * both);
+  if (parameters) {
+    fill_parameters(parameters, p.w, p.w_type, 1.0f, p.width, threads * 8 * NV);
+    fill_parameters(parameters + threads * 8 * NV, p.b, p.b_type, 0.0f, p.width, threads * 8 * NV);
+  }
+  __syncthreads();
   const long long first = (long long)blockIdx.x * groups + number, step = (long long)gridDim.x * groups;
   const auto fetch = [&](long long row, int stage) {
     if (row < p.rows) {
@@ -180,7 +222,7 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(co
       for (int i = 0; i < Part::kPairs; ++i) h[i] = add2_rn(h[i], r[i]);
       part.store_rounded(p.sum + row * p.sum_stride * Part::kBytes, h);
     }
-    finish_row(p, part, group, row, h);
+    finish_row(p, part, group, row, parameters, h);
     stage = stage + 1 == stages ? 0 : stage + 1;
   }
 }
@@ -247,14 +289,14 @@ bool launch_warp_rows(const RowParams& p, bool vec, cudaStream_t st) {
   return vec ? launch(warp_row_kernel<TY, NV, true>, grid, kWarpRowThreads, 0, 0, st, p) : launch(warp_row_kernel<TY, NV, false>, grid, kWarpRowThreads, 0, 0, st, p);
 }
 
-// CTAs of `threads` threads that an SM has at a time (of most_threads), and stages of `bytes` that each of them has then: 2 or 3,
-// or none if two do not fit.
+// CTAs of `threads` threads that an SM has at a time (of most_threads), and stages of `bytes`, with `besides` of their own, that each of
+// them has then: 2 or 3, or none if two do not fit.
 struct Residents {
   int per_sm, stages;
 };
-Residents residents(int threads, int most_threads, int bytes) {
-  const int per_sm = std::max(1, std::min(most_threads / threads, kRingBytes / (2 * bytes + 2048)));
-  const int stages = std::min(3, (kRingBytes / per_sm - 2048) / bytes);
+Residents residents(int threads, int most_threads, int bytes, int besides) {
+  const int per_sm = std::max(1, std::min(most_threads / threads, kRingBytes / (2 * bytes + besides + 2048)));
+  const int stages = std::min(3, (kRingBytes / per_sm - 2048 - besides) / bytes);
   return {per_sm, stages < 2 ? 0 : stages};
 }
 
@@ -267,13 +309,16 @@ bool allow_ring(K kernel, size_t bytes) {
 template <int TY, int NV, bool VEC>
 bool launch_group_rows(const RowParams& p, cudaStream_t st) {
   const int warps = (p.width + 256 * NV - 1) / (256 * NV), groups = std::max(1, kGroupWarps / warps);
-  const int threads = warps * groups * 32, bytes = RowPart<TY, NV, VEC>::slot_bytes(p.width) * (p.r ? 2 : 1) * groups;
-  const Residents r = residents(threads, kGroupMostThreads, bytes);
+  const int threads = warps * groups * 32, bytes = RowPart<TY, NV, VEC>::slot_bytes(warps * 32) * (p.r ? 2 : 1) * groups;
+  // w and b in shared memory, if they take no more than a quarter of it
+  const int parameters = p.w || p.b ? 2 * warps * 32 * 8 * NV * (int)sizeof(float) : 0;
+  const int kept = parameters * 4 <= kRingBytes / std::max(1, kGroupMostThreads / threads) ? parameters : 0;
+  const Residents r = residents(threads, kGroupMostThreads, bytes, kept);
   if (r.stages == 0) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
   const auto kernel = threads <= 256 ? group_row_kernel<TY, NV, VEC, 256> : group_row_kernel<TY, NV, VEC, 512>;
-  return allow_ring(kernel, (size_t)r.stages * bytes) &&
-         launch(kernel, std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm), threads, (size_t)r.stages * bytes, 0, st, p, warps,
-                r.stages);
+  const size_t smem = (size_t)r.stages * bytes + kept;
+  return allow_ring(kernel, smem) &&
+         launch(kernel, std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm), threads, smem, 0, st, p, warps, r.stages, kept ? 1 : 0);
 }
 template <int TY, int NV>
 bool launch_group_rows(const RowParams& p, bool vec, cudaStream_t st) {
@@ -300,7 +345,8 @@ int enqueue_rows(const RowParams& p, int type, bool vec, cudaStream_t st) {
 
 // ---------------------------------------------------------------- gradients
 
-constexpr int kGradWarps = 12;                             // of a CTA, in groups, or one group of up to 32
+constexpr int kGradWarps = 6;                              // of a CTA, in groups, two CTAs to an SM; or one group of up to 11 in a CTA of its own
+constexpr int kGradMostWarps = 12;
 constexpr int kGradGroupWidth = 8192;                      // beyond, rows are read again, and the columns' sums are a pass of their own
 
 struct GradParams {
@@ -310,54 +356,61 @@ struct GradParams {
   long long x_stride;
   const char* ds;
   long long ds_stride;
+  int ds_ahead;                                            // ds is fetched ahead as the others are (there is room for it)
   char* dx;
   long long dx_stride;
   const float* mean;
   const float* rstd;
   const void* w;
-  int w_type, w_vec;
+  int w_type;
   float* partial;                                          // [gridDim.x][2][width], or NULL
   long long rows;
   int width;
 };
 
-// A group of warps, eight elements to a thread, goes from row to row, with the next ones under way, and adds up its rows' part of the
+// A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
 // weight's and bias's gradients in registers; the CTA's sums go to the workspace.  One read, one write: bound by HBM.
-template <int TY, bool VEC, int MOST>
-__global__ void __launch_bounds__(MOST, MOST <= kGradWarps * 32 ? 2 : 1) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
-  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][2 or 3][a row]; at the end the groups' sums [groups][2][width]
-  __shared__ GroupShared shared[kGradWarps];
+// A row is read from shared memory twice, before and behind its sums: held in registers between, it would leave room for half as
+// many rows on an SM.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
+// row, not for elements.)
+template <int TY, int NV, bool VEC, bool MANY, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, kGradMostWarps / WARPS) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
+  extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][2 or 3][a row], w; at the end the groups' sums [groups][2][width]
+  __shared__ GroupShared shared[MANY ? kGradWarps : 1];
   wait_for_previous_launch();
-  using Part = RowPart<TY, 1, VEC>;
+  using Part = RowPart<TY, NV, VEC>;
   constexpr int kBytes = Part::kBytes;
-  const int threads = warps * 32, number = (int)threadIdx.x / threads;
+  const int threads = MANY ? warps * 32 : 32, number = (int)threadIdx.x / threads;
   const int groups = blockDim.x / threads;
   const Part part(p.width, threads, (int)threadIdx.x % threads);
-  RowGroup<true> group(&shared[number], warps, number);
-  const int each = Part::slot_bytes(p.width), all_of = p.ds ? 3 * each : 2 * each;
+  RowGroup<MANY> group(&shared[MANY ? number : 0], warps, number);
+  const int each = Part::slot_bytes(threads), all_of = p.ds_ahead ? 3 * each : 2 * each;
   uint8_t* ring = slots + number * stages * all_of;
+  const float* w = reinterpret_cast<const float*>(slots + groups * stages * all_of);
+  clear_shared(slots, groups * stages * all_of);
+  fill_parameters(reinterpret_cast<float*>(slots + groups * stages * all_of), p.w, p.w_type, 1.0f, p.width, threads * 8 * NV);
+  __syncthreads();
   const float per = 1.0f / (float)p.width;
   const long long first = (long long)blockIdx.x * groups + number, step = (long long)gridDim.x * groups;
+  // rows to come: where they lie
+  const char *next_x = p.x + first * p.x_stride * kBytes, *next_dy = p.dy + first * p.dy_stride * kBytes, *next_ds = p.ds + first * p.ds_stride * kBytes;
+  const long long x_step = step * p.x_stride * kBytes, dy_step = step * p.dy_stride * kBytes, ds_step = step * p.ds_stride * kBytes;
   const auto fetch = [&](long long row, int stage) {
     if (row < p.rows) {
       uint8_t* to = ring + stage * all_of;
-      part.fetch(to, p.x + row * p.x_stride * kBytes);
-      part.fetch(to + each, p.dy + row * p.dy_stride * kBytes);
-      if (p.ds) part.fetch(to + 2 * each, p.ds + row * p.ds_stride * kBytes);
+      part.fetch(to, next_x);
+      part.fetch(to + each, next_dy);
+      if (p.ds_ahead) part.fetch(to + 2 * each, next_ds);
     }
+    next_x += x_step;
+    next_dy += dy_step;
+    next_ds += ds_step;
     fetched();
   };
   for (int i = 0; i + 1 < stages; ++i) fetch(first + i * step, i);
-  typename Part::Row dw, db, w;
+  typename Part::Row dw, db;
 #pragma unroll
-  for (int i = 0; i < Part::kPairs; ++i) {
-    dw[i] = db[i] = make_float2(0.0f, 0.0f);
-    w[i] = make_float2(1.0f, 1.0f);
-  }
-  if (p.w) {
-#pragma unroll
-    for (int q = 0; q < Part::kPieces; q += Part::kStep) part.read_parameters(p.w, p.w_type, p.w_vec, q, &w[q / Part::kStep * Part::kStepPairs]);
-  }
+  for (int i = 0; i < Part::kPairs; ++i) dw[i] = db[i] = make_float2(0.0f, 0.0f);
   int stage = 0;
   for (long long row = first; row < p.rows; row += step) {
     const float mean = p.mean[row], rstd = p.rstd[row];
@@ -365,35 +418,50 @@ __global__ void __launch_bounds__(MOST, MOST <= kGradWarps * 32 ? 2 : 1) row_gra
     if constexpr (!VEC) group.sync();                      // (what others have copied; what the row before has left)
     fetch(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
     const uint8_t* from = ring + stage * all_of;
+    // (of these rows' addresses only the last four bits count, and those only where pieces do not begin on 16 bytes)
+    const char *x = p.x + row * p.x_stride * kBytes, *dy = p.dy + row * p.dy_stride * kBytes, *ds = p.ds + row * p.ds_stride * kBytes;
     const float2 less = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
-    typename Part::Row h, g;
-    part.read_slot(from, p.x + row * p.x_stride * kBytes, h);
-    part.read_slot(from + each, p.dy + row * p.dy_stride * kBytes, g);
     float2 along2 = make_float2(0.0f, 0.0f), all2 = along2;
 #pragma unroll
-    for (int i = 0; i < Part::kPairs; ++i) {               // (beyond the row g is zero)
-      h[i] = mul2_rn(add2_rn(h[i], less), times);
-      dw[i] = fma2_rn(g[i], h[i], dw[i]);
-      db[i] = add2_rn(db[i], g[i]);
-      g[i] = mul2_rn(g[i], w[i]);
-      along2 = fma2_rn(g[i], h[i], along2);
-      all2 = add2_rn(all2, g[i]);
+    for (int q = 0; q < Part::kPieces; q += Part::kStep) {
+      float2 h[Part::kStepPairs], g[Part::kStepPairs], by[Part::kStepPairs];
+      part.read_piece(from, x, q, h);
+      part.read_piece(from + each, dy, q, g);
+      part.read_shared(w, q, by);
+#pragma unroll
+      for (int k = 0; k < Part::kStepPairs; ++k) {         // (beyond the row g is zero)
+        const int i = q / Part::kStep * Part::kStepPairs + k;
+        h[k] = mul2_rn(add2_rn(h[k], less), times);
+        dw[i] = fma2_rn(g[k], h[k], dw[i]);
+        db[i] = add2_rn(db[i], g[k]);
+        g[k] = mul2_rn(g[k], by[k]);
+        along2 = fma2_rn(g[k], h[k], along2);
+        all2 = add2_rn(all2, g[k]);
+      }
     }
     float along = along2.x + along2.y, all = all2.x + all2.y;
     group.add2(along, all);
-    along *= -per;
-    all *= -per;
-    typename Part::Row s;
-    if (p.ds) {
-      part.read_slot(from + 2 * each, p.ds + row * p.ds_stride * kBytes, s);
-    } else {
+    const float2 minus_along = make_float2(-along * per, -along * per), minus_all = make_float2(-all * per, -all * per);
+    asm volatile("" ::: "memory");                         // the row is read again, not held
+    char* dx = p.dx + row * p.dx_stride * kBytes;
 #pragma unroll
-      for (int i = 0; i < Part::kPairs; ++i) s[i] = make_float2(0.0f, 0.0f);
+    for (int q = 0; q < Part::kPieces; q += Part::kStep) {
+      float2 h[Part::kStepPairs], g[Part::kStepPairs], by[Part::kStepPairs], s[Part::kStepPairs];
+      part.read_piece(from, x, q, h);
+      part.read_piece(from + each, dy, q, g);
+#pragma unroll
+      for (int k = 0; k < Part::kStepPairs; ++k) s[k] = make_float2(0.0f, 0.0f);
+      if (p.ds_ahead) part.read_piece(from + 2 * each, ds, q, s);
+      else if (p.ds) part.load_piece(ds, q, s);
+      part.read_shared(w, q, by);
+#pragma unroll
+      for (int k = 0; k < Part::kStepPairs; ++k) {
+        h[k] = mul2_rn(add2_rn(h[k], less), times);
+        g[k] = mul2_rn(g[k], by[k]);
+        s[k] = fma2_rn(times, fma2_rn(h[k], minus_along, add2_rn(g[k], minus_all)), s[k]);
+      }
+      part.store_piece(dx, q, s);
     }
-#pragma unroll
-    for (int i = 0; i < Part::kPairs; ++i)
-      s[i] = fma2_rn(times, fma2_rn(h[i], make_float2(along, along), add2_rn(g[i], make_float2(all, all))), s[i]);
-    part.store(p.dx + row * p.dx_stride * kBytes, s);
     stage = stage + 1 == stages ? 0 : stage + 1;
   }
   if (!p.partial) return;
@@ -404,7 +472,7 @@ __global__ void __launch_bounds__(MOST, MOST <= kGradWarps * 32 ? 2 : 1) row_gra
     __syncthreads();
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < 2 * Part::kPairs; ++e) {
     if (part.has(Part::piece_of(e))) {
       const int col = part.column(Part::piece_of(e)) + e % Part::kPiece;
       to[col] = e % 2 ? dw[e / 2].y : dw[e / 2].x;
@@ -480,11 +548,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float*
   const int col = blockIdx.x * 32 + lane;
   float a = 0.0f, b = 0.0f;
   if (col < width) {
-#pragma unroll 4
-    for (int i = warp; i < parts; i += kJoinWarps) {
-      const float* part = partial + (size_t)i * 2 * width;
-      a += part[col];
-      b += part[width + col];
+    const float* part = partial + (size_t)warp * 2 * width + col;
+#pragma unroll 10
+    for (int i = warp; i < parts; i += kJoinWarps, part += (size_t)kJoinWarps * 2 * width) {
+      a += part[0];
+      b += part[width];
     }
   }
   sum[warp][0][lane] = a;
@@ -501,15 +569,22 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float*
 
 // CTAs of the gradient, and so partial sums: as many as are on the device's SMs at a time, at most one to the rows of its groups.
 struct GradShape {
-  int warps, groups, threads, most, per_sm;                // most: threads of an SM that there are registers for
+  int pieces;                                              // NV of the kernel: 8 elements each
+  int warps, groups, threads, per_sm;
 };
 GradShape grad_shape(int width) {
   GradShape g;
-  g.warps = (width + 255) / 256;
+  // 16 or 24 elements to a thread, whichever leaves fewer threads without (8 where a warp has enough with that)
+  const int two = (width + 511) / 512, three = (width + 767) / 768;
+  g.pieces = width <= 256 ? 1 : two * 512 < three * 768 ? 2 : 3;
+  g.warps = g.pieces == 1 ? 1 : g.pieces == 2 ? two : three;
+  if (g.warps > kGradMostWarps) {                          // (two pieces, beyond 6144)
+    g.pieces = 3;
+    g.warps = three;
+  }
   g.groups = std::max(1, kGradWarps / g.warps);
   g.threads = g.warps * g.groups * 32;
-  g.most = g.warps <= kGradWarps ? 2 * kGradWarps * 32 : 1024;
-  g.per_sm = g.most / g.threads;
+  g.per_sm = g.threads <= kGradWarps * 32 ? 2 : 1;
   return g;
 }
 int grad_parts(long long rows, int width) {
@@ -518,14 +593,26 @@ int grad_parts(long long rows, int width) {
   return (int)std::min<long long>((rows + g.groups - 1) / g.groups, g.per_sm * kSms);
 }
 
+template <int TY, int NV, bool VEC, bool MANY, int WARPS>
+bool launch_grad(GradParams p, const GradShape& g, int parts, cudaStream_t st) {
+  const int slot = RowPart<TY, NV, VEC>::slot_bytes(g.warps * 32) * g.groups, weights = g.warps * 32 * 8 * NV * (int)sizeof(float);
+  p.ds_ahead = p.ds && residents(g.threads, g.threads, 3 * slot, weights).stages > 0;               // (not for fp32 rows beyond 6144)
+  const int bytes = (p.ds_ahead ? 3 : 2) * slot;
+  const Residents r = residents(g.threads, g.per_sm * g.threads, bytes, weights);
+  static_assert(kRingBytes - 2048 >= 4 * (kGradMostWarps * 768 * 4 + 32) + kGradMostWarps * 768 * 4, "two stages of two rows");
+  const size_t smem = std::max((size_t)r.stages * bytes + weights, g.groups == 1 ? 0 : (size_t)g.groups * 2 * p.width * sizeof(float));
+  const auto kernel = row_grad_kernel<TY, NV, VEC, MANY, WARPS>;
+  return allow_ring(kernel, smem) && launch(kernel, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
+}
 template <int TY, bool VEC>
 bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
   const GradShape g = grad_shape(p.width);
-  const int bytes = RowPart<TY, 1, VEC>::slot_bytes(p.width) * (p.ds ? 3 : 2) * g.groups;
-  const Residents r = residents(g.threads, g.most, bytes);       // (at least two stages: 3 x 32 KB at the most)
-  const size_t smem = std::max((size_t)r.stages * bytes, g.groups == 1 ? 0 : (size_t)g.groups * 2 * p.width * sizeof(float));
-  const auto kernel = g.warps <= kGradWarps ? row_grad_kernel<TY, VEC, kGradWarps * 32> : row_grad_kernel<TY, VEC, 1024>;
-  return allow_ring(kernel, smem) && launch(kernel, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
+  if (g.warps == 1) {
+    return g.pieces == 1 ? launch_grad<TY, 1, VEC, false, kGradWarps>(p, g, parts, st)
+           : g.pieces == 2 ? launch_grad<TY, 2, VEC, false, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, false, kGradWarps>(p, g, parts, st);
+  }
+  if (g.warps <= kGradWarps) return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradWarps>(p, g, parts, st);
+  return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradMostWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);
 }
 
 template <int TY>
@@ -564,7 +651,7 @@ __global__ void __launch_bounds__(kColThreads) column_max_kernel(const __grid_co
   const int chunk = (int)(blockIdx.x % p.chunks);
   const long long from = p.rows * chunk / p.chunks, to = p.rows * (chunk + 1) / p.chunks;
   uint32_t m[8] = {};
-#pragma unroll 4
+#pragma unroll 8
   for (long long row = from + warp; row < to; row += kColThreads / 32) {
     const char* x = p.x + row * p.stride * kBytes;
     if constexpr (VEC) {
@@ -594,8 +681,11 @@ __global__ void __launch_bounds__(kColThreads) column_max_kernel(const __grid_co
 
 template <int TY, bool VEC>
 __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_constant__ ColumnParams p, int row_tiles) {
+  __shared__ uint32_t most[kColThreads / kTileCols][kTileCols];
   __shared__ float per[kTileCols];
-  __shared__ __align__(16) uint32_t tile[kTileCols][kTileRows / 4 + 4];     // a column's bytes, rows 16 apart in banks
+  // a column's bytes; the words of columns that a warp writes at a time are swapped so that they fall into different banks
+  __shared__ __align__(16) uint32_t tile[kTileCols][kTileRows / 4];
+  const auto swap = [](int c) { return (VEC ? c >> 3 : c) & 7; };
   wait_for_previous_launch();
   constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
   const long long first = (long long)(blockIdx.x / row_tiles) * kTileCols;
@@ -605,33 +695,43 @@ __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_
   const int quad = warp * 4 + lane / 8;                                      // 32 groups of 4 rows
   const int c0 = VEC ? lane % 8 * 8 : lane % 8;
   float v[4][8];
+  const int rows_left = (int)min((long long)4, p.rows - top - quad * 4), columns_left = (int)min((long long)kTileCols, p.width - first) - c0;
+  const char* x = p.x + ((top + quad * 4) * p.stride + first + c0) * kBytes;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const long long row = top + quad * 4 + i;
-    const char* x = p.x + row * p.stride * kBytes;
+  for (int i = 0; i < 4; ++i, x += p.stride * kBytes) {
     if constexpr (VEC) {
       Raw8<TY> raw = {};
-      if (row < p.rows && first + c0 < p.width) raw = load_raw8<TY>(x + (first + c0) * kBytes);
+      if (i < rows_left && columns_left > 0) raw = load_raw8<TY>(x);
       raw8_to_floats<TY>(raw, v[i]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = row < p.rows && first + c0 + 8 * k < p.width ? load_one<TY>(x, first + c0 + 8 * k) : 0.0f;
+      for (int k = 0; k < 8; ++k) v[i][k] = i < rows_left && 8 * k < columns_left ? load_one<TY>(x, 8 * k) : 0.0f;
     }
   }
-  if (threadIdx.x < kTileCols && first + threadIdx.x < p.width) {
+  const int mine = threadIdx.x % kTileCols;
+  if (first + mine < p.width) {
+    constexpr int kShare = kColThreads / kTileCols;
     uint32_t m = 0u;
-    for (int i = 0; i < p.chunks; ++i) m = max(m, p.largest[(size_t)i * p.width + first + threadIdx.x]);
-    const ByteScale s = byte_scale(m);
+    const uint32_t* from = p.largest + (size_t)(threadIdx.x / kTileCols) * p.width + first + mine;
+#pragma unroll 8
+    for (int chunk = threadIdx.x / kTileCols; chunk < p.chunks; chunk += kShare, from += (size_t)kShare * p.width) m = max(m, *from);
+    most[threadIdx.x / kTileCols][mine] = m;
+  }
+  __syncthreads();
+  if (threadIdx.x < kTileCols && first + threadIdx.x < p.width) {
+    const ByteScale s = byte_scale(max(max(most[0][threadIdx.x], most[1][threadIdx.x]), max(most[2][threadIdx.x], most[3][threadIdx.x])));
     per[threadIdx.x] = s.per;
     if (top == 0) p.scale[first + threadIdx.x] = s.worth;
   }
   __syncthreads();
+  uint32_t* to = &tile[c0][quad ^ swap(c0) << 2];            // (the same swap for all columns of a thread)
+  constexpr int kNext = VEC ? 1 : 8;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int c = VEC ? c0 + k : c0 + 8 * k;
-    if (first + c < p.width) {
-      const float f = per[c];
-      tile[c][quad] = four_bytes(to_byte(v[0][k], f), to_byte(v[1][k], f), to_byte(v[2][k], f), to_byte(v[3][k], f));
+    if (k * kNext < columns_left) {
+      const float f = per[c0 + k * kNext];
+      const uint32_t bytes = to_bytes(make_float2(v[0][k], v[1][k]), make_float2(v[2][k], v[3][k]), f);
+      to[k * kNext * (kTileRows / 4)] = f > 0.0f ? bytes : 0u;
     }
   }
   __syncthreads();
@@ -640,13 +740,13 @@ __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_
     const int c = i / (kTileRows / 16), part = i % (kTileRows / 16);
     const long long row = top + part * 16;
     if (first + c < p.width && row < p.rows)
-      *reinterpret_cast<uint4*>(p.q + (first + c) * p.q_stride + row) = *reinterpret_cast<const uint4*>(&tile[c][part * 4]);
+      *reinterpret_cast<uint4*>(p.q + (first + c) * p.q_stride + row) = *reinterpret_cast<const uint4*>(&tile[c][(part ^ swap(c)) * 4]);
   }
 }
 
 int column_chunks(long long rows, long long width) {
   const long long strips = (width + 255) / 256;
-  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 32, 4 * kSms / strips}));
+  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 64, (2 * kSms + strips - 1) / strips}));
 }
 
 template <int TY, bool VEC>
@@ -708,6 +808,11 @@ constexpr int64_t kMostRows = (int64_t)1 << 31, kMostWidth = (int64_t)1 << 24;
 bool bad_rows(int64_t rows, int64_t width) { return rows < 0 || rows >= kMostRows || width < 1 || width > kMostWidth; }
 bool bad_stride(int64_t stride, int64_t width) { return stride < width || stride > (int64_t)1 << 40; }
 bool whole(int64_t width, int type) { return width * type_bytes(type) % 16 == 0; }               // pieces of 16 bytes
+// What a row's parameters may be read as (see RowParams): vec: they have to begin on 16 bytes for it.
+int alike_type(const void* w, int w_type, const void* b, int b_type, bool vec) {
+  if (!w || (b && b_type != w_type) || (vec && (!is_aligned(w, 16) || !is_aligned(b, 16)))) return kAnyType;
+  return w_type;
+}
 bool on16(const void* p, int64_t stride, int type) { return is_aligned(p, 16) && stride * type_bytes(type) % 16 == 0; }
 
 }  // namespace
@@ -734,8 +839,8 @@ int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* 
   RowParams p = {};
   p.x = static_cast<const char*>(x); p.x_stride = x_stride;
   p.r = static_cast<const char*>(residual); p.r_stride = residual_stride;
-  p.w = weight; p.w_type = weight_type; p.w_vec = is_aligned(weight, 16);
-  p.b = bias; p.b_type = bias_type; p.b_vec = is_aligned(bias, 16);
+  p.w = weight; p.w_type = weight_type;
+  p.b = bias; p.b_type = bias_type;
   p.sum = static_cast<char*>(sum); p.sum_stride = sum_stride;
   p.out = static_cast<char*>(out); p.out_stride = out_stride;
   p.mean = mean; p.rstd = rstd;
@@ -743,6 +848,7 @@ int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* 
   p.rows = rows; p.width = (int)width; p.normed = 1; p.eps = eps;
   const bool vec = whole(width, type) && on16(x, x_stride, type) && (!residual || (on16(residual, residual_stride, type) && on16(sum, sum_stride, type))) &&
                    (!out || on16(out, out_stride, type));
+  p.alike = alike_type(weight, weight_type, bias, bias_type, vec);
   return enqueue_rows(p, type, vec, static_cast<cudaStream_t>(stream));
 }
 
@@ -757,10 +863,12 @@ int qadam_quantize_rows(const void* x, int32_t type, int64_t x_stride, const flo
   if (rows == 0) return QADAM_OK;
   RowParams p = {};
   p.x = static_cast<const char*>(x); p.x_stride = x_stride;
-  p.w = columns; p.w_type = QADAM_F32; p.w_vec = is_aligned(columns, 16);
+  p.w = columns; p.w_type = QADAM_F32;
   p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride; p.scale = scale; p.sums = sums;
   p.rows = rows; p.width = (int)width;
-  return enqueue_rows(p, type, whole(width, type) && on16(x, x_stride, type), static_cast<cudaStream_t>(stream));
+  const bool vec = whole(width, type) && on16(x, x_stride, type);
+  p.alike = alike_type(columns, QADAM_F32, nullptr, 0, vec);
+  return enqueue_rows(p, type, vec, static_cast<cudaStream_t>(stream));
 }
 
 int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes) {
@@ -795,7 +903,7 @@ int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const
     p.ds = static_cast<const char*>(dsum); p.ds_stride = dsum_stride;
     p.dx = static_cast<char*>(dx); p.dx_stride = dx_stride;
     p.mean = mean; p.rstd = rstd;
-    p.w = weight; p.w_type = weight_type; p.w_vec = is_aligned(weight, 16);
+    p.w = weight; p.w_type = weight_type;
     p.partial = sums ? static_cast<float*>(workspace) : nullptr;
     p.rows = rows; p.width = (int)width;
     const bool vec = whole(width, type) && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&

@@ -202,53 +202,85 @@ class RowGroup {
   int warps_, barrier_, turn_ = 0;
 };
 
-// How a row's elements are dealt out, 8 NV to each of a group's threads, in pairs.  VEC: in pieces of 16 bytes; else one by one, a
-// group's width apart.  An element beyond the row reads as zero.
+// How a row's elements are dealt out, 8 NV to each of a group's threads, in pairs: a warp has 256 NV elements in a row, its lanes take
+// turns with pieces of 16 bytes (VEC), or with elements.  So the distances between a thread's pieces are known when the kernel is
+// compiled, and whether one is in the row is a comparison with a constant.  An element beyond the row reads as zero.
 template <int TY, int NV, bool VEC>
 struct RowPart {
   static constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
   static constexpr int kPiece = VEC ? 16 / kBytes : 1;     // consecutive elements
   static constexpr int kPieces = 8 * NV / kPiece;
   static constexpr int kPairs = 4 * NV;
+  static constexpr int kStep = VEC ? 1 : 2;                // pieces that hold whole pairs
+  static constexpr int kStepPairs = VEC ? kPiece / 2 : 1;
   using Row = float2[kPairs];
 
   int width, threads, t;
-  unsigned live;                                           // bits of the pieces that are in the row
-  __device__ __forceinline__ RowPart(int w, int n, int i) : width(w), threads(n), t(i), live(0u) {
-#pragma unroll
-    for (int q = 0; q < kPieces; ++q) live |= (unsigned)(column(q) < w) << q;
+  int first, left;                                         // column of the first piece; from there to the row's end
+  __device__ __forceinline__ RowPart(int w, int n, int i) : width(w), threads(n), t(i) {
+    first = i / 32 * (256 * NV) + i % 32 * kPiece;
+    left = w - first;
   }
-  __device__ __forceinline__ int column(int q) const { return (q * threads + t) * kPiece; }           // a piece's first
-  __device__ __forceinline__ bool has(int q) const { return live >> q & 1u; }
+  __device__ __forceinline__ int column(int q) const { return first + q * 32 * kPiece; }             // a piece's first
+  __device__ __forceinline__ bool has(int q) const { return q * 32 * kPiece < left; }
   __device__ __forceinline__ static constexpr int piece_of(int e) { return e / kPiece; }
 
   // from global or shared memory
   __device__ __forceinline__ void read(const void* row, Row& x) const {
+    const char* from = static_cast<const char*>(row) + (long long)first * kBytes;
     if constexpr (VEC) {
       uint4 r[kPieces];
 #pragma unroll
-      for (int q = 0; q < kPieces; ++q) r[q] = has(q) ? static_cast<const uint4*>(row)[q * threads + t] : make_uint4(0u, 0u, 0u, 0u);
+      for (int q = 0; q < kPieces; ++q) r[q] = has(q) ? *reinterpret_cast<const uint4*>(from + q * 512) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
       for (int q = 0; q < kPieces; ++q) unpack(r[q], &x[q * kPiece / 2]);
     } else {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        x[i].x = has(2 * i) ? load_one<TY>(row, column(2 * i)) : 0.0f;
-        x[i].y = has(2 * i + 1) ? load_one<TY>(row, column(2 * i + 1)) : 0.0f;
+        x[i].x = has(2 * i) ? load_one<TY>(from, 64 * i) : 0.0f;
+        x[i].y = has(2 * i + 1) ? load_one<TY>(from, 64 * i + 32) : 0.0f;
       }
     }
   }
   __device__ __forceinline__ void store(void* row, const Row& x) const {
+    char* to = static_cast<char*>(row) + (long long)first * kBytes;
     if constexpr (VEC) {
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (has(q)) static_cast<uint4*>(row)[q * threads + t] = packed(&x[q * kPiece / 2]);
+        if (has(q)) *reinterpret_cast<uint4*>(to + q * 512) = packed(&x[q * kPiece / 2]);
     } else {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        if (has(2 * i)) store_one<TY>(row, column(2 * i), x[i].x);
-        if (has(2 * i + 1)) store_one<TY>(row, column(2 * i + 1), x[i].y);
+        if (has(2 * i)) store_one<TY>(to, 64 * i, x[i].x);
+        if (has(2 * i + 1)) store_one<TY>(to, 64 * i + 32, x[i].y);
       }
+    }
+  }
+  // Piece q of a row in shared memory (see slot_bytes; `row`: where it lies in global memory), and its counterpart in global memory.  (The
+  // pair of elements of q and q + 1, where a piece is one element.)
+  __device__ __forceinline__ void read_piece(const uint8_t* slot, const char* row, int q, float2* x) const {
+    if constexpr (VEC) {
+      unpack(*reinterpret_cast<const uint4*>(slot + first * kBytes + q * 512), x);
+    } else {
+      const uint8_t* from = slot + (reinterpret_cast<uintptr_t>(row) & 15u) + first * kBytes;
+      x[0] = make_float2(load_one<TY>(from, 32 * q), load_one<TY>(from, 32 * q + 32));
+    }
+  }
+  __device__ __forceinline__ void load_piece(const char* row, int q, float2* x) const {
+    const char* from = row + (long long)first * kBytes;
+    if constexpr (VEC) {
+      unpack(has(q) ? *reinterpret_cast<const uint4*>(from + q * 512) : make_uint4(0u, 0u, 0u, 0u), x);
+    } else {
+      x[0] = make_float2(has(q) ? load_one<TY>(from, 32 * q) : 0.0f, has(q + 1) ? load_one<TY>(from, 32 * q + 32) : 0.0f);
+    }
+  }
+  __device__ __forceinline__ void store_piece(char* row, int q, const float2* x) const {
+    char* to = row + (long long)first * kBytes;
+    if constexpr (VEC) {
+      if (has(q)) *reinterpret_cast<uint4*>(to + q * 512) = packed(x);
+    } else {
+      if (has(q)) store_one<TY>(to, 32 * q, x[0].x);
+      if (has(q + 1)) store_one<TY>(to, 32 * q + 32, x[0].y);
     }
   }
   // x becomes what is stored.
@@ -257,62 +289,87 @@ struct RowPart {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) x[i] = make_float2(rounded<TY>(x[i].x), rounded<TY>(x[i].y));
   }
-  // Parameters of any type; on16: they begin on 16 bytes.
-  __device__ __forceinline__ void read_parameters(const void* p, int type, bool on16, int q, float2* x) const {
+  // Parameters of one type, beginning on 16 bytes if VEC, of piece q (and the next one, where a piece is one element).
+  template <int PT>
+  __device__ __forceinline__ void read_parameters(const void* p, int q, float2* x) const {
+    const char* from = static_cast<const char*>(p) + (long long)column(q) * (PT == QADAM_F32 ? 4 : 2);
     if constexpr (VEC) {
       if (!has(q)) return;
-      const int col = column(q);
 #pragma unroll
       for (int k = 0; k < kPiece; k += 4) {
-        float y[4];
-        if (!on16) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = load_one_of(p, type, col + k + i);
-        } else if (type == QADAM_F32) {
-          const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + col + k);
-          y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w;
+        if constexpr (PT == QADAM_F32) {
+          const float4 v = *reinterpret_cast<const float4*>(from + 4 * k);
+          x[k / 2] = make_float2(v.x, v.y);
+          x[k / 2 + 1] = make_float2(v.z, v.w);
         } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const unsigned short*>(p) + col + k);
-          to_floats(Raw4{{v.x, v.y, 0u, 0u}}, type, y);
+          const uint2 v = *reinterpret_cast<const uint2*>(from + 2 * k);
+          float y[4];
+          to_floats(Raw4{{v.x, v.y, 0u, 0u}}, PT, y);
+          x[k / 2] = make_float2(y[0], y[1]);
+          x[k / 2 + 1] = make_float2(y[2], y[3]);
         }
-        x[k / 2] = make_float2(y[0], y[1]);
-        x[k / 2 + 1] = make_float2(y[2], y[3]);
       }
-    } else {                                               // two pieces: a pair
-      if (has(q)) x[0].x = load_one_of(p, type, column(q));
-      if (has(q + 1)) x[0].y = load_one_of(p, type, column(q + 1));
+    } else {
+      if (has(q)) x[0].x = load_one<PT>(from, 0);
+      if (has(q + 1)) x[0].y = load_one<PT>(from, 32);
     }
   }
-  static constexpr int kStep = VEC ? 1 : 2;                // pieces that hold whole pairs
-  static constexpr int kStepPairs = VEC ? kPiece / 2 : 1;
+  // Parameters of any type, anywhere.
+  __device__ __forceinline__ void read_any(const void* p, int type, int q, float2* x) const {
+#pragma unroll
+    for (int k = 0; k < kStep * kPiece; ++k) {
+      const int at = VEC ? column(q) + k : column(q + k);
+      if (has(VEC ? q : q + k)) (k % 2 ? x[k / 2].y : x[k / 2].x) = load_one_of(p, type, at);
+    }
+  }
 
-  // ---- a row in shared memory: its bytes, as far from 16 as in memory
-  __host__ __device__ static constexpr int slot_bytes(int width) { return (width * kBytes + 15) / 16 * 16 + (VEC ? 0 : 16); }
+  // ---- a row in shared memory: its bytes, as far from 16 as in memory, then zeros for all the group's threads (who clear the place
+  // once; a copy clears what a row that lay further behind may have left)
+  __host__ __device__ static constexpr int slot_bytes(int threads) { return threads * 8 * NV * kBytes + (VEC ? 0 : 32); }
 
   // Copies a row behind the threads' backs: what is whole pieces of 16 bytes in memory asynchronously, what is left at its ends
   // by the first threads' own hands.  VEC: a thread copies what it will read.
   __device__ __forceinline__ void fetch(uint8_t* slot, const char* row) const {
     const unsigned at = (unsigned)__cvta_generic_to_shared(slot);
     if constexpr (VEC) {
+      const char* from = row + (long long)first * kBytes;
+      const unsigned to = at + (unsigned)(first * kBytes);
 #pragma unroll
-      for (int q = 0; q < kPieces; ++q) {
-        const unsigned piece = (unsigned)(q * threads + t) * 16u;
-        if (has(q)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + piece), "l"(row + piece) : "memory");
-      }
+      for (int q = 0; q < kPieces; ++q)
+        if (has(q)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + q * 512u), "l"(from + q * 512) : "memory");
     } else {
       const int bytes = width * kBytes, phase = (int)(reinterpret_cast<uintptr_t>(row) & 15u);
       const int head = min((16 - phase) & 15, bytes), body = (bytes - head) >> 4, tail = bytes - head - body * 16;
-      for (int i = t; i < body; i += threads)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (unsigned)(phase + head + i * 16)), "l"(row + head + i * 16) : "memory");
-      if (t < (head + tail) / kBytes) {
-        const int i = t < head / kBytes ? t : t + body * (16 / kBytes);
-        if constexpr (TY == QADAM_F32) *reinterpret_cast<uint32_t*>(slot + phase + i * 4) = reinterpret_cast<const uint32_t*>(row)[i];
-        else *reinterpret_cast<unsigned short*>(slot + phase + i * 2) = reinterpret_cast<const unsigned short*>(row)[i];
+      const unsigned to = at + (unsigned)(phase + head + t * 16);
+      const char* from = row + head + t * 16;
+#pragma unroll
+      for (int q = 0; q < (8 * NV * kBytes + 15) / 16; ++q)
+        if (q * threads + t < body)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (unsigned)(q * threads * 16)), "l"(from + q * threads * 16) : "memory");
+      const int ends = (head + tail) / kBytes;
+      if (t < ends + 16 / kBytes) {                        // behind the row: zeros
+        const int i = t < head / kBytes ? t : t < ends ? t + body * (16 / kBytes) : width + t - ends;
+        if constexpr (TY == QADAM_F32) *reinterpret_cast<uint32_t*>(slot + phase + i * 4) = t < ends ? reinterpret_cast<const uint32_t*>(row)[i] : 0u;
+        else *reinterpret_cast<unsigned short*>(slot + phase + i * 2) = t < ends ? reinterpret_cast<const unsigned short*>(row)[i] : (unsigned short)0;
       }
     }
   }
   __device__ __forceinline__ void read_slot(const uint8_t* slot, const char* row, Row& x) const {
-    read(VEC ? slot : slot + (reinterpret_cast<uintptr_t>(row) & 15u), x);
+#pragma unroll
+    for (int q = 0; q < kPieces; q += kStep) read_piece(slot, row, q, &x[q / kStep * kStepPairs]);
+  }
+  // Binary32 parameters in shared memory, one for each element that the group's threads have.
+  __device__ __forceinline__ void read_shared(const float* p, int q, float2* x) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + column(q) + k);
+        x[k / 2] = make_float2(v.x, v.y);
+        x[k / 2 + 1] = make_float2(v.z, v.w);
+      }
+    } else {
+      x[0] = make_float2(p[column(q)], p[column(q + 1)]);
+    }
   }
 
  private:
@@ -344,6 +401,15 @@ __device__ __forceinline__ void wait_fetched(int left) {
   if (left == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
   else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// Clears n bytes (a multiple of 16) of shared memory with all of a CTA's threads.
+__device__ __forceinline__ void clear_shared(uint8_t* p, int n) {
+  for (int i = threadIdx.x * 16; i < n; i += blockDim.x * 16) *reinterpret_cast<uint4*>(p + i) = make_uint4(0u, 0u, 0u, 0u);
+}
+// A row of parameters as binary32, zeros from its width on up to n; `without`: what stands for parameters that there are none of.
+__device__ __forceinline__ void fill_parameters(float* to, const void* p, int type, float without, int width, int n) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) to[i] = i >= width ? 0.0f : p ? load_one_of(p, type, i) : without;
 }
 
 // Rows in 8 bits: a = max(largest |x|, 2^-100), q = rne(x fl(127 / a)), worth a / 127.  `largest`: the bits of the largest
