@@ -41,6 +41,7 @@ struct RowParams {
   int* sums;
   long long rows;
   int width;
+  float per;                                               // 1 / width
   int normed;                                              // 0: the rows are quantized as they are (times w, if given)
   float eps;
 };
@@ -85,21 +86,21 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
     float2 s = h[0];
 #pragma unroll
     for (int i = 1; i < Part::kPairs; ++i) s = add2_rn(s, h[i]);
-    const float mean = group.add(s.x + s.y) / (float)p.width;
+    const float mean = group.add(s.x + s.y) * p.per;
     const float2 less = make_float2(-mean, -mean);
+#pragma unroll
+    for (int i = 0; i < Part::kPairs; ++i) h[i] = add2_rn(h[i], less);
+    if (!part.all) {
+#pragma unroll
+      for (int i = 0; i < Part::kPairs; ++i) {
+        if (!part.has(Part::piece_of(2 * i))) h[i].x = 0.0f;
+        if (!part.has(Part::piece_of(2 * i + 1))) h[i].y = 0.0f;
+      }
+    }
     s = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int i = 0; i < Part::kPairs; ++i) {
-      h[i] = add2_rn(h[i], less);
-      if constexpr (VEC) {
-        if (!part.has(Part::piece_of(2 * i))) h[i] = make_float2(0.0f, 0.0f);
-      } else {
-        if (!part.has(2 * i)) h[i].x = 0.0f;
-        if (!part.has(2 * i + 1)) h[i].y = 0.0f;
-      }
-      s = fma2_rn(h[i], h[i], s);
-    }
-    const float rstd = 1.0f / sqrtf(group.add(s.x + s.y) / (float)p.width + p.eps);
+    for (int i = 0; i < Part::kPairs; ++i) s = fma2_rn(h[i], h[i], s);
+    const float rstd = rsqrtf(fmaf(group.add(s.x + s.y), p.per, p.eps));           // (off by at most 2 in its last place)
     if (part.t == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
@@ -108,7 +109,7 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
     for (int i = 0; i < Part::kPairs; ++i) h[i] = mul2_rn(h[i], make_float2(rstd, rstd));
   }
   if (p.w || p.b) {
-    if (MANY && shared) {
+    if (shared) {
       scale_and_shift<kShared>(p, part, shared, h);
     } else {
       switch (p.alike) {                                   // (told apart once, not for each element)
@@ -178,18 +179,18 @@ __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_
   finish_row(p, part, group, row, nullptr, h);
 }
 
-// Wider rows: a group of warps goes from row to row, with the next ones under way.
+// Wider rows, and many: a group of warps (a warp) goes from row to row, with the next ones under way.
 constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
-template <int TY, int NV, bool VEC, int MOST>
+template <int TY, int NV, bool VEC, bool MANY, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages, int with_parameters) {
   extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][1 or 2][a row]; with_parameters: then w, b
   __shared__ GroupShared shared[kGroupWarps];
   wait_for_previous_launch();
   using Part = RowPart<TY, NV, VEC>;
-  const int threads = warps * 32, number = (int)threadIdx.x / threads;
+  const int threads = MANY ? warps * 32 : 32, number = (int)threadIdx.x / threads;
   const int groups = blockDim.x / threads;
   const Part part(p.width, threads, (int)threadIdx.x % threads);
-  RowGroup<true> group(&shared[number], warps, number);
+  RowGroup<MANY> group(&shared[number], warps, number);
   const int each = Part::slot_bytes(threads), both = p.r ? 2 * each : each;
   uint8_t* ring = slots + number * stages * both;
   float* parameters = with_parameters ? reinterpret_cast<float*>(slots + groups * stages * both) : nullptr;
@@ -245,13 +246,13 @@ __global__ void __launch_bounds__(kWideThreads) wide_row_kernel(const __grid_con
   if (p.normed) {
     float s = 0.0f;
     for (int col = threadIdx.x; col < p.width; col += kWideThreads) s += element(col);
-    mean = group.add(s) / (float)p.width;
+    mean = group.add(s) * p.per;
     s = 0.0f;
     for (int col = threadIdx.x; col < p.width; col += kWideThreads) {
       const float d = element(col) - mean;
       s = fmaf(d, d, s);
     }
-    rstd = 1.0f / sqrtf(group.add(s) / (float)p.width + p.eps);
+    rstd = rsqrtf(fmaf(group.add(s), p.per, p.eps));
     if (threadIdx.x == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
@@ -283,12 +284,6 @@ __global__ void __launch_bounds__(kWideThreads) wide_row_kernel(const __grid_con
   }
 }
 
-template <int TY, int NV>
-bool launch_warp_rows(const RowParams& p, bool vec, cudaStream_t st) {
-  const long long grid = (p.rows + kWarpRowThreads / 32 - 1) / (kWarpRowThreads / 32);
-  return vec ? launch(warp_row_kernel<TY, NV, true>, grid, kWarpRowThreads, 0, 0, st, p) : launch(warp_row_kernel<TY, NV, false>, grid, kWarpRowThreads, 0, 0, st, p);
-}
-
 // CTAs of `threads` threads that an SM has at a time (of most_threads), and stages of `bytes`, with `besides` of their own, that each of
 // them has then: 2 or 3, or none if two do not fit.
 struct Residents {
@@ -306,7 +301,7 @@ bool allow_ring(K kernel, size_t bytes) {
   return bytes <= 40 * 1024 || cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes));
 }
 
-template <int TY, int NV, bool VEC>
+template <int TY, int NV, bool VEC, bool MANY>
 bool launch_group_rows(const RowParams& p, cudaStream_t st) {
   const int warps = (p.width + 256 * NV - 1) / (256 * NV), groups = std::max(1, kGroupWarps / warps);
   const int threads = warps * groups * 32, bytes = RowPart<TY, NV, VEC>::slot_bytes(warps * 32) * (p.r ? 2 : 1) * groups;
@@ -315,14 +310,24 @@ bool launch_group_rows(const RowParams& p, cudaStream_t st) {
   const int kept = parameters * 4 <= kRingBytes / std::max(1, kGroupMostThreads / threads) ? parameters : 0;
   const Residents r = residents(threads, kGroupMostThreads, bytes, kept);
   if (r.stages == 0) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
-  const auto kernel = threads <= 256 ? group_row_kernel<TY, NV, VEC, 256> : group_row_kernel<TY, NV, VEC, 512>;
+  const auto kernel = !MANY ? group_row_kernel<TY, NV, VEC, false, 256> : threads <= 256 ? group_row_kernel<TY, NV, VEC, true, 256> : group_row_kernel<TY, NV, VEC, true, 512>;
   const size_t smem = (size_t)r.stages * bytes + kept;
   return allow_ring(kernel, smem) &&
          launch(kernel, std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm), threads, smem, 0, st, p, warps, r.stages, kept ? 1 : 0);
 }
 template <int TY, int NV>
 bool launch_group_rows(const RowParams& p, bool vec, cudaStream_t st) {
-  return vec ? launch_group_rows<TY, NV, true>(p, st) : launch_group_rows<TY, NV, false>(p, st);
+  return vec ? launch_group_rows<TY, NV, true, true>(p, st) : launch_group_rows<TY, NV, false, true>(p, st);
+}
+
+// Rows of a warp: each its own, until there are so many that an SM's warps would do several one after the other: then they go from row
+// to row (65536 x 768 bf16: a warp for each 46 us).
+constexpr long long kManyRows = 4 * kSms * (kGroupMostThreads / 32);
+template <int TY, int NV>
+bool launch_warp_rows(const RowParams& p, bool vec, cudaStream_t st) {
+  if (p.rows >= kManyRows) return vec ? launch_group_rows<TY, NV, true, false>(p, st) : launch_group_rows<TY, NV, false, false>(p, st);
+  const long long grid = (p.rows + kWarpRowThreads / 32 - 1) / (kWarpRowThreads / 32);
+  return vec ? launch(warp_row_kernel<TY, NV, true>, grid, kWarpRowThreads, 0, 0, st, p) : launch(warp_row_kernel<TY, NV, false>, grid, kWarpRowThreads, 0, 0, st, p);
 }
 
 template <int TY>
@@ -368,13 +373,16 @@ struct GradParams {
   int width;
 };
 
+// Warps of an SM that there are registers for.
+__host__ __device__ constexpr int grad_warps_of_sm(int nv, bool many) { return many && nv == 2 ? 18 : 12; }
+
 // A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
 // weight's and bias's gradients in registers; the CTA's sums go to the workspace.  One read, one write: bound by HBM.
 // A row is read from shared memory twice, before and behind its sums: held in registers between, it would leave room for half as
 // many rows on an SM.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
 // row, not for elements.)
 template <int TY, int NV, bool VEC, bool MANY, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, kGradMostWarps / WARPS) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
+__global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
   extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][2 or 3][a row], w; at the end the groups' sums [groups][2][width]
   __shared__ GroupShared shared[MANY ? kGradWarps : 1];
   wait_for_previous_launch();
@@ -538,32 +546,30 @@ __global__ void __launch_bounds__(256) wide_column_grad_kernel(const __grid_cons
   part[p.width + col] = db;
 }
 
-// The CTAs' sums joined, in an order that the sizes fix: 32 columns to a CTA, the partial sums dealt out to its warps.
-constexpr int kJoinWarps = 32;
+// The CTAs' sums joined, in an order that the sizes fix: 32 columns of either sum to a CTA, the parts dealt out to its warps, who
+// ask for ten at a time.
+constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float* partial, int parts, int width, void* dw, void* db, int type,
                                                                    int accumulate) {
-  __shared__ float sum[kJoinWarps][2][32];
+  __shared__ float sum[kJoinWarps][32];
   wait_for_previous_launch();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int col = blockIdx.x * 32 + lane;
-  float a = 0.0f, b = 0.0f;
+  const int tiles = (width + 31) / 32, which = (int)blockIdx.x / tiles;
+  const int col = ((int)blockIdx.x - which * tiles) * 32 + lane;
+  void* to = which == 0 ? dw : db;
+  if (!to) return;
+  float a = 0.0f;
   if (col < width) {
-    const float* part = partial + (size_t)warp * 2 * width + col;
+    const float* part = partial + ((size_t)warp * 2 + which) * width + col;
 #pragma unroll 10
-    for (int i = warp; i < parts; i += kJoinWarps, part += (size_t)kJoinWarps * 2 * width) {
-      a += part[0];
-      b += part[width];
-    }
+    for (int i = warp; i < parts; i += kJoinWarps, part += (size_t)kJoinWarps * 2 * width) a += *part;
   }
-  sum[warp][0][lane] = a;
-  sum[warp][1][lane] = b;
+  sum[warp][lane] = a;
   __syncthreads();
-  if (warp >= 2 || col >= width) return;
+  if (warp > 0 || col >= width) return;
   float s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kJoinWarps; ++i) s += sum[i][warp][lane];
-  void* to = warp == 0 ? dw : db;
-  if (!to) return;
+  for (int i = 0; i < kJoinWarps; ++i) s += sum[i][lane];
   store_one_of(to, type, col, accumulate ? load_one_of(to, type, col) + s : s);
 }
 
@@ -572,24 +578,20 @@ struct GradShape {
   int pieces;                                              // NV of the kernel: 8 elements each
   int warps, groups, threads, per_sm;
 };
-GradShape grad_shape(int width) {
+GradShape grad_shape(int width, bool vec) {
   GradShape g;
-  // 16 or 24 elements to a thread, whichever leaves fewer threads without (8 where a warp has enough with that)
-  const int two = (width + 511) / 512, three = (width + 767) / 768;
-  g.pieces = width <= 256 ? 1 : two * 512 < three * 768 ? 2 : 3;
-  g.warps = g.pieces == 1 ? 1 : g.pieces == 2 ? two : three;
-  if (g.warps > kGradMostWarps) {                          // (two pieces, beyond 6144)
-    g.pieces = 3;
-    g.warps = three;
-  }
+  // Rows of a warp: 8, 16 or 24 elements to a thread.  Wider ones: 16, and so more warps on an SM (30012 x 2048 fp32: 121 us, with 24 147),
+  // but 24 where elements are taken one by one and a row's ends cost more (30011 x 2049 fp32: 194 us, with 16 222), and beyond 6144.
+  g.pieces = width <= 768 ? (width + 255) / 256 : vec && width <= kGradMostWarps * 512 ? 2 : 3;
+  g.warps = (width + 256 * g.pieces - 1) / (256 * g.pieces);
   g.groups = std::max(1, kGradWarps / g.warps);
   g.threads = g.warps * g.groups * 32;
-  g.per_sm = g.threads <= kGradWarps * 32 ? 2 : 1;
+  g.per_sm = std::max(1, grad_warps_of_sm(g.pieces, g.warps > 1) * 32 / g.threads);
   return g;
 }
-int grad_parts(long long rows, int width) {
+int grad_parts(long long rows, int width, bool vec) {
   if (width > kGradGroupWidth) return (int)std::min<long long>(rows, std::max(1, 4 * kSms * 256 / width));
-  const GradShape g = grad_shape(width);
+  const GradShape g = grad_shape(width, vec);
   return (int)std::min<long long>((rows + g.groups - 1) / g.groups, g.per_sm * kSms);
 }
 
@@ -606,13 +608,17 @@ bool launch_grad(GradParams p, const GradShape& g, int parts, cudaStream_t st) {
 }
 template <int TY, bool VEC>
 bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
-  const GradShape g = grad_shape(p.width);
+  const GradShape g = grad_shape(p.width, VEC);
   if (g.warps == 1) {
     return g.pieces == 1 ? launch_grad<TY, 1, VEC, false, kGradWarps>(p, g, parts, st)
            : g.pieces == 2 ? launch_grad<TY, 2, VEC, false, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, false, kGradWarps>(p, g, parts, st);
   }
-  if (g.warps <= kGradWarps) return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradWarps>(p, g, parts, st);
-  return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradMostWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);
+  if constexpr (VEC) {
+    if (g.warps <= kGradWarps) return launch_grad<TY, 2, VEC, true, kGradWarps>(p, g, parts, st);
+    return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradMostWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);
+  } else {
+    return g.warps <= kGradWarps ? launch_grad<TY, 3, VEC, true, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);
+  }
 }
 
 template <int TY>
@@ -628,7 +634,7 @@ bool enqueue_grad_of(const GradParams& p, int parts, bool vec, cudaStream_t st) 
 // first has read, as long as it is not larger than that.
 constexpr int kColThreads = 256;
 constexpr int kColMaxChunks = 64;
-constexpr int kTileRows = 128, kTileCols = 64;
+constexpr int kTileRows = 128, kTileCols = 64, kTilesEach = 4;       // kTilesEach: tiles below each other that a CTA takes
 
 struct ColumnParams {
   const char* x;
@@ -651,7 +657,7 @@ __global__ void __launch_bounds__(kColThreads) column_max_kernel(const __grid_co
   const int chunk = (int)(blockIdx.x % p.chunks);
   const long long from = p.rows * chunk / p.chunks, to = p.rows * (chunk + 1) / p.chunks;
   uint32_t m[8] = {};
-#pragma unroll 8
+#pragma unroll 16
   for (long long row = from + warp; row < to; row += kColThreads / 32) {
     const char* x = p.x + row * p.stride * kBytes;
     if constexpr (VEC) {
@@ -680,7 +686,7 @@ __global__ void __launch_bounds__(kColThreads) column_max_kernel(const __grid_co
 }
 
 template <int TY, bool VEC>
-__global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_constant__ ColumnParams p, int row_tiles) {
+__global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_constant__ ColumnParams p, int row_blocks) {
   __shared__ uint32_t most[kColThreads / kTileCols][kTileCols];
   __shared__ float per[kTileCols];
   // a column's bytes; the words of columns that a warp writes at a time are swapped so that they fall into different banks
@@ -688,26 +694,34 @@ __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_
   const auto swap = [](int c) { return (VEC ? c >> 3 : c) & 7; };
   wait_for_previous_launch();
   constexpr int kBytes = TY == QADAM_F32 ? 4 : 2;
-  const long long first = (long long)(blockIdx.x / row_tiles) * kTileCols;
-  const long long top = (long long)(blockIdx.x % row_tiles) * kTileRows;
+  const long long first = (long long)(blockIdx.x / row_blocks) * kTileCols;
+  const long long from = (long long)(blockIdx.x % row_blocks) * (kTilesEach * kTileRows);
   // a warp has 4 rows at a time in each of 4 groups of eight lanes; a lane 8 columns
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int quad = warp * 4 + lane / 8;                                      // 32 groups of 4 rows
   const int c0 = VEC ? lane % 8 * 8 : lane % 8;
-  float v[4][8];
-  const int rows_left = (int)min((long long)4, p.rows - top - quad * 4), columns_left = (int)min((long long)kTileCols, p.width - first) - c0;
-  const char* x = p.x + ((top + quad * 4) * p.stride + first + c0) * kBytes;
+  const int columns_left = (int)min((long long)kTileCols, p.width - first) - c0;
+  const char* x = p.x + ((from + quad * 4) * p.stride + first + c0) * kBytes;
+  const long long row_bytes = p.stride * kBytes;
+  // four rows of the tile that begins at `top`, as they lie in memory
+  struct Four {
+    Raw8<VEC ? TY : QADAM_F32> row[4];
+  };
+  const auto load = [&](long long top, const char* at) {
+    Four f = {};
+    const int rows_left = (int)max(0ll, min((long long)4, p.rows - top - quad * 4));
 #pragma unroll
-  for (int i = 0; i < 4; ++i, x += p.stride * kBytes) {
-    if constexpr (VEC) {
-      Raw8<TY> raw = {};
-      if (i < rows_left && columns_left > 0) raw = load_raw8<TY>(x);
-      raw8_to_floats<TY>(raw, v[i]);
-    } else {
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (VEC) {
+        if (i < rows_left && columns_left > 0) f.row[i] = load_raw8<TY>(at + i * row_bytes);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = i < rows_left && 8 * k < columns_left ? load_one<TY>(x, 8 * k) : 0.0f;
+        for (int k = 0; k < 8; ++k) f.row[i].w[k] = i < rows_left && 8 * k < columns_left ? __float_as_uint(load_one<TY>(at + i * row_bytes, 8 * k)) : 0u;
+      }
     }
-  }
+    return f;
+  };
+  Four now = load(from, x);
   const int mine = threadIdx.x % kTileCols;
   if (first + mine < p.width) {
     constexpr int kShare = kColThreads / kTileCols;
@@ -721,40 +735,52 @@ __global__ void __launch_bounds__(kColThreads) column_bytes_kernel(const __grid_
   if (threadIdx.x < kTileCols && first + threadIdx.x < p.width) {
     const ByteScale s = byte_scale(max(max(most[0][threadIdx.x], most[1][threadIdx.x]), max(most[2][threadIdx.x], most[3][threadIdx.x])));
     per[threadIdx.x] = s.per;
-    if (top == 0) p.scale[first + threadIdx.x] = s.worth;
+    if (from == 0) p.scale[first + threadIdx.x] = s.worth;
   }
   __syncthreads();
-  uint32_t* to = &tile[c0][quad ^ swap(c0) << 2];            // (the same swap for all columns of a thread)
+  float f[8];
   constexpr int kNext = VEC ? 1 : 8;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    if (k * kNext < columns_left) {
-      const float f = per[c0 + k * kNext];
-      const uint32_t bytes = to_bytes(make_float2(v[0][k], v[1][k]), make_float2(v[2][k], v[3][k]), f);
-      to[k * kNext * (kTileRows / 4)] = f > 0.0f ? bytes : 0u;
+  for (int k = 0; k < 8; ++k) f[k] = k * kNext < columns_left ? per[c0 + k * kNext] : 0.0f;
+  uint32_t* to = &tile[c0][quad ^ swap(c0) << 2];            // (the same swap for all columns of a thread)
+#pragma unroll 1
+  for (int n = 0; n < kTilesEach; ++n) {
+    const long long top = from + n * kTileRows;
+    if (top >= p.rows) return;
+    x += kTileRows * row_bytes;
+    const Four next = n + 1 < kTilesEach ? load(top + kTileRows, x) : now;
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw8_to_floats<VEC ? TY : QADAM_F32>(now.row[i], v[i]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t bytes = to_bytes(make_float2(v[0][k], v[1][k]), make_float2(v[2][k], v[3][k]), f[k]);
+      if (k * kNext < columns_left) to[k * kNext * (kTileRows / 4)] = f[k] > 0.0f ? bytes : 0u;
     }
-  }
-  __syncthreads();
-  // 16 rows' bytes of a column at a time; columns of the result have room up to a multiple of 16
-  for (int i = threadIdx.x; i < kTileCols * (kTileRows / 16); i += kColThreads) {
-    const int c = i / (kTileRows / 16), part = i % (kTileRows / 16);
-    const long long row = top + part * 16;
-    if (first + c < p.width && row < p.rows)
-      *reinterpret_cast<uint4*>(p.q + (first + c) * p.q_stride + row) = *reinterpret_cast<const uint4*>(&tile[c][(part ^ swap(c)) * 4]);
+    __syncthreads();
+    // 16 rows' bytes of a column at a time; columns of the result have room up to a multiple of 16
+    for (int i = threadIdx.x; i < kTileCols * (kTileRows / 16); i += kColThreads) {
+      const int c = i / (kTileRows / 16), part = i % (kTileRows / 16);
+      const long long row = top + part * 16;
+      if (first + c < p.width && row < p.rows)
+        *reinterpret_cast<uint4*>(p.q + (first + c) * p.q_stride + row) = *reinterpret_cast<const uint4*>(&tile[c][(part ^ swap(c)) * 4]);
+    }
+    __syncthreads();
+    now = next;
   }
 }
 
 int column_chunks(long long rows, long long width) {
   const long long strips = (width + 255) / 256;
-  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 64, (2 * kSms + strips - 1) / strips}));
+  return (int)std::max<long long>(1, std::min<long long>({(long long)kColMaxChunks, rows / 32, (6 * kSms + strips - 1) / strips}));
 }
 
 template <int TY, bool VEC>
 bool launch_columns(const ColumnParams& p, cudaStream_t st) {
   const long long strips = (p.width + 255) / 256, tiles = (p.width + kTileCols - 1) / kTileCols;
-  const int row_tiles = (int)((p.rows + kTileRows - 1) / kTileRows);
+  const int row_blocks = (int)((p.rows + kTilesEach * kTileRows - 1) / (kTilesEach * kTileRows));
   return launch(column_max_kernel<TY, VEC>, strips * p.chunks, kColThreads, 0, 0, st, p) &&
-         launch(column_bytes_kernel<TY, VEC>, tiles * row_tiles, kColThreads, 0, 0, st, p, row_tiles);
+         launch(column_bytes_kernel<TY, VEC>, tiles * row_blocks, kColThreads, 0, 0, st, p, row_blocks);
 }
 
 // ---------------------------------------------------------------- packed weights as rows of 8 bits
@@ -845,7 +871,7 @@ int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* 
   p.out = static_cast<char*>(out); p.out_stride = out_stride;
   p.mean = mean; p.rstd = rstd;
   p.q = reinterpret_cast<signed char*>(q); p.q_stride = q_stride; p.scale = scale; p.sums = sums;
-  p.rows = rows; p.width = (int)width; p.normed = 1; p.eps = eps;
+  p.rows = rows; p.width = (int)width; p.per = 1.0f / (float)width; p.normed = 1; p.eps = eps;
   const bool vec = whole(width, type) && on16(x, x_stride, type) && (!residual || (on16(residual, residual_stride, type) && on16(sum, sum_stride, type))) &&
                    (!out || on16(out, out_stride, type));
   p.alike = alike_type(weight, weight_type, bias, bias_type, vec);
@@ -873,7 +899,8 @@ int qadam_quantize_rows(const void* x, int32_t type, int64_t x_stride, const flo
 
 int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes) {
   if (bad_rows(rows, width)) return QADAM_ERR_SIZE;
-  if (workspace_bytes) *workspace_bytes = round_up256((size_t)grad_parts(rows, (int)width) * 2 * (size_t)width * sizeof(float));
+  const int parts = std::max(grad_parts(rows, (int)width, true), grad_parts(rows, (int)width, false));   // (the call may meet either)
+  if (workspace_bytes) *workspace_bytes = round_up256((size_t)parts * 2 * (size_t)width * sizeof(float));
   return QADAM_OK;
 }
 
@@ -884,7 +911,9 @@ int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const
   if (bad_rows(rows, width)) return QADAM_ERR_SIZE;
   const bool sums = dweight || dbias;
   if (!known_type(type) || (weight && !known_type(weight_type)) || (sums && !known_type(grad_type))) return QADAM_ERR_TYPE;
-  const int parts = grad_parts(rows, (int)width);
+  const bool vec = whole(width, type) && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&
+                   (!dsum || on16(dsum, dsum_stride, type));
+  const int parts = grad_parts(rows, (int)width, vec);
   if ((rows > 0 && (!dy || !x || !mean || !rstd || !dx)) || (sums && parts > 0 && !workspace)) return QADAM_ERR_NULL;
   if (bad_stride(dy_stride, width) || bad_stride(x_stride, width) || bad_stride(dx_stride, width) || (dsum && bad_stride(dsum_stride, width)))
     return QADAM_ERR_SIZE;
@@ -906,14 +935,12 @@ int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const
     p.w = weight; p.w_type = weight_type;
     p.partial = sums ? static_cast<float*>(workspace) : nullptr;
     p.rows = rows; p.width = (int)width;
-    const bool vec = whole(width, type) && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&
-                     (!dsum || on16(dsum, dsum_stride, type));
     const bool ok = type == QADAM_F32 ? enqueue_grad_of<QADAM_F32>(p, parts, vec, st)
                     : type == QADAM_BF16 ? enqueue_grad_of<QADAM_BF16>(p, parts, vec, st) : enqueue_grad_of<QADAM_F16>(p, parts, vec, st);
     if (!ok) return QADAM_ERR_CUDA;
   }
   if (sums && (rows > 0 || !accumulate)) {
-    if (!launch(join_grad_kernel, (width + 31) / 32, kJoinWarps * 32, 0, 0, st, static_cast<const float*>(workspace), parts, (int)width, dweight, dbias,
+    if (!launch(join_grad_kernel, 2 * ((width + 31) / 32), kJoinWarps * 32, 0, 0, st, static_cast<const float*>(workspace), parts, (int)width, dweight, dbias,
                 (int)grad_type, (int)accumulate))
       return QADAM_ERR_CUDA;
   }

@@ -217,9 +217,11 @@ struct RowPart {
 
   int width, threads, t;
   int first, left;                                         // column of the first piece; from there to the row's end
+  bool all;                                                // the warp's elements are all in the row
   __device__ __forceinline__ RowPart(int w, int n, int i) : width(w), threads(n), t(i) {
     first = i / 32 * (256 * NV) + i % 32 * kPiece;
     left = w - first;
+    all = (i / 32 + 1) * (256 * NV) <= w;
   }
   __device__ __forceinline__ int column(int q) const { return first + q * 32 * kPiece; }             // a piece's first
   __device__ __forceinline__ bool has(int q) const { return q * 32 * kPiece < left; }
