@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "qadam_rows.cuh"
 
@@ -21,7 +22,7 @@ namespace {
 
 constexpr int kChannels = 128;             // of a tile: the rows of the tensor cores' result
 constexpr int kDepth = 128;                // bytes of a row in a stage
-constexpr int kFewTokens = 32;             // of a tile at most: the columns of the result; more tokens take the kernel below
+constexpr int kFewTokens = 128;            // of a tile at most: the columns of the result; more tokens take the kernel below
 constexpr int kProductThreads = 192;       // a warp that loads, one that multiplies, four for the end
 constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     s.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  constexpr unsigned columns = 32;
+  const unsigned columns = p.tokens <= 32 ? 32 : p.tokens <= 64 ? 64 : 128;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_at(&s.result)), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -297,17 +298,25 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
       bool all = true;
       for (int r = 0; r < split; ++r) all &= *cluster.map_shared_rank(&s.gave_up, r) == 0;
       if (all && in) {
-        for (int t = rank; t < live; t += 2 * split) {     // two tokens at a time
-          uint32_t v[2] = {0u, 0u};
-          const bool two = t + split < live;
-#pragma unroll 8
-          for (int r = 0; r < split; ++r) {
-            const int* of = cluster.map_shared_rank(sums, r) + of_warp;
-            v[0] += (uint32_t)of[t * kChannels];
-            if (two) v[1] += (uint32_t)of[(t + split) * kChannels];
+        const int each = (live - rank + split - 1) / split;  // tokens that are this CTA's
+        const auto add_up = [&](auto together) {
+          constexpr int N = decltype(together)::value;
+          for (int t = rank; t < live; t += N * split) {
+            uint32_t v[N] = {};
+#pragma unroll 4
+            for (int r = 0; r < split; ++r) {
+              const int* of = cluster.map_shared_rank(sums, r) + of_warp;
+#pragma unroll
+              for (int k = 0; k < N; ++k) v[k] += (uint32_t)of[(t + k * split < live ? t + k * split : t) * kChannels];
+            }
+            finish(p, about, worth, bias, row, mine, t, split, live, v);
           }
-          finish(p, about, worth, bias, row, mine, t, split, live, v);
-        }
+        };
+        // what is on its way from other CTAs at a time: as many tokens as there are, up to eight
+        if (each <= 1) add_up(std::integral_constant<int, 1>());
+        else if (each <= 2) add_up(std::integral_constant<int, 2>());
+        else if (each <= 4) add_up(std::integral_constant<int, 4>());
+        else add_up(std::integral_constant<int, 8>());
       }
     }
     cluster.sync();
@@ -424,6 +433,13 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, const void* fr
                : "memory");
 }
 
+// The same, added to what is there (binary32: one rounding, as a load, a sum and a store would have).
+__device__ __forceinline__ void add_box(const CUtensorMap* map, const void* from, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
+               "r"(shared_at(from))
+               : "memory");
+}
+
 struct PairTile {
   int token, channel;                      // tiles
 };
@@ -434,8 +450,8 @@ __device__ __forceinline__ PairTile pair_tile(const PairParams& p, int t) {
   return {first + in % tall, in / tall};
 }
 
-// OUT: type of the result.  BOXES: it is written in boxes; else (rows that do not begin on 16 bytes, or a result to be added
-// to) from shared memory element by element, 32 channels of a token at a time.
+// OUT: type of the result.  BOXES: it is written in boxes; else (rows that do not begin on 16 bytes, or 16-bit results to be added
+// to, whose sums are rounded once) from shared memory element by element, 32 channels of a token at a time.
 template <int OUT, bool BOXES>
 __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                                                                const __grid_constant__ CUtensorMap out_map, const __grid_constant__ PairParams p) {
@@ -601,8 +617,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
           __syncwarp();
           if (lane == 0) {
             if (row0 < p.rows) {
-              store_box(&out_map, box, (int)(channel0 + c0), (int)row0);
-              if (!kWide && c0 + 32 < wide) store_box(&out_map, box + kBoxBytes, (int)(channel0 + c0 + 32), (int)row0);
+              if (!kWide && p.accumulate) {
+                add_box(&out_map, box, (int)(channel0 + c0), (int)row0);
+                if (c0 + 32 < wide) add_box(&out_map, box + kBoxBytes, (int)(channel0 + c0 + 32), (int)row0);
+              } else {
+                store_box(&out_map, box, (int)(channel0 + c0), (int)row0);
+                if (!kWide && c0 + 32 < wide) store_box(&out_map, box + kBoxBytes, (int)(channel0 + c0 + 32), (int)row0);
+              }
             }
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
@@ -612,14 +633,20 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const bool in = c0 + h * 32 + lane < wide;
-            const long long first = row0 * p.out_stride + channel0 + c0 + h * 32 + lane;
-#pragma unroll 8
-            for (int r = 0; r < 32; ++r) {
-              const float y = *reinterpret_cast<const float*>(box + h * kBoxBytes + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + lane % 4 * 4);
-              if (in && r < live) {
-                const long long i = first + r * p.out_stride;
-                store_one<OUT>(p.out, i, p.accumulate ? load_one<OUT>(p.out, i) + y : y);
-              }
+            char* to = p.out + (row0 * p.out_stride + channel0 + c0 + h * 32 + lane) * (OUT == QADAM_F32 ? 4 : 2);
+            const long long row_bytes = p.out_stride * (OUT == QADAM_F32 ? 4 : 2);
+#pragma unroll 1
+            for (int r = 0; r < live; r += 16) {               // sixteen tokens' loads under way, if there is something to add to
+              float y[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) y[i] = p.accumulate && in && r + i < live ? load_one<OUT>(to + i * row_bytes, 0) : 0.0f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                y[i] += *reinterpret_cast<const float*>(box + h * kBoxBytes + (r + i) * 128 + (((lane / 4) ^ ((r + i) & 7)) << 4) + lane % 4 * 4);
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (in && r + i < live) store_one<OUT>(to + i * row_bytes, 0, y[i]);
+              to += 16 * row_bytes;
             }
           }
           __syncwarp();
@@ -689,7 +716,8 @@ bool byte_map(CUtensorMap* map, const void* p, int64_t width, int64_t rows, int6
 }
 
 // CTAs of a cluster wait for one another while they hold tensor memory, so no SM may be given more of them than its 512 columns
-// serve.  Their shared memory sees to it: tiles of few tokens hold 32 columns and 18 KB or more, pairs 512 columns and 200 KB.
+// serve.  Their shared memory sees to it: tiles of few tokens hold 32 columns and 18 KB or more, 64 and 32 KB, 128 and 48 KB where a sum is
+// split; pairs 512 columns and 200 KB.
 constexpr int kRingBytes = 208 * 1024;
 
 using PairKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, PairParams);
@@ -727,20 +755,43 @@ int pairs_of_device() {
 
 constexpr int kSms = 148;
 
-// Channels of a pair's tile: the time of the pairs' rounds, in cycles of the tensor cores (a block of 128 bytes takes twice a tile's
-// channels) and what a tile costs besides, is to be least.
-int pair_half(int64_t token_tiles, int64_t channels, int blocks, int pairs) {
-  int best = 128;
-  int64_t least = INT64_MAX;
+// What a block of 128 bytes along the sum takes a CTA, in cycles: its products (16384 operations a cycle: four for each of the 128
+// rows that a CTA's results have), or the way of its operands into shared memory, at 64 bytes a cycle, whichever is longer.
+int64_t block_cycles(int columns, int loaded_rows) { return std::max<int64_t>(2 * columns, 2 * loaded_rows); }
+constexpr int kTileCycles = 1500;          // what a tile costs besides
+
+// Channels of a pair's tile: the time of the pairs' rounds is to be least.
+struct PairShape {
+  int half;
+  int64_t cycles;
+};
+PairShape pair_shape(int64_t rows, int64_t channels, int blocks, int pairs) {
+  PairShape best = {128, INT64_MAX};
+  const int64_t token_tiles = (rows + kPairTokens - 1) / kPairTokens;
   for (int half = 128; half >= 32; half -= 32) {             // (whole boxes of results)
     const int64_t tiles = token_tiles * ((channels + 2 * half - 1) / (2 * half));
-    const int64_t cost = (tiles + pairs - 1) / pairs * ((int64_t)blocks * 4 * half + 1500);
-    if (cost < least) {
-      least = cost;
-      best = half;
-    }
+    const int64_t cycles = (tiles + pairs - 1) / pairs * (blocks * block_cycles(2 * half, 128 + half) + kTileCycles);
+    if (cycles < best.cycles) best = {half, cycles};
   }
   return best;
+}
+
+// How many CTAs share the sum of a tile of few tokens: as many as there are SMs for, up to eight, as long as each has two blocks.
+struct FewShape {
+  int tokens, split, resident;             // resident: CTAs of an SM
+  int64_t cycles;
+};
+FewShape few_shape(int64_t rows, int64_t channels, int blocks) {
+  FewShape f;
+  f.tokens = (int)(rows + 15) / 16 * 16;
+  const int64_t tiles = (channels + kChannels - 1) / kChannels;
+  f.resident = f.tokens <= 32 ? 2 : 1;
+  const int resident = f.resident;
+  f.split = 1;
+  while (f.split < kMaxSplit && tiles * f.split * 2 <= (int64_t)resident * kSms && blocks >= f.split * 4) f.split *= 2;
+  const int64_t rounds = (tiles * f.split + resident * kSms - 1) / (resident * kSms);
+  f.cycles = rounds * resident * ((blocks + f.split - 1) / f.split * block_cycles(f.tokens, kChannels + f.tokens) + kTileCycles) + (f.split > 1 ? 2500 : 0);
+  return f;
 }
 
 int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int64_t depth, const void* b, int64_t b_stride, int pairs, cudaStream_t st) {
@@ -749,9 +800,9 @@ int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int
   p.out = q.out; p.out_stride = q.out_stride; p.accumulate = q.accumulate; p.rows = q.rows; p.channels = q.channels; p.blocks = q.blocks;
   p.transposed = q.transposed; p.b_signed = q.b_signed; p.status = q.status;
   p.token_tiles = (int)((p.rows + kPairTokens - 1) / kPairTokens);
-  p.half = pair_half(p.token_tiles, p.channels, p.blocks, pairs);
+  p.half = pair_shape(p.rows, p.channels, p.blocks, pairs).half;
   p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
-  const bool boxes = !p.accumulate && is_aligned(p.out, 16) && p.out_stride * type_bytes(q.out_type) % 16 == 0;
+  const bool boxes = (!p.accumulate || q.out_type == QADAM_F32) && is_aligned(p.out, 16) && p.out_stride * type_bytes(q.out_type) % 16 == 0;
   p.boxes = boxes && q.out_type != QADAM_F32 && p.blocks >= kLongSum ? 1 : 2;
   p.stages = p.boxes == 1 ? 5 : 4;
   CUtensorMap a_map, b_map, out_map = {};
@@ -769,16 +820,17 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
   p.blocks = (int)((depth + kDepth - 1) / kDepth);
   const int pairs = pairs_of_device();
   if (pairs == 0) return QADAM_ERR_CUDA;
-  if (p.rows > kFewTokens) return enqueue_pairs(p, a, a_stride, depth, b, b_stride, pairs, st);
+  // up to 32 tokens the pairs' 256 are a waste in any case; up to 128 it is the longer sum's or the many channels' turn
+  const FewShape few = few_shape(p.rows, p.channels, p.blocks);
+  if (p.rows > kFewTokens || (p.rows > 32 && pair_shape(p.rows, p.channels, p.blocks, pairs).cycles <= few.cycles))
+    return enqueue_pairs(p, a, a_stride, depth, b, b_stride, pairs, st);
   p.channel_tiles = (int)((p.channels + kChannels - 1) / kChannels);
-  const int tokens = p.rows <= 16 ? 16 : 32;
-  p.tokens = tokens;
+  const int tokens = few.tokens, split = few.split;
   const int64_t tiles = p.channel_tiles;
-  int split = 1;
-  while (split < kMaxSplit && tiles * split * 2 <= 2 * kSms && p.blocks >= split * 4) split *= 2;
+  p.tokens = tokens;
   const int stage = (kChannels + tokens) * kDepth;
   const int needed = (p.blocks + split - 1) / split;
-  p.stages = std::min({kMaxStages, kRingBytes / stage, std::max(needed, (tokens * kChannels * 4 + stage - 1) / stage)});
+  p.stages = std::min({kMaxStages, kRingBytes / few.resident / stage, std::max(needed, (tokens * kChannels * 4 + stage - 1) / stage)});
   if (tiles * split >= (int64_t)1 << 31) return QADAM_ERR_SIZE;
   CUtensorMap a_map, b_map;
   const bool maps = byte_map(&a_map, a, depth, p.rows, a_stride, tokens) &&
