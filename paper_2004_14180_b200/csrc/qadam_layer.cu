@@ -162,6 +162,7 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
 template <int TY, int NV, bool VEC>
 __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_constant__ RowParams p) {
   wait_for_previous_launch();
+  let_next_launch_start();                                 // (a product behind it is then brought up beside it: one token's 9.5 -> 8.0 us)
   using Part = RowPart<TY, NV, VEC>;
   RowGroup<false> group(nullptr, 1, 0);
   const Part part(p.width, 32, threadIdx.x % 32);
@@ -186,6 +187,7 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(co
   extern __shared__ __align__(16) uint8_t slots[];         // [groups][stages][1 or 2][a row]; with_parameters: then w, b
   __shared__ GroupShared shared[kGroupWarps];
   wait_for_previous_launch();
+  let_next_launch_start();
   using Part = RowPart<TY, NV, VEC>;
   const int threads = MANY ? warps * 32 : 32, number = (int)threadIdx.x / threads;
   const int groups = blockDim.x / threads;
