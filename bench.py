@@ -55,7 +55,7 @@ def ncu_traffic():
 
 
 # Sources of the operators beside the quantized step: nothing of the step is made of them.
-OTHER_OPERATORS = ("qadam_adamw.cu", "qadam_embedding.cu", "qadam_norm.cu", "qadam_tensors.cuh")
+OTHER_OPERATORS = ("qadam_adamw.cu", "qadam_embedding.cu", "qadam_norm.cu", "qadam_tensors.cuh", "qadam_layer.cu", "qadam_product.cu", "qadam_rows.cuh")
 
 
 def csrc_digest() -> str:

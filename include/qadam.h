@@ -584,15 +584,15 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
                     int64_t q_stride, float* scale, void* stream);
 
 /* out[m][n] = round(a_scale[m] b_scale[n] sum_k a[m][k] B[k][n] + bias[n]), m < rows, n < channels, k < depth; accumulate = 1:
- * round(out[m][n] + the same).  The sum is exact (depth <= 131072), the rest binary32.
+ * round(out[m][n] + the same).  The sum is exact (depth <= 131072), the rest binary32.  b_scale = NULL: b_worth for all n.
  * transposed = 0: B[k][n] = b[n][k], b is [channels][b_stride >= depth] and b_scale [channels], as a layer's output needs it.
  * transposed = 1: B[k][n] = b[k][n], b is [depth][b_stride >= channels], as the gradient of a layer's input needs it; b_scale is
- * not read (the scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
+ * NULL (scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
  * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
 int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
-                      const float* b_scale, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type, void* out,
-                      int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream);
+                      const float* b_scale, float b_worth, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type,
+                      void* out, int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream);
 
 /* The same with the weights that a worker holds in codes of one byte (kx = 6, QADAM_ERR_LEVEL otherwise): b is a table of the elements from
  * `first` on, [channels][depth], or [depth][channels] if transposed, read as it lies in wcodes; b_scale is 2^-7.  a_sums: the

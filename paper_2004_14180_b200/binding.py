@@ -187,7 +187,7 @@ def load_library():
         "quantize_columns_query_sizes": [i64, i64, C.POINTER(size)],
         "quantize_columns": [vp, i32, i64, i64, i64, vp, i64, vp, vp, size, vp],
         "held_rows": [vp, size, i32, i64, i64, i64, vp, i64, vp, vp],
-        "row_product": [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
+        "row_product": [vp, i64, vp, i64, i64, vp, i64, vp, f32, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
         "held_product": [vp, i64, vp, vp, i64, i64, vp, size, i32, i64, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
     }.items():
         fn = getattr(L, "qadam_" + name)

@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -23,7 +25,7 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     # IEEE arithmetic everywhere: no FMA contraction, exact division and root, subnormals kept
     "--fmad=false", "--prec-div=true", "--prec-sqrt=true", "--ftz=false",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC",
 ]
 
 
@@ -44,11 +46,15 @@ def is_stale() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
-    cmd = [_nvcc()] + NVCC_FLAGS + ["-I", os.path.join(_ROOT, "include"), "-I", CSRC]
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += ["-o", LIB] + SOURCES
-    subprocess.run(cmd, check=True)
+    flags = NVCC_FLAGS + ["-I", os.path.join(_ROOT, "include"), "-I", CSRC] + (["-Xptxas", "-v"] if verbose else [])
+    with tempfile.TemporaryDirectory() as work:           # the sources at the same time, then one library of their objects
+        def compile_one(source: str) -> str:
+            target = os.path.join(work, os.path.basename(source) + ".o")
+            subprocess.run([_nvcc()] + flags + ["-c", "-o", target, source], check=True)
+            return target
+        with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
+            objects = list(pool.map(compile_one, SOURCES))
+        subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", LIB] + objects, check=True)
     return LIB
 
 

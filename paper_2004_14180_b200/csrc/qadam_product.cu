@@ -860,16 +860,17 @@ int check_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64
 extern "C" {
 
 int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
-                      const float* b_scale, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type, void* out,
-                      int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream) {
+                      const float* b_scale, float b_worth, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type,
+                      void* out, int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream) {
   const int rc = check_product(a, a_stride, a_scale, rows, depth, channels, bias, bias_type, out, out_type, out_stride, transposed, accumulate, status);
   if (rc != QADAM_OK) return rc;
-  if (rows > 0 && (!b || (!transposed && !b_scale))) return QADAM_ERR_NULL;
+  if (rows > 0 && !b) return QADAM_ERR_NULL;
+  if (transposed && b_scale) return QADAM_ERR_SIZE;
   if (b_stride < (transposed ? channels : depth) || b_stride >= (int64_t)1 << 40) return QADAM_ERR_SIZE;
   if (!is_aligned(b, 16) || b_stride % 16 != 0 || !is_aligned(b_scale, 4)) return QADAM_ERR_ALIGN;
   if (rows == 0) return QADAM_OK;
   ProductParams p = {};
-  p.a_scale = a_scale; p.b_scale = transposed ? nullptr : b_scale; p.worth = 1.0f;
+  p.a_scale = a_scale; p.b_scale = b_scale; p.worth = b_worth;
   p.bias = bias; p.bias_type = bias_type;
   p.out = static_cast<char*>(out); p.out_type = out_type; p.out_stride = out_stride; p.accumulate = accumulate;
   p.rows = rows; p.channels = channels; p.transposed = transposed; p.b_signed = 1; p.status = status;

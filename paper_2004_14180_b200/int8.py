@@ -205,10 +205,15 @@ def int8_matmul(a: Int8Rows, b: Int8Rows, bias: Optional[torch.Tensor] = None, o
     The sums over the common width (at most 131072) are exact.  transpose: a b instead, [rows of a, width of b]; b's scales belong
     to the axis that is then summed over and are not applied: quantize a with columns=b.scale.
     status: one int32 on the device that gets ST_TIMEOUT if a wait inside the kernel gives up."""
+    return _product(a, b, None, bias, out_dtype, out, accumulate, transpose, status)
+
+
+def _product(a, b, worth, bias, out_dtype, out, accumulate, transpose, status):
+    """int8_matmul; worth: what all of b's numbers are worth, in place of its scales."""
     device, rows, depth = a.device, a.rows, a.width
     if _elsewhere(device):
         with torch.cuda.device(device):
-            return int8_matmul(a, b, bias, out_dtype, out, accumulate, transpose, status)
+            return _product(a, b, worth, bias, out_dtype, out, accumulate, transpose, status)
     if b.device != device:
         raise ValueError(f"a on {device}, b on {b.device}")
     common, channels = (b.rows, b.width) if transpose else (b.width, b.rows)
@@ -217,7 +222,8 @@ def int8_matmul(a: Int8Rows, b: Int8Rows, bias: Optional[torch.Tensor] = None, o
     given = out is not None
     out, out_stride, bias_at, bias_type = _output(rows, channels, out, out_dtype, accumulate, bias, device)
     rc = load_library().qadam_row_product(
-        a.q_at, a.stride, a.scale_at, rows, depth, b.q_at, b.stride, b.scale_at, channels, int(transpose),
+        a.q_at, a.stride, a.scale_at, rows, depth, b.q_at, b.stride,
+        None if transpose or worth is not None else b.scale_at, 1.0 if worth is None else worth, channels, int(transpose),
         bias_at, bias_type, out.data_ptr(), _type(out, "out"), out_stride, int(accumulate),
         None if status is None else _status(status, device), stream_of(device))
     if rc:
@@ -244,11 +250,9 @@ def held_matmul(a: Int8Rows, wcodes: torch.Tensor, kx: int, rows: int, width: in
             return held_matmul(a, wcodes, kx, rows, width, first, bias, out_dtype, out, accumulate, transpose, status)
     if depth != (rows if transpose else width):
         raise ValueError(f"a [{a_rows}, {depth}] and W [{rows}, {width}] have no common axis{' (transposed)' if transpose else ''}")
-    if kx != 6 or width % 16 or first % 16 or wcodes.data_ptr() % 16:
+    if kx != 6 or width % 16 or first % 16:
         w = held_rows(wcodes, kx, rows, width, first)
-        if transpose:              # the weights' worth is the same for all: it goes to a
-            a = Int8Rows(a.q, a.scale * 2.0 ** -(kx + 1))          # (a power of two)
-        return int8_matmul(a, w, bias, out_dtype, out, accumulate, transpose, status)
+        return _product(a, w, 2.0 ** -(kx + 1), bias, out_dtype, out, accumulate, transpose, status)
     if a.sums_at is None:
         raise ValueError("a: the sums of its rows are needed")
     channels = width if transpose else rows
