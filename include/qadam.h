@@ -589,6 +589,7 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
  * transposed = 1: B[k][n] = b[k][n], b is [depth][b_stride >= channels], as the gradient of a layer's input needs it; b_scale is
  * NULL (scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
+ * rows = 0 is allowed; rows, channels <= 2^31 - 512.
  * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
 int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
                       const float* b_scale, float b_worth, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type,

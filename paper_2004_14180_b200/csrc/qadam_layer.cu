@@ -3,6 +3,7 @@
 #include "qadam.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "qadam_rows.cuh"
@@ -297,10 +298,18 @@ Residents residents(int threads, int most_threads, int bytes, int besides) {
   return {per_sm, stages < 2 ? 0 : stages};
 }
 
-// The limit of dynamic shared memory belongs to the kernel: it is raised to the same for every launch that needs it.
-template <typename K>
-bool allow_ring(K kernel, size_t bytes) {
-  return bytes <= 40 * 1024 || cuda_call(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes));
+// The limit of dynamic shared memory belongs to the kernel and the device: it is raised once, to the same for every launch.
+template <auto KERNEL>
+bool allow_ring(size_t bytes) {
+  if (bytes <= 40 * 1024) return true;
+  static std::atomic<uint64_t> raised{0};
+  int device = 0;
+  if (!cuda_call(cudaGetDevice(&device))) return false;
+  const uint64_t bit = (uint64_t)1 << (device % 64);
+  if (raised.load() & bit) return true;
+  if (!cuda_call(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes))) return false;
+  raised.fetch_or(bit);
+  return true;
 }
 
 template <int TY, int NV, bool VEC, bool MANY>
@@ -312,10 +321,15 @@ bool launch_group_rows(const RowParams& p, cudaStream_t st) {
   const int kept = parameters * 4 <= kRingBytes / std::max(1, kGroupMostThreads / threads) ? parameters : 0;
   const Residents r = residents(threads, kGroupMostThreads, bytes, kept);
   if (r.stages == 0) return launch(wide_row_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p);
-  const auto kernel = !MANY ? group_row_kernel<TY, NV, VEC, false, 256> : threads <= 256 ? group_row_kernel<TY, NV, VEC, true, 256> : group_row_kernel<TY, NV, VEC, true, 512>;
   const size_t smem = (size_t)r.stages * bytes + kept;
-  return allow_ring(kernel, smem) &&
-         launch(kernel, std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm), threads, smem, 0, st, p, warps, r.stages, kept ? 1 : 0);
+  const long long grid = std::min<long long>((p.rows + groups - 1) / groups, (long long)kSms * r.per_sm);
+  if (threads <= 256)
+    return allow_ring<group_row_kernel<TY, NV, VEC, MANY, 256>>(smem) &&
+           launch(group_row_kernel<TY, NV, VEC, MANY, 256>, grid, threads, smem, 0, st, p, warps, r.stages, kept ? 1 : 0);
+  if constexpr (MANY)
+    return allow_ring<group_row_kernel<TY, NV, VEC, true, 512>>(smem) &&
+           launch(group_row_kernel<TY, NV, VEC, true, 512>, grid, threads, smem, 0, st, p, warps, r.stages, kept ? 1 : 0);
+  return false;                                            // (one warp to a row: eight to a CTA)
 }
 template <int TY, int NV>
 bool launch_group_rows(const RowParams& p, bool vec, cudaStream_t st) {
@@ -605,8 +619,7 @@ bool launch_grad(GradParams p, const GradShape& g, int parts, cudaStream_t st) {
   const Residents r = residents(g.threads, g.per_sm * g.threads, bytes, weights);
   static_assert(kRingBytes - 2048 >= 4 * (kGradMostWarps * 768 * 4 + 32) + kGradMostWarps * 768 * 4, "two stages of two rows");
   const size_t smem = std::max((size_t)r.stages * bytes + weights, g.groups == 1 ? 0 : (size_t)g.groups * 2 * p.width * sizeof(float));
-  const auto kernel = row_grad_kernel<TY, NV, VEC, MANY, WARPS>;
-  return allow_ring(kernel, smem) && launch(kernel, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
+  return allow_ring<row_grad_kernel<TY, NV, VEC, MANY, WARPS>>(smem) && launch(row_grad_kernel<TY, NV, VEC, MANY, WARPS>, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
 }
 template <int TY, bool VEC>
 bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {

@@ -839,12 +839,12 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
   return launch(product_kernel, tiles * split, kProductThreads, (size_t)p.stages * stage + 1024, split, st, a_map, b_map, p) ? QADAM_OK : QADAM_ERR_CUDA;
 }
 
-constexpr int64_t kMostRows = (int64_t)1 << 31, kMostDepth = 131072;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 512, kMostDepth = 131072;                         // (places in a tile's rows stay below 2^31)
 
 int check_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, int64_t channels, const void* bias,
                   int32_t bias_type, const void* out, int32_t out_type, int64_t out_stride, int32_t transposed, int32_t accumulate,
                   const uint32_t* status) {
-  if (rows < 0 || rows >= kMostRows || channels < 1 || channels >= kMostRows || depth < 1 || depth > kMostDepth) return QADAM_ERR_SIZE;
+  if (rows < 0 || rows > kMostRows || channels < 1 || channels > kMostRows || depth < 1 || depth > kMostDepth) return QADAM_ERR_SIZE;
   if ((transposed != 0 && transposed != 1) || (accumulate != 0 && accumulate != 1)) return QADAM_ERR_SIZE;
   if (!known_type(out_type) || (bias && !known_type(bias_type))) return QADAM_ERR_TYPE;
   if (rows > 0 && (!a || !a_scale || !out)) return QADAM_ERR_NULL;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from _layer import DTYPES, gen_of, randn
+from _layer import DTYPES, U, gen_of, grad64, randn
 from test_gpu_int8 import check, int8_rows, scaled
 from test_gpu_layer_norm import near, norm64
 
@@ -202,6 +202,21 @@ def test_a_long_batch_of_short_rows_and_a_short_batch_of_long_ones():
         one = qb.layer_norm(x[-1:].contiguous(), w, b, residual=x[-1:].contiguous(), int8=True)
         step = float(want[-1].abs().max()) / 127
         assert float((one.rows.values() - got.rows.values()[-1:]).abs().max()) <= step * 1.01 and int(got.rows.sums[0]) == int(got.rows.q[0].sum(dtype=torch.int32))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,width", [(9000, 250), (5000, 513), (700, 1536), (260, 2304), (200, 5119), (150, 5120), (40, 6145), (33, 7008), (20, 8191)])
+def test_gradients_by_every_number_of_warps_to_a_row(rows, width, kind):
+    gen = gen_of(rows, width, 2)
+    x, dy, ds = ((randn(gen, rows, width) * f).to(DTYPES[kind]) for f in (1.0, 1e-2, 1e-2))
+    w = 1 + 0.1 * randn(gen, width)
+    ran = qb.layer_norm(x, w)
+    dx, dw, db = qb.layer_norm_grad(dy, x, ran.mean, ran.rstd, w, dsum=ds)
+    wx, ww, wb, off, sw, sb = grad64(dy, x, ran.mean, ran.rstd, w, ds)
+    near(dx, wx, off, kind)
+    few = 3 + min(rows, rows / 64 + 80)                          # (as in the test of the gradient)
+    near(dw, ww, few * U * sw, "f32")
+    near(db, wb, few * U * sb, "f32")
 
 
 def test_bytes_behind_rows_are_not_read():

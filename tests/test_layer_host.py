@@ -123,7 +123,7 @@ PRODUCT_BASE = dict(a=A, a_stride=64, a_scale=A, rows=0, depth=64, b=A, b_stride
 
 @pytest.mark.parametrize("kw,code", [
     ({}, 0), (dict(b_scale=None), 0), (dict(rows=4, a=None), NULL), (dict(rows=4, a_scale=None), NULL), (dict(rows=4, out=None), NULL),
-    (dict(rows=4, b=None), NULL), (dict(rows=1 << 31), SIZE), (dict(depth=0), SIZE), (dict(depth=131073, a_stride=131088, b_stride=131088), SIZE),
+    (dict(rows=4, b=None), NULL), (dict(rows=(1 << 31) - 511), SIZE), (dict(channels=1 << 31, out_stride=1 << 31), SIZE), (dict(depth=0), SIZE), (dict(depth=131073, a_stride=131088, b_stride=131088), SIZE),
     (dict(channels=0), SIZE), (dict(a_stride=48), SIZE), (dict(a_stride=72), ALIGN), (dict(b_stride=48), SIZE), (dict(b_stride=68), ALIGN),
     (dict(a=A + 8), ALIGN), (dict(b=A + 8), ALIGN), (dict(transposed=2), SIZE), (dict(transposed=1), SIZE), (dict(transposed=1, b_scale=None), 0),
     (dict(transposed=1, b_scale=None, b_stride=0), SIZE), (dict(accumulate=-1), SIZE), (dict(out_type=3), TYPE), (dict(bias=A, bias_type=4), TYPE),
