@@ -539,10 +539,19 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
  * weight, bias: device, [width], each of a type of its own, or NULL (1, 0).  mean, rstd: device, [rows], or NULL.
  * q (NULL: none): y before its rounding, in 8 bits, with scale and sums as qadam_quantize_rows writes them.  Of out, q, mean and
  * rstd at least one is needed; sum goes with residual.  rows = 0 is allowed; rows < 2^31, width <= 2^24. */
-int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
-                     int32_t weight_type, const void* bias, int32_t bias_type, int64_t rows, int64_t width, float eps, void* sum,
-                     int64_t sum_stride, void* out, int64_t out_stride, float* mean, float* rstd, int8_t* q, int64_t q_stride,
-                     float* scale, int32_t* sums, void* stream);
+typedef struct {
+  const void* x; int64_t x_stride;
+  const void* residual; int64_t residual_stride;
+  const void* weight; const void* bias;
+  int64_t rows, width;
+  void* sum; int64_t sum_stride;
+  void* out; int64_t out_stride;
+  float* mean; float* rstd;
+  int8_t* q; int64_t q_stride; float* scale; int32_t* sums;
+  int32_t type, weight_type, bias_type;
+  float eps;                               /* >= 0 */
+} qadam_layer_norm_args;
+int qadam_layer_norm(const qadam_layer_norm_args* args, void* stream);
 
 /* Scratch of qadam_layer_norm_grad. */
 int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* workspace_bytes);
@@ -555,10 +564,19 @@ int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* works
  * reaches h by other ways, or NULL; dx is then the gradient of x and of residual both.  dy, x, dsum, dx are of `type`.  dweight, dbias: device,
  * [width] of grad_type, either may be NULL; accumulate = 1 adds to what is there.  rows = 0: the sums are zero.
  * workspace: 256-byte aligned, needed for dweight or dbias. */
-int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const void* x, int64_t x_stride, const float* mean,
-                          const float* rstd, const void* weight, int32_t weight_type, const void* dsum, int64_t dsum_stride,
-                          int64_t rows, int64_t width, void* dx, int64_t dx_stride, void* dweight, void* dbias, int32_t grad_type,
-                          int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+typedef struct {
+  const void* dy; int64_t dy_stride;
+  const void* x; int64_t x_stride;
+  const float* mean; const float* rstd;
+  const void* weight;
+  const void* dsum; int64_t dsum_stride;
+  int64_t rows, width;
+  void* dx; int64_t dx_stride;
+  void* dweight; void* dbias;
+  void* workspace; int64_t workspace_bytes;
+  int32_t type, weight_type, grad_type, accumulate;
+} qadam_layer_norm_grad_args;
+int qadam_layer_norm_grad(const qadam_layer_norm_grad_args* args, void* stream);
 
 /* ---- products in 8 bits -------------------------------------------------------------------
  * A row in 8 bits is q[k], -127 .. 127, each worth `scale`: with a = max(max |x[k]|, 2^-100),
@@ -591,18 +609,25 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
  * rows = 0 is allowed; rows, channels <= 2^31 - 512.
  * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
-int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
-                      const float* b_scale, float b_worth, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type,
-                      void* out, int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream);
+typedef struct {
+  const int8_t* a; int64_t a_stride; const float* a_scale; const int32_t* a_sums;   /* a_sums: qadam_held_product only */
+  int64_t rows, depth;
+  const void* b; int64_t b_stride; const float* b_scale;   /* qadam_held_product: b is wcodes, the other two are not read */
+  int64_t channels;
+  const void* bias;
+  void* out; int64_t out_stride;
+  uint32_t* status;
+  int64_t first, wcode_bytes;              /* qadam_held_product only, as kx */
+  int32_t transposed, bias_type, out_type, accumulate, kx;
+  float b_worth;                           /* qadam_row_product only */
+} qadam_product_args;
+int qadam_row_product(const qadam_product_args* args, void* stream);
 
 /* The same with the weights that a worker holds in codes of one byte (kx = 6, QADAM_ERR_LEVEL otherwise): b is a table of the elements from
  * `first` on, [channels][depth], or [depth][channels] if transposed, read as it lies in wcodes; b_scale is 2^-7.  a_sums: the
  * sums of a's rows.  QADAM_ERR_ALIGN unless wcodes, first and the table's width are multiples of 16: take qadam_held_rows then,
  * and for other kx. */
-int qadam_held_product(const int8_t* a, int64_t a_stride, const float* a_scale, const int32_t* a_sums, int64_t rows, int64_t depth,
-                       const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t channels, int32_t transposed,
-                       const void* bias, int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, int32_t accumulate,
-                       uint32_t* status, void* stream);
+int qadam_held_product(const qadam_product_args* args, void* stream);
 
 const char* qadam_strerror(int err);
 

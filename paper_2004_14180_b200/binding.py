@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -106,6 +107,23 @@ class AdamWBuffers(C.Structure):
     ]
 
 
+class PackedArgs:
+    """A struct of arguments as the C interface declares it (fields of 8 bytes first, so that nothing is between them), packed at each call:
+    `pack` takes the fields in their order, 0 for NULL.  (Twenty arguments one by one cost ctypes 1.5 us more.)"""
+
+    def __init__(self, long_fields: str, int_fields: str, float_field: str = ""):
+        self.fields = tuple((long_fields + " " + int_fields + " " + float_field).split())
+        self._struct = struct.Struct(f"@{len(long_fields.split())}q{len(int_fields.split())}i" + ("f" if float_field else ""))
+        self.pack = self._struct.pack
+
+
+LAYER_NORM_ARGS = PackedArgs("x x_stride residual residual_stride weight bias rows width sum sum_stride out out_stride mean rstd q q_stride scale "
+                             "sums", "type weight_type bias_type", "eps")
+LAYER_NORM_GRAD_ARGS = PackedArgs("dy dy_stride x x_stride mean rstd weight dsum dsum_stride rows width dx dx_stride dweight dbias workspace "
+                                  "workspace_bytes", "type weight_type grad_type accumulate")
+PRODUCT_ARGS = PackedArgs("a a_stride a_scale a_sums rows depth b b_stride b_scale channels bias out out_stride status first wcode_bytes",
+                          "transposed bias_type out_type accumulate kx", "b_worth")
+
 _lib = None
 
 
@@ -180,15 +198,15 @@ def load_library():
         "held_lookup": [vp, size, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp, vp],
         "embedding_grad_query_sizes": [i64, i64, i64, C.POINTER(size)],
         "embedding_grad": [vp, i32, i64, vp, i32, i64, f32, i64, vp, i32, i64, i64, i64, i32, vp, size, vp, vp],
-        "layer_norm": [vp, i32, i64, vp, i64, vp, i32, vp, i32, i64, i64, f32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp],
+        "layer_norm": [C.c_char_p, vp],
         "layer_norm_grad_query_sizes": [i64, i64, C.POINTER(size)],
-        "layer_norm_grad": [vp, i32, i64, vp, i64, vp, vp, vp, i32, vp, i64, i64, i64, vp, i64, vp, vp, i32, i32, vp, size, vp],
+        "layer_norm_grad": [C.c_char_p, vp],
         "quantize_rows": [vp, i32, i64, vp, i64, i64, vp, i64, vp, vp, vp],
         "quantize_columns_query_sizes": [i64, i64, C.POINTER(size)],
         "quantize_columns": [vp, i32, i64, i64, i64, vp, i64, vp, vp, size, vp],
         "held_rows": [vp, size, i32, i64, i64, i64, vp, i64, vp, vp],
-        "row_product": [vp, i64, vp, i64, i64, vp, i64, vp, f32, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
-        "held_product": [vp, i64, vp, vp, i64, i64, vp, size, i32, i64, i64, i32, vp, i32, vp, i32, i64, i32, vp, vp],
+        "row_product": [C.c_char_p, vp],
+        "held_product": [C.c_char_p, vp],
     }.items():
         fn = getattr(L, "qadam_" + name)
         fn.restype, fn.argtypes = C.c_int, args

@@ -860,10 +860,10 @@ bool on16(const void* p, int64_t stride, int type) { return is_aligned(p, 16) &&
 
 extern "C" {
 
-int qadam_layer_norm(const void* x, int32_t type, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
-                     int32_t weight_type, const void* bias, int32_t bias_type, int64_t rows, int64_t width, float eps, void* sum,
-                     int64_t sum_stride, void* out, int64_t out_stride, float* mean, float* rstd, int8_t* q, int64_t q_stride,
-                     float* scale, int32_t* sums, void* stream) {
+int qadam_layer_norm(const qadam_layer_norm_args* args, void* stream) {
+  if (!args) return QADAM_ERR_NULL;
+  const auto [x, x_stride, residual, residual_stride, weight, bias, rows, width, sum, sum_stride, out, out_stride, mean, rstd, q, q_stride, scale, sums, type,
+              weight_type, bias_type, eps] = *args;
   if (bad_rows(rows, width)) return QADAM_ERR_SIZE;
   if (!known_type(type) || (weight && !known_type(weight_type)) || (bias && !known_type(bias_type))) return QADAM_ERR_TYPE;
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return QADAM_ERR_HYPER;
@@ -919,10 +919,10 @@ int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* works
   return QADAM_OK;
 }
 
-int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const void* x, int64_t x_stride, const float* mean,
-                          const float* rstd, const void* weight, int32_t weight_type, const void* dsum, int64_t dsum_stride,
-                          int64_t rows, int64_t width, void* dx, int64_t dx_stride, void* dweight, void* dbias, int32_t grad_type,
-                          int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+int qadam_layer_norm_grad(const qadam_layer_norm_grad_args* args, void* stream) {
+  if (!args) return QADAM_ERR_NULL;
+  const auto [dy, dy_stride, x, x_stride, mean, rstd, weight, dsum, dsum_stride, rows, width, dx, dx_stride, dweight, dbias, workspace, workspace_bytes, type,
+              weight_type, grad_type, accumulate] = *args;
   if (bad_rows(rows, width)) return QADAM_ERR_SIZE;
   const bool sums = dweight || dbias;
   if (!known_type(type) || (weight && !known_type(weight_type)) || (sums && !known_type(grad_type))) return QADAM_ERR_TYPE;
@@ -938,7 +938,7 @@ int qadam_layer_norm_grad(const void* dy, int32_t type, int64_t dy_stride, const
       (weight && !is_aligned(weight, type_bytes(weight_type))) ||
       (sums && (!is_aligned(dweight, type_bytes(grad_type)) || !is_aligned(dbias, type_bytes(grad_type)) || !is_aligned(workspace, 256))))
     return QADAM_ERR_ALIGN;
-  if (sums && workspace_bytes < (size_t)parts * 2 * (size_t)width * sizeof(float)) return QADAM_ERR_WORKSPACE;
+  if (sums && workspace_bytes < parts * 2 * width * (int64_t)sizeof(float)) return QADAM_ERR_WORKSPACE;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (rows > 0) {
     GradParams p = {};

@@ -841,61 +841,60 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
 
 constexpr int64_t kMostRows = ((int64_t)1 << 31) - 512, kMostDepth = 131072;                         // (places in a tile's rows stay below 2^31)
 
-int check_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, int64_t channels, const void* bias,
-                  int32_t bias_type, const void* out, int32_t out_type, int64_t out_stride, int32_t transposed, int32_t accumulate,
-                  const uint32_t* status) {
-  if (rows < 0 || rows > kMostRows || channels < 1 || channels > kMostRows || depth < 1 || depth > kMostDepth) return QADAM_ERR_SIZE;
-  if ((transposed != 0 && transposed != 1) || (accumulate != 0 && accumulate != 1)) return QADAM_ERR_SIZE;
-  if (!known_type(out_type) || (bias && !known_type(bias_type))) return QADAM_ERR_TYPE;
-  if (rows > 0 && (!a || !a_scale || !out)) return QADAM_ERR_NULL;
-  if (a_stride < depth || a_stride >= (int64_t)1 << 40 || out_stride < channels || out_stride > (int64_t)1 << 40) return QADAM_ERR_SIZE;
-  if (!is_aligned(a, 16) || a_stride % 16 != 0 || !is_aligned(a_scale, 4) || (bias && !is_aligned(bias, type_bytes(bias_type))) ||
-      !is_aligned(out, type_bytes(out_type)) || !is_aligned(status, 4))
+int check_product(const qadam_product_args& p) {
+  if (p.rows < 0 || p.rows > kMostRows || p.channels < 1 || p.channels > kMostRows || p.depth < 1 || p.depth > kMostDepth) return QADAM_ERR_SIZE;
+  if ((p.transposed != 0 && p.transposed != 1) || (p.accumulate != 0 && p.accumulate != 1)) return QADAM_ERR_SIZE;
+  if (!known_type(p.out_type) || (p.bias && !known_type(p.bias_type))) return QADAM_ERR_TYPE;
+  if (p.rows > 0 && (!p.a || !p.a_scale || !p.out)) return QADAM_ERR_NULL;
+  if (p.a_stride < p.depth || p.a_stride >= (int64_t)1 << 40 || p.out_stride < p.channels || p.out_stride > (int64_t)1 << 40) return QADAM_ERR_SIZE;
+  if (!is_aligned(p.a, 16) || p.a_stride % 16 != 0 || !is_aligned(p.a_scale, 4) || (p.bias && !is_aligned(p.bias, type_bytes(p.bias_type))) ||
+      !is_aligned(p.out, type_bytes(p.out_type)) || !is_aligned(p.status, 4))
     return QADAM_ERR_ALIGN;
   return QADAM_OK;
+}
+
+ProductParams product_params(const qadam_product_args& g) {
+  ProductParams p = {};
+  p.a_scale = g.a_scale;
+  p.bias = g.bias; p.bias_type = g.bias_type;
+  p.out = static_cast<char*>(g.out); p.out_type = g.out_type; p.out_stride = g.out_stride; p.accumulate = g.accumulate;
+  p.rows = g.rows; p.channels = g.channels; p.transposed = g.transposed; p.status = g.status;
+  return p;
 }
 
 }  // namespace
 
 extern "C" {
 
-int qadam_row_product(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, int64_t depth, const int8_t* b, int64_t b_stride,
-                      const float* b_scale, float b_worth, int64_t channels, int32_t transposed, const void* bias, int32_t bias_type,
-                      void* out, int32_t out_type, int64_t out_stride, int32_t accumulate, uint32_t* status, void* stream) {
-  const int rc = check_product(a, a_stride, a_scale, rows, depth, channels, bias, bias_type, out, out_type, out_stride, transposed, accumulate, status);
+int qadam_row_product(const qadam_product_args* args, void* stream) {
+  if (!args) return QADAM_ERR_NULL;
+  const qadam_product_args& g = *args;
+  const int rc = check_product(g);
   if (rc != QADAM_OK) return rc;
-  if (rows > 0 && !b) return QADAM_ERR_NULL;
-  if (transposed && b_scale) return QADAM_ERR_SIZE;
-  if (b_stride < (transposed ? channels : depth) || b_stride >= (int64_t)1 << 40) return QADAM_ERR_SIZE;
-  if (!is_aligned(b, 16) || b_stride % 16 != 0 || !is_aligned(b_scale, 4)) return QADAM_ERR_ALIGN;
-  if (rows == 0) return QADAM_OK;
-  ProductParams p = {};
-  p.a_scale = a_scale; p.b_scale = b_scale; p.worth = b_worth;
-  p.bias = bias; p.bias_type = bias_type;
-  p.out = static_cast<char*>(out); p.out_type = out_type; p.out_stride = out_stride; p.accumulate = accumulate;
-  p.rows = rows; p.channels = channels; p.transposed = transposed; p.b_signed = 1; p.status = status;
-  return enqueue_product(p, a, a_stride, depth, b, b_stride, static_cast<cudaStream_t>(stream));
+  if (g.rows > 0 && !g.b) return QADAM_ERR_NULL;
+  if (g.transposed && g.b_scale) return QADAM_ERR_SIZE;
+  if (g.b_stride < (g.transposed ? g.channels : g.depth) || g.b_stride >= (int64_t)1 << 40) return QADAM_ERR_SIZE;
+  if (!is_aligned(g.b, 16) || g.b_stride % 16 != 0 || !is_aligned(g.b_scale, 4)) return QADAM_ERR_ALIGN;
+  if (g.rows == 0) return QADAM_OK;
+  ProductParams p = product_params(g);
+  p.b_scale = g.b_scale; p.worth = g.b_worth; p.b_signed = 1;
+  return enqueue_product(p, g.a, g.a_stride, g.depth, g.b, g.b_stride, static_cast<cudaStream_t>(stream));
 }
 
-int qadam_held_product(const int8_t* a, int64_t a_stride, const float* a_scale, const int32_t* a_sums, int64_t rows, int64_t depth,
-                       const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t first, int64_t channels, int32_t transposed,
-                       const void* bias, int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, int32_t accumulate,
-                       uint32_t* status, void* stream) {
-  const int rc = check_product(a, a_stride, a_scale, rows, depth, channels, bias, bias_type, out, out_type, out_stride, transposed, accumulate, status);
+int qadam_held_product(const qadam_product_args* args, void* stream) {
+  if (!args) return QADAM_ERR_NULL;
+  const qadam_product_args& g = *args;
+  const int rc = check_product(g);
   if (rc != QADAM_OK) return rc;
-  if (kx != 6) return QADAM_ERR_LEVEL;
-  if (!wcodes || (rows > 0 && !a_sums)) return QADAM_ERR_NULL;
-  const int64_t width = transposed ? channels : depth, table = transposed ? depth : channels;
-  if (!is_aligned(wcodes, 16) || first % 16 != 0 || width % 16 != 0 || !is_aligned(a_sums, 4)) return QADAM_ERR_ALIGN;
-  if (first < 0 || first > (int64_t)1 << 44 || wcode_bytes / 2 > (size_t)1 << 44) return QADAM_ERR_SIZE;
-  if (first > (int64_t)wcode_bytes || table > ((int64_t)wcode_bytes - first) / width) return QADAM_ERR_SIZE;
-  if (rows == 0) return QADAM_OK;
-  ProductParams p = {};
-  p.a_scale = a_scale; p.a_sums = a_sums; p.zero = 64; p.worth = 1.0f / 128.0f;
-  p.bias = bias; p.bias_type = bias_type;
-  p.out = static_cast<char*>(out); p.out_type = out_type; p.out_stride = out_stride; p.accumulate = accumulate;
-  p.rows = rows; p.channels = channels; p.transposed = transposed; p.b_signed = 0; p.status = status;
-  return enqueue_product(p, a, a_stride, depth, static_cast<const uint8_t*>(wcodes) + first, width, static_cast<cudaStream_t>(stream));
+  if (g.kx != 6) return QADAM_ERR_LEVEL;
+  if (!g.b || (g.rows > 0 && !g.a_sums)) return QADAM_ERR_NULL;
+  const int64_t width = g.transposed ? g.channels : g.depth, table = g.transposed ? g.depth : g.channels;
+  if (!is_aligned(g.b, 16) || g.first % 16 != 0 || width % 16 != 0 || !is_aligned(g.a_sums, 4)) return QADAM_ERR_ALIGN;
+  if (g.first < 0 || g.wcode_bytes < 0 || g.first > g.wcode_bytes || table > (g.wcode_bytes - g.first) / width) return QADAM_ERR_SIZE;
+  if (g.rows == 0) return QADAM_OK;
+  ProductParams p = product_params(g);
+  p.a_sums = g.a_sums; p.zero = 64; p.worth = 1.0f / 128.0f; p.b_signed = 0;
+  return enqueue_product(p, g.a, g.a_stride, g.depth, static_cast<const uint8_t*>(g.b) + g.first, width, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -18,7 +18,7 @@ from typing import Optional
 import torch
 
 from .adamw import _need_cuda, stream_of, written
-from .binding import _check, load_library
+from .binding import PRODUCT_ARGS, _check, load_library
 from .embedding import _elsewhere, _row_stride, _status, _type
 
 
@@ -64,6 +64,10 @@ class Int8Rows:
         self.sums_at = self.scale_at + 4 * rows if sums else None
         self._q = self._scale = self._sums = None
         return self
+
+    def _at(self):
+        """q, q_stride, scale, sums"""
+        return self.q_at, self.stride, self.scale_at, self.sums_at
 
     @property
     def q(self) -> torch.Tensor:
@@ -191,7 +195,7 @@ def _output(rows, channels, out, out_dtype, accumulate, bias, device):
             raise ValueError(f"out is {out.dtype}, {out_dtype} was asked for")
         stride = _row_stride(out, "out", (rows, channels), device)
     if bias is None:
-        return out, stride, None, 0
+        return out, stride, 0, 0
     if bias.device != device or bias.shape != (channels,) or not bias.is_contiguous():
         raise ValueError(f"bias: {channels} contiguous elements on {device} are needed")
     return out, stride, bias.data_ptr(), _type(bias, "bias")
@@ -221,11 +225,10 @@ def _product(a, b, worth, bias, out_dtype, out, accumulate, transpose, status):
         raise ValueError(f"a [{rows}, {depth}] and b [{b.rows}, {b.width}] have no common axis{' (transposed)' if transpose else ''}")
     given = out is not None
     out, out_stride, bias_at, bias_type = _output(rows, channels, out, out_dtype, accumulate, bias, device)
-    rc = load_library().qadam_row_product(
-        a.q_at, a.stride, a.scale_at, rows, depth, b.q_at, b.stride,
-        None if transpose or worth is not None else b.scale_at, 1.0 if worth is None else worth, channels, int(transpose),
-        bias_at, bias_type, out.data_ptr(), _type(out, "out"), out_stride, int(accumulate),
-        None if status is None else _status(status, device), stream_of(device))
+    rc = load_library().qadam_row_product(PRODUCT_ARGS.pack(
+        a.q_at, a.stride, a.scale_at, 0, rows, depth, b.q_at, b.stride, 0 if transpose or worth is not None else b.scale_at, channels, bias_at,
+        out.data_ptr(), out_stride, 0 if status is None else _status(status, device), 0, 0, transpose, bias_type, _type(out, "out"), accumulate, 0,
+        1.0 if worth is None else worth), stream_of(device))
     if rc:
         _check(rc, "qadam_row_product")
     if given:
@@ -258,10 +261,10 @@ def held_matmul(a: Int8Rows, wcodes: torch.Tensor, kx: int, rows: int, width: in
     channels = width if transpose else rows
     given = out is not None
     out, out_stride, bias_at, bias_type = _output(a_rows, channels, out, out_dtype, accumulate, bias, device)
-    rc = load_library().qadam_held_product(
-        a.q_at, a.stride, a.scale_at, a.sums_at, a_rows, depth, wcodes.data_ptr(), wcodes.numel(), kx, first,
-        channels, int(transpose), bias_at, bias_type, out.data_ptr(), _type(out, "out"), out_stride, int(accumulate),
-        None if status is None else _status(status, device), stream_of(device))
+    rc = load_library().qadam_held_product(PRODUCT_ARGS.pack(
+        a.q_at, a.stride, a.scale_at, a.sums_at, a_rows, depth, wcodes.data_ptr(), 0, 0, channels, bias_at, out.data_ptr(), out_stride,
+        0 if status is None else _status(status, device), first, wcodes.numel(), transpose, bias_type, _type(out, "out"), accumulate, kx, 0.0),
+        stream_of(device))
     if rc:
         _check(rc, "qadam_held_product")
     if given:

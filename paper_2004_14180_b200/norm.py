@@ -11,7 +11,7 @@ from typing import NamedTuple, Optional, Tuple
 import torch
 
 from .adamw import _need_cuda, stream_of, written
-from .binding import _check, load_library
+from .binding import LAYER_NORM_ARGS, LAYER_NORM_GRAD_ARGS, _check, load_library
 from .embedding import _elsewhere, _row_stride, _type
 from .int8 import Int8Rows
 
@@ -33,7 +33,7 @@ def _like(x: torch.Tensor, whole: bool) -> torch.Tensor:
 
 def _parameter(t: Optional[torch.Tensor], what: str, width: int, device: torch.device):
     if t is None:
-        return None, 0
+        return 0, 0
     if t.device != device or t.shape != (width,) or not t.is_contiguous():
         raise ValueError(f"{what}: {width} contiguous elements on {device} are needed")
     return t.data_ptr(), _type(t, what)
@@ -60,7 +60,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     stride = width if whole else _row_stride(x, "x", x.shape, device)
     weight_at, weight_type = _parameter(weight, "weight", width, device)
     bias_at, bias_type = _parameter(bias, "bias", width, device)
-    total, residual_at, residual_stride = x, None, 0
+    total, residual_at, residual_stride = x, 0, 0
     if residual is not None:
         if residual.dtype != x.dtype:
             raise ValueError(f"residual is {residual.dtype}, x {x.dtype}")
@@ -71,11 +71,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     rstd = torch.empty(n, dtype=torch.float32, device=device)
     rows = Int8Rows._make(n, width, device, True) if int8 else None
     if n:
-        rc = load_library().qadam_layer_norm(
-            x.data_ptr(), kind, stride, residual_at, residual_stride, weight_at, weight_type, bias_at, bias_type, n, width, eps,
-            None if residual is None else total.data_ptr(), width, None if out is None else out.data_ptr(), width, mean.data_ptr(),
-            rstd.data_ptr(), None if rows is None else rows.q_at, 0 if rows is None else rows.stride,
-            None if rows is None else rows.scale_at, None if rows is None else rows.sums_at, stream_of(device))
+        rc = load_library().qadam_layer_norm(LAYER_NORM_ARGS.pack(
+            x.data_ptr(), stride, residual_at, residual_stride, weight_at, bias_at, n, width, 0 if residual is None else total.data_ptr(), width,
+            0 if out is None else out.data_ptr(), width, mean.data_ptr(), rstd.data_ptr(), *((0, 0, 0, 0) if rows is None else rows._at()),
+            kind, weight_type, bias_type, eps), stream_of(device))
         if rc:
             _check(rc, "qadam_layer_norm")
     return Normed(out, total, mean, rstd, rows)
@@ -128,13 +127,13 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd:
     weight_at, weight_type = _parameter(weight, "weight", width, device)
     whole = x.is_contiguous()
     x_stride, dy_stride = width if whole else _row_stride(x, "x", x.shape, device), _row_stride(dy, "dy", x.shape, device)
-    ds_at, ds_stride = (None, 0) if dsum is None else (dsum.data_ptr(), _row_stride(dsum, "dsum", x.shape, device))
+    ds_at, ds_stride = (0, 0) if dsum is None else (dsum.data_ptr(), _row_stride(dsum, "dsum", x.shape, device))
     dx = _like(x, whole)
     size = _grad_workspace(n, width)
     scratch = torch.empty(size, dtype=torch.uint8, device=device)
-    rc = load_library().qadam_layer_norm_grad(
-        dy.data_ptr(), kind, dy_stride, x.data_ptr(), x_stride, mean.data_ptr(), rstd.data_ptr(), weight_at, weight_type, ds_at, ds_stride,
-        n, width, dx.data_ptr(), width, dw_at, db_at, dw_type, int(accumulate), scratch.data_ptr(), size, stream_of(device))
+    rc = load_library().qadam_layer_norm_grad(LAYER_NORM_GRAD_ARGS.pack(
+        dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, mean.data_ptr(), rstd.data_ptr(), weight_at, ds_at, ds_stride, n, width, dx.data_ptr(), width,
+        dw_at, db_at, scratch.data_ptr(), size, kind, weight_type, dw_type, int(accumulate)), stream_of(device))
     if rc:
         _check(rc, "qadam_layer_norm_grad")
     for t in given:

@@ -1,12 +1,15 @@
 """Refusals of layer norm, rows in 8 bits and products in 8 bits, on the host: the C interface checks its arguments before any
 CUDA call, so none of this needs a GPU."""
 import ctypes as C
+import os
+import re
 
 import pytest
 import torch
 
 import paper_2004_14180_b200 as qb
 from paper_2004_14180_b200 import build as qbuild
+from paper_2004_14180_b200.binding import LAYER_NORM_ARGS, LAYER_NORM_GRAD_ARGS, PRODUCT_ARGS, PackedArgs
 
 NULL, SIZE, LEVEL, ALIGN, WORKSPACE, HYPER, TYPE = -1, -2, -3, -4, -5, -8, -12
 A = 1 << 20                                    # an aligned address; nothing here follows it
@@ -20,12 +23,40 @@ def lib():
 
 def call(fn, names, base, **kw):
     args = dict(base, **kw)
-    assert set(args) == set(names), set(args) ^ set(names)
-    return fn(*[args[n] for n in names])
+    if not isinstance(names, PackedArgs):
+        assert set(args) == set(names), set(args) ^ set(names)
+        return fn(*[args[n] for n in names])
+    stream = args.pop("stream")
+    assert set(args) <= set(names.fields), set(args) - set(names.fields)
+    return fn(names.pack(*[args.get(n) or 0 for n in names.fields]), stream)
 
 
-NORM = ("x type x_stride residual residual_stride weight weight_type bias bias_type rows width eps sum sum_stride out out_stride mean rstd q "
-        "q_stride scale sums stream").split()
+@pytest.mark.parametrize("name,packed", [("qadam_layer_norm_args", LAYER_NORM_ARGS), ("qadam_layer_norm_grad_args", LAYER_NORM_GRAD_ARGS),
+                                         ("qadam_product_args", PRODUCT_ARGS)])
+def test_packed_arguments_are_those_of_the_header(name, packed):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qadam.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    body = text[:text.index("} " + name + ";")]
+    body = body[body.rindex("typedef struct {") + len("typedef struct {"):]
+    names, wide = [], True
+    for declaration in body.split(";"):
+        if not declaration.strip():
+            continue
+        fields = declaration.split(",")
+        kind = fields[0].split()[0] if "*" not in fields[0] else "*"
+        small = kind in ("int32_t", "float")
+        assert wide or small                                      # (8 bytes first)
+        wide = wide and not small
+        names += [f.split()[-1].strip("*") for f in fields]
+    assert tuple(names) == packed.fields
+
+
+def test_no_arguments(lib):
+    for fn in (lib.qadam_layer_norm, lib.qadam_layer_norm_grad, lib.qadam_row_product, lib.qadam_held_product):
+        assert fn(None, None) == NULL
+
+
+NORM = LAYER_NORM_ARGS
 NORM_BASE = dict(x=A, type=1, x_stride=768, residual=None, residual_stride=0, weight=A, weight_type=0, bias=A, bias_type=0, rows=0, width=768,
                  eps=1e-5, sum=None, sum_stride=0, out=A, out_stride=768, mean=A, rstd=A, q=None, q_stride=0, scale=None, sums=None, stream=None)
 
@@ -46,8 +77,7 @@ def test_layer_norm(lib, kw, code):
     assert call(lib.qadam_layer_norm, NORM, NORM_BASE, **kw) == code
 
 
-GRAD = ("dy type dy_stride x x_stride mean rstd weight weight_type dsum dsum_stride rows width dx dx_stride dweight dbias grad_type accumulate "
-        "workspace workspace_bytes stream").split()
+GRAD = LAYER_NORM_GRAD_ARGS
 GRAD_BASE = dict(dy=A, type=1, dy_stride=768, x=A, x_stride=768, mean=A, rstd=A, weight=A, weight_type=0, dsum=None, dsum_stride=0, rows=0,
                  width=768, dx=A, dx_stride=768, dweight=None, dbias=None, grad_type=0, accumulate=0, workspace=A, workspace_bytes=1 << 24,
                  stream=None)
@@ -115,8 +145,7 @@ def test_held_rows(lib, kw, code):
     assert call(lib.qadam_held_rows, HELD, HELD_BASE, **kw) == code
 
 
-PRODUCT = ("a a_stride a_scale rows depth b b_stride b_scale b_worth channels transposed bias bias_type out out_type out_stride accumulate status "
-           "stream").split()
+PRODUCT = PRODUCT_ARGS
 PRODUCT_BASE = dict(a=A, a_stride=64, a_scale=A, rows=0, depth=64, b=A, b_stride=64, b_scale=A, b_worth=1.0, channels=10, transposed=0, bias=None,
                     bias_type=0, out=A, out_type=1, out_stride=10, accumulate=0, status=None, stream=None)
 
@@ -133,15 +162,14 @@ def test_row_product(lib, kw, code):
     assert call(lib.qadam_row_product, PRODUCT, PRODUCT_BASE, **kw) == code
 
 
-HELD_PRODUCT = ("a a_stride a_scale a_sums rows depth wcodes wcode_bytes kx first channels transposed bias bias_type out out_type out_stride "
-                "accumulate status stream").split()
-HELD_PRODUCT_BASE = dict(a=A, a_stride=64, a_scale=A, a_sums=A, rows=0, depth=64, wcodes=A, wcode_bytes=1280, kx=6, first=0, channels=20, transposed=0,
+HELD_PRODUCT = PRODUCT_ARGS
+HELD_PRODUCT_BASE = dict(a=A, a_stride=64, a_scale=A, a_sums=A, rows=0, depth=64, b=A, wcode_bytes=1280, kx=6, first=0, channels=20, transposed=0,
                          bias=None, bias_type=0, out=A, out_type=1, out_stride=20, accumulate=0, status=None, stream=None)
 
 
 @pytest.mark.parametrize("kw,code", [
-    ({}, 0), (dict(kx=5), LEVEL), (dict(kx=14), LEVEL), (dict(wcodes=None), NULL), (dict(rows=2, a_sums=None), NULL), (dict(channels=21, out_stride=21), SIZE),
-    (dict(first=128), SIZE), (dict(first=128, channels=18), 0), (dict(first=8), ALIGN), (dict(first=-16), SIZE), (dict(wcodes=A + 4), ALIGN),
+    ({}, 0), (dict(kx=5), LEVEL), (dict(kx=14), LEVEL), (dict(b=None), NULL), (dict(rows=2, a_sums=None), NULL), (dict(channels=21, out_stride=21), SIZE),
+    (dict(first=128), SIZE), (dict(first=128, channels=18), 0), (dict(first=8), ALIGN), (dict(first=-16), SIZE), (dict(b=A + 4), ALIGN),
     (dict(depth=50), ALIGN), (dict(transposed=1), ALIGN), (dict(transposed=1, channels=16), 0), (dict(transposed=1, channels=32, out_stride=32), SIZE),
     (dict(a_sums=A + 1), ALIGN), (dict(a_stride=32), SIZE),
 ])
