@@ -1,5 +1,14 @@
 // Layer norm and its gradients, rows and columns in 8 bits, packed weights as rows of 8 bits:
 // qadam_layer_norm*, qadam_quantize_*, qadam_held_rows.
+//
+//   xhat = (h - mean) rstd,  y = xhat w + b                         mean, rstd: of the row
+//   dx = rstd (g - mean(g) - xhat mean(g xhat)) + ds,  g = dy w      dw = sum over rows of dy xhat,  db = sum over rows of dy
+//   q = rne(x (127 / a)),  a = max(max |x|, 2^-100)
+//
+// All of it is bound by HBM in principle: a row is read once and written once, a few operations an element.  In practice these kernels are bound by
+// instructions (10 to 25 an element and thread) as soon as a row costs more than its elements: what is done for a row (places, reductions over
+// its threads, reciprocals) is why a thread has 16 to 32 elements, and a row no more threads than that takes.  Arithmetic is binary32, in
+// packed pairs; 16-bit results are rounded once, at the end.
 #include "qadam.h"
 
 #include <algorithm>
@@ -159,7 +168,8 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
 }
 
 // One pass: a row is read once, held in registers for mean, sum of squares around it and largest value, and written once.
-// Bound by HBM.  There is a warp for each row: enough of them are on an SM to keep its share of the loads under way.
+// There is a warp for each row: enough of them are on an SM to keep its share of the loads under way.  8192 x 768 bf16, the sum with a residual
+// and its norm: 8.4 us (50 MB; 7.8 at the copy rate); 16 rows: 2.0 us in a row of such launches.
 template <int TY, int NV, bool VEC>
 __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_constant__ RowParams p) {
   wait_for_previous_launch();
@@ -181,7 +191,9 @@ __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_
   finish_row(p, part, group, row, nullptr, h);
 }
 
-// Wider rows, and many: a group of warps (a warp) goes from row to row, with the next ones under way.
+// Wider rows, and many: a group of warps (a warp) goes from row to row, with the next ones under way in shared memory, where the parameters are
+// too.  65536 x 768 bf16: norm 42 us (201 MB, 4.8 TB/s: instructions), into 8 bits 24 (151 MB, 6.3 TB/s); 16384 x 8192 bf16 into 8
+// bits 76 to 88 us (403 MB, 62 at the copy rate; 117 with a CTA for each row); norm of 30011 x 2049 fp32, which begin anywhere, 114 us (492 MB, 76).
 constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
 template <int TY, int NV, bool VEC, bool MANY, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages, int with_parameters) {
@@ -393,7 +405,9 @@ struct GradParams {
 __host__ __device__ constexpr int grad_warps_of_sm(int nv, bool many) { return many && nv == 2 ? 18 : 12; }
 
 // A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
-// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  One read, one write: bound by HBM.
+// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 72 us (403 MB, 62 at the copy
+// rate); 8192 x 768: 9.3 us, and 7.4 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 121 us (114); 30011 x 2049: 199.
+// (Clusters of four CTAs that join their sums first: fewer CTAs find room, 30 us in place of 17 for 8192 x 768.)
 // A row is read from shared memory twice, before and behind its sums: held in registers between, it would leave room for half as
 // many rows on an SM.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
 // row, not for elements.)
@@ -646,7 +660,8 @@ bool enqueue_grad_of(const GradParams& p, int parts, bool vec, cudaStream_t st) 
 // ---------------------------------------------------------------- columns in 8 bits
 
 // The largest values of 256 columns over a chunk of rows, then the transposed bytes: the second pass finds in L2 what the
-// first has read, as long as it is not larger than that.
+// first has read, as long as it is not larger than that.  8192 x 2304 bf16: 13 us (57 MB, 8.8 at the copy rate; the second pass is bound by its
+// instructions, 10 an element); 16384 x 4096, read twice from HBM: 65 us (335 MB, 52).
 constexpr int kColThreads = 256;
 constexpr int kColMaxChunks = 64;
 constexpr int kTileRows = 128, kTileCols = 64, kTilesEach = 4;       // kTilesEach: tiles below each other that a CTA takes
@@ -811,7 +826,7 @@ struct HeldParams {
   float* scale;
 };
 
-// A thread decodes 16 consecutive codes: (16 BITS + 31) / 32 + 1 words at most, one store of 16 bytes.
+// A thread decodes 16 consecutive codes: (16 BITS + 31) / 32 + 1 words at most, one store of 16 bytes.  1537 x 1001 codes of 4 bits: 1.7 us.
 template <int BITS>
 __global__ void __launch_bounds__(256) held_rows_kernel(const __grid_constant__ HeldParams p) {
   wait_for_previous_launch();
