@@ -82,6 +82,11 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, vol
   return false;
 }
 
+// The same for a whole warp, which goes on as one.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, volatile int* gave_up) {
+  return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, gave_up)) != 0;
+}
+
 __device__ __forceinline__ void load_tile(void* to, const CUtensorMap* map, int x, int y, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(shared_at(to)),
@@ -233,7 +238,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   int loaded = 0;                          // stages' fills asked for (warp 0)
   if (warp == 0) {
     for (int i = from; i < to; ++i, ++loaded, at.next(p.stages)) {
-      if (!barrier_wait(&s.empty[at.stage], at.phase ^ 1u, &s.gave_up)) break;
+      if (!warp_wait(&s.empty[at.stage], at.phase ^ 1u, &s.gave_up)) break;
       if (elected()) {
         uint8_t* b = ring + at.stage * stage_bytes;
         barrier_expect(&s.full[at.stage], stage_bytes);
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
                           (unsigned)(kChannels / 16) << 24;
     const unsigned step = p.transposed ? 32 * 128 / 16 : 32 / 16;
     for (int i = from; i < to; ++i, at.next(p.stages)) {
-      if (!barrier_wait(&s.full[at.stage], at.phase, &s.gave_up)) break;
+      if (!warp_wait(&s.full[at.stage], at.phase, &s.gave_up)) break;
       after_sync();
       const unsigned b = shared_at(ring) + (unsigned)at.stage * stage_bytes;
       const uint64_t wd = operand(b), td = operand(b + b_bytes);
@@ -277,7 +282,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     if (in && p.bias) bias = load_one_of(p.bias, p.bias_type, mine);
   }
   __syncthreads();
-  const bool ok = barrier_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0;
+  const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0) != 0;
   after_sync();
   const unsigned from_result = result + (unsigned)(warp % 4 * 32) * 65536u;
   if (split == 1) {
@@ -327,6 +332,8 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     }
     cluster.sync();
   }
+  before_sync();
+  __syncthreads();
   if (s.gave_up && warp == 0 && lane == 0) {
     // what was asked for has to land before this CTA's memory is anyone else's
     for (int i = 0; i < loaded && i < p.stages; ++i) {
@@ -335,8 +342,6 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     }
     if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
   }
-  before_sync();
-  __syncthreads();
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(columns));
 }
 
@@ -504,7 +509,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       const PairTile tile = pair_tile(p, t);
       const int row = tile.token * kPairTokens + rank * 128, channel = tile.channel * 2 * p.half + rank * p.half;
       for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
-        ok = barrier_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up);
+        ok = warp_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up);
         if (!ok) break;
         if (elected()) {
           uint8_t* a = ring + place.stage * kPairStageBytes;
@@ -526,12 +531,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
     RingPlace turn;
     bool ok = true;
     for (int t = blockIdx.x / 2; t < tiles && ok; t += step, turn.next(2)) {
-      ok = barrier_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up);
+      ok = warp_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up);
       if (!ok) break;
       after_sync();
       const unsigned at = result + (unsigned)turn.stage * 256u;
       for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
-        ok = barrier_wait(&s.full[place.stage], place.phase, &s.gave_up);
+        ok = warp_wait(&s.full[place.stage], place.phase, &s.gave_up);
         if (!ok) break;
         after_sync();
         const unsigned a = shared_at(ring) + (unsigned)place.stage * kPairStageBytes;
@@ -585,7 +590,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       const float times = a_scale;
       const int off = less * p.zero;
       __syncwarp();
-      if (!barrier_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up)) break;
+      if (!warp_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up)) break;
       after_sync();
       ask(t + step);
       const unsigned at = result + (unsigned)turn.stage * 256u + (unsigned)(quarter * 32) * 65536u;
@@ -670,18 +675,22 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   }
-  __syncwarp();
-  if (s.gave_up && warp == 0 && lane == 0) {
-    // what was asked for has to land before these CTAs' memory is anyone else's
-    for (int i = 0; rank == 0 && i < loaded; ++i) {
-      place.back(p.stages);
-      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[place.stage], place.phase); ++n) {}
-    }
-    if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
-  }
+  if (*static_cast<volatile int*>(&s.gave_up)) *cluster.map_shared_rank(&s.gave_up, rank ^ 1) = 1;         // (who gave up comes by here afterwards)
   before_sync();
   cluster.sync();
   after_sync();
+  if (s.gave_up) {                         // in both, then
+    // what was asked for has to land before these CTAs' memory is anyone else's: the first one's barriers count both's
+    if (rank == 0 && warp == 0 && lane == 0) {
+      for (int i = 0; i < loaded; ++i) {
+        place.back(p.stages);
+        for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[place.stage], place.phase); ++n) {}
+      }
+      if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
+    }
+    __syncwarp();
+    cluster.sync();
+  }
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(512));
 }
 
@@ -812,7 +821,8 @@ int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int
   p.token_tiles = (int)((p.rows + kPairTokens - 1) / kPairTokens);
   p.half = pair_shape(p.rows, p.channels, p.blocks, pairs).half;
   p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
-  const bool boxes = (!p.accumulate || q.out_type == QADAM_F32) && is_aligned(p.out, 16) && p.out_stride * type_bytes(q.out_type) % 16 == 0;
+  const int64_t out_pitch = p.out_stride * type_bytes(q.out_type);
+  const bool boxes = (!p.accumulate || q.out_type == QADAM_F32) && is_aligned(p.out, 16) && out_pitch % 16 == 0 && out_pitch < (int64_t)1 << 40;
   p.boxes = boxes && q.out_type != QADAM_F32 && p.blocks >= kLongSum ? 1 : 2;
   p.stages = p.boxes == 1 ? 5 : 4;
   CUtensorMap a_map, b_map, out_map = {};

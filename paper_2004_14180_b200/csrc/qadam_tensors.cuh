@@ -49,9 +49,10 @@ inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintpt
 inline size_t round_up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Launches `kernel` so that it may be brought up while what is before it in the stream ends (every kernel that is launched
-// so begins with wait_for_previous_launch).  The kernels before it say nothing early, so what is gained is the launch
-// alone: 2 us of 14 (norm of 11.7 x 10^6 elements), 11 us of 161 over the five launches of a long embedding gradient.
-// Saying so early gained nothing more.  cluster > 0: CTAs of a cluster.
+// so begins with wait_for_previous_launch, or touches nothing but its own SM before it).  The kernels before it say nothing
+// early, so what is gained is the launch alone: 2 us of 14 (norm of 11.7 x 10^6 elements), 11 us of 161 over the five launches of a
+// long embedding gradient.  Saying so early gained nothing more there; the kernels over token rows do (qadam_layer.cu).
+// cluster > 0: CTAs of a cluster.
 template <typename... P, typename... A>
 inline bool launch(void (*kernel)(P...), long long grid, int block, size_t smem, int cluster, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t config = {};
