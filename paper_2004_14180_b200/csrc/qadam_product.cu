@@ -388,6 +388,7 @@ struct PairParams {
   int blocks;
   int half;                                // channels of a tile that a CTA's shared memory has the weights of: 32, 64, 96 or 128
   int token_tiles, channel_tiles;
+  unsigned group_magic;                    // 2^32 / (kTokenGroup channel_tiles), rounded up
   int transposed, b_signed;
   int stages, boxes;
   unsigned* status;
@@ -458,10 +459,16 @@ __device__ __forceinline__ void add_box(const CUtensorMap* map, const void* from
 struct PairTile {
   int token, channel;                      // tiles
 };
+// (A division by multiplication, which may be one too large, and one by eight: with divisions for every tile the end of a tile took 0.3 us more.)
 __device__ __forceinline__ PairTile pair_tile(const PairParams& p, int t) {
-  const int group = t / (kTokenGroup * p.channel_tiles);
-  const int first = group * kTokenGroup, tall = min(kTokenGroup, p.token_tiles - first);
-  const int in = t - first * p.channel_tiles;
+  const int wide = kTokenGroup * p.channel_tiles;
+  int group = (int)__umulhi((unsigned)t, p.group_magic), in = t - group * wide;
+  if (in < 0) {
+    --group;
+    in += wide;
+  }
+  const int first = group * kTokenGroup, tall = p.token_tiles - first;
+  if (tall >= kTokenGroup) return {first + in % kTokenGroup, in / kTokenGroup};
   return {first + in % tall, in / tall};
 }
 
@@ -553,7 +560,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   } else if (warp >= 4) {
     const int end = warp - 4, quarter = warp % 4, side = end / 4;
     uint8_t* boxes = ring + p.stages * kPairStageBytes + end * p.boxes * kBoxBytes;
-    float2* about = reinterpret_cast<float2*>(ring + p.stages * kPairStageBytes + kEndWarps * p.boxes * kBoxBytes) + end * kEndChannels;   // scale, bias
+    float2* about = reinterpret_cast<float2*>(ring + p.stages * kPairStageBytes + kEndWarps * p.boxes * kBoxBytes) + end * kEndChannels;   // two scales, two biases, ...
     constexpr bool kWide = BOXES && OUT != QADAM_F32;                        // a box has 64 channels of 16 bits, or 32 of 32 bits
     // what the end of a tile needs to know is asked for while the tile before it is at its end
     float2 channels[kEndChannels / 32];
@@ -562,15 +569,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
     const auto ask = [&](int t) {
       if (t >= tiles) return;
       const PairTile tile = pair_tile(p, t);
-      const long long row = (long long)tile.token * kPairTokens + rank * 128 + quarter * 32 + lane;
-      a_scale = row < p.rows ? p.a_scale[row] : 0.0f;
-      less = row < p.rows && p.a_sums ? p.a_sums[row] : 0;
+      const int row = tile.token * kPairTokens + rank * 128 + quarter * 32 + lane;
+      a_scale = row < (int)p.rows ? p.a_scale[row] : 0.0f;
+      less = row < (int)p.rows && p.a_sums ? p.a_sums[row] : 0;
 #pragma unroll
       for (int i = 0; i < kEndChannels / 32; ++i) {                          // this warp's: every other unit of the tile
         const int n = i * 32 + lane, c = (n / kUnit * 2 + side) * kUnit + n % kUnit;
-        const long long at = (long long)tile.channel * 2 * p.half + c;
+        const int at = tile.channel * 2 * p.half + c;
         channels[i] = make_float2(p.worth, 0.0f);
-        if (c < 2 * p.half && at < p.channels) {
+        if (c < 2 * p.half && at < (int)p.channels) {
           if (p.b_scale) channels[i].x = p.b_scale[at];
           if (p.bias) channels[i].y = load_one_of(p.bias, p.bias_type, at);
         }
@@ -586,7 +593,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       const int wide = (int)min((long long)2 * p.half, p.channels - channel0);
       __syncwarp();
 #pragma unroll
-      for (int i = 0; i < kEndChannels / 32; ++i) about[i * 32 + lane] = channels[i];
+      for (int i = 0; i < kEndChannels / 32; ++i) {
+        float* to = reinterpret_cast<float*>(about) + (i * 32 + (lane & ~1)) * 2 + (lane & 1);
+        to[0] = channels[i].x;
+        to[2] = channels[i].y;
+      }
       const float times = a_scale;
       const int off = less * p.zero;
       __syncwarp();
@@ -616,8 +627,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
 #pragma unroll
           for (int i = 0; i < 8; i += 2) {
             const float4 g = f[(k + i) / 2];
-            y[i] = fmaf((float)((int)v[k + i] - off) * times, g.x, g.y);
-            y[i + 1] = fmaf((float)((int)v[k + i + 1] - off) * times, g.z, g.w);
+            const float2 sum = make_float2((float)((int)v[k + i] - off), (float)((int)v[k + i + 1] - off));
+            const float2 z = fma2_rn(mul2_rn(sum, make_float2(times, times)), make_float2(g.x, g.y), make_float2(g.z, g.w));
+            y[i] = z.x;
+            y[i + 1] = z.y;
           }
           if constexpr (kWide) {
             store_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(line + (((k / 8) ^ (lane & 7)) << 4), floats_to_raw8<OUT == QADAM_F32 ? QADAM_BF16 : OUT>(y));
@@ -821,6 +834,7 @@ int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int
   p.token_tiles = (int)((p.rows + kPairTokens - 1) / kPairTokens);
   p.half = pair_shape(p.rows, p.channels, p.blocks, pairs).half;
   p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
+  p.group_magic = (unsigned)((((uint64_t)1 << 32) + kTokenGroup * (uint64_t)p.channel_tiles - 1) / (kTokenGroup * (uint64_t)p.channel_tiles));
   const int64_t out_pitch = p.out_stride * type_bytes(q.out_type);
   const bool boxes = (!p.accumulate || q.out_type == QADAM_F32) && is_aligned(p.out, 16) && out_pitch % 16 == 0 && out_pitch < (int64_t)1 << 40;
   p.boxes = boxes && q.out_type != QADAM_F32 && p.blocks >= kLongSum ? 1 : 2;
