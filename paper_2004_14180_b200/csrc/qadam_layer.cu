@@ -405,8 +405,8 @@ struct GradParams {
 __host__ __device__ constexpr int grad_warps_of_sm(int nv, bool many) { return many && nv == 2 ? 18 : 12; }
 
 // A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
-// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 72 us (403 MB, 62 at the copy
-// rate); 8192 x 768: 9.3 us, and 7.4 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 121 us (114); 30011 x 2049: 199.
+// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 70 us (403 MB, 62 at the copy
+// rate); 8192 x 768: 9.4 us, and 5.6 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 121 us (114); 30011 x 2049: 199.
 // (Clusters of four CTAs that join their sums first: fewer CTAs find room, 30 us in place of 17 for 8192 x 768.)
 // A row is read from shared memory twice, before and behind its sums: held in registers between, it would leave room for half as
 // many rows on an SM.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
@@ -510,11 +510,19 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
     __syncthreads();
   }
 #pragma unroll
-  for (int e = 0; e < 2 * Part::kPairs; ++e) {
-    if (part.has(Part::piece_of(e))) {
-      const int col = part.column(Part::piece_of(e)) + e % Part::kPiece;
-      to[col] = e % 2 ? dw[e / 2].y : dw[e / 2].x;
-      to[p.width + col] = e % 2 ? db[e / 2].y : db[e / 2].x;
+  for (int q = 0; q < Part::kPieces; ++q) {
+    if (part.has(q)) {
+      if constexpr (VEC) {                                 // (16 bytes at a time: one by one, eight lanes would meet in a bank)
+#pragma unroll
+        for (int k = 0; k < Part::kPiece; k += 4) {
+          const int i = (q * Part::kPiece + k) / 2, col = part.column(q) + k;
+          *reinterpret_cast<float4*>(to + col) = make_float4(dw[i].x, dw[i].y, dw[i + 1].x, dw[i + 1].y);
+          *reinterpret_cast<float4*>(to + p.width + col) = make_float4(db[i].x, db[i].y, db[i + 1].x, db[i + 1].y);
+        }
+      } else {
+        to[part.column(q)] = q % 2 ? dw[q / 2].y : dw[q / 2].x;
+        to[p.width + part.column(q)] = q % 2 ? db[q / 2].y : db[q / 2].x;
+      }
     }
   }
   if (groups > 1) {

@@ -351,9 +351,9 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
 // channels' weights in its shared memory, and the results of its 128 tokens in its tensor memory.  That halves the weights'
 // way into shared memory.  The pairs go from tile to tile; results have two places, so that the end of a tile (eight warps: numbers of
 // 32 bits times scales, rounded, through shared memory and out in boxes) runs beside the next one's products.  16384 x 8192 x 8192: 643 us
-// (3.42 x 10^15 operations a second; twice the measured bf16 rate is 3.36), 4096 x 4096 x 4096 51 us (2.7); products alone, from shared memory as it
+// (3.42 x 10^15 operations a second; twice the measured bf16 rate is 3.36), 4096 x 4096 x 4096 46 us (3.0); products alone, from shared memory as it
 // is, take 0.25 us a block, with their loads 0.36: shared memory takes 32 KB in and gives 48 KB out for each block.  8192 x 768 x 2304
-// (sums of six blocks): 18.4 us, of which 3.5 are start and end; without the results' stores 15.7, without their arithmetic too 13.0.
+// (sums of six blocks): 17.8 us, of which 3.5 are start and end; before it was 18.7, without the results' stores 15.7, without their arithmetic too 13.0.
 // (Weights that stay in shared memory from tile to tile, for short sums: 18.6 us, and 53 in place of 47 for 65536 x 768 x 768.)
 constexpr int kPairThreads = 384;          // a warp that loads, one that multiplies, one for tensor memory, one idle, eight for the end
 constexpr int kPairTokens = 256;
