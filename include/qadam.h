@@ -538,7 +538,8 @@ int qadam_embedding_grad(const void* ids, int32_t id_bits, int64_t count, const 
  * in binary32; out = round(y).  x, residual, sum, out: device, rows a stride (in elements, >= width) apart, all of `type`.
  * weight, bias: device, [width], each of a type of its own, or NULL (1, 0).  mean, rstd: device, [rows], or NULL.
  * q (NULL: none): y before its rounding, in 8 bits, with scale and sums as qadam_quantize_rows writes them.  Of out, q, mean and
- * rstd at least one is needed; sum goes with residual.  rows = 0 is allowed; rows < 2^31, width <= 2^24. */
+ * rstd at least one is needed; sum goes with residual.  rows = 0 is allowed; rows < 2^31, width <= 2^24.  What is written may not
+ * overlap what is read (here and in the calls below): wide rows are read more than once. */
 typedef struct {
   const void* x; int64_t x_stride;
   const void* residual; int64_t residual_stride;
@@ -607,7 +608,7 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
  * transposed = 1: B[k][n] = b[k][n], b is [depth][b_stride >= channels], as the gradient of a layer's input needs it; b_scale is
  * NULL (scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
- * rows = 0 is allowed; rows, channels <= 2^31 - 512.
+ * rows = 0 is allowed; rows, channels <= 2^31 - 512.  accumulate in binary32: numbers below 2^-126 may count as zero, in out too.
  * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
 typedef struct {
   const int8_t* a; int64_t a_stride; const float* a_scale; const int32_t* a_sums;   /* a_sums: qadam_held_product only */
