@@ -608,7 +608,7 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
  * transposed = 1: B[k][n] = b[k][n], b is [depth][b_stride >= channels], as the gradient of a layer's input needs it; b_scale is
  * NULL (scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
- * rows = 0 is allowed; rows, channels <= 2^31 - 512.  accumulate in binary32: numbers below 2^-126 may count as zero, in out too.
+ * rows = 0 is allowed; rows, channels <= 2^31 - 512.
  * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
 typedef struct {
   const int8_t* a; int64_t a_stride; const float* a_scale; const int32_t* a_sums;   /* a_sums: qadam_held_product only */

@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_
 
 // Wider rows, and many: a group of warps (a warp) goes from row to row, with the next ones under way in shared memory, where the parameters are
 // too.  65536 x 768 bf16: norm 42 us (201 MB, 4.8 TB/s: instructions), into 8 bits 24 (151 MB, 6.3 TB/s); 16384 x 8192 bf16 into 8
-// bits 76 to 88 us (403 MB, 62 at the copy rate; 117 with a CTA for each row); norm of 30011 x 2049 fp32, which begin anywhere, 114 us (492 MB, 76).
+// bits 76 to 88 us (403 MB, 62 at the copy rate; 117 with a CTA for each row); norm of 30011 x 2049 fp32, which begin anywhere, 111 us (492 MB, 76).
 constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
 template <int TY, int NV, bool VEC, bool MANY, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages, int with_parameters) {
@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(co
   const long long first = (long long)blockIdx.x * groups + number, step = (long long)gridDim.x * groups;
   const auto fetch = [&](long long row, int stage) {
     if (row < p.rows) {
-      part.fetch(ring + stage * both, p.x + row * p.x_stride * Part::kBytes);
-      if (p.r) part.fetch(ring + stage * both + each, p.r + row * p.r_stride * Part::kBytes);
+      part.fetch(ring + stage * both, p.x + row * p.x_stride * Part::kBytes, p.x);
+      if (p.r) part.fetch(ring + stage * both + each, p.r + row * p.r_stride * Part::kBytes, p.r);
     }
     fetched();
   };
@@ -379,7 +379,7 @@ int enqueue_rows(const RowParams& p, int type, bool vec, cudaStream_t st) {
 // ---------------------------------------------------------------- gradients
 
 constexpr int kGradWarps = 6;                              // of a CTA, in groups, two CTAs to an SM; or one group of up to 11 in a CTA of its own
-constexpr int kGradMostWarps = 12;
+constexpr int kGradMoreWarps = 8, kGradMostWarps = 12;          // (8: registers for two such CTAs, 16384 x 4096 fp32 and fp16 too)
 constexpr int kGradGroupWidth = 8192;                      // beyond, rows are read again, and the columns' sums are a pass of their own
 
 struct GradParams {
@@ -405,11 +405,11 @@ struct GradParams {
 __host__ __device__ constexpr int grad_warps_of_sm(int nv, bool many) { return many && nv == 2 ? 18 : 12; }
 
 // A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
-// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 70 us (403 MB, 62 at the copy
-// rate); 8192 x 768: 9.4 us, and 5.6 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 121 us (114); 30011 x 2049: 199.
+// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 69 us (403 MB, 62 at the copy
+// rate); 8192 x 768: 8.8 us, and 5.8 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 119 us (114); 30011 x 2049: 146.
 // (Clusters of four CTAs that join their sums first: fewer CTAs find room, 30 us in place of 17 for 8192 x 768.)
-// A row is read from shared memory twice, before and behind its sums: held in registers between, it would leave room for half as
-// many rows on an SM.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
+// Where an SM gets 12 warps, registers hold a row between its sums and its result (2 to 4 % less time); where it gets 18, the row is read from
+// shared memory again.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
 // row, not for elements.)
 template <int TY, int NV, bool VEC, bool MANY, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS) row_grad_kernel(const __grid_constant__ GradParams p, int warps, int stages) {
@@ -418,6 +418,7 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
   wait_for_previous_launch();
   using Part = RowPart<TY, NV, VEC>;
   constexpr int kBytes = Part::kBytes;
+  constexpr bool kHold = grad_warps_of_sm(NV, MANY) == 12;
   const int threads = MANY ? warps * 32 : 32, number = (int)threadIdx.x / threads;
   const int groups = blockDim.x / threads;
   const Part part(p.width, threads, (int)threadIdx.x % threads);
@@ -436,9 +437,9 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
   const auto fetch = [&](long long row, int stage) {
     if (row < p.rows) {
       uint8_t* to = ring + stage * all_of;
-      part.fetch(to, next_x);
-      part.fetch(to + each, next_dy);
-      if (p.ds_ahead) part.fetch(to + 2 * each, next_ds);
+      part.fetch(to, next_x, p.x);
+      part.fetch(to + each, next_dy, p.dy);
+      if (p.ds_ahead) part.fetch(to + 2 * each, next_ds, p.ds);
     }
     next_x += x_step;
     next_dy += dy_step;
@@ -460,6 +461,7 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
     const char *x = p.x + row * p.x_stride * kBytes, *dy = p.dy + row * p.dy_stride * kBytes, *ds = p.ds + row * p.ds_stride * kBytes;
     const float2 less = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
     float2 along2 = make_float2(0.0f, 0.0f), all2 = along2;
+    typename Part::Row held_h, held_g;
 #pragma unroll
     for (int q = 0; q < Part::kPieces; q += Part::kStep) {
       float2 h[Part::kStepPairs], g[Part::kStepPairs], by[Part::kStepPairs];
@@ -475,27 +477,38 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
         g[k] = mul2_rn(g[k], by[k]);
         along2 = fma2_rn(g[k], h[k], along2);
         all2 = add2_rn(all2, g[k]);
+        if constexpr (kHold) {
+          held_h[i] = h[k];
+          held_g[i] = g[k];
+        }
       }
     }
     float along = along2.x + along2.y, all = all2.x + all2.y;
     group.add2(along, all);
     const float2 minus_along = make_float2(-along * per, -along * per), minus_all = make_float2(-all * per, -all * per);
-    asm volatile("" ::: "memory");                         // the row is read again, not held
+    if constexpr (!kHold) asm volatile("" ::: "memory");  // the row is read again
     char* dx = p.dx + row * p.dx_stride * kBytes;
 #pragma unroll
     for (int q = 0; q < Part::kPieces; q += Part::kStep) {
       float2 h[Part::kStepPairs], g[Part::kStepPairs], by[Part::kStepPairs], s[Part::kStepPairs];
-      part.read_piece(from, x, q, h);
-      part.read_piece(from + each, dy, q, g);
+      if constexpr (!kHold) {
+        part.read_piece(from, x, q, h);
+        part.read_piece(from + each, dy, q, g);
+      }
 #pragma unroll
       for (int k = 0; k < Part::kStepPairs; ++k) s[k] = make_float2(0.0f, 0.0f);
       if (p.ds_ahead) part.read_piece(from + 2 * each, ds, q, s);
       else if (p.ds) part.load_piece(ds, q, s);
-      part.read_shared(w, q, by);
+      if constexpr (!kHold) part.read_shared(w, q, by);
 #pragma unroll
       for (int k = 0; k < Part::kStepPairs; ++k) {
-        h[k] = mul2_rn(add2_rn(h[k], less), times);
-        g[k] = mul2_rn(g[k], by[k]);
+        if constexpr (kHold) {
+          h[k] = held_h[q / Part::kStep * Part::kStepPairs + k];
+          g[k] = held_g[q / Part::kStep * Part::kStepPairs + k];
+        } else {
+          h[k] = mul2_rn(add2_rn(h[k], less), times);
+          g[k] = mul2_rn(g[k], by[k]);
+        }
         s[k] = fma2_rn(times, fma2_rn(h[k], minus_along, add2_rn(g[k], minus_all)), s[k]);
       }
       part.store_piece(dx, q, s);
@@ -618,8 +631,8 @@ struct GradShape {
 };
 GradShape grad_shape(int width, bool vec) {
   GradShape g;
-  // Rows of a warp: 8, 16 or 24 elements to a thread.  Wider ones: 16, and so more warps on an SM (30012 x 2048 fp32: 121 us, with 24 147),
-  // but 24 where elements are taken one by one and a row's ends cost more (30011 x 2049 fp32: 194 us, with 16 222), and beyond 6144.
+  // Rows of a warp: 8, 16 or 24 elements to a thread.  Wider ones: 16, and so more warps on an SM (30012 x 2048 fp32: 119 us, with 24 147),
+  // but 24 where elements are taken one by one and a row's ends cost more (30011 x 2049 fp32, when a row's ends were not yet fetched ahead: 194 us, with 16 222), and beyond 6144.
   g.pieces = width <= 768 ? (width + 255) / 256 : vec && width <= kGradMostWarps * 512 ? 2 : 3;
   g.warps = (width + 256 * g.pieces - 1) / (256 * g.pieces);
   g.groups = std::max(1, kGradWarps / g.warps);
@@ -652,6 +665,7 @@ bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
   }
   if constexpr (VEC) {
     if (g.warps <= kGradWarps) return launch_grad<TY, 2, VEC, true, kGradWarps>(p, g, parts, st);
+    if (g.pieces == 2 && g.warps <= kGradMoreWarps) return launch_grad<TY, 2, VEC, true, kGradMoreWarps>(p, g, parts, st);
     return g.pieces == 2 ? launch_grad<TY, 2, VEC, true, kGradMostWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);
   } else {
     return g.warps <= kGradWarps ? launch_grad<TY, 3, VEC, true, kGradWarps>(p, g, parts, st) : launch_grad<TY, 3, VEC, true, kGradMostWarps>(p, g, parts, st);

@@ -449,7 +449,7 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, const void* fr
                : "memory");
 }
 
-// The same, added to what is there (binary32: one rounding, as a load, a sum and a store would have, but subnormal numbers are zero).
+// The same, added to what is there (binary32: one rounding, as a load, a sum and a store would have).
 __device__ __forceinline__ void add_box(const CUtensorMap* map, const void* from, int x, int y) {
   asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
                "r"(shared_at(from))

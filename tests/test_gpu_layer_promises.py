@@ -219,6 +219,33 @@ def test_gradients_by_every_number_of_warps_to_a_row(rows, width, kind):
     near(db, wb, few * U * sb, "f32")
 
 
+def among_nans(t, left, gap):
+    """The same rows, `left` elements from 16 bytes and `gap` apart, with NaN before, between and behind them."""
+    rows, width = t.shape
+    room = torch.full((left + rows * (width + gap) + 16,), float("nan"), dtype=t.dtype, device="cuda")
+    r = room[left:left + rows * (width + gap)].view(rows, width + gap)[:, :width]
+    r.copy_(t)
+    return r
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,width", [(4000, 1025), (3500, 1535), (16000, 3), (16000, 255), (16000, 767), (2500, 2303), (700, 8191), (4000, 1)])
+def test_rows_anywhere_among_numbers_that_are_not_theirs(rows, width, kind):
+    # many rows to a place in shared memory, each as far from 16 bytes as it happens to lie
+    gen = gen_of(rows, width, 3)
+    x, dy, ds = ((randn(gen, rows, width)).to(DTYPES[kind]) for _ in range(3))
+    w = 1 + 0.1 * randn(gen, width)
+    ran = qb.layer_norm(x, w, residual=ds, int8=True)
+    want = qb.layer_norm_grad(dy, x, ran.mean, ran.rstd, w, dsum=ds)
+    for left, gap in ((1, 0), (3, 1), (5, 2), (7, 3), (2, 4)):
+        a, b, c = among_nans(x, left, gap), among_nans(dy, left + 1, gap), among_nans(ds, left, gap + 1)
+        here = qb.layer_norm(a, w, residual=c, int8=True)
+        assert torch.equal(here.out, ran.out) and torch.equal(here.sum, ran.sum) and torch.equal(here.mean, ran.mean) and torch.equal(here.rstd, ran.rstd)
+        assert torch.equal(here.rows.q, ran.rows.q) and torch.equal(here.rows.sums, ran.rows.sums)
+        for got, wanted in zip(qb.layer_norm_grad(b, a, ran.mean, ran.rstd, w, dsum=c), want):
+            assert torch.equal(got, wanted)
+
+
 def test_bytes_behind_rows_are_not_read():
     gen = gen_of(12)
     for k in (5, 100, 131):
