@@ -285,6 +285,14 @@ struct RowPart {
       if (has(q + 1)) store_one<TY>(to, 32 * q + 32, x[0].y);
     }
   }
+  // Clears what of piece q (and the next one, where a piece is one element) is beyond the row.
+  __device__ __forceinline__ void clear_beyond(int q, float2* x) const {
+#pragma unroll
+    for (int k = 0; k < kStepPairs; ++k) {
+      if (!has(q)) x[k].x = 0.0f;
+      if (!has(VEC ? q : q + 1)) x[k].y = 0.0f;
+    }
+  }
   // x becomes what is stored.
   __device__ __forceinline__ void store_rounded(void* row, Row& x) const {
     store(row, x);
