@@ -120,6 +120,19 @@ __device__ __forceinline__ float warp_add(float v) {
   return v;
 }
 
+// Sums over a row divided by its width, correctly rounded (but for quotients below 2^-126), without a division for each row: a quotient from the
+// rounded reciprocal, and what it leaves over, which is exact (P. Markstein, Computation of elementary functions on the IBM RISC
+// System/6000 processor, 1990).  The product with the reciprocal alone may be off by a unit in the last place: the mean of
+// 1000 times 200 was 200.00002.  Divisions: 25.3 in place of 22.9 us for the norm of 65536 x 256 bf16.
+struct RowWidth {
+  float n, per;
+  __host__ __device__ static RowWidth of(int width) { return {(float)width, 1.0f / (float)width}; }
+  __device__ __forceinline__ float mean_of(float sum) const {
+    const float q = sum * per;
+    return fabsf(q) < __int_as_float(0x7F800000) ? fmaf(fmaf(-q, n, sum), per, q) : q;
+  }
+};
+
 // Reductions over the threads that share a row: a warp, or (MANY) up to 32 warps of a CTA, that have a barrier of their own.  Reductions
 // take turns with two buffers, so one barrier each is enough: a buffer is written again only behind the barrier of the reduction
 // between.
@@ -147,8 +160,8 @@ class RowGroup {
     }
     return v;
   }
-  // Two sums at the price of one: the warp's lower half adds up a, its upper half b.
-  __device__ __forceinline__ void add2(float& a, float& b) {
+  // The means of two sums at the price of one: the warp's lower half has a, its upper half b.
+  __device__ __forceinline__ void mean2(float& a, float& b, const RowWidth& width) {
     const bool upper = threadIdx.x % 32 >= 16;
     float mine = upper ? b : a;
     mine += __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
@@ -162,6 +175,7 @@ class RowGroup {
       mine = half_add(mine);
       turn_ ^= 1;
     }
+    mine = width.mean_of(mine);
     const float other = __shfl_xor_sync(0xFFFFFFFFu, mine, 16);
     a = upper ? other : mine;
     b = upper ? mine : other;

@@ -26,3 +26,33 @@ def test_gradient_of_rows_whose_mean_times_rstd_is_beyond_binary32(width, kind):
         near(dx, want, off, kind)
         assert not dw.any()                                                     # x is its row's mean: xhat = 0
         near(db, wb, 9 * 2.0 ** -24 * sb, "f32")                                # nine terms in any order
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,width", [(3, 41), (3, 896), (3, 1000), (8000, 1000), (3, 3584), (2000, 3584), (3, 7001), (2, 20001)])
+def test_rows_of_one_whole_number_have_no_spread(rows, width, kind):
+    # The sum is a whole number below 2^24, so exact, and the mean is the value: xhat = 0, and rstd = 1 / sqrt(eps), of which quotient, sum, root and
+    # reciprocal leave 3 halves of a step: the root's argument is eps itself.
+    x = torch.arange(1, rows + 1, device="cuda").remainder(256).to(DTYPES[kind])[:, None].repeat(1, width)
+    b = torch.full((width,), 0.75, device="cuda")
+    for eps in (1e-12, 1e-5):
+        got = qb.layer_norm(x, None, b, eps=eps, int8=True)
+        assert torch.equal(got.mean, x[:, 0].float())
+        want = 1 / torch.tensor(eps, dtype=torch.float32, device="cuda").double().sqrt()
+        assert bool(((got.rstd.double() - want).abs() <= 3 * 2.0 ** -24 * want).all())
+        assert bool((got.out == 0.75).all()) and bool((got.rows.q == 127).all())
+    # and the gradient of equal gradients is nothing: g is its own mean
+    dy = torch.full_like(x, 3.0)
+    dx, dw, db = qb.layer_norm_grad(dy, x, got.mean, got.rstd)
+    assert not dx.any() and not dw.any() and torch.equal(db, torch.full_like(db, 3.0 * rows))
+
+
+@pytest.mark.parametrize("width", [3, 41, 896, 1000, 1025, 3584, 7001, 16384, 20001])
+def test_means_of_whole_numbers_are_rounded_once(width):
+    # sums of whole numbers below 2^24 are exact in any order, and the mean is the quotient, correctly rounded (as torch's division is)
+    gen = gen_of(width, 62)
+    x = torch.randint(-300, 701, (500, width), generator=gen, device="cuda").float()
+    got = qb.layer_norm(x)
+    assert torch.equal(got.mean, x.double().sum(1).float() / torch.full((500,), float(width), device="cuda"))
+    big = torch.full((2, width), 3e38, device="cuda")                             # sums beyond binary32: as sum / width has it
+    assert bool(qb.layer_norm(big).mean.isinf().all())
