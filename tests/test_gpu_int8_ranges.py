@@ -53,3 +53,17 @@ def test_what_is_beyond_binary16_is_infinite(m, n):
     want = (a.q.double() @ b.q.double().T).float().half()
     assert bool(want.isinf().any()) and bool(want.isfinite().any())
     assert torch.equal(qb.int8_matmul(a, b, out_dtype=torch.float16), want)
+
+
+@pytest.mark.parametrize("m,left", [(16, 0), (300, 0), (300, 1)])
+def test_sums_that_are_added_to_keep_numbers_below_the_normal_ones(m, left):
+    # few tokens, boxes, elements; kept, added and what is left of normal numbers: as a binary32 sum has it
+    q = torch.zeros(m, 64, dtype=torch.int8, device="cuda")
+    q[:, 0] = 1
+    a = qb.Int8Rows(q, torch.ones(m, device="cuda"))
+    least = 2.0 ** -126
+    for before, more in ((1e-41, 0.0), (0.0, 1e-41), (1.5 * least, -least), (1e-41, 2e-41), (-1e-41, least), (least, 2.0 ** -140)):
+        b = qb.Int8Rows(q[:1].expand(300, 64).contiguous(), torch.full((300,), more, device="cuda"))
+        out = torch.full((m, 304), before, device="cuda")[:, left:left + 300]
+        want = (out.double() + b.scale.double()).float()
+        assert torch.equal(qb.int8_matmul(a, b, out=out, accumulate=True), want) and bool((want != 0).all())
