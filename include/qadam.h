@@ -609,7 +609,9 @@ int qadam_held_rows(const void* wcodes, size_t wcode_bytes, int32_t kx, int64_t 
  * NULL (scales of b's rows belong to the axis that is summed over: see `columns` of qadam_quantize_rows).
  * a: [rows][a_stride >= depth].  bias: [channels], or NULL.  All device memory; out's rows are out_stride >= channels apart.
  * rows = 0 is allowed; rows, channels <= 2^31 - 512.
- * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written). */
+ * status: device word or NULL: QADAM_ST_TIMEOUT if a wait inside the kernel gave up (a fault; part of out is then not written).
+ * wait_polls: bound on the polls of every such wait (0: some tenths of a second at least).  test_missing_blocks (0 unless a test makes
+ * waits run out): bit r, CTA r of a cluster leaves the last 128 terms of its share of the sum out, which the others wait for in vain. */
 typedef struct {
   const int8_t* a; int64_t a_stride; const float* a_scale; const int32_t* a_sums;   /* a_sums: qadam_held_product only */
   int64_t rows, depth;
@@ -620,6 +622,7 @@ typedef struct {
   uint32_t* status;
   int64_t first, wcode_bytes;              /* qadam_held_product only, as kx */
   int32_t transposed, bias_type, out_type, accumulate, kx;
+  int32_t wait_polls, test_missing_blocks; /* 0, or for tests: see above */
   float b_worth;                           /* qadam_row_product only */
 } qadam_product_args;
 int qadam_row_product(const qadam_product_args* args, void* stream);

@@ -122,7 +122,7 @@ LAYER_NORM_ARGS = PackedArgs("x x_stride residual residual_stride weight bias ro
 LAYER_NORM_GRAD_ARGS = PackedArgs("dy dy_stride x x_stride mean rstd weight dsum dsum_stride rows width dx dx_stride dweight dbias workspace "
                                   "workspace_bytes", "type weight_type grad_type accumulate")
 PRODUCT_ARGS = PackedArgs("a a_stride a_scale a_sums rows depth b b_stride b_scale channels bias out out_stride status first wcode_bytes",
-                          "transposed bias_type out_type accumulate kx", "b_worth")
+                          "transposed bias_type out_type accumulate kx wait_polls test_missing_blocks", "b_worth")
 
 _lib = None
 

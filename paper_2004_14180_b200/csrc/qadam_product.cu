@@ -29,7 +29,7 @@ constexpr int kFewTokens = 128;            // of a tile at most: the columns of 
 constexpr int kProductThreads = 192;       // a warp that loads, one that multiplies, four for the end
 constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
-constexpr unsigned kPolls = 1u << 23;      // of a wait: some tenths of a second at least, where a tile takes microseconds
+constexpr unsigned kPolls = 1u << 23;      // of a wait, unless a call says otherwise: some tenths of a second at least, where a tile takes microseconds
 
 struct ProductParams {
   const float* a_scale;
@@ -50,6 +50,8 @@ struct ProductParams {
   int transposed;
   int b_signed;
   int stages;
+  unsigned polls;
+  int missing;                             // bit r: CTA r of a cluster does not ask for its last block (tests)
   unsigned* status;
 };
 
@@ -60,6 +62,10 @@ __device__ __forceinline__ void barrier_init(uint64_t* bar, unsigned count) {
 }
 __device__ __forceinline__ void barrier_expect(uint64_t* bar, unsigned bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_at(bar)), "r"(bytes) : "memory");
+}
+// As if so many bytes had come.
+__device__ __forceinline__ void barrier_complete(uint64_t* bar, unsigned bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(shared_at(bar)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ bool barrier_try(uint64_t* bar, unsigned parity) {
   unsigned ok;
@@ -72,9 +78,9 @@ __device__ __forceinline__ bool barrier_try(uint64_t* bar, unsigned parity) {
       : "memory");
   return ok != 0;
 }
-// Gives up after kPolls polls, or once another thread has.
-__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, volatile int* gave_up) {
-  for (unsigned i = 0; i < kPolls; ++i) {
+// Gives up after so many polls, or once another thread has.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, volatile int* gave_up, unsigned polls) {
+  for (unsigned i = 0; i < polls; ++i) {
     if (barrier_try(bar, parity)) return true;
     if (*gave_up) return false;
   }
@@ -83,8 +89,12 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* bar, unsigned parity, vol
 }
 
 // The same for a whole warp, which goes on as one.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, volatile int* gave_up) {
-  return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, gave_up)) != 0;
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, volatile int* gave_up, unsigned polls) {
+  return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, gave_up, polls)) != 0;
+}
+// For what is on its way when a kernel has given up: it has to end before memory is anyone else's.
+__device__ __forceinline__ void settle(uint64_t* bar, unsigned parity) {
+  for (unsigned n = 0; n < kPolls && !barrier_try(bar, parity); ++n) {}
 }
 
 __device__ __forceinline__ void load_tile(void* to, const CUtensorMap* map, int x, int y, uint64_t* bar) {
@@ -147,6 +157,8 @@ struct RingPlace {
       phase ^= 1u;
     }
   }
+  // How many places it has come along, modulo twice the ring.
+  __device__ __forceinline__ int turns(int stages) const { return (int)phase * stages + stage; }
   __device__ __forceinline__ void back(int stages) {
     if (--stage < 0) {
       stage = stages - 1;
@@ -237,8 +249,9 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   RingPlace at;
   int loaded = 0;                          // stages' fills asked for (warp 0)
   if (warp == 0) {
-    for (int i = from; i < to; ++i, ++loaded, at.next(p.stages)) {
-      if (!warp_wait(&s.empty[at.stage], at.phase ^ 1u, &s.gave_up)) break;
+    const int end = to - (p.missing >> rank & 1);
+    for (int i = from; i < end; ++i, ++loaded, at.next(p.stages)) {
+      if (!warp_wait(&s.empty[at.stage], at.phase ^ 1u, &s.gave_up, p.polls)) break;
       if (elected()) {
         uint8_t* b = ring + at.stage * stage_bytes;
         barrier_expect(&s.full[at.stage], stage_bytes);
@@ -254,7 +267,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
                           (unsigned)(kChannels / 16) << 24;
     const unsigned step = p.transposed ? 32 * 128 / 16 : 32 / 16;
     for (int i = from; i < to; ++i, at.next(p.stages)) {
-      if (!warp_wait(&s.full[at.stage], at.phase, &s.gave_up)) break;
+      if (!warp_wait(&s.full[at.stage], at.phase, &s.gave_up, p.polls)) break;
       after_sync();
       const unsigned b = shared_at(ring) + (unsigned)at.stage * stage_bytes;
       const uint64_t wd = operand(b), td = operand(b + b_bytes);
@@ -282,7 +295,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     if (in && p.bias) bias = load_one_of(p.bias, p.bias_type, mine);
   }
   __syncthreads();
-  const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(&s.done, 0, &s.gave_up) && *static_cast<volatile int*>(&s.gave_up) == 0) != 0;
+  const bool ok = __all_sync(0xFFFFFFFFu, warp_wait(&s.done, 0, &s.gave_up, p.polls) && *static_cast<volatile int*>(&s.gave_up) == 0) != 0;
   after_sync();
   const unsigned from_result = result + (unsigned)(warp % 4 * 32) * 65536u;
   if (split == 1) {
@@ -334,13 +347,16 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   }
   before_sync();
   __syncthreads();
-  if (s.gave_up && warp == 0 && lane == 0) {
-    // what was asked for has to land before this CTA's memory is anyone else's
-    for (int i = 0; i < loaded && i < p.stages; ++i) {
-      at.back(p.stages);
-      for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[at.stage], at.phase); ++n) {}
+  if (s.gave_up) {                         // the same for all threads: who sets it does so before the barrier
+    if (warp == 0 && lane == 0) {
+      for (int i = 0; i < loaded && i < p.stages; ++i) {
+        at.back(p.stages);
+        settle(&s.full[at.stage], at.phase);
+      }
+      settle(&s.done, 0);                  // (committed to in any case: behind it no product reads or writes)
+      if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
     }
-    if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
+    __syncthreads();
   }
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(result), "r"(columns));
 }
@@ -391,6 +407,8 @@ struct PairParams {
   unsigned group_magic;                    // 2^32 / (kTokenGroup channel_tiles), rounded up
   int transposed, b_signed;
   int stages, boxes;
+  unsigned polls;
+  int missing;
   unsigned* status;
 };
 
@@ -398,6 +416,7 @@ struct PairShared {
   uint64_t full[kPairMaxStages], empty[kPairMaxStages], result_full[2], result_empty[2];
   unsigned result;
   int gave_up;
+  int asked, multiplied, ended;            // turns of the ring at the end: blocks asked for by this CTA, multiplied; of the results: tiles
 };
 
 __device__ __forceinline__ unsigned of_first(unsigned at) {                // the same place in the pair's first CTA
@@ -509,14 +528,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
 
   const unsigned b_bytes = p.transposed ? kOperandBytes : (unsigned)p.half * kDepth;
   RingPlace place;
-  int loaded = 0;                          // stages' fills asked for, up to all of them
   if (warp == 0) {
     bool ok = true;
     for (int t = blockIdx.x / 2; t < tiles && ok; t += step) {
       const PairTile tile = pair_tile(p, t);
       const int row = tile.token * kPairTokens + rank * 128, channel = tile.channel * 2 * p.half + rank * p.half;
-      for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
-        ok = warp_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up);
+      const int blocks = p.blocks - (t + step >= tiles ? p.missing >> rank & 1 : 0);
+      for (int i = 0; i < blocks; ++i, place.next(p.stages)) {
+        ok = warp_wait(&s.empty[place.stage], place.phase ^ 1u, &s.gave_up, p.polls);
         if (!ok) break;
         if (elected()) {
           uint8_t* a = ring + place.stage * kPairStageBytes;
@@ -527,9 +546,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
           else pair_load(a + kOperandBytes, &b_map, i * kDepth, channel, bar);
         }
         __syncwarp();
-        loaded = min(loaded + 1, p.stages);
       }
     }
+    if (lane == 0) s.asked = place.turns(p.stages);
   } else if (warp == 1 && rank == 0) {
     // result 32 bits signed; first operand signed, second by its type; sizes in eights and sixteens
     const unsigned kind = 2u << 4 | 1u << 7 | (unsigned)p.b_signed << 10 | (unsigned)p.transposed << 16 | (unsigned)(2 * p.half / 8) << 17 |
@@ -537,13 +556,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
     const unsigned b_step = p.transposed ? 32 * 128 / 16 : 32 / 16;
     RingPlace turn;
     bool ok = true;
-    for (int t = blockIdx.x / 2; t < tiles && ok; t += step, turn.next(2)) {
-      ok = warp_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up);
+    for (int t = blockIdx.x / 2; t < tiles; t += step, turn.next(2)) {
+      ok = warp_wait(&s.result_empty[turn.stage], turn.phase ^ 1u, &s.gave_up, p.polls);
       if (!ok) break;
       after_sync();
       const unsigned at = result + (unsigned)turn.stage * 256u;
       for (int i = 0; i < p.blocks; ++i, place.next(p.stages)) {
-        ok = warp_wait(&s.full[place.stage], place.phase, &s.gave_up);
+        ok = warp_wait(&s.full[place.stage], place.phase, &s.gave_up, p.polls);
         if (!ok) break;
         after_sync();
         const unsigned a = shared_at(ring) + (unsigned)place.stage * kPairStageBytes;
@@ -556,6 +575,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
         }
         __syncwarp();
       }
+      if (!ok) break;
+    }
+    if (lane == 0) {
+      s.multiplied = place.turns(p.stages);
+      s.ended = turn.turns(2);
     }
   } else if (warp >= 4) {
     const int end = warp - 4, quarter = warp % 4, side = end / 4;
@@ -601,7 +625,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
       const float times = a_scale;
       const int off = less * p.zero;
       __syncwarp();
-      if (!warp_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up)) break;
+      if (!warp_wait(&s.result_full[turn.stage], turn.phase, &s.gave_up, p.polls)) break;
       after_sync();
       ask(t + step);
       const unsigned at = result + (unsigned)turn.stage * 256u + (unsigned)(quarter * 32) * 65536u;
@@ -693,13 +717,27 @@ __global__ void __launch_bounds__(kPairThreads, 1) pair_kernel(const __grid_cons
   cluster.sync();
   after_sync();
   if (s.gave_up) {                         // in both, then
-    // what was asked for has to land before these CTAs' memory is anyone else's: the first one's barriers count both's
-    if (rank == 0 && warp == 0 && lane == 0) {
-      for (int i = 0; i < loaded; ++i) {
-        place.back(p.stages);
-        for (unsigned n = 0; n < kPolls && !barrier_try(&s.full[place.stage], place.phase); ++n) {}
+    if (warp == 0 && lane == 0) {
+      // The first CTA's barriers count both's copies, and one may have asked for more blocks than the other, both for no more than there are stages
+      // since the last one that was multiplied: what only the second has asked for is expected alone, what only the first has is counted as there.
+      const int ring = 2 * p.stages, multiplied = *cluster.map_shared_rank(&s.multiplied, 0), ended = *cluster.map_shared_rank(&s.ended, 0);
+      const int first = (*cluster.map_shared_rank(&s.asked, 0) - multiplied + ring) % ring;
+      const int second = (*cluster.map_shared_rank(&s.asked, 1) - multiplied + ring) % ring;
+      if (rank == 0) {
+        for (int i = 0; i < max(first, second); ++i) {
+          const int at = (multiplied + i) % ring;
+          uint64_t* full = &s.full[at % p.stages];
+          if (i >= first) barrier_expect(full, kOperandBytes + b_bytes);
+          if (i >= second) barrier_complete(full, kOperandBytes + b_bytes);
+          settle(full, (unsigned)(at / p.stages));
+        }
+        if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
       }
-      if (p.status) atomicOr(p.status, (unsigned)QADAM_ST_TIMEOUT);
+      // products end in the order in which they were begun, each block's, and each tile's, with a commit to both CTAs (a place that nothing has come
+      // by yet counts as left behind)
+      const int last = (multiplied + ring - 1) % ring, tile = (ended + 3) % 4;
+      settle(&s.empty[last % p.stages], (unsigned)(last / p.stages));
+      settle(&s.result_full[tile % 2], (unsigned)(tile / 2));
     }
     __syncwarp();
     cluster.sync();
@@ -830,7 +868,7 @@ int enqueue_pairs(const ProductParams& q, const int8_t* a, int64_t a_stride, int
   PairParams p = {};
   p.a_scale = q.a_scale; p.a_sums = q.a_sums; p.b_scale = q.b_scale; p.worth = q.worth; p.zero = q.zero; p.bias = q.bias; p.bias_type = q.bias_type;
   p.out = q.out; p.out_stride = q.out_stride; p.accumulate = q.accumulate; p.rows = q.rows; p.channels = q.channels; p.blocks = q.blocks;
-  p.transposed = q.transposed; p.b_signed = q.b_signed; p.status = q.status;
+  p.transposed = q.transposed; p.b_signed = q.b_signed; p.polls = q.polls; p.missing = q.missing; p.status = q.status;
   p.token_tiles = (int)((p.rows + kPairTokens - 1) / kPairTokens);
   p.half = pair_shape(p.rows, p.channels, p.blocks, pairs).half;
   p.channel_tiles = (int)((p.channels + 2 * p.half - 1) / (2 * p.half));
@@ -878,6 +916,7 @@ constexpr int64_t kMostRows = ((int64_t)1 << 31) - 512, kMostDepth = 131072;    
 int check_product(const qadam_product_args& p) {
   if (p.rows < 0 || p.rows > kMostRows || p.channels < 1 || p.channels > kMostRows || p.depth < 1 || p.depth > kMostDepth) return QADAM_ERR_SIZE;
   if ((p.transposed != 0 && p.transposed != 1) || (p.accumulate != 0 && p.accumulate != 1)) return QADAM_ERR_SIZE;
+  if (p.wait_polls < 0 || p.test_missing_blocks < 0 || p.test_missing_blocks >= 1 << kMaxSplit) return QADAM_ERR_SIZE;
   if (!known_type(p.out_type) || (p.bias && !known_type(p.bias_type))) return QADAM_ERR_TYPE;
   if (p.rows > 0 && (!p.a || !p.a_scale || !p.out)) return QADAM_ERR_NULL;
   if (p.a_stride < p.depth || p.a_stride >= (int64_t)1 << 40 || p.out_stride < p.channels || p.out_stride > (int64_t)1 << 40) return QADAM_ERR_SIZE;
@@ -893,6 +932,7 @@ ProductParams product_params(const qadam_product_args& g) {
   p.bias = g.bias; p.bias_type = g.bias_type;
   p.out = static_cast<char*>(g.out); p.out_type = g.out_type; p.out_stride = g.out_stride; p.accumulate = g.accumulate;
   p.rows = g.rows; p.channels = g.channels; p.transposed = g.transposed; p.status = g.status;
+  p.polls = g.wait_polls ? (unsigned)g.wait_polls : kPolls; p.missing = g.test_missing_blocks;
   return p;
 }
 

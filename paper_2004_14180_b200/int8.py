@@ -227,7 +227,7 @@ def _product(a, b, worth, bias, out_dtype, out, accumulate, transpose, status):
     out, out_stride, bias_at, bias_type = _output(rows, channels, out, out_dtype, accumulate, bias, device)
     rc = load_library().qadam_row_product(PRODUCT_ARGS.pack(
         a.q_at, a.stride, a.scale_at, 0, rows, depth, b.q_at, b.stride, 0 if transpose or worth is not None else b.scale_at, channels, bias_at,
-        out.data_ptr(), out_stride, 0 if status is None else _status(status, device), 0, 0, transpose, bias_type, _type(out, "out"), accumulate, 0,
+        out.data_ptr(), out_stride, 0 if status is None else _status(status, device), 0, 0, transpose, bias_type, _type(out, "out"), accumulate, 0, 0, 0,
         1.0 if worth is None else worth), stream_of(device))
     if rc:
         _check(rc, "qadam_row_product")
@@ -263,7 +263,7 @@ def held_matmul(a: Int8Rows, wcodes: torch.Tensor, kx: int, rows: int, width: in
     out, out_stride, bias_at, bias_type = _output(a_rows, channels, out, out_dtype, accumulate, bias, device)
     rc = load_library().qadam_held_product(PRODUCT_ARGS.pack(
         a.q_at, a.stride, a.scale_at, a.sums_at, a_rows, depth, wcodes.data_ptr(), 0, 0, channels, bias_at, out.data_ptr(), out_stride,
-        0 if status is None else _status(status, device), first, wcodes.numel(), transpose, bias_type, _type(out, "out"), accumulate, kx, 0.0),
+        0 if status is None else _status(status, device), first, wcodes.numel(), transpose, bias_type, _type(out, "out"), accumulate, kx, 0, 0, 0.0),
         stream_of(device))
     if rc:
         _check(rc, "qadam_held_product")
