@@ -397,6 +397,7 @@ class QAdam:
             self.wfeedback = z(D) if want_wfeedback else None      # error buffer of the broadcast (optional)
             self.workspace = z(sz["workspace_bytes"] + 256, dtype=torch.uint8)
             self.status = z(4, dtype=torch.int32)
+            self._status_word = self.status[:1]
             if x1 is not None:
                 self.x.copy_(self.to_padded(x1.to(self.device, torch.float32)))
             ws_ptr = (self.workspace.data_ptr() + 255) // 256 * 256
@@ -492,14 +493,14 @@ class QAdam:
 
     def matmul(self, segment: int, width: int, a, transpose: bool = False, **kw):
         """8-bit rows times a tensor as the workers hold it, see `held_matmul`: the tensor's rows are `width` long.  Runs on the
-        current stream, as `lookup` does."""
+        current stream, as `lookup` does.  Without a `status` of the caller's own, `poll_status` tells of a wait that gave up."""
         from .int8 import held_matmul
         if self.kx < 0:
             raise ValueError("nothing is broadcast in packed form with kx = -1: quantize the rows of x")
         if width < 1 or self.seg_len[segment] % width:
             raise ValueError(f"segment {segment} of {self.seg_len[segment]} elements has no rows of {width}")
         return held_matmul(a, self.wcodes[:self.wcode_bytes], self.kx, self.seg_len[segment] // width, width, first=self.seg_off[segment],
-                           transpose=transpose, **kw)
+                           transpose=transpose, **{"status": self._status_word, **kw})
 
     def set_moment_rates(self, beta_t: float, theta_t: float) -> None:
         """beta_t, theta_t of Algorithm 1 for the steps that follow."""

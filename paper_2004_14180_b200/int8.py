@@ -208,7 +208,8 @@ def int8_matmul(a: Int8Rows, b: Int8Rows, bias: Optional[torch.Tensor] = None, o
 
     The sums over the common width (at most 131072) are exact.  transpose: a b instead, [rows of a, width of b]; b's scales belong
     to the axis that is then summed over and are not applied: quantize a with columns=b.scale.
-    status: one int32 on the device that gets ST_TIMEOUT if a wait inside the kernel gives up."""
+    status: one int32 on the device that gets ST_TIMEOUT if a wait inside the kernel gives up; part of the result is then not written, and
+    without it nothing says so."""
     return _product(a, b, None, bias, out_dtype, out, accumulate, transpose, status)
 
 

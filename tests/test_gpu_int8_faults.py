@@ -53,3 +53,19 @@ def test_a_wait_that_runs_out_is_told_and_the_device_stays_usable(m, k, n, masks
         product(a, b, out, status, 0 if i % 2 else masks[-1])
     torch.cuda.synchronize()
     assert int(status) == qb.ST_TIMEOUT and torch.equal(many[1], want) and torch.equal(many[3], want)
+
+
+def test_a_contexts_status_word_goes_with_its_products(monkeypatch):
+    from paper_2004_14180_b200 import int8
+    q = qb.QAdam([32 * 64], 1, kg=0, kx=6)
+    given = []
+    held = int8.held_matmul
+    monkeypatch.setattr(int8, "held_matmul", lambda *args, **kw: given.append(kw["status"]) or held(*args, **kw))
+    a, own = int8_rows(gen_of(3), 5, 64), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q.matmul(0, 64, a)
+    q.matmul(0, 64, a, status=own)
+    assert given[0].data_ptr() == q.bufs.status and given[1] is own and q.poll_status() == 0
+    given[0].fill_(qb.ST_TIMEOUT)
+    torch.cuda.synchronize()
+    assert q.poll_status() == qb.ST_TIMEOUT
+    q.close()
