@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kChannels = 128;             // of a tile: the rows of the tensor cores' result
 constexpr int kDepth = 128;                // bytes of a row in a stage
-constexpr int kFewTokens = 128;            // of a tile at most: the columns of the result; more tokens take the kernel below
+constexpr int kFewTokens = 128;            // at most: the columns of the result; more tokens take the kernel below
 constexpr int kProductThreads = 192;       // a warp that loads, one that multiplies, four for the end
 constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
@@ -45,8 +45,7 @@ struct ProductParams {
   int accumulate;
   long long rows, channels;
   int blocks;                              // of kDepth along the sum
-  int tokens;                              // of a tile
-  int channel_tiles;
+  int tokens;                              // the rows rounded up to 16
   int transposed;
   int b_signed;
   int stages;
@@ -179,15 +178,15 @@ struct EndShared {
   int less[kFewTokens];
 };
 template <int N>
-__device__ __forceinline__ void finish(const ProductParams& p, const EndShared& e, float worth, float bias, long long row, long long channel, int t,
-                                       int step, int live, const uint32_t (&sum)[N]) {
+__device__ __forceinline__ void finish(const ProductParams& p, const EndShared& e, float worth, float bias, long long channel, int t, int step,
+                                       int live, const uint32_t (&sum)[N]) {
   float y[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const int i = t + k * step < live ? t + k * step : t;
     y[k] = fmaf((float)(int)(sum[k] - (uint32_t)e.less[i]) * e.scale[i], worth, bias);
   }
-  const long long first = (row + t) * p.out_stride + channel, next = (long long)step * p.out_stride;
+  const long long first = t * p.out_stride + channel, next = (long long)step * p.out_stride;
   if (p.accumulate) {
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -222,8 +221,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
   cg::cluster_group cluster = cg::this_cluster();
   const int split = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const unsigned b_bytes = kChannels * kDepth, a_bytes = (unsigned)p.tokens * kDepth, stage_bytes = a_bytes + b_bytes;
-  const long long tile = blockIdx.x / split;
-  const long long channel = tile % p.channel_tiles * kChannels, row = tile / p.channel_tiles * p.tokens;
+  const long long channel = (long long)(blockIdx.x / split) * kChannels;
   const int from = (int)((long long)p.blocks * rank / split), to = (int)((long long)p.blocks * (rank + 1) / split);
 
   if (threadIdx.x == 0) {
@@ -257,7 +255,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
         barrier_expect(&s.full[at.stage], stage_bytes);
         if (p.transposed) load_tile(b, &b_map, (int)channel, i * kDepth, &s.full[at.stage]);
         else load_tile(b, &b_map, i * kDepth, (int)channel, &s.full[at.stage]);
-        load_tile(b + b_bytes, &a_map, i * kDepth, (int)row, &s.full[at.stage]);
+        load_tile(b + b_bytes, &a_map, i * kDepth, 0, &s.full[at.stage]);
       }
       __syncwarp();
     }
@@ -281,15 +279,14 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
     if (elected()) commit(&s.done);
     __syncwarp();
   }
-  const long long left = p.rows - row;
-  const int live = left < p.tokens ? (int)left : p.tokens;
+  const int live = (int)p.rows;
   const long long mine = channel + warp % 4 * 32 + lane;     // a warp can read the rows of the result that its number names
   const bool in = warp >= 2 && mine < p.channels;
   float worth = p.worth, bias = 0.0f;
   if (warp >= 2) {                         // what the end needs is here when the sums are
     for (int i = threadIdx.x - 64; i < live; i += 128) {
-      about.scale[i] = p.a_scale[row + i];
-      about.less[i] = p.a_sums ? p.zero * p.a_sums[row + i] : 0;
+      about.scale[i] = p.a_scale[i];
+      about.less[i] = p.a_sums ? p.zero * p.a_sums[i] : 0;
     }
     if (in && p.b_scale) worth = p.b_scale[mine];
     if (in && p.bias) bias = load_one_of(p.bias, p.bias_type, mine);
@@ -303,7 +300,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
       for (int t = 0; t < live; t += 16) {
         uint32_t v[16];
         read_columns(from_result + (unsigned)t, v);
-        if (in) finish(p, about, worth, bias, row, mine, t, 1, live, v);
+        if (in) finish(p, about, worth, bias, mine, t, 1, live, v);
       }
     }
   } else {
@@ -333,7 +330,7 @@ __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_c
 #pragma unroll
               for (int k = 0; k < N; ++k) v[k] += (uint32_t)of[(t + k * split < live ? t + k * split : t) * kChannels];
             }
-            finish(p, about, worth, bias, row, mine, t, split, live, v);
+            finish(p, about, worth, bias, mine, t, split, live, v);
           }
         };
         // what is on its way from other CTAs at a time: as many tokens as there are, up to eight
@@ -896,9 +893,8 @@ int enqueue_product(ProductParams& p, const int8_t* a, int64_t a_stride, int64_t
   const FewShape few = few_shape(p.rows, p.channels, p.blocks);
   if (p.rows > kFewTokens || (p.rows > 32 && pair_shape(p.rows, p.channels, p.blocks, pairs).cycles <= few.cycles))
     return enqueue_pairs(p, a, a_stride, depth, b, b_stride, pairs, st);
-  p.channel_tiles = (int)((p.channels + kChannels - 1) / kChannels);
   const int tokens = few.tokens, split = few.split;
-  const int64_t tiles = p.channel_tiles;
+  const int64_t tiles = (p.channels + kChannels - 1) / kChannels;
   p.tokens = tokens;
   const int stage = (kChannels + tokens) * kDepth;
   const int needed = (p.blocks + split - 1) / split;

@@ -100,20 +100,6 @@ __device__ __forceinline__ void store_one_of(void* p, int type, long long i, flo
   else store_one<QADAM_F16>(p, i, v);
 }
 
-// Eight elements from i on; vec: they begin on 16 bytes.
-__device__ __forceinline__ void load_eight_of(const void* p, int type, long long i, bool vec, float (&x)[8]) {
-  if (!vec) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = load_one_of(p, type, i + k);
-  } else if (type == QADAM_F32) {
-    raw8_to_floats<QADAM_F32>(load_raw8<QADAM_F32>(static_cast<const float*>(p) + i), x);
-  } else if (type == QADAM_BF16) {
-    raw8_to_floats<QADAM_BF16>(load_raw8<QADAM_BF16>(static_cast<const unsigned short*>(p) + i), x);
-  } else {
-    raw8_to_floats<QADAM_F16>(load_raw8<QADAM_F16>(static_cast<const unsigned short*>(p) + i), x);
-  }
-}
-
 __device__ __forceinline__ float warp_add(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
@@ -471,8 +457,5 @@ __device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b, float per) {
 }
 __device__ __forceinline__ int to_byte(float x, float per) { return __float2int_rn(__fmul_rn(x, per)); }      // (a NaN gives 0)
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t four_bytes(int a, int b, int c, int d) {
-  return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
-}
 
 }  // namespace qadam
