@@ -561,7 +561,7 @@ int qadam_layer_norm_grad_query_sizes(int64_t rows, int64_t width, size_t* works
  * has written.  With xhat = (x - mean) rstd and g = dy weight:
  *     dx = round(rstd (g - sum g / width - xhat sum(g xhat) / width) + dsum)
  *     dweight = sum over rows of dy xhat,  dbias = sum over rows of dy
- * in binary32; the sums over rows in an order that the sizes alone fix: the same bits every time.  dsum: the gradient that
+ * in binary32; the sums over rows in an order that sizes, types and alignment fix: the same bits every time.  dsum: the gradient that
  * reaches h by other ways, or NULL; dx is then the gradient of x and of residual both.  dy, x, dsum, dx are of `type`.  dweight, dbias: device,
  * [width] of grad_type, either may be NULL; accumulate = 1 adds to what is there.  rows = 0: the sums are zero.
  * workspace: 256-byte aligned, needed for dweight or dbias. */

@@ -642,7 +642,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float*
   store_one_of(to, type, col, accumulate ? load_one_of(to, type, col) + s : s);
 }
 
-// CTAs of the gradient, and so partial sums: as many as are on the device's SMs at a time, at most one to the rows of its groups.
+// CTAs of the gradient, and so partial sums: as many as are on the device's SMs at a time, at most one to the rows of its groups.  (Shared memory may
+// have room for fewer: then there are fewer, see launch_grad.)
 struct GradShape {
   int pieces;                                              // NV of the kernel: 8 elements each
   int warps, groups, threads, per_sm;
@@ -665,17 +666,20 @@ int grad_parts(long long rows, int width, bool vec) {
 }
 
 template <int TY, int NV, bool VEC, bool MANY, int WARPS>
-bool launch_grad(GradParams p, const GradShape& g, int parts, cudaStream_t st) {
+bool launch_grad(GradParams p, const GradShape& g, int& parts, cudaStream_t st) {
   const int slot = RowPart<TY, NV, VEC>::slot_bytes(g.warps * 32) * g.groups, weights = g.warps * 32 * 8 * NV * (int)sizeof(float);
   p.ds_ahead = p.ds && residents(g.threads, g.threads, 3 * slot, weights).stages > 0;               // (not for fp32 rows beyond 6144)
   const int bytes = (p.ds_ahead ? 3 : 2) * slot;
   const Residents r = residents(g.threads, g.per_sm * g.threads, bytes, weights);
+  // (More CTAs than there is room for would come in a second wave: 30012 x 2048 fp32 with ds 191 us in place of 151.  With ds not fetched ahead, so
+  // that there is room for all: 218.)
+  parts = std::min(parts, r.per_sm * kSms);
   static_assert(kRingBytes - 2048 >= 4 * (kGradMostWarps * 768 * 4 + 32) + kGradMostWarps * 768 * 4, "two stages of two rows");
   const size_t smem = std::max((size_t)r.stages * bytes + weights, g.groups == 1 ? 0 : (size_t)g.groups * 2 * p.width * sizeof(float));
   return allow_ring<row_grad_kernel<TY, NV, VEC, MANY, WARPS>>(smem) && launch(row_grad_kernel<TY, NV, VEC, MANY, WARPS>, parts, g.threads, smem, 0, st, p, g.warps, r.stages);
 }
 template <int TY, bool VEC>
-bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
+bool launch_grad(const GradParams& p, int& parts, cudaStream_t st) {
   const GradShape g = grad_shape(p.width, VEC);
   if (g.warps == 1) {
     return g.pieces == 1 ? launch_grad<TY, 1, VEC, false, kGradWarps>(p, g, parts, st)
@@ -691,7 +695,7 @@ bool launch_grad(const GradParams& p, int parts, cudaStream_t st) {
 }
 
 template <int TY>
-bool enqueue_grad_of(const GradParams& p, int parts, bool vec, cudaStream_t st) {
+bool enqueue_grad_of(const GradParams& p, int& parts, bool vec, cudaStream_t st) {
   if (p.width <= kGradGroupWidth) return vec ? launch_grad<TY, true>(p, parts, st) : launch_grad<TY, false>(p, parts, st);
   if (!launch(wide_row_grad_kernel<TY>, p.rows, kWideThreads, 0, 0, st, p)) return false;
   return !p.partial || launch(wide_column_grad_kernel<TY>, (long long)(p.width + 255) / 256 * parts, 256, 0, 0, st, p, parts);
@@ -983,7 +987,7 @@ int qadam_layer_norm_grad(const qadam_layer_norm_grad_args* args, void* stream) 
   if (!known_type(type) || (weight && !known_type(weight_type)) || (sums && !known_type(grad_type))) return QADAM_ERR_TYPE;
   const bool vec = whole(width, type) && on16(dy, dy_stride, type) && on16(x, x_stride, type) && on16(dx, dx_stride, type) &&
                    (!dsum || on16(dsum, dsum_stride, type));
-  const int parts = grad_parts(rows, (int)width, vec);
+  int parts = grad_parts(rows, (int)width, vec);
   if ((rows > 0 && (!dy || !x || !mean || !rstd || !dx)) || (sums && parts > 0 && !workspace)) return QADAM_ERR_NULL;
   if (bad_stride(dy_stride, width) || bad_stride(x_stride, width) || bad_stride(dx_stride, width) || (dsum && bad_stride(dsum_stride, width)))
     return QADAM_ERR_SIZE;
