@@ -782,9 +782,15 @@ bool byte_map(CUtensorMap* map, const void* p, int64_t width, int64_t rows, int6
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// CTAs of a cluster wait for one another while they hold tensor memory, so no SM may be given more of them than its 512 columns
-// serve.  Their shared memory sees to it: tiles of few tokens hold 32 columns and 18 KB or more, 64 and 32 KB, 128 and 48 KB where a sum is
-// split; pairs 512 columns and 200 KB.
+// CTAs of a cluster wait for one another while they hold tensor memory, so no SM may be given more of those than its 512 columns serve.  Their
+// shared memory sees to it.  Where few tokens share a sum, a CTA has two stages or more: up to 32 tokens 32 columns and 36 KB, up to 64
+// 64 and 44 KB, up to 128 128 and 52 KB; pairs 512 columns and 201 KB, beside which none of those fits.  (A CTA with one stage does, or several, and may
+// have to wait for columns, or a pair for its.  But one stage means one block, a sum that is not shared: it holds columns only while it waits
+// for nothing but its own copies, and gives them back.)
+constexpr int kSmBytes = 228 * 1024;
+constexpr int two_stages(int tokens) { return 2 * (kChannels + tokens) * kDepth; }
+static_assert(kPairBytes + two_stages(16) > kSmBytes, "no CTA that shares a sum beside a pair's");
+static_assert(4 * two_stages(80) + two_stages(16) > kSmBytes, "the least that more than 512 columns of CTAs that share sums come with");
 constexpr int kRingBytes = 208 * 1024;
 
 using PairKernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, PairParams);
@@ -827,7 +833,9 @@ constexpr int kSms = 148;
 int64_t block_cycles(int columns, int loaded_rows) { return std::max<int64_t>(2 * columns, 2 * loaded_rows); }
 constexpr int kTileCycles = 1500;          // what a tile costs besides
 
-// Channels of a pair's tile: the time of the pairs' rounds is to be least.
+// Channels of a pair's tile: the time of the pairs' rounds is to be least.  (Of transposed weights a copy takes 128 channels whatever `half` is.
+// Counting those would choose wider tiles on fewer SMs, which take longer: 2048 x 4096 x 768 14.7 us in place of 12.2, 8192 x 768 x 768
+// 10.5 in place of 9.6, 620 x 142 x 532 11.2 in place of 7.2; 5498 x 4436 x 134 would take 21.1 in place of 23.3.)
 struct PairShape {
   int half;
   int64_t cycles;
