@@ -177,7 +177,7 @@ __device__ __forceinline__ void finish_row(const RowParams& p, const RowPart<TY,
 
 // One pass: a row is read once, held in registers for mean, sum of squares around it and largest value, and written once.
 // There is a warp for each row: enough of them are on an SM to keep its share of the loads under way.  8192 x 768 bf16, the sum with a residual
-// and its norm: 8.4 us (50 MB; 7.8 at the copy rate); 16 rows: 2.0 us in a row of such launches.
+// and its norm: 8.6 us (50 MB; 7.8 at the copy rate); 16 rows: 2.1 us in a row of such launches.
 template <int TY, int NV, bool VEC>
 __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_constant__ RowParams p) {
   wait_for_previous_launch();
@@ -200,8 +200,9 @@ __global__ void __launch_bounds__(kWarpRowThreads) warp_row_kernel(const __grid_
 }
 
 // Wider rows, and many: a group of warps (a warp) goes from row to row, with the next ones under way in shared memory, where the parameters are
-// too.  65536 x 768 bf16: norm 42 us (201 MB, 4.8 TB/s: instructions), into 8 bits 24 (151 MB, 6.3 TB/s); 16384 x 8192 bf16 into 8
-// bits 76 to 88 us (403 MB, 62 at the copy rate; 117 with a CTA for each row); norm of 30011 x 2049 fp32, which begin anywhere, 111 us (492 MB, 76).
+// too.  65536 x 768 bf16: norm 44 us (201 MB, 4.6 TB/s: instructions), norm into 8 bits 46, rows as they are into 8 bits 25 (151 MB,
+// 6.0 TB/s); 16384 x 8192 bf16 into 8 bits 76 to 88 us (403 MB, 62 at the copy rate; 117 with a CTA for each row); norm of 30011 x 2049 fp32, which
+// begin anywhere, 120 us (492 MB, 76).
 constexpr int kGroupWarps = 8;                             // of a CTA, in groups, or one group of up to 16
 template <int TY, int NV, bool VEC, bool MANY, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(const __grid_constant__ RowParams p, int warps, int stages, int with_parameters) {
@@ -251,7 +252,8 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) group_row_kernel(co
   }
 }
 
-// Rows too wide for a CTA's registers: read again for each thing that is known only at the row's end.
+// Rows too wide for a CTA's registers: read again for each thing that is known only at the row's end.  2000 x 20001 fp32: 130 us (320 MB, 50 at the
+// copy rate), 2000 x 32768 bf16 182 (262 MB, 41): an element to an access.
 template <int TY>
 __global__ void __launch_bounds__(kWideThreads) wide_row_kernel(const __grid_constant__ RowParams p) {
   __shared__ GroupShared shared;
@@ -413,8 +415,8 @@ struct GradParams {
 __host__ __device__ constexpr int grad_warps_of_sm(int nv, bool many) { return many && nv == 2 ? 18 : 12; }
 
 // A warp (rows of up to 768 elements), or a group of them, goes from row to row, with the next ones under way, and adds up its rows' part of the
-// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 69 us (403 MB, 62 at the copy
-// rate); 8192 x 768: 8.8 us, and 5.8 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 119 us (114); 30011 x 2049: 146.
+// weight's and bias's gradients in registers; the CTA's sums go to the workspace.  65536 x 768 bf16 with ds: 70 us (403 MB, 62 at the copy
+// rate); 8192 x 768: 9.1 us, and 6.0 more for the sums' end and the launch that joins them; 30012 x 2048 fp32: 119 us (114); 30011 x 2049: 144.
 // (Clusters of four CTAs that join their sums first: fewer CTAs find room, 30 us in place of 17 for 8192 x 768.)
 // Where an SM gets 12 warps, registers hold a row between its sums and its result (2 to 4 % less time); where it gets 18, the row is read from
 // shared memory again.  (Eight elements to a thread, and more warps to a row: 375 instructions for 256 elements, most of them for the
@@ -569,7 +571,8 @@ __global__ void __launch_bounds__(WARPS * 32, grad_warps_of_sm(NV, MANY) / WARPS
   }
 }
 
-// Rows too wide for registers: the rows' gradient by reading twice, the columns' sums by another pass.
+// Rows too wide for registers: the rows' gradient by reading twice, the columns' sums by another pass.  2000 x 20001 fp32: 280 us (480 MB, 74 at the
+// copy rate).
 template <int TY>
 __global__ void __launch_bounds__(kWideThreads) wide_row_grad_kernel(const __grid_constant__ GradParams p) {
   __shared__ GroupShared shared;
@@ -615,7 +618,7 @@ __global__ void __launch_bounds__(256) wide_column_grad_kernel(const __grid_cons
   part[p.width + col] = db;
 }
 
-// The CTAs' sums joined, in an order that the sizes fix: 32 columns of either sum to a CTA, the parts dealt out to its warps, who
+// The CTAs' sums joined, in an order that their number fixes: 32 columns of either sum to a CTA, the parts dealt out to its warps, who
 // ask for ten at a time.
 constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(kJoinWarps * 32) join_grad_kernel(const float* partial, int parts, int width, void* dw, void* db, int type,
@@ -870,7 +873,8 @@ struct HeldParams {
   float* scale;
 };
 
-// A thread decodes 16 consecutive codes: (16 BITS + 31) / 32 + 1 words at most, one store of 16 bytes.  1537 x 1001 codes of 4 bits: 1.7 us.
+// A thread decodes 16 consecutive codes: (16 BITS + 31) / 32 + 1 words at most, one store of 16 bytes.  1537 x 1001 codes of 4 bits: 1.7 us; 8192 x 8192
+// of 8 bits 24.5 (134 MB, 21 at the copy rate), of 4 bits 23.5 (16).
 template <int BITS>
 __global__ void __launch_bounds__(256) held_rows_kernel(const __grid_constant__ HeldParams p) {
   wait_for_previous_launch();

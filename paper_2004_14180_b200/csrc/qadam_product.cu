@@ -209,8 +209,8 @@ __device__ __forceinline__ void finish(const ProductParams& p, const EndShared& 
 
 // Few tokens: the weights' channels are the rows of the tensor cores' result, so that a tile is as wide as there are tokens.  One tile of
 // kChannels x tokens to a cluster; its CTAs share the sum's blocks, so that enough SMs fetch weights, and add up in each other's
-// shared memory (whole numbers: in any order the same).  1 x 4096 x 4096: 6.6 us (16.8 MB, 2.6 at the copy rate: launch, first load,
-// last sum); 16 x 768 x 30522 packed codes, fp32: 5.5 us (25 MB, 3.9).
+// shared memory (whole numbers: in any order the same).  1 x 4096 x 4096: 6.8 us (16.8 MB, 2.6 at the copy rate: launch, first load,
+// last sum); 16 x 768 x 30522 packed codes, fp32: 5.8 us (25 MB, 3.9).
 __global__ void __launch_bounds__(kProductThreads) product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                                                                   const __grid_constant__ ProductParams p) {
   extern __shared__ uint8_t raw[];
