@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+from math import inf
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -14,6 +15,9 @@ from .adamw import _need_cuda, stream_of, written
 from .binding import LAYER_NORM_ARGS, LAYER_NORM_GRAD_ARGS, _check, load_library
 from .embedding import _elsewhere, _row_stride, _type
 from .int8 import Int8Rows
+
+
+MOST_F32 = 3.4028234663852886e38      # beyond it struct raises an error of its own
 
 
 class Normed(NamedTuple):
@@ -74,7 +78,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         rc = load_library().qadam_layer_norm(LAYER_NORM_ARGS.pack(
             x.data_ptr(), stride, residual_at, residual_stride, weight_at, bias_at, n, width, 0 if residual is None else total.data_ptr(), width,
             0 if out is None else out.data_ptr(), width, mean.data_ptr(), rstd.data_ptr(), *((0, 0, 0, 0) if rows is None else rows._at()),
-            kind, weight_type, bias_type, eps), stream_of(device))
+            kind, weight_type, bias_type, eps if -MOST_F32 <= eps <= MOST_F32 else inf), stream_of(device))
         if rc:
             _check(rc, "qadam_layer_norm")
     return Normed(out, total, mean, rstd, rows)

@@ -56,3 +56,10 @@ def test_means_of_whole_numbers_are_rounded_once(width):
     assert torch.equal(got.mean, x.double().sum(1).float() / torch.full((500,), float(width), device="cuda"))
     big = torch.full((2, width), 3e38, device="cuda")                             # sums beyond binary32: as sum / width has it
     assert bool(qb.layer_norm(big).mean.isinf().all())
+
+
+@pytest.mark.parametrize("eps", [1e39, -1e39, float("inf"), float("nan"), -1e-5])
+def test_an_eps_that_is_not_one_is_refused(eps):
+    with pytest.raises(qb.QAdamError) as e:
+        qb.layer_norm(torch.ones(2, 8, device="cuda"), eps=eps)
+    assert e.value.code == -8
